@@ -19,7 +19,8 @@
  * Conventions for every call below.
  *  - All data pointers are DEVICE pointers unless the comment says "host".
  *  - The caller owns every buffer it passes.  The library allocates device
- *    memory only inside grawa_plan_create and frees it in grawa_plan_destroy.
+ *    memory only inside grawa_plan_create and grawa_sublayer_create and frees it in
+ *    grawa_plan_destroy and grawa_sublayer_destroy.
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *    Calls enqueue their kernels on it and return without synchronising; two
  *    calls that use the same plan must be ordered on one stream (the plan's
@@ -305,6 +306,123 @@ grawa_status_t grawa_lgrawa_update_static(int K, int64_t P, int L, const int64_t
                                           float *x, int64_t ldx, const void *g, int64_t ldg,
                                           grawa_dtype_t g_dtype, float lambda, float *center_out,
                                           float *weights_out, void *stream);
+
+/*
+ * The feed-forward sublayer of a transformer block, forward and backward, for all K
+ * workers of a GPU in one call each: what fills the gradient rows that the calls
+ * above take.  Every worker's parameters are read from its row of a flat array and
+ * its gradients are written to its row of another, where they stand.
+ *
+ *   layer norm     y = (x - mean) / sqrt(var + eps) * weight + bias   over the last axis
+ *   feed-forward   y = (act(x Wg^T) * (x Wu^T)) Wd^T                  Wg, Wu: [f][d], Wd: [d][f]
+ *   dropout        y = residual + keep(x) / (1 - p)
+ *
+ * Types.  One type a plan (a call of grawa_dropout): activations, parameters and
+ * gradients are all float32 or all bfloat16.  Sums, statistics and the products'
+ * accumulation are float32.  With bfloat16 the inner activations H, dG and dU are
+ * rounded to bfloat16 once; with float32 the products are formed from exact
+ * three-term bfloat16 splittings with an error of a float32 product's order.
+ *
+ * Layouts.  grawa_rows_t is K x T rows of `width` elements: worker k's row t starts
+ * at data + k * worker + t * row elements; elements of a row are adjacent.  Strides
+ * of inputs are not negative (0 shares one batch among the workers); rows of
+ * outputs must not overlap.  grawa_mats_t is one matrix or vector for each worker,
+ * without gaps inside, `worker` elements apart (the views of a flat row).  Any
+ * alignment to whole elements is accepted; matrices whose bases, strides and widths
+ * are multiples of 16 bytes are read in place, others are copied to the plan's
+ * workspace first.  Outputs must not overlap inputs except where a call says so.
+ *
+ * Limits: 1 <= K <= GRAWA_MAX_WORKERS, 0 <= T, K T <= 2^30, 1 <= d < 2^20,
+ * 0 <= f < 2^20; UNSUPPORTED beyond.  T = 0 is no error: gradients of parameters are
+ * then zero.
+ */
+typedef enum {
+    GRAWA_ACT_SILU = 0, /* z / (1 + exp(-z)) */
+    GRAWA_ACT_GELU = 1, /* z (1 + erf(z / sqrt 2)) / 2 */
+    GRAWA_ACT_RELU = 2  /* z where z > 0 */
+} grawa_act_t;
+
+typedef struct {
+    void *data;
+    int64_t worker, row; /* strides in elements */
+} grawa_rows_t;
+
+typedef struct {
+    void *data;
+    int64_t worker; /* stride in elements */
+} grawa_mats_t;
+
+typedef struct grawa_sublayer grawa_sublayer_t; /* opaque */
+
+/*
+ * Shape and device workspace of the calls below.  T is the most tokens of a worker
+ * that a call may have; f = 0 makes a plan for the layer norm alone.  The
+ * workspace is allocated here, on the current device, and freed by
+ * grawa_sublayer_destroy (the caller must have synchronised the streams that used
+ * it; NULL is accepted).  Two calls on one plan must be ordered on one stream.
+ */
+grawa_status_t grawa_sublayer_create(grawa_sublayer_t **out, int K, int64_t T, int64_t d, int64_t f,
+                                     grawa_dtype_t dtype, grawa_act_t act);
+grawa_status_t grawa_sublayer_destroy(grawa_sublayer_t *plan);
+
+/* Bytes of the buffer that grawa_ffn leaves to grawa_ffn_backward for T tokens (host pointer). */
+grawa_status_t grawa_sublayer_save_bytes(const grawa_sublayer_t *plan, int64_t T, int64_t *bytes);
+
+/*
+ * Layer norm of T tokens of every worker.  weight, bias: vectors of d; bias may be
+ * NULL.  eps >= 0 and finite.  stats: float32 [K][T][2], mean and 1 / sqrt(var + eps),
+ * 8-byte aligned, or NULL if no backward pass follows.  y may be x.
+ */
+grawa_status_t grawa_layer_norm(grawa_sublayer_t *plan, int64_t T, const grawa_rows_t *x,
+                                const grawa_mats_t *weight, const grawa_mats_t *bias, float eps,
+                                const grawa_rows_t *y, float *stats, void *stream);
+
+/*
+ * Its backward pass: dx [+ add], dweight, dbias.  add and dbias may be NULL; dx may
+ * be dy or add.  accumulate != 0 adds to dweight and dbias instead of replacing them.
+ */
+grawa_status_t grawa_layer_norm_backward(grawa_sublayer_t *plan, int64_t T, const grawa_rows_t *dy,
+                                         const grawa_rows_t *x, const grawa_mats_t *weight,
+                                         const float *stats, const grawa_rows_t *add,
+                                         const grawa_rows_t *dx, const grawa_mats_t *dweight,
+                                         const grawa_mats_t *dbias, int accumulate, void *stream);
+
+/*
+ * y = residual + dropout((act(x Wg^T) * (x Wu^T)) Wd^T).  residual may be NULL (none;
+ * it may be x) and y may be residual; p = 0 drops nothing and needs no rng, see grawa_dropout.
+ * save: grawa_sublayer_save_bytes bytes, 16-byte aligned, filled for the backward
+ * pass; NULL if none follows.
+ */
+grawa_status_t grawa_ffn(grawa_sublayer_t *plan, int64_t T, const grawa_rows_t *x,
+                         const grawa_mats_t *wg, const grawa_mats_t *wu, const grawa_mats_t *wd,
+                         const grawa_rows_t *residual, float p, const int64_t *rng, uint32_t site,
+                         const grawa_rows_t *y, void *save, void *stream);
+
+/*
+ * From dy, the gradient of the product with Wd (of the dropout's input, where there
+ * is one): dx, dWg, dWu, dWd.  x and the weights are those of the forward call.
+ * accumulate != 0 adds to dWg, dWu and dWd instead of replacing them.
+ */
+grawa_status_t grawa_ffn_backward(grawa_sublayer_t *plan, int64_t T, const grawa_rows_t *dy,
+                                  const grawa_rows_t *x, const grawa_mats_t *wg,
+                                  const grawa_mats_t *wu, const grawa_mats_t *wd, const void *save,
+                                  const grawa_rows_t *dx, const grawa_mats_t *dwg,
+                                  const grawa_mats_t *dwu, const grawa_mats_t *dwd, int accumulate,
+                                  void *stream);
+
+/*
+ * y = residual + keep(x) / (1 - p), 0 <= p < 1; residual may be NULL, y may be x or
+ * residual.  The mask is never stored: element (k, t, c) is kept if word c % 4 of
+ * Philox4x32 with 7 rounds for the counter (c / 4, k T + t, site, step) under the key
+ * `seed` is at least floor(p 2^32), so that the same call on dy without a residual is
+ * the backward pass.  A dropped element is 0 whatever x holds.  rng: device int64 [2],
+ * the seed and the step (its lower 32 bits count), read when the kernel runs: a
+ * program moves the step on between training steps, under a captured graph too.
+ * site tells the dropouts of a model apart.  Needs no plan.
+ */
+grawa_status_t grawa_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype, const grawa_rows_t *x,
+                             const grawa_rows_t *residual, float p, const int64_t *rng, uint32_t site,
+                             const grawa_rows_t *y, void *stream);
 
 /*
  * Measurement aids (not part of the method).

@@ -1,0 +1,397 @@
+// The gated feed-forward block of K workers, forward and backward:
+//   G = x Wg^T;  U = x Wu^T;  H = act(G) U;  y = H Wd^T [dropped, plus a residual]
+//   dH = dy Wd;  dU = dH act(G);  dG = dH U act'(G);  dx = dG Wg + dU Wu;  dWg = dG^T x;  dWu = dU^T x;  dWd = dy^T H
+// Three kinds of product in the forward pass and six in the backward, 18 K T d f operations together: bound by the matrix cores but
+// for a few tokens.  Gate and up come from one kernel, whose epilogue has both in registers and leaves H; the backward's first
+// kernel makes dH and from it dG and dU in its epilogue, so that no pass over [T][f] arrays stands between the products.
+//
+// Roundings.  bfloat16: H, dG and dU are rounded to bfloat16, as the matrix instructions take them; G and U are kept for the
+// backward pass in float32 (a rounding of theirs would be a third one on the way to dWg, dWu and dx).  float32: every matrix
+// element is split exactly into three bfloat16 terms and the six largest of the nine products of terms are summed in float32;
+// what is left out is below 2^-24 of a product.  (An infinity times a number that is exactly a bfloat16 gives NaN there.)
+#include "grawa_gemm.h"
+
+namespace {
+
+// The three terms, each the number's upper 16 bits after the terms before it: the remainders are exact, and nothing can overflow.
+__device__ __forceinline__ void split3(float v, uint16_t t[3])
+{
+    uint32_t u = __float_as_uint(v);
+    if ((u & 0x7fffffffu) > 0x7f800000u) u = 0x7fc00000u; // a NaN whose mark stands in the lower bits
+    t[0] = (uint16_t)(u >> 16);
+    const float r = (u & 0x7f800000u) == 0x7f800000u ? 0.f : v - __uint_as_float(u & 0xffff0000u);
+    const uint32_t w = __float_as_uint(r);
+    t[1] = (uint16_t)(w >> 16);
+    t[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(w & 0xffff0000u)) >> 16);
+}
+
+// Eight numbers to the planes at p, p + plane, p + 2 plane (bytes): 16 bytes each.
+template <int PLANES> __device__ __forceinline__ void store_planes8(char *p, int64_t plane, const float *v)
+{
+    if constexpr (PLANES == 1) {
+        store_elements<true, 8>(p, v);
+    } else {
+        uint16_t t[8][3];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) split3(v[j], t[j]);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = t[2 * j][q] | ((uint32_t)t[2 * j + 1][q] << 16);
+            *(uint4 *)(p + q * plane) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
+// Copies [K][R][C] elements into planes of pitch Cp with zeros behind C.  Eight elements a thread.
+template <bool BF16> __global__ __launch_bounds__(256) void k_planes(const char *src, int64_t worker, int64_t row, char *dst, int64_t plane, int64_t R, int C, int Cp, int wide)
+{
+    constexpr int S = BF16 ? 2 : 4;
+    const int64_t groups = Cp / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int k = blockIdx.y;
+    const int64_t r = i / groups;
+    if (r >= R) return;
+    const int c = (int)(i - r * groups) * 8;
+    const char *p = src + ((int64_t)k * worker + r * row + c) * S;
+    float v[8] = {};
+    if (wide) {
+        load_elements<BF16, 8>(p, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < C) load_elements<BF16, 1>(p + j * S, v + j);
+    }
+    store_planes8<BF16 ? 1 : 3>(dst + (((int64_t)k * R + r) * Cp + c) * 2, plane, v);
+}
+
+// e^z: for results that are rounded to bfloat16 by the hardware's 2^z, whose argument's rounding costs z 2^-24 of it.
+template <int PLANES> __device__ __forceinline__ float exp_of(float z) { return PLANES == 1 ? __expf(z) : expf(z); }
+
+// The activation and its derivative.
+template <int PLANES, int ACT> __device__ __forceinline__ float act_of(float z)
+{
+    if constexpr (ACT == GRAWA_ACT_SILU) return z / (1.f + exp_of<PLANES>(-z));
+    if constexpr (ACT == GRAWA_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    return z * (z > 0.f ? 1.f : 0.f);
+}
+
+template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z, float &a, float &da)
+{
+    if constexpr (ACT == GRAWA_ACT_SILU) {
+        const float s = 1.f / (1.f + exp_of<PLANES>(-z));
+        a = z * s;
+        da = s * (1.f + z * (1.f - s));
+    } else if constexpr (ACT == GRAWA_ACT_GELU) {
+        const float cdf = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        a = z * cdf;
+        da = cdf + z * exp_of<PLANES>(-0.5f * z * z) * 0.39894228040143268f;
+    } else {
+        da = z > 0.f ? 1.f : 0.f;
+        a = z * da;
+    }
+}
+
+// Epilogue of gate and up: H, and for a backward pass G and U.
+template <int PLANES, int ACT> struct EpiGateUp {
+    char *h;            // [PLANES][K][M][pitch]
+    float *gate, *up;   // [K][M][pitch], or null
+    int64_t plane;      // bytes between the planes of h
+    int64_t worker;     // elements of a worker
+    int N, pitch;
+    __device__ __forceinline__ void tile(int k)
+    {
+        h += k * worker * 2;
+        if (gate) {
+            gate += k * worker;
+            up += k * worker;
+        }
+    }
+    __device__ __forceinline__ void put8(int m, int n, const float *g, const float *u) const
+    {
+        const int64_t at = (int64_t)m * pitch + n;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = n + j < N ? act_of<PLANES, ACT>(g[j]) * u[j] : 0.f;
+        store_planes8<PLANES>(h + at * 2, plane, v);
+        if (gate) {
+            store_elements<false, 8>((char *)(gate + at), g);
+            store_elements<false, 8>((char *)(up + at), u);
+        }
+    }
+};
+
+// Epilogue of dH: dG and dU.
+template <int PLANES, int ACT> struct EpiBack {
+    const float *gate, *up;
+    char *dg, *du;
+    int64_t plane, worker;
+    int N, pitch;
+    __device__ __forceinline__ void tile(int k)
+    {
+        gate += k * worker;
+        up += k * worker;
+        dg += k * worker * 2;
+        du += k * worker * 2;
+    }
+    __device__ __forceinline__ void put16(int m, int n, const float *dh) const
+    {
+#pragma unroll
+        for (int q = 0; q < 2; ++q, n += 8, dh += 8) {
+            if (n >= N) break;
+            const int64_t at = (int64_t)m * pitch + n;
+            float g[8], u[8];
+            load_elements<false, 8>((const char *)(gate + at), g);
+            load_elements<false, 8>((const char *)(up + at), u);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float a, da;
+                act_both<PLANES, ACT>(g[j], a, da);
+                g[j] = n + j < N ? dh[j] * u[j] * da : 0.f;
+                u[j] = n + j < N ? dh[j] * a : 0.f;
+            }
+            store_planes8<PLANES>(dg + at * 2, plane, g);
+            store_planes8<PLANES>(du + at * 2, plane, u);
+        }
+    }
+};
+
+// Epilogue of everything else: to an array of the caller's, rounded once, added to what is there (ACC) or dropped and added to a
+// residual (OUT).
+template <bool BF16, bool OUT> struct EpiStore {
+    GrawaRows y, res;   // OUT: res.p may be null
+    GrawaDrop drop;     // OUT
+    int N, T, accumulate, wide;
+    uint32_t row0;      // of the worker, for the dropout
+    __device__ __forceinline__ void tile(int k)
+    {
+        constexpr int S = BF16 ? 2 : 4;
+        y.p += (int64_t)k * y.worker * S;
+        if (OUT && res.p) res.p += (int64_t)k * res.worker * S;
+        row0 = (uint32_t)k * (uint32_t)T;
+    }
+    __device__ __forceinline__ void put16(int m, int n, float *v) const
+    {
+        constexpr int S = BF16 ? 2 : 4;
+        if (OUT && drop.threshold) {
+            const GrawaDropKey key = grawa_drop_key(drop);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) grawa_drop4(drop, key, row0 + (uint32_t)m, (uint32_t)n / 4 + q, v + 4 * q);
+        }
+        char *p = y.p + ((int64_t)m * y.row + n) * S;
+        const char *from = OUT ? (res.p ? res.p + ((int64_t)m * res.row + n) * S : nullptr) : accumulate ? p : nullptr;
+        if (wide && n + 16 <= N) {
+            float r[16] = {};
+            if (from) {
+                load_elements<BF16, 16>(from, r);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] += r[j];
+            }
+            store_elements<BF16, 16>(p, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (n + j >= N) break;
+                float r = 0.f;
+                if (from) load_elements<BF16, 1>(from + j * S, &r);
+                r = from ? v[j] + r : v[j];
+                store_elements<BF16, 1>(p + j * S, &r);
+            }
+        }
+    }
+};
+
+// A matrix operand as the products read it.
+struct Operand {
+    const char *p;
+    int64_t worker, plane; // bytes
+    int64_t ld;
+};
+
+constexpr int64_t MAX_LD = ((int64_t)1 << 31) / 256 - 128; // bytes; a tile's offsets have 31 bits
+
+template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const GrawaGemm &g, const Epi &epi, hipStream_t st)
+{
+    auto tiles = [&](int bm, int bn) { return (int64_t)g.K * ((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
+    // Tiles of 256 x 256 where they give each CU one, else of 128 x 128, of which a CU takes two at a time.
+    const int64_t large = tiles(256, DUAL ? 128 : 256);
+    if (large >= 256) {
+        k_gemm<256, 256, 2, 4, AT, BT, DUAL, Epi><<<dim3((unsigned)large), 512, 0, st>>>(g, epi);
+    } else {
+        const int64_t small = tiles(128, DUAL ? 64 : 128);
+        k_gemm<128, 128, 2, 2, AT, BT, DUAL, Epi><<<dim3((unsigned)small), 256, 0, st>>>(g, epi);
+    }
+    return hipGetLastError();
+}
+
+// Segments of A B, small products first.
+void add_segments(GrawaGemm &g, int planes, const Operand &a, const Operand &b, const Operand *b2)
+{
+    static const int pairs[6][2] = {{0, 2}, {2, 0}, {1, 1}, {0, 1}, {1, 0}, {0, 0}};
+    const int n = planes == 1 ? 1 : 6;
+    for (int i = 0; i < n; ++i) {
+        const int *q = planes == 1 ? pairs[5] : pairs[i];
+        g.a[g.nseg] = GrawaSeg{a.p + q[0] * a.plane, a.worker};
+        g.b[g.nseg] = GrawaSeg{b.p + q[1] * b.plane, b.worker};
+        if (b2) g.b[n + i] = GrawaSeg{b2->p + q[1] * b2->plane, b2->worker};
+        ++g.nseg;
+    }
+    g.lda = a.ld;
+    g.ldb = b.ld;
+}
+
+struct Sublayer { // one call
+    const grawa_sublayer *s;
+    int64_t T;
+    hipStream_t st;
+    hipError_t err = hipSuccess;
+
+    int S() const { return s->dtype == GRAWA_BF16 ? 2 : 4; }
+    // An operand read in place where it can be, else a copy in `room`.
+    Operand operand(const char *p, int64_t worker, int64_t row, int64_t R, int64_t C, int64_t Cp, char *room)
+    {
+        const bool bf = s->dtype == GRAWA_BF16;
+        if (bf && C % 8 == 0 && !(((uintptr_t)p | (uint64_t)worker * 2 | (uint64_t)row * 2) & 15) && row >= C && row * 2 <= MAX_LD)
+            return Operand{p, worker * 2, 0, row * 2};
+        const Operand o{room, R * Cp * 2, (int64_t)s->K * R * Cp * 2, Cp * 2};
+        const int wide = C % 8 == 0 && !(((uintptr_t)p | (uint64_t)worker * S() | (uint64_t)row * S()) & 15);
+        const dim3 grid((unsigned)((R * (Cp / 8) + 255) / 256), (unsigned)s->K);
+        if (bf)
+            k_planes<true><<<grid, 256, 0, st>>>(p, worker, row, room, o.plane, R, (int)C, (int)Cp, wide);
+        else
+            k_planes<false><<<grid, 256, 0, st>>>(p, worker, row, room, o.plane, R, (int)C, (int)Cp, wide);
+        if (err == hipSuccess) err = hipGetLastError();
+        return o;
+    }
+    Operand tokens(const GrawaRows &x, char *room) { return operand(x.p, x.worker, x.row, T, s->d, s->dp, room); }
+    Operand up_matrix(const GrawaMat &w, char *room) { return operand(w.p, w.worker, s->d, s->f, s->d, s->dp, room); }
+    Operand down_matrix(const GrawaMat &w, char *room) { return operand(w.p, w.worker, s->f, s->d, s->f, s->fp, room); }
+    Operand inner(char *p) const { return Operand{p, T * s->fp * 2, s->K * T * s->fp * 2, s->fp * 2}; }
+    GrawaGemm product(int64_t M, int64_t N, int64_t len) const
+    {
+        GrawaGemm g{};
+        g.K = s->K;
+        g.M = (int)M;
+        g.N = (int)N;
+        g.len = (int)len;
+        return g;
+    }
+    template <class F> void run(const F &f)
+    {
+        if (err == hipSuccess) err = f();
+    }
+    bool wide(const GrawaRows &r) const { return !(((uintptr_t)r.p | (uint64_t)r.worker * S() | (uint64_t)r.row * S()) & 15); }
+};
+
+template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, GrawaMat wg, GrawaMat wu, GrawaMat wd, GrawaRows residual, GrawaDrop drop, GrawaRows y, char *save)
+{
+    const grawa_sublayer *s = c.s;
+    const Operand ox = c.tokens(x, s->x), og = c.up_matrix(wg, s->wg), ou = c.up_matrix(wu, s->wu), od = c.down_matrix(wd, s->wd);
+    const int64_t n = c.T * s->fp;
+    float *gate = (float *)save;
+    char *h = save ? save + s->K * n * 8 : s->h;
+    {
+        GrawaGemm g = c.product(c.T, s->f, s->d);
+        add_segments(g, PLANES, ox, og, &ou);
+        const EpiGateUp<PLANES, ACT> epi{h, gate, gate ? gate + s->K * n : nullptr, s->K * n * 2, n, (int)s->f, (int)s->fp};
+        c.run([&] { return launch_gemm<false, false, true>(g, epi, c.st); });
+    }
+    {
+        GrawaGemm g = c.product(c.T, s->d, s->f);
+        add_segments(g, PLANES, c.inner(h), od, nullptr);
+        const EpiStore<PLANES == 1, true> epi{y, residual, drop, (int)s->d, (int)c.T, 0, c.wide(y) && (!residual.p || c.wide(residual)), 0};
+        c.run([&] { return launch_gemm<false, false, false>(g, epi, c.st); });
+    }
+    return c.err;
+}
+
+template <int PLANES, int ACT>
+hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat wu, GrawaMat wd, const char *save, GrawaRows dx, GrawaMat dwg, GrawaMat dwu, GrawaMat dwd, int accumulate)
+{
+    const grawa_sublayer *s = c.s;
+    const Operand ox = c.tokens(x, s->x), ody = c.tokens(dy, s->dy);
+    const Operand og = c.up_matrix(wg, s->wg), ou = c.up_matrix(wu, s->wu), od = c.down_matrix(wd, s->wd);
+    const int64_t n = c.T * s->fp;
+    const float *gate = (const float *)save;
+    const Operand oh = c.inner((char *)save + s->K * n * 8), odg = c.inner(s->dg), odu = c.inner(s->du);
+    {
+        GrawaGemm g = c.product(c.T, s->f, s->d);
+        add_segments(g, PLANES, ody, od, nullptr);
+        const EpiBack<PLANES, ACT> epi{gate, gate + s->K * n, s->dg, s->du, s->K * n * 2, n, (int)s->f, (int)s->fp};
+        c.run([&] { return launch_gemm<false, true, false>(g, epi, c.st); });
+    }
+    auto store = [&](const Operand &a, const Operand &b, GrawaMat w, int64_t M, int64_t N) {
+        GrawaGemm g = c.product(M, N, c.T);
+        add_segments(g, PLANES, a, b, nullptr);
+        const GrawaRows out{w.p, w.worker, N};
+        const EpiStore<PLANES == 1, false> epi{out, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, c.wide(out), 0};
+        c.run([&] { return launch_gemm<true, true, false>(g, epi, c.st); });
+    };
+    store(odg, ox, dwg, s->f, s->d);
+    store(odu, ox, dwu, s->f, s->d);
+    store(ody, oh, dwd, s->d, s->f);
+    {
+        GrawaGemm g = c.product(c.T, s->d, s->f);
+        add_segments(g, PLANES, odg, og, nullptr);
+        add_segments(g, PLANES, odu, ou, nullptr);
+        const EpiStore<PLANES == 1, false> epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, c.wide(dx), 0};
+        c.run([&] { return launch_gemm<false, true, false>(g, epi, c.st); });
+    }
+    return c.err;
+}
+
+// Gradients of no tokens.
+template <bool BF16> __global__ __launch_bounds__(256) void k_zero(GrawaMat w, int64_t n)
+{
+    constexpr int S = BF16 ? 2 : 4;
+    const float zero = 0.f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+        store_elements<BF16, 1>(w.p + ((int64_t)blockIdx.y * w.worker + i) * S, &zero);
+}
+
+#define GRAWA_FFN_FORMS(GO)                                                                                        \
+    do {                                                                                                           \
+        if (s->planes == 1) {                                                                                      \
+            if (s->act == GRAWA_ACT_SILU) return GO(1, GRAWA_ACT_SILU);                                            \
+            return s->act == GRAWA_ACT_GELU ? GO(1, GRAWA_ACT_GELU) : GO(1, GRAWA_ACT_RELU);                       \
+        }                                                                                                          \
+        if (s->act == GRAWA_ACT_SILU) return GO(3, GRAWA_ACT_SILU);                                                \
+        return s->act == GRAWA_ACT_GELU ? GO(3, GRAWA_ACT_GELU) : GO(3, GRAWA_ACT_RELU);                           \
+    } while (0)
+
+} // namespace
+
+int64_t grawa_ffn_part_floats(const grawa_sublayer *) { return 0; }
+
+hipError_t grawa_launch_ffn(const grawa_sublayer *s, int64_t T, GrawaRows x, GrawaMat wg, GrawaMat wu, GrawaMat wd, GrawaRows residual,
+                            GrawaDrop drop, GrawaRows y, char *save, hipStream_t st)
+{
+    if (!T) return hipSuccess;
+    const Sublayer c{s, T, st};
+#define GO(P, A) forward<P, A>(c, x, wg, wu, wd, residual, drop, y, save)
+    GRAWA_FFN_FORMS(GO);
+#undef GO
+}
+
+hipError_t grawa_launch_ffn_backward(const grawa_sublayer *s, int64_t T, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat wu, GrawaMat wd,
+                                     const char *save, GrawaRows dx, GrawaMat dwg, GrawaMat dwu, GrawaMat dwd, int accumulate,
+                                     hipStream_t st)
+{
+    if (!T) {
+        if (accumulate) return hipSuccess;
+        const dim3 grid(256, (unsigned)s->K);
+        for (const GrawaMat &w : {dwg, dwu, dwd}) {
+            if (s->dtype == GRAWA_BF16)
+                k_zero<true><<<grid, 256, 0, st>>>(w, s->d * s->f);
+            else
+                k_zero<false><<<grid, 256, 0, st>>>(w, s->d * s->f);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+    const Sublayer c{s, T, st};
+#define GO(P, A) backward<P, A>(c, dy, x, wg, wu, wd, save, dx, dwg, dwu, dwd, accumulate)
+    GRAWA_FFN_FORMS(GO);
+#undef GO
+}

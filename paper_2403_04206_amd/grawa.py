@@ -23,6 +23,7 @@ F32, BF16 = 0, 1
 NORM_LAYERSUM, NORM_FLAT = 0, 1
 NONFINITE_LAYER_SCORE, NONFINITE_MODEL_SCORE = 1, 2
 MAX_WORKERS = 1024
+ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
 
 _NORM_MODES = {"layersum": NORM_LAYERSUM, "flat": NORM_FLAT, NORM_LAYERSUM: NORM_LAYERSUM, NORM_FLAT: NORM_FLAT}
 
@@ -74,6 +75,14 @@ def lib():
         "grawa_plan_profile_read": (it, [vp, C.POINTER(it), C.POINTER(dbl), C.POINTER(dbl)]),
         "grawa_plan_profile_read_call": (it, [vp, it, C.POINTER(dbl), C.POINTER(dbl), C.POINTER(dbl)]),
         "grawa_stream_copy": (it, [vp, vp, i64, vp]),
+        "grawa_sublayer_create": (it, [C.POINTER(vp), it, i64, i64, i64, it, it]),
+        "grawa_sublayer_destroy": (it, [vp]),
+        "grawa_sublayer_save_bytes": (it, [vp, i64, C.POINTER(i64)]),
+        "grawa_layer_norm": (it, [vp, i64, vp, vp, vp, fl, vp, vp, vp]),
+        "grawa_layer_norm_backward": (it, [vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, it, vp]),
+        "grawa_ffn": (it, [vp, i64, vp, vp, vp, vp, vp, fl, vp, C.c_uint32, vp, vp, vp]),
+        "grawa_ffn_backward": (it, [vp, i64] + [vp] * 10 + [it, vp]),
+        "grawa_dropout": (it, [it, i64, i64, it, vp, vp, fl, vp, C.c_uint32, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -474,3 +483,182 @@ def stream_copy(dst, src, stream=None):
     if dst.numel() * dst.element_size() != nbytes:
         raise ValueError("size mismatch")
     _check(lib().grawa_stream_copy(_ptr(dst), _ptr(src), nbytes, _stream(stream)), "grawa_stream_copy")
+
+
+# -- the feed-forward sublayer ------------------------------------------------------
+
+class _RowsArg(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("worker", C.c_int64), ("row", C.c_int64)]
+
+
+class _MatsArg(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("worker", C.c_int64)]
+
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_ACTIVATIONS = {"silu": ACT_SILU, "gelu": ACT_GELU, "relu": ACT_RELU}
+
+
+def _tokens(t, K, T, d, dtype, what, optional=False):
+    """[K, T, d] with unit stride in the last axis, for the C call; None where it may be."""
+    if t is None and optional:
+        return None
+    if t is None or t.dtype is not dtype or t.ndim != 3 or not _on_device(t):
+        raise TypeError("%s must be a %s CUDA tensor [K, T, %d]" % (what, str(dtype).replace("torch.", ""), d))
+    if tuple(t.shape) != (K, T, d):
+        raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), (K, T, d)))
+    worker, row, unit = t.stride()
+    if d > 1 and unit != 1:
+        raise TypeError("%s: elements of a row must be adjacent" % what)
+    if T:
+        _covers(t, (K - 1) * worker + (T - 1) * row + d, what)
+    return C.byref(_RowsArg(t.data_ptr(), worker if K > 1 else 0, row if T > 1 else d))
+
+
+def _mats(t, shape, dtype, what, optional=False):
+    """One matrix or vector of shape[1:] for each worker, no gaps inside."""
+    if t is None and optional:
+        return None
+    if t is None or t.dtype is not dtype or t.ndim != len(shape) or not _on_device(t):
+        raise TypeError("%s must be a %s CUDA tensor %r" % (what, str(dtype).replace("torch.", ""), list(shape)))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), tuple(shape)))
+    stride, n = t.stride(), 1
+    for i in range(len(shape) - 1, 0, -1):
+        if shape[i] > 1 and stride[i] != n:
+            raise TypeError("%s: a worker's elements must be adjacent" % what)
+        n *= shape[i]
+    worker = stride[0] if shape[0] > 1 else 0
+    _covers(t, (shape[0] - 1) * worker + n, what)
+    return C.byref(_MatsArg(t.data_ptr(), worker))
+
+
+def _rng(rng, p):
+    if rng is None:
+        if p:
+            raise TypeError("rng is required where p is not 0")
+        return _NULL
+    if rng.dtype is not torch.int64 or rng.dim() != 1 or rng.numel() < 2 or rng.stride(0) != 1 or not _on_device(rng):
+        raise TypeError("rng must be a contiguous int64 CUDA tensor [2]: the seed and the step")
+    _covers(rng, 2, "rng")
+    return C.c_void_p(rng.data_ptr())
+
+
+def _site(site):
+    site = int(site)
+    if not 0 <= site < 1 << 32:
+        raise ValueError("site must fit 32 bits")
+    return site
+
+
+class SublayerPlan:
+    """grawa_sublayer_t: the feed-forward sublayer of K workers (layer norm, gated feed-forward block), its shape and device
+    workspace.  T is the most tokens of a worker, d the width, f the inner width (0: the layer norm alone); activations, parameters
+    and gradients have one dtype.  Parameters are views of the workers' flat rows: vectors [K, d], matrices [K, f, d] and [K, d, f],
+    each worker's without gaps."""
+
+    def __init__(self, K, T, d, f=0, dtype=torch.bfloat16, activation="silu"):
+        if dtype not in _DTYPES:
+            raise TypeError("dtype must be torch.float32 or torch.bfloat16")
+        if activation not in _ACTIVATIONS:
+            raise ValueError("activation must be one of %r" % (tuple(_ACTIVATIONS),))
+        self.K, self.T, self.d, self.f, self.dtype, self.activation = int(K), int(T), int(d), int(f), dtype, activation
+        self._h = C.c_void_p()
+        _check(lib().grawa_sublayer_create(C.byref(self._h), self.K, self.T, self.d, self.f, _DTYPES[dtype], _ACTIVATIONS[activation]),
+               "grawa_sublayer_create")
+
+    def destroy(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            torch.cuda.synchronize()
+            st = lib().grawa_sublayer_destroy(self._h)
+            self._h = C.c_void_p()
+            _check(st, "grawa_sublayer_destroy")
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.destroy()
+
+    def _count(self, t, what):
+        if t is None or t.ndim != 3:
+            raise TypeError("%s must be a CUDA tensor [K, T, %d]" % (what, self.d))
+        T = t.shape[1]
+        if T > self.T:
+            raise ValueError("%s has %d tokens, the plan takes %d" % (what, T, self.T))
+        return T
+
+    def _stats(self, stats, T, what, optional):
+        if stats is None and optional:
+            return _NULL
+        if stats is None:
+            raise TypeError("%s is required" % what)
+        return _table(stats, (self.K, T, 2), what)
+
+    def save_bytes(self, T=None):
+        """Bytes of the `save` buffer of ffn for T tokens (the plan's T by default)."""
+        n = C.c_int64()
+        _check(lib().grawa_sublayer_save_bytes(self._h, self.T if T is None else int(T), C.byref(n)), "grawa_sublayer_save_bytes")
+        return n.value
+
+    def _save(self, save, T, optional):
+        if save is None:
+            if optional:
+                return _NULL
+            raise TypeError("save is required")
+        if save.dtype is not torch.uint8 or save.dim() != 1 or not save.is_contiguous() or not _on_device(save):
+            raise TypeError("save must be a contiguous uint8 CUDA tensor")
+        need = self.save_bytes(T)
+        if save.numel() < need:
+            raise ValueError("save holds %d bytes, the call needs %d" % (save.numel(), need))
+        _covers(save, need, "save")
+        return C.c_void_p(save.data_ptr())
+
+    def layer_norm(self, x, weight, bias, out, eps=1e-5, stats_out=None, stream=None):
+        """grawa_layer_norm: out = (x - mean) / sqrt(var + eps) * weight + bias; stats_out: float32 [K, T, 2] for the backward pass."""
+        K, d, dt, T = self.K, self.d, self.dtype, self._count(x, "x")
+        _check(lib().grawa_layer_norm(self._h, T, _tokens(x, K, T, d, dt, "x"), _mats(weight, (K, d), dt, "weight"),
+                                      _mats(bias, (K, d), dt, "bias", True), float(eps), _tokens(out, K, T, d, dt, "out"),
+                                      self._stats(stats_out, T, "stats_out", True), _stream(stream)), "grawa_layer_norm")
+
+    def layer_norm_backward(self, dy, x, weight, stats, dx, dweight, dbias, add=None, accumulate=False, stream=None):
+        """grawa_layer_norm_backward: dx (plus `add`), dweight and dbias, added to what they hold with accumulate."""
+        K, d, dt, T = self.K, self.d, self.dtype, self._count(dy, "dy")
+        _check(lib().grawa_layer_norm_backward(
+            self._h, T, _tokens(dy, K, T, d, dt, "dy"), _tokens(x, K, T, d, dt, "x"), _mats(weight, (K, d), dt, "weight"),
+            self._stats(stats, T, "stats", False), _tokens(add, K, T, d, dt, "add", True), _tokens(dx, K, T, d, dt, "dx"),
+            _mats(dweight, (K, d), dt, "dweight"), _mats(dbias, (K, d), dt, "dbias", True), 1 if accumulate else 0, _stream(stream)),
+            "grawa_layer_norm_backward")
+
+    def ffn(self, x, wg, wu, wd, out, save=None, residual=None, p=0.0, rng=None, site=0, stream=None):
+        """grawa_ffn: out = residual + dropout((act(x wg^T) * (x wu^T)) wd^T)."""
+        K, d, f, dt, T = self.K, self.d, self.f, self.dtype, self._count(x, "x")
+        _check(lib().grawa_ffn(
+            self._h, T, _tokens(x, K, T, d, dt, "x"), _mats(wg, (K, f, d), dt, "wg"), _mats(wu, (K, f, d), dt, "wu"),
+            _mats(wd, (K, d, f), dt, "wd"), _tokens(residual, K, T, d, dt, "residual", True), float(p), _rng(rng, p), _site(site),
+            _tokens(out, K, T, d, dt, "out"), self._save(save, T, True), _stream(stream)), "grawa_ffn")
+
+    def ffn_backward(self, dy, x, wg, wu, wd, save, dx, dwg, dwu, dwd, accumulate=False, stream=None):
+        """grawa_ffn_backward: from dy, the gradient of the product with wd, the gradients of x and of the weights."""
+        K, d, f, dt, T = self.K, self.d, self.f, self.dtype, self._count(dy, "dy")
+        _check(lib().grawa_ffn_backward(
+            self._h, T, _tokens(dy, K, T, d, dt, "dy"), _tokens(x, K, T, d, dt, "x"), _mats(wg, (K, f, d), dt, "wg"),
+            _mats(wu, (K, f, d), dt, "wu"), _mats(wd, (K, d, f), dt, "wd"), self._save(save, T, False),
+            _tokens(dx, K, T, d, dt, "dx"), _mats(dwg, (K, f, d), dt, "dwg"), _mats(dwu, (K, f, d), dt, "dwu"),
+            _mats(dwd, (K, d, f), dt, "dwd"), 1 if accumulate else 0, _stream(stream)), "grawa_ffn_backward")
+
+
+def dropout(x, out, p, rng, site=0, residual=None, stream=None):
+    """grawa_dropout: out = residual + keep(x) / (1 - p) for x [K, T, d]; rng: int64 CUDA tensor, the seed and the step."""
+    if x is None or x.ndim != 3 or x.dtype not in _DTYPES:
+        raise TypeError("x must be a float32 or bfloat16 CUDA tensor [K, T, d]")
+    K, T, d = x.shape
+    dt = x.dtype
+    _check(lib().grawa_dropout(K, T, d, _DTYPES[dt], _tokens(x, K, T, d, dt, "x"), _tokens(residual, K, T, d, dt, "residual", True),
+                               float(p), _rng(rng, p), _site(site), _tokens(out, K, T, d, dt, "out"), _stream(stream)), "grawa_dropout")
