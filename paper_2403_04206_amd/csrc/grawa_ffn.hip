@@ -92,73 +92,85 @@ template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z,
     }
 }
 
+// Gate and up before the activation are kept for the backward pass as the fragments of the matrix instruction: blocks of 16 x 16, each
+// 64 lanes by 16 bytes, so that both kernels move them by whole KiB straight from and to the registers.
+__device__ __forceinline__ int64_t fragment_at(int mb, int nb, int nblocks, int lane) { return (((int64_t)mb * nblocks + nb) * 64 + lane) * 4; }
+
 // Epilogue of gate and up: H, and for a backward pass G and U.
 template <int PLANES, int ACT> struct EpiGateUp {
+    static constexpr int OUTS = 1, VEC = 8;
     char *h;            // [PLANES][K][M][pitch]
-    float *gate, *up;   // [K][M][pitch], or null
+    float *gate, *up;   // [K][fragments], or null
     int64_t plane;      // bytes between the planes of h
-    int64_t worker;     // elements of a worker
+    int64_t worker;     // elements of a worker's h
+    int64_t blocks;     // fragments of a worker, elements
     int N, pitch;
     __device__ __forceinline__ void tile(int k)
     {
         h += k * worker * 2;
         if (gate) {
-            gate += k * worker;
-            up += k * worker;
+            gate += k * blocks;
+            up += k * blocks;
         }
     }
-    __device__ __forceinline__ void put8(int m, int n, const float *g, const float *u) const
+    __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &g, grawa_f32x4 &u) const
     {
-        const int64_t at = (int64_t)m * pitch + n;
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = n + j < N ? act_of<PLANES, ACT>(g[j]) * u[j] : 0.f;
-        store_planes8<PLANES>(h + at * 2, plane, v);
         if (gate) {
-            store_elements<false, 8>((char *)(gate + at), g);
-            store_elements<false, 8>((char *)(up + at), u);
+            const int64_t at = fragment_at(mb, nb, (N + 15) >> 4, lane);
+            *(grawa_f32x4 *)(gate + at) = g;
+            *(grawa_f32x4 *)(up + at) = u;
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) g[j] = act_of<PLANES, ACT>(g[j]) * u[j];
+    }
+    __device__ __forceinline__ void put(int, int m, int n, float *v) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (n + j >= N) v[j] = 0.f;
+        store_planes8<PLANES>(h + ((int64_t)m * pitch + n) * 2, plane, v);
     }
 };
 
 // Epilogue of dH: dG and dU.
 template <int PLANES, int ACT> struct EpiBack {
+    static constexpr int OUTS = 2, VEC = 8;
     const float *gate, *up;
     char *dg, *du;
-    int64_t plane, worker;
+    int64_t plane, worker, blocks;
     int N, pitch;
     __device__ __forceinline__ void tile(int k)
     {
-        gate += k * worker;
-        up += k * worker;
+        gate += k * blocks;
+        up += k * blocks;
         dg += k * worker * 2;
         du += k * worker * 2;
     }
-    __device__ __forceinline__ void put16(int m, int n, const float *dh) const
+    __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &dh, grawa_f32x4 &out) const
+    {
+        const int64_t at = fragment_at(mb, nb, (N + 15) >> 4, lane);
+        const grawa_f32x4 g = *(const grawa_f32x4 *)(gate + at), u = *(const grawa_f32x4 *)(up + at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float a, da;
+            act_both<PLANES, ACT>(g[j], a, da);
+            out[j] = dh[j] * a;
+            dh[j] = dh[j] * u[j] * da;
+        }
+    }
+    __device__ __forceinline__ void put(int o, int m, int n, float *v) const
     {
 #pragma unroll
-        for (int q = 0; q < 2; ++q, n += 8, dh += 8) {
-            if (n >= N) break;
-            const int64_t at = (int64_t)m * pitch + n;
-            float g[8], u[8];
-            load_elements<false, 8>((const char *)(gate + at), g);
-            load_elements<false, 8>((const char *)(up + at), u);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float a, da;
-                act_both<PLANES, ACT>(g[j], a, da);
-                g[j] = n + j < N ? dh[j] * u[j] * da : 0.f;
-                u[j] = n + j < N ? dh[j] * a : 0.f;
-            }
-            store_planes8<PLANES>(dg + at * 2, plane, g);
-            store_planes8<PLANES>(du + at * 2, plane, u);
-        }
+        for (int j = 0; j < 8; ++j)
+            if (n + j >= N) v[j] = 0.f;
+        store_planes8<PLANES>((o ? du : dg) + ((int64_t)m * pitch + n) * 2, plane, v);
     }
 };
 
-// Epilogue of everything else: to an array of the caller's, rounded once, added to what is there (ACC) or dropped and added to a
+// Epilogue of everything else: to an array of the caller's, rounded once, added to what is there (accumulate) or dropped and added to a
 // residual (OUT).
 template <bool BF16, bool OUT> struct EpiStore {
+    static constexpr int OUTS = 1, VEC = BF16 ? 8 : 4;
     GrawaRows y, res;   // OUT: res.p may be null
     GrawaDrop drop;     // OUT
     int N, T, accumulate, wide;
@@ -170,31 +182,34 @@ template <bool BF16, bool OUT> struct EpiStore {
         if (OUT && res.p) res.p += (int64_t)k * res.worker * S;
         row0 = (uint32_t)k * (uint32_t)T;
     }
-    __device__ __forceinline__ void put16(int m, int n, float *v) const
+    __device__ __forceinline__ void fragment(int, int, int, grawa_f32x4 &, grawa_f32x4 &) const {}
+    __device__ __forceinline__ void put(int, int m, int n, float *v) const
     {
         constexpr int S = BF16 ? 2 : 4;
         if (OUT && drop.threshold) {
             const GrawaDropKey key = grawa_drop_key(drop);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) grawa_drop4(drop, key, row0 + (uint32_t)m, (uint32_t)n / 4 + q, v + 4 * q);
+            for (int q = 0; q < VEC / 4; ++q) grawa_drop4(drop, key, row0 + (uint32_t)m, (uint32_t)n / 4 + q, v + 4 * q);
         }
         char *p = y.p + ((int64_t)m * y.row + n) * S;
         const char *from = OUT ? (res.p ? res.p + ((int64_t)m * res.row + n) * S : nullptr) : accumulate ? p : nullptr;
-        if (wide && n + 16 <= N) {
-            float r[16] = {};
+        if (wide && n + VEC <= N) {
             if (from) {
-                load_elements<BF16, 16>(from, r);
+                float r[VEC];
+                load_elements<BF16, VEC>(from, r);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] += r[j];
+                for (int j = 0; j < VEC; ++j) v[j] += r[j];
             }
-            store_elements<BF16, 16>(p, v);
+            store_elements<BF16, VEC>(p, v);
         } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
+            for (int j = 0; j < VEC; ++j) {
                 if (n + j >= N) break;
-                float r = 0.f;
-                if (from) load_elements<BF16, 1>(from + j * S, &r);
-                r = from ? v[j] + r : v[j];
+                float r = v[j], old;
+                if (from) {
+                    load_elements<BF16, 1>(from + j * S, &old);
+                    r += old;
+                }
                 store_elements<BF16, 1>(p + j * S, &r);
             }
         }
@@ -288,12 +303,13 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
     const grawa_sublayer *s = c.s;
     const Operand ox = c.tokens(x, s->x), og = c.up_matrix(wg, s->wg), ou = c.up_matrix(wu, s->wu), od = c.down_matrix(wd, s->wd);
     const int64_t n = c.T * s->fp;
+    const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
     float *gate = (float *)save;
-    char *h = save ? save + s->K * n * 8 : s->h;
+    char *h = save ? save + s->K * blocks * 8 : s->h;
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ox, og, &ou);
-        const EpiGateUp<PLANES, ACT> epi{h, gate, gate ? gate + s->K * n : nullptr, s->K * n * 2, n, (int)s->f, (int)s->fp};
+        const EpiGateUp<PLANES, ACT> epi{h, gate, gate ? gate + s->K * blocks : nullptr, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
         c.run([&] { return launch_gemm<false, false, true>(g, epi, c.st); });
     }
     {
@@ -312,12 +328,13 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
     const Operand ox = c.tokens(x, s->x), ody = c.tokens(dy, s->dy);
     const Operand og = c.up_matrix(wg, s->wg), ou = c.up_matrix(wu, s->wu), od = c.down_matrix(wd, s->wd);
     const int64_t n = c.T * s->fp;
+    const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
     const float *gate = (const float *)save;
-    const Operand oh = c.inner((char *)save + s->K * n * 8), odg = c.inner(s->dg), odu = c.inner(s->du);
+    const Operand oh = c.inner((char *)save + s->K * blocks * 8), odg = c.inner(s->dg), odu = c.inner(s->du);
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ody, od, nullptr);
-        const EpiBack<PLANES, ACT> epi{gate, gate + s->K * n, s->dg, s->du, s->K * n * 2, n, (int)s->f, (int)s->fp};
+        const EpiBack<PLANES, ACT> epi{gate, gate + s->K * blocks, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
         c.run([&] { return launch_gemm<false, true, false>(g, epi, c.st); });
     }
     auto store = [&](const Operand &a, const Operand &b, GrawaMat w, int64_t M, int64_t N) {

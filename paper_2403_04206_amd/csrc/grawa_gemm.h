@@ -12,8 +12,7 @@
 // LDS layout, k contiguous: rows of 128 bytes, the 16-byte piece c of row r at place c ^ (r % 8), so that the sixteen rows that a
 // fragment is read from fall on different banks.  m contiguous: 64 rows of BM elements, read by the transposing LDS load, piece c of
 // row r at place c ^ 2 (r % 4 + 4 (r / 8 % 2)): the eight rows that half a wave reads from fall on different banks.
-// Fragments go into the instruction as (B, A): a lane then has four consecutive n of one m, and after an exchange between the
-// quarters of the wave sixteen, which it stores by 16 bytes.
+// Fragments go into the instruction as (B, A): a lane then has four consecutive n of one m.
 #pragma once
 #include "grawa_elements.h"
 #include "grawa_sublayer.h"
@@ -46,9 +45,9 @@ template <bool TR, int R, int NW> struct GrawaTileLoad {
     static constexpr int LOADS = R * 128 / 1024 / NW;
     static_assert(LOADS * NW * 1024 == R * 128, "whole loads");
     static_assert(!TR || R >= 128, "the swizzle of a transposed tile takes sixteen pieces");
-    uint32_t off[LOADS];
-    uint32_t ld;
-    int kpiece; // first k of the lane's piece (k contiguous only)
+    uint32_t first; // byte offset of the lane's piece in the wave's first load
+    uint32_t ld, step;
+    int kpiece;     // first k of the lane's piece (k contiguous only)
 
     __device__ __forceinline__ void init(int wave, int lane, uint32_t ld_)
     {
@@ -56,35 +55,35 @@ template <bool TR, int R, int NW> struct GrawaTileLoad {
         if constexpr (!TR) {
             const int c = (lane & 7) ^ (lane >> 3);
             kpiece = c * 8;
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) off[i] = (uint32_t)((wave + NW * i) * 8 + (lane >> 3)) * ld + c * 16;
+            first = (uint32_t)(wave * 8 + (lane >> 3)) * ld + c * 16;
+            step = NW * 8 * ld;
         } else {
             constexpr int PIECES = R / 8, RPL = 64 / PIECES;
+            static_assert(NW * RPL % 16 == 0, "a wave's loads have the same swizzle");
+            const int row = wave * RPL + lane / PIECES, p = lane % PIECES;
+            const int c = p ^ (((row & 3) | (((row >> 3) & 1) << 2)) << 1);
             kpiece = 0;
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int row = (wave + NW * i) * RPL + lane / PIECES, p = lane % PIECES;
-                const int c = p ^ (((row & 3) | (((row >> 3) & 1) << 2)) << 1);
-                off[i] = (uint32_t)row * ld + c * 16;
-            }
+            first = (uint32_t)row * ld + c * 16;
+            step = NW * RPL * ld;
         }
     }
 
-    // base: of the tile's first row (k contiguous) or column (m contiguous) at k = 0; rows: of it that the matrix has, > 0; krem: k
-    // that are left, > 0.  I0, I1: which of the loads.
-    template <int I0, int I1> __device__ __forceinline__ void go(char *lds, int wave, const char *base, int k0, int rows, int krem) const
+    // Descriptor of what the tile has: b is the address of its first row (k contiguous) or column (m contiguous) at its first k, rows
+    // (> 0) what the matrix has from there on, krem the k that are left; none: all comes as zeros and nothing is read.
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const char *b, int rows, int krem) const
     {
-        const char *b = TR ? base + (int64_t)k0 * ld : base + (int64_t)k0 * 2;
-        const uint32_t valid = TR ? (uint32_t)((krem < GRAWA_BK ? krem : GRAWA_BK) - 1) * ld + (uint32_t)(((rows < R ? rows : R) + 7) & ~7) * 2
-                                  : (uint32_t)((rows < R ? rows : R) - 1) * ld + (uint32_t)(((krem < GRAWA_BK ? krem : GRAWA_BK) + 7) & ~7) * 2;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)b, 0, valid, 0x00020000);
-        const bool tail = !TR && krem < GRAWA_BK;
-#pragma unroll
-        for (int i = I0; i < I1; ++i) {
-            uint32_t o = off[i];
-            if (tail && kpiece >= krem) o = 0x80000000u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (GRAWA_LDS void *)(lds + (wave + NW * i) * 1024), 16, o, 0, 0, 0);
-        }
+        const int kn = krem < GRAWA_BK ? krem : GRAWA_BK, rn = rows < R ? rows : R;
+        const uint32_t valid = TR ? (uint32_t)(kn - 1) * ld + (uint32_t)((rn + 7) & ~7) * 2 : (uint32_t)(rn - 1) * ld + (uint32_t)((kn + 7) & ~7) * 2;
+        return __builtin_amdgcn_make_buffer_rsrc((void *)b, 0, krem > 0 ? valid : 0, 0x00020000);
+    }
+
+    __device__ __forceinline__ void go(int i, char *lds, int wave, __amdgpu_buffer_rsrc_t r, int krem) const
+    {
+        uint32_t o = first;
+        asm("" : "+v"(o)); // worked out where it is used: held in registers these would not fit
+        o += (uint32_t)i * step;
+        if (!TR && kpiece >= krem) o = 0x80000000u; // a piece behind the last k is another row's
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS void *)(lds + (wave + NW * i) * 1024), 16, o, 0, 0, 0);
     }
 };
 
@@ -138,29 +137,35 @@ __device__ __forceinline__ GrawaTile2 grawa_tile_of(uint32_t id, uint32_t total,
     return GrawaTile2{(int)k, (int)(g * GROUP + v % rows), (int)(v / rows)};
 }
 
-// Rows of sixteen lanes: the odd ones of a change places with the even ones of b.
-__device__ __forceinline__ void swap16(float &a, float &b)
+// All but the wave's last N loads into LDS have landed and its reads from LDS are done; then the other waves' too.
+template <int N> __device__ __forceinline__ void grawa_landed()
 {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    a = __uint_as_float(r[0]);
-    b = __uint_as_float(r[1]);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
-// The upper half of a changes places with the lower half of b.
-__device__ __forceinline__ void swap32(float &a, float &b)
+// c += a b with the sums where they are.  The builtin leaves it to the register allocator whether a sum stays in its registers; it moves
+// them about, and the fragments then do not fit beside them.  The operands are waited for as any others' are.
+__device__ __forceinline__ void mfma_in_place(grawa_f32x4 &c, const grawa_bf16x8 &a, const grawa_bf16x8 &b)
 {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    a = __uint_as_float(r[0]);
-    b = __uint_as_float(r[1]);
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
 
 // The kernel.  DUAL: B is two operands, BN / 2 columns of each.  Epi: what becomes of the sums, see grawa_ffn.hip:
-//   epi.tile(worker)                       once
-//   epi.put16(m, n, v)                     sixteen columns from n on, m < M, n < N
-//   epi.put8(m, n, v, u)                   DUAL: eight columns of both products
+//   epi.tile(worker)                     once
+//   epi.fragment(mb, nb, lane, v, u)     a fragment of 16 x 16 sums, rows 16 mb ..., columns 16 nb ...: the lane has row lane % 16, columns
+//                                        4 (lane / 16) ...; v the product, with DUAL u the second one.  Leaves in v, and with OUTS = 2 in u,
+//                                        what goes on to
+//   epi.put(o, m, n, v)                  VEC columns from n on of row m of output o; m < M, n < N
+namespace {
+
 template <int BM, int BN, int WM, int WN, bool AT, bool BT, bool DUAL, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
 {
+#ifdef __HIP_DEVICE_COMPILE__ // the host pass needs the signature alone; given this body it leaves the launch stubs out without a word
     constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
     static_assert(NI == 4, "a wave has 64 columns");
     constexpr int BR = DUAL ? BN / 2 : BN; // columns of B operand in a tile
@@ -185,79 +190,149 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
     const int64_t aoff = AT ? (int64_t)m0 * 2 : (int64_t)m0 * g.lda, boff = BT ? (int64_t)n0 * 2 : (int64_t)n0 * g.ldb;
     const int mrows = g.M - m0, nrows = g.N - n0;
     const int kt = (g.len + GRAWA_BK - 1) / GRAWA_BK, tiles = kt * g.nseg;
-    int seg = 0, k0 = 0; // of the next tile to load
-    auto load = [&](char *buf) {
-        const char *pa = g.a[seg].p + tile.k * g.a[seg].worker + aoff, *pb = g.b[seg].p + tile.k * g.b[seg].worker + boff;
-        const int krem = g.len - k0;
-        la.template go<0, la.LOADS>(buf, wave, pa, k0, mrows, krem);
-        lb.template go<0, lb.LOADS>(buf + ABYTES, wave, pb, k0, nrows, krem);
-        if constexpr (DUAL) {
-            const char *pc = g.b[g.nseg + seg].p + tile.k * g.b[g.nseg + seg].worker + boff;
-            lb.template go<0, lb.LOADS>(buf + ABYTES + BR * 128, wave, pc, k0, nrows, krem);
-        }
-        k0 += GRAWA_BK;
-        if (k0 >= g.len) {
-            k0 = 0;
+    const int64_t astep = AT ? GRAWA_BK * g.lda : GRAWA_BK * 2, bstep = BT ? GRAWA_BK * g.ldb : GRAWA_BK * 2;
+    int seg = -1, krem = 0; // of the next tile to load
+    const char *pa = nullptr, *pb = nullptr, *pc = nullptr;
+    __amdgpu_buffer_rsrc_t ra, rb, rc;
+    int kload = 0; // k that the tile in the descriptors has
+    auto prepare = [&]() {
+        if (krem <= 0 && seg + 1 < g.nseg) {
             ++seg;
+            krem = g.len;
+            pa = g.a[seg].p + tile.k * g.a[seg].worker + aoff;
+            pb = g.b[seg].p + tile.k * g.b[seg].worker + boff;
+            if (DUAL) pc = g.b[g.nseg + seg].p + tile.k * g.b[g.nseg + seg].worker + boff;
         }
+        kload = krem;
+        ra = la.rsrc(pa, mrows, krem);
+        rb = lb.rsrc(pb, nrows, krem);
+        if constexpr (DUAL) rc = lb.rsrc(pc, nrows, krem);
+        pa += astep;
+        pb += bstep;
+        if (DUAL) pc += bstep;
+        krem -= GRAWA_BK;
+    };
+    constexpr int LA = GrawaTileLoad<AT, BM, NW>::LOADS, LB = GrawaTileLoad<BT, BR, NW>::LOADS, LOADS = LA + LB * (DUAL ? 2 : 1);
+    auto load = [&](char *buf, int i) {
+        if (i < LA)
+            la.go(i, buf, wave, ra, kload);
+        else if (i < LA + LB)
+            lb.go(i - LA, buf + ABYTES, wave, rb, kload);
+        else
+            lb.go(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, kload);
     };
     grawa_f32x4 acc[MI][NI] = {};
-    auto compute = [&](const char *buf) {
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            grawa_bf16x8 b[NI];
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-                b[j] = DUAL ? fb.get(buf + ABYTES + (j >= 2 ? BR * 128 : 0), j & 1, ks) : fb.get(buf + ABYTES, j, ks);
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const grawa_bf16x8 a = fa.get(buf, i, ks);
-#pragma unroll
-                for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a, acc[i][j], 0, 0, 0);
-            }
-        }
-    };
-    load(buf0);
-    __syncthreads(); // waits for the loads into LDS too
-    for (int t = 0;;) {
-        if (t + 1 < tiles) load(buf1);
-        compute(buf0);
-        __syncthreads();
-        if (++t >= tiles) break;
-        if (t + 1 < tiles) load(buf0);
-        compute(buf1);
-        __syncthreads();
-        if (++t >= tiles) break;
-    }
-
-    epi.tile(tile.k);
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const int m = m0 + wm * TM + i * 16 + (lane & 15);
-        float v[NI][4];
+    constexpr int MH = MI / 2;
+    grawa_bf16x8 a0[MH], a1[MH], b0[NI], b1[NI];
+    // Everything but the matrix instructions is issued between them, a little after each row of NI of them.
+    auto row = [&](int mh, int i, const grawa_bf16x8 &a, const grawa_bf16x8 (&b)[NI]) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < NI; ++j)
+            mfma_in_place(acc[mh * MH + i][j], b[j], a);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto read_b = [&](const char *buf, int j, int ks) {
+        return DUAL ? fb.get(buf + ABYTES + (j >= 2 ? BR * 128 : 0), j & 1, ks) : fb.get(buf + ABYTES, j, ks);
+    };
+    // One tile of 64 k, two instructions deep (ks), the upper half of the wave's rows (mh = 0) before the lower.  The fragments of its
+    // first 32 k have been read; those of the others are read behind the instructions that use a register last.  The buffer is
+    // free when every wave has read all of it, a quarter of the tile before its end: then the tile after the next goes there, and has
+    // a whole tile's time to arrive.
+    auto step = [&](char *cur, const char *next) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[j][r] = acc[i][j][r];
-        // Lane quarter q has n = 16 j + 4 q + r.
-        if constexpr (DUAL) {
+        for (int i = 0; i < MH; ++i) {
+            row(0, i, a0[i], b0);
+            a0[i] = fa.get(cur, i, 1);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                swap16(v[0][r], v[1][r]);
-                swap16(v[2][r], v[3][r]);
-            }
-            const int q = lane >> 4, n = n0 + wn * (TN / 2) + ((q & 1) << 4) + ((q >> 1) << 3);
-            if (m < g.M && n < g.N) epi.put8(m, n, v[0], v[2]); // v[0], v[1] and v[2], v[3] follow each other
-        } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                swap32(v[0][r], v[2][r]);
-                swap32(v[1][r], v[3][r]);
-                swap16(v[0][r], v[1][r]);
-                swap16(v[2][r], v[3][r]);
-            }
-            const int n = n0 + wn * TN + ((lane >> 4) << 4);
-            if (m < g.M && n < g.N) epi.put16(m, n, v[0]);
+            for (int j = i * NI / MH; j < (i + 1) * NI / MH; ++j) b1[j] = read_b(cur, j, 1);
         }
+#pragma unroll
+        for (int i = 0; i < MH; ++i) {
+            row(1, i, a1[i], b0);
+            a1[i] = fa.get(cur, MH + i, 1);
+        }
+        prepare();
+#pragma unroll
+        for (int i = 0; i < MH; ++i) row(0, i, a0[i], b1);
+        grawa_landed<0>();
+#pragma unroll
+        for (int i = 0; i < MH; ++i) {
+            row(1, i, a1[i], b1);
+            a0[i] = fa.get(next, i, 0);
+#pragma unroll
+            for (int j = i * NI / MH; j < (i + 1) * NI / MH; ++j) b0[j] = read_b(next, j, 0);
+            a1[i] = fa.get(next, MH + i, 0);
+#pragma unroll
+            for (int j = i * LOADS / MH; j < (i + 1) * LOADS / MH; ++j) load(cur, j);
+        }
+    };
+    prepare();
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) load(buf0, j);
+    prepare();
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) load(buf1, j);
+    grawa_landed<LOADS>();
+#pragma unroll
+    for (int i = 0; i < MH; ++i) a0[i] = fa.get(buf0, i, 0);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) b0[j] = read_b(buf0, j, 0);
+#pragma unroll
+    for (int i = 0; i < MH; ++i) a1[i] = fa.get(buf0, MH + i, 0);
+    for (int t = 0; t < tiles; t += 2) { // tiles that are not there are zeros
+        step(buf0, buf1);
+        step(buf1, buf0);
     }
+    grawa_landed<0>(); // nothing may be on its way into LDS when the block ends
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); // the last sums are written: the compiler does not see which instructions write them
+
+    // A lane has four consecutive columns of one row of every fragment.  What goes to rows in memory passes through a corner of LDS of the
+    // wave's own, sixteen rows at a time, so that a store instruction writes whole runs of a row: straight from the fragments it would
+    // write 64 separate pieces of 16 bytes.  The 16-byte piece c of row r stands at place c ^ r.
+    epi.tile(tile.k);
+    constexpr int NJ = DUAL ? NI / 2 : NI, COLS = NJ * 16, PIECES = COLS / 4, LPR = COLS / Epi::VEC, ROWS = 64 / LPR;
+    static_assert(NW * Epi::OUTS * 16 * COLS * 4 <= ABYTES + BBYTES, "the corners fit a buffer");
+    float *const corner = (float *)buf0 + wave * (Epi::OUTS * 16 * COLS);
+    const int n1 = n0 + wn * COLS;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int m1 = m0 + wm * TM + i * 16;
+        if (m1 >= g.M) break;
+        grawa_f32x4 v[Epi::OUTS][NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            v[0][j] = acc[i][j];
+            grawa_f32x4 second = DUAL ? acc[i][j + NI - NJ] : grawa_f32x4{};
+            if (n1 + j * 16 < g.N) epi.fragment(m1 >> 4, (n1 >> 4) + j, lane, v[0][j], second);
+            if constexpr (Epi::OUTS > 1) v[1][j] = second;
+        }
+#pragma unroll
+        for (int o = 0; o < Epi::OUTS; ++o)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int r = lane & 15, c = 4 * j + (lane >> 4);
+                *(grawa_f32x4 *)(corner + o * 16 * COLS + r * COLS + (c ^ (r & (PIECES - 1))) * 4) = v[o][j];
+            }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int o = 0; o < Epi::OUTS; ++o)
+#pragma unroll
+            for (int q = 0; q < 16 / ROWS; ++q) {
+                const int r = q * ROWS + lane / LPR, n = n1 + lane % LPR * Epi::VEC;
+                float w[Epi::VEC];
+#pragma unroll
+                for (int x = 0; x < Epi::VEC / 4; ++x) {
+                    const int c = lane % LPR * (Epi::VEC / 4) + x;
+                    const grawa_f32x4 u = *(const grawa_f32x4 *)(corner + o * 16 * COLS + r * COLS + (c ^ (r & (PIECES - 1))) * 4);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) w[4 * x + y] = u[y];
+                }
+                if (m1 + r < g.M && n < g.N) epi.put(o, m1 + r, n, w);
+            }
+        __builtin_amdgcn_wave_barrier();
+    }
+#endif
 }
+
+} // namespace

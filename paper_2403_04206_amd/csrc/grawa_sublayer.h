@@ -42,9 +42,14 @@ struct GrawaMat {
 
 static inline int64_t grawa_round8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 
-// The buffer that a training forward leaves to its backward: gate and up before the activation in float32, [K][T][fp] each, then
+static inline int64_t grawa_round16(int64_t n) { return (n + 15) & ~(int64_t)15; }
+
+// The buffer that a training forward leaves to its backward: gate and up before the activation in float32, in fragments of 16 x 16, then
 // their product in bfloat16 planes, [planes][K][T][fp].
-static inline int64_t grawa_save_bytes(const grawa_sublayer *s, int64_t T) { return (int64_t)s->K * T * s->fp * (8 + 2 * s->planes); }
+static inline int64_t grawa_save_bytes(const grawa_sublayer *s, int64_t T)
+{
+    return (int64_t)s->K * (grawa_round16(T) * grawa_round16(s->f) * 8 + T * s->fp * 2 * s->planes);
+}
 
 hipError_t grawa_launch_layer_norm(const grawa_sublayer *s, int64_t T, GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y,
                                    float *stats, hipStream_t st);
