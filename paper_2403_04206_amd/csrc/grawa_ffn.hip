@@ -94,7 +94,6 @@ template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z,
 
 // Gate and up before the activation are kept for the backward pass as the fragments of the matrix instruction: blocks of 16 x 16, each
 // 64 lanes by 16 bytes, so that both kernels move them by whole KiB straight from and to the registers.
-__device__ __forceinline__ int64_t fragment_at(int mb, int nb, int nblocks, int lane) { return (((int64_t)mb * nblocks + nb) * 64 + lane) * 4; }
 
 // Epilogue of gate and up: H, and for a backward pass G and U.
 template <int PLANES, int ACT> struct EpiGateUp {
@@ -105,7 +104,7 @@ template <int PLANES, int ACT> struct EpiGateUp {
     int64_t worker;     // elements of a worker's h
     int64_t blocks;     // fragments of a worker, elements
     int N, pitch;
-    __device__ __forceinline__ void tile(int k)
+    __device__ __forceinline__ void tile(int k, int)
     {
         h += k * worker * 2;
         if (gate) {
@@ -116,7 +115,7 @@ template <int PLANES, int ACT> struct EpiGateUp {
     __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &g, grawa_f32x4 &u) const
     {
         if (gate) {
-            const int64_t at = fragment_at(mb, nb, (N + 15) >> 4, lane);
+            const int64_t at = grawa_fragment_at(mb, nb, (N + 15) >> 4, lane);
             *(grawa_f32x4 *)(gate + at) = g;
             *(grawa_f32x4 *)(up + at) = u;
         }
@@ -139,7 +138,7 @@ template <int PLANES, int ACT> struct EpiBack {
     char *dg, *du;
     int64_t plane, worker, blocks;
     int N, pitch;
-    __device__ __forceinline__ void tile(int k)
+    __device__ __forceinline__ void tile(int k, int)
     {
         gate += k * blocks;
         up += k * blocks;
@@ -148,7 +147,7 @@ template <int PLANES, int ACT> struct EpiBack {
     }
     __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &dh, grawa_f32x4 &out) const
     {
-        const int64_t at = fragment_at(mb, nb, (N + 15) >> 4, lane);
+        const int64_t at = grawa_fragment_at(mb, nb, (N + 15) >> 4, lane);
         const grawa_f32x4 g = *(const grawa_f32x4 *)(gate + at), u = *(const grawa_f32x4 *)(up + at);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -175,7 +174,7 @@ template <bool BF16, bool OUT> struct EpiStore {
     GrawaDrop drop;     // OUT
     int N, T, accumulate, wide;
     uint32_t row0;      // of the worker, for the dropout
-    __device__ __forceinline__ void tile(int k)
+    __device__ __forceinline__ void tile(int k, int)
     {
         constexpr int S = BF16 ? 2 : 4;
         y.p += (int64_t)k * y.worker * S;
@@ -225,16 +224,63 @@ struct Operand {
 
 constexpr int64_t MAX_LD = ((int64_t)1 << 31) / 256 - 128; // bytes; a tile's offsets have 31 bits
 
-template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const GrawaGemm &g, const Epi &epi, hipStream_t st)
+// How a product is cut: tiles of 256 x 256 or 128 x 128, and the parts that its sum over k is split into.
+struct Cut {
+    bool large;
+    int splits;
+    int64_t tiles;
+};
+
+constexpr int64_t PART_FLOATS = (int64_t)512 * 256 * 256; // most that the parts of a product take
+constexpr int MAX_SPLITS = 16;
+
+// The cut with the least time by what was measured (us): a tile of 64 k takes 1.75 in a block of 256 x 256, of which a CU holds one; in
+// one of 128 x 128 it takes 1.3 where a CU holds two and 0.75 where it has one; a block costs about three such tiles more; parts are
+// written and read at 4 TB/s by a launch more.
+Cut cut_of(int64_t K, int64_t M, int64_t N, int64_t ktiles, bool dual, int64_t part_floats)
 {
-    auto tiles = [&](int bm, int bn) { return (int64_t)g.K * ((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
-    // Tiles of 256 x 256 where they give each CU one, else of 128 x 128, of which a CU takes two at a time.
-    const int64_t large = tiles(256, DUAL ? 128 : 256);
-    if (large >= 256) {
-        k_gemm<256, 256, 2, 4, AT, BT, DUAL, Epi><<<dim3((unsigned)large), 512, 0, st>>>(g, epi);
+    Cut best{};
+    double least = 0;
+    const int64_t padded = K * grawa_round16(M) * grawa_round16(N) * (dual ? 2 : 1);
+    for (int large = 1; large >= 0; --large) {
+        const int64_t bm = large ? 256 : 128, bn = dual ? bm / 2 : bm;
+        const int64_t tiles = K * ((M + bm - 1) / bm) * ((N + bn - 1) / bn), slots = large ? 256 : 512;
+        for (int s = 1; s <= MAX_SPLITS; ++s) {
+            if (s > 1 && (s * padded > part_floats || ktiles / s < 4 || s * tiles > 2 * slots)) break;
+            const int64_t rounds = (s * tiles + slots - 1) / slots;
+            double us = (double)rounds * ((double)((ktiles + s - 1) / s) + 3) * (large ? 1.75 : s * tiles <= 256 ? 0.75 : 1.3);
+            if (s > 1) us += 5 + 8e-6 * (double)(s * padded) / 4;
+            if (!best.splits || us < least) {
+                best = Cut{large != 0, s, tiles};
+                least = us;
+            }
+        }
+    }
+    return best;
+}
+
+template <bool AT, bool BT, bool DUAL, class Epi> void launch_tiles(const GrawaGemm &g, const Cut &cut, const Epi &epi, hipStream_t st)
+{
+    const dim3 grid((unsigned)(cut.tiles * cut.splits));
+    if (cut.large)
+        k_gemm<256, 256, 2, 4, AT, BT, DUAL, Epi><<<grid, 512, 0, st>>>(g, epi);
+    else
+        k_gemm<128, 128, 2, 2, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
+}
+
+template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const grawa_sublayer *s, GrawaGemm g, const Epi &epi, hipStream_t st)
+{
+    const Cut cut = cut_of(g.K, g.M, g.N, (int64_t)((g.len + GRAWA_BK - 1) / GRAWA_BK) * g.nseg, DUAL, s->part_floats);
+    g.splits = cut.splits;
+    if (cut.splits == 1) {
+        launch_tiles<AT, BT, DUAL>(g, cut, epi, st);
     } else {
-        const int64_t small = tiles(128, DUAL ? 64 : 128);
-        k_gemm<128, 128, 2, 2, AT, BT, DUAL, Epi><<<dim3((unsigned)small), 256, 0, st>>>(g, epi);
+        const int64_t blocks = grawa_round16(g.M) * grawa_round16(g.N);
+        const GrawaParts parts{s->part, blocks, g.K, DUAL ? 2 : 1, (g.N + 15) >> 4};
+        launch_tiles<AT, BT, DUAL>(g, cut, EpiParts{parts, nullptr, nullptr}, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        k_join<DUAL, Epi><<<dim3((unsigned)((g.N + 127) / 128), (unsigned)((g.M + 15) / 16), (unsigned)g.K), 256, 0, st>>>(parts, cut.splits, g.M, g.N, epi);
     }
     return hipGetLastError();
 }
@@ -310,13 +356,13 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ox, og, &ou);
         const EpiGateUp<PLANES, ACT> epi{h, gate, gate ? gate + s->K * blocks : nullptr, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
-        c.run([&] { return launch_gemm<false, false, true>(g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, false, true>(s, g, epi, c.st); });
     }
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
         add_segments(g, PLANES, c.inner(h), od, nullptr);
         const EpiStore<PLANES == 1, true> epi{y, residual, drop, (int)s->d, (int)c.T, 0, c.wide(y) && (!residual.p || c.wide(residual)), 0};
-        c.run([&] { return launch_gemm<false, false, false>(g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, false, false>(s, g, epi, c.st); });
     }
     return c.err;
 }
@@ -335,14 +381,14 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ody, od, nullptr);
         const EpiBack<PLANES, ACT> epi{gate, gate + s->K * blocks, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
-        c.run([&] { return launch_gemm<false, true, false>(g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
     auto store = [&](const Operand &a, const Operand &b, GrawaMat w, int64_t M, int64_t N) {
         GrawaGemm g = c.product(M, N, c.T);
         add_segments(g, PLANES, a, b, nullptr);
         const GrawaRows out{w.p, w.worker, N};
         const EpiStore<PLANES == 1, false> epi{out, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, c.wide(out), 0};
-        c.run([&] { return launch_gemm<true, true, false>(g, epi, c.st); });
+        c.run([&] { return launch_gemm<true, true, false>(s, g, epi, c.st); });
     };
     store(odg, ox, dwg, s->f, s->d);
     store(odu, ox, dwu, s->f, s->d);
@@ -352,7 +398,7 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
         add_segments(g, PLANES, odg, og, nullptr);
         add_segments(g, PLANES, odu, ou, nullptr);
         const EpiStore<PLANES == 1, false> epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, c.wide(dx), 0};
-        c.run([&] { return launch_gemm<false, true, false>(g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
     return c.err;
 }
@@ -378,7 +424,16 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_zero(GrawaMat w, i
 
 } // namespace
 
-int64_t grawa_ffn_part_floats(const grawa_sublayer *) { return 0; }
+// Enough for every product of a call of at most T tokens: MAX_SPLITS parts of the largest one, but no more than a product's parts may
+// take.
+int64_t grawa_ffn_part_floats(const grawa_sublayer *s)
+{
+    const int64_t t = grawa_round16(s->T), d = grawa_round16(s->d), f = grawa_round16(s->f);
+    int64_t most = 2 * t * f;
+    for (const int64_t n : {t * d, d * f}) most = most > n ? most : n;
+    most *= s->K * MAX_SPLITS;
+    return most < PART_FLOATS ? most : PART_FLOATS;
+}
 
 hipError_t grawa_launch_ffn(const grawa_sublayer *s, int64_t T, GrawaRows x, GrawaMat wg, GrawaMat wu, GrawaMat wd, GrawaRows residual,
                             GrawaDrop drop, GrawaRows y, char *save, hipStream_t st)

@@ -34,6 +34,7 @@ struct GrawaGemm {
     int M, N;         // of one worker; with two B operands N counts the columns of one
     int len;          // k of a segment, > 0; where k is contiguous a row holds zeros from there to the next multiple of 8
     int nseg;
+    int splits;       // blocks that share a tile's sum, each a run of its tiles of 64 k
     int64_t lda, ldb; // bytes between rows as stored, times 256 below 2^31
     GrawaSeg a[GRAWA_MAX_SEGS], b[GRAWA_MAX_SEGS]; // two B operands: the second's segments from nseg on
 };
@@ -124,17 +125,17 @@ template <bool TR, int R, int N> struct GrawaFrag {
 // Which tile a block makes.  Blocks go round the eight XCDs; each XCD gets a run of consecutive tiles, in which GROUP rows of tiles
 // are walked column by column, so that the tiles that are worked on at a time share rows and columns in that XCD's L2.
 struct GrawaTile2 {
-    int k, m, n;
+    int k, m, n, split;
 };
 
-__device__ __forceinline__ GrawaTile2 grawa_tile_of(uint32_t id, uint32_t total, uint32_t tm, uint32_t tn)
+__device__ __forceinline__ GrawaTile2 grawa_tile_of(uint32_t id, uint32_t total, uint32_t tm, uint32_t tn, uint32_t workers)
 {
     constexpr uint32_t GROUP = 8;
     const uint32_t q = total / 8, r = total % 8, xcd = id % 8;
     const uint32_t t = xcd * q + (xcd < r ? xcd : r) + id / 8;
-    const uint32_t k = t / (tm * tn), u = t - k * (tm * tn);
+    const uint32_t ks = t / (tm * tn), u = t - ks * (tm * tn), split = ks / workers, k = ks - split * workers;
     const uint32_t g = u / (GROUP * tn), rows = tm - g * GROUP < GROUP ? tm - g * GROUP : GROUP, v = u - g * GROUP * tn;
-    return GrawaTile2{(int)k, (int)(g * GROUP + v % rows), (int)(v / rows)};
+    return GrawaTile2{(int)k, (int)(g * GROUP + v % rows), (int)(v / rows), (int)split};
 }
 
 // All but the wave's last N loads into LDS have landed and its reads from LDS are done; then the other waves' too.
@@ -154,12 +155,52 @@ __device__ __forceinline__ void mfma_in_place(grawa_f32x4 &c, const grawa_bf16x8
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
 
-// The kernel.  DUAL: B is two operands, BN / 2 columns of each.  Epi: what becomes of the sums, see grawa_ffn.hip:
-//   epi.tile(worker)                     once
+// What becomes of the sums is up to an epilogue, see grawa_ffn.hip:
+//   epi.tile(worker, split)              once
 //   epi.fragment(mb, nb, lane, v, u)     a fragment of 16 x 16 sums, rows 16 mb ..., columns 16 nb ...: the lane has row lane % 16, columns
-//                                        4 (lane / 16) ...; v the product, with DUAL u the second one.  Leaves in v, and with OUTS = 2 in u,
-//                                        what goes on to
+//                                        4 (lane / 16) ...; v the product, u the second one where there are two.  Leaves in v, and
+//                                        with OUTS = 2 in u, what goes on to
 //   epi.put(o, m, n, v)                  VEC columns from n on of row m of output o; m < M, n < N
+// Sixteen rows of NJ fragments of a wave.  A lane has four consecutive columns of one row of every fragment.  What goes to rows in memory
+// passes through a corner of LDS of the wave's own, so that a store instruction writes whole runs of a row: straight from the
+// fragments it would write 64 separate pieces of 16 bytes.  The 16-byte piece c of row r stands at place c ^ r.
+template <int NJ, class Epi>
+__device__ __forceinline__ void grawa_finish(const Epi &epi, float *corner, int m1, int n1, int lane, int M, int N, grawa_f32x4 (&v)[NJ], grawa_f32x4 (&u)[NJ])
+{
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+        if (n1 + j * 16 < N) epi.fragment(m1 >> 4, (n1 >> 4) + j, lane, v[j], u[j]);
+    if constexpr (Epi::OUTS > 0) {
+        constexpr int COLS = NJ * 16, PIECES = COLS / 4, LPR = COLS / Epi::VEC, ROWS = 64 / LPR < 16 ? 64 / LPR : 16;
+#pragma unroll
+        for (int o = 0; o < Epi::OUTS; ++o)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int r = lane & 15, c = 4 * j + (lane >> 4);
+                *(grawa_f32x4 *)(corner + o * 16 * COLS + r * COLS + (c ^ (r & (PIECES - 1))) * 4) = o ? u[j] : v[j];
+            }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int o = 0; o < Epi::OUTS; ++o)
+#pragma unroll
+            for (int q = 0; q < 16 / ROWS; ++q) {
+                const int r = q * ROWS + lane / LPR, n = n1 + lane % LPR * Epi::VEC;
+                if (ROWS * LPR < 64 && lane >= ROWS * LPR) break;
+                float w[Epi::VEC];
+#pragma unroll
+                for (int x = 0; x < Epi::VEC / 4; ++x) {
+                    const int c = lane % LPR * (Epi::VEC / 4) + x;
+                    const grawa_f32x4 t = *(const grawa_f32x4 *)(corner + o * 16 * COLS + r * COLS + (c ^ (r & (PIECES - 1))) * 4);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) w[4 * x + y] = t[y];
+                }
+                if (m1 + r < M && n < N) epi.put(o, m1 + r, n, w);
+            }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// The kernel.  DUAL: B is two operands, BN / 2 columns of each.
 namespace {
 
 template <int BM, int BN, int WM, int WN, bool AT, bool BT, bool DUAL, class Epi>
@@ -175,7 +216,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const uint32_t tm = (uint32_t)(g.M + BM - 1) / BM, tn = (uint32_t)(g.N + BR - 1) / BR;
-    const GrawaTile2 tile = grawa_tile_of(blockIdx.x, gridDim.x, tm, tn);
+    const GrawaTile2 tile = grawa_tile_of(blockIdx.x, gridDim.x, tm, tn, (uint32_t)g.K);
     const int m0 = tile.m * BM, n0 = tile.n * BR;
 
     GrawaTileLoad<AT, BM, NW> la;
@@ -189,28 +230,31 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
 
     const int64_t aoff = AT ? (int64_t)m0 * 2 : (int64_t)m0 * g.lda, boff = BT ? (int64_t)n0 * 2 : (int64_t)n0 * g.ldb;
     const int mrows = g.M - m0, nrows = g.N - n0;
-    const int kt = (g.len + GRAWA_BK - 1) / GRAWA_BK, tiles = kt * g.nseg;
+    const int kt = (g.len + GRAWA_BK - 1) / GRAWA_BK, all = kt * g.nseg;
+    const int t0 = (int)((int64_t)all * tile.split / g.splits), tiles = (int)((int64_t)all * (tile.split + 1) / g.splits) - t0;
     const int64_t astep = AT ? GRAWA_BK * g.lda : GRAWA_BK * 2, bstep = BT ? GRAWA_BK * g.ldb : GRAWA_BK * 2;
-    int seg = -1, krem = 0; // of the next tile to load
+    int seg = t0 / kt, skip = t0 - seg * kt, todo = tiles, krem = 0; // of the next tile to load
     const char *pa = nullptr, *pb = nullptr, *pc = nullptr;
     __amdgpu_buffer_rsrc_t ra, rb, rc;
     int kload = 0; // k that the tile in the descriptors has
     auto prepare = [&]() {
-        if (krem <= 0 && seg + 1 < g.nseg) {
+        if (krem <= 0 && todo > 0) {
+            pa = g.a[seg].p + tile.k * g.a[seg].worker + aoff + skip * astep;
+            pb = g.b[seg].p + tile.k * g.b[seg].worker + boff + skip * bstep;
+            if (DUAL) pc = g.b[g.nseg + seg].p + tile.k * g.b[g.nseg + seg].worker + boff + skip * bstep;
+            krem = g.len - skip * GRAWA_BK;
+            skip = 0;
             ++seg;
-            krem = g.len;
-            pa = g.a[seg].p + tile.k * g.a[seg].worker + aoff;
-            pb = g.b[seg].p + tile.k * g.b[seg].worker + boff;
-            if (DUAL) pc = g.b[g.nseg + seg].p + tile.k * g.b[g.nseg + seg].worker + boff;
         }
-        kload = krem;
-        ra = la.rsrc(pa, mrows, krem);
-        rb = lb.rsrc(pb, nrows, krem);
-        if constexpr (DUAL) rc = lb.rsrc(pc, nrows, krem);
+        kload = todo > 0 ? krem : 0;
+        ra = la.rsrc(pa, mrows, kload);
+        rb = lb.rsrc(pb, nrows, kload);
+        if constexpr (DUAL) rc = lb.rsrc(pc, nrows, kload);
         pa += astep;
         pb += bstep;
         if (DUAL) pc += bstep;
         krem -= GRAWA_BK;
+        --todo;
     };
     constexpr int LA = GrawaTileLoad<AT, BM, NW>::LOADS, LB = GrawaTileLoad<BT, BR, NW>::LOADS, LOADS = LA + LB * (DUAL ? 2 : 1);
     auto load = [&](char *buf, int i) {
@@ -287,52 +331,71 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
     grawa_landed<0>(); // nothing may be on its way into LDS when the block ends
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); // the last sums are written: the compiler does not see which instructions write them
 
-    // A lane has four consecutive columns of one row of every fragment.  What goes to rows in memory passes through a corner of LDS of the
-    // wave's own, sixteen rows at a time, so that a store instruction writes whole runs of a row: straight from the fragments it would
-    // write 64 separate pieces of 16 bytes.  The 16-byte piece c of row r stands at place c ^ r.
-    epi.tile(tile.k);
-    constexpr int NJ = DUAL ? NI / 2 : NI, COLS = NJ * 16, PIECES = COLS / 4, LPR = COLS / Epi::VEC, ROWS = 64 / LPR;
+    epi.tile(tile.k, tile.split);
+    constexpr int NJ = DUAL ? NI / 2 : NI, COLS = NJ * 16;
     static_assert(NW * Epi::OUTS * 16 * COLS * 4 <= ABYTES + BBYTES, "the corners fit a buffer");
-    float *const corner = (float *)buf0 + wave * (Epi::OUTS * 16 * COLS);
-    const int n1 = n0 + wn * COLS;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         const int m1 = m0 + wm * TM + i * 16;
         if (m1 >= g.M) break;
-        grawa_f32x4 v[Epi::OUTS][NJ];
+        grawa_f32x4 v[NJ], u[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-            v[0][j] = acc[i][j];
-            grawa_f32x4 second = DUAL ? acc[i][j + NI - NJ] : grawa_f32x4{};
-            if (n1 + j * 16 < g.N) epi.fragment(m1 >> 4, (n1 >> 4) + j, lane, v[0][j], second);
-            if constexpr (Epi::OUTS > 1) v[1][j] = second;
+            v[j] = acc[i][j];
+            u[j] = DUAL ? acc[i][j + NI - NJ] : grawa_f32x4{};
         }
-#pragma unroll
-        for (int o = 0; o < Epi::OUTS; ++o)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int r = lane & 15, c = 4 * j + (lane >> 4);
-                *(grawa_f32x4 *)(corner + o * 16 * COLS + r * COLS + (c ^ (r & (PIECES - 1))) * 4) = v[o][j];
-            }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int o = 0; o < Epi::OUTS; ++o)
-#pragma unroll
-            for (int q = 0; q < 16 / ROWS; ++q) {
-                const int r = q * ROWS + lane / LPR, n = n1 + lane % LPR * Epi::VEC;
-                float w[Epi::VEC];
-#pragma unroll
-                for (int x = 0; x < Epi::VEC / 4; ++x) {
-                    const int c = lane % LPR * (Epi::VEC / 4) + x;
-                    const grawa_f32x4 u = *(const grawa_f32x4 *)(corner + o * 16 * COLS + r * COLS + (c ^ (r & (PIECES - 1))) * 4);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) w[4 * x + y] = u[y];
-                }
-                if (m1 + r < g.M && n < g.N) epi.put(o, m1 + r, n, w);
-            }
-        __builtin_amdgcn_wave_barrier();
+        grawa_finish<NJ>(epi, (float *)buf0 + wave * (Epi::OUTS * 16 * COLS), m1, n0 + wn * COLS, lane, g.M, g.N, v, u);
     }
 #endif
+}
+
+// Where a sum over k is split: the parts as fragments, [split][worker][product][fragments].
+struct GrawaParts {
+    float *p;
+    int64_t blocks; // fragments of a product of a worker, elements
+    int K, products, nb;
+    __device__ __forceinline__ const float *at(int k, int split, int product) const { return p + (((int64_t)split * K + k) * products + product) * blocks; }
+};
+
+__device__ __forceinline__ int64_t grawa_fragment_at(int mb, int nb, int nblocks, int lane) { return (((int64_t)mb * nblocks + nb) * 64 + lane) * 4; }
+
+struct EpiParts {
+    static constexpr int OUTS = 0, VEC = 4;
+    GrawaParts parts;
+    float *v0, *u0;
+    __device__ __forceinline__ void tile(int k, int split)
+    {
+        v0 = const_cast<float *>(parts.at(k, split, 0));
+        u0 = const_cast<float *>(parts.at(k, split, parts.products - 1));
+    }
+    __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &v, grawa_f32x4 &u) const
+    {
+        const int64_t at = grawa_fragment_at(mb, nb, parts.nb, lane);
+        *(grawa_f32x4 *)(v0 + at) = v;
+        if (parts.products > 1) *(grawa_f32x4 *)(u0 + at) = u;
+    }
+    __device__ __forceinline__ void put(int, int, int, float *) const {}
+};
+
+// The parts added, in order, and the product's own epilogue: a wave for sixteen rows of 32 columns.
+template <bool DUAL, class Epi> __global__ __launch_bounds__(256) void k_join(GrawaParts parts, int splits, int M, int N, Epi epi)
+{
+    constexpr int NJ = 2;
+    __shared__ __attribute__((aligned(16))) float corners[4][Epi::OUTS * 16 * NJ * 16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = blockIdx.z;
+    const int m1 = blockIdx.y * 16, n1 = (blockIdx.x * 4 + wave) * NJ * 16;
+    if (n1 >= N) return;
+    grawa_f32x4 v[NJ] = {}, u[NJ] = {};
+    for (int s = 0; s < splits; ++s)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            if (n1 + j * 16 < N) {
+                const int64_t at = grawa_fragment_at(m1 >> 4, (n1 >> 4) + j, parts.nb, lane);
+                v[j] += *(const grawa_f32x4 *)(parts.at(k, s, 0) + at);
+                if (DUAL) u[j] += *(const grawa_f32x4 *)(parts.at(k, s, 1) + at);
+            }
+    epi.tile(k, 0);
+    grawa_finish<NJ>(epi, corners[wave], m1, n1, lane, M, N, v, u);
 }
 
 } // namespace
