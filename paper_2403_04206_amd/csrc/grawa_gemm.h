@@ -47,6 +47,7 @@ template <bool TR, int R, int NW> struct GrawaTileLoad {
     static_assert(LOADS * NW * 1024 == R * 128, "whole loads");
     static_assert(!TR || R >= 128, "the swizzle of a transposed tile takes sixteen pieces");
     uint32_t first; // byte offset of the lane's piece in the wave's first load
+    uint32_t odd;   // where loads take turns between two swizzles, that of the second
     uint32_t ld, step;
     int kpiece;     // first k of the lane's piece (k contiguous only)
 
@@ -56,18 +57,23 @@ template <bool TR, int R, int NW> struct GrawaTileLoad {
         if constexpr (!TR) {
             const int c = (lane & 7) ^ (lane >> 3);
             kpiece = c * 8;
+            odd = 0;
             first = (uint32_t)(wave * 8 + (lane >> 3)) * ld + c * 16;
             step = NW * 8 * ld;
         } else {
-            constexpr int PIECES = R / 8, RPL = 64 / PIECES;
-            static_assert(NW * RPL % 16 == 0, "a wave's loads have the same swizzle");
-            const int row = wave * RPL + lane / PIECES, p = lane % PIECES;
-            const int c = p ^ (((row & 3) | (((row >> 3) & 1) << 2)) << 1);
+            const int row = row_of(wave, lane), p = lane % (R / 8);
             kpiece = 0;
-            first = (uint32_t)row * ld + c * 16;
-            step = NW * RPL * ld;
+            first = (uint32_t)row * ld + (uint32_t)(p ^ key(row)) * 16;
+            odd = TURN ? (uint32_t)(row + 8) * ld + (uint32_t)(p ^ key(row + 8)) * 16 : 0;
+            step = (TURN ? 16 : NW * RPL) * ld;
         }
     }
+
+    static constexpr int RPL = 512 / R;                    // rows of a transposed tile in a load
+    static constexpr bool TURN = TR && NW * RPL == 8;      // a wave's loads are 8 rows apart: every other one has another swizzle
+    static_assert(!TR || TURN || NW * RPL % 16 == 0, "the swizzles of a wave's loads");
+    static __device__ __forceinline__ int row_of(int wave, int lane) { return wave * RPL + lane / (R / 8); }
+    static __device__ __forceinline__ int key(int row) { return ((row & 3) | (((row >> 3) & 1) << 2)) << 1; }
 
     // Descriptor of what the tile has: b is the address of its first row (k contiguous) or column (m contiguous) at its first k, rows
     // (> 0) what the matrix has from there on, krem the k that are left; none: all comes as zeros and nothing is read.
@@ -78,13 +84,27 @@ template <bool TR, int R, int NW> struct GrawaTileLoad {
         return __builtin_amdgcn_make_buffer_rsrc((void *)b, 0, krem > 0 ? valid : 0, 0x00020000);
     }
 
-    __device__ __forceinline__ void go(int i, char *lds, int wave, __amdgpu_buffer_rsrc_t r, int krem) const
+    // Offset of the 128-byte line that a lane below PF asks for when a quarter of a tile's lines is fetched into L2 ahead of its loads.
+    static constexpr int PF = R / 4 / NW;
+    static __device__ __forceinline__ uint32_t line(int quarter, int wave, int lane, uint32_t ld)
     {
-        uint32_t o = first;
-        asm("" : "+v"(o)); // worked out where it is used: held in registers these would not fit
-        o += (uint32_t)i * step;
-        if (!TR && kpiece >= krem) o = 0x80000000u; // a piece behind the last k is another row's
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS void *)(lds + (wave + NW * i) * 1024), 16, o, 0, 0, 0);
+        const int i = quarter * (R / 4) + wave * PF + lane;
+        return lane < PF ? (TR ? (uint32_t)(i / (R / 64)) * ld + (uint32_t)(i % (R / 64)) * 128 : (uint32_t)i * ld) : 0x80000000u;
+    }
+    static __device__ __forceinline__ void fetch(char *lds, __amdgpu_buffer_rsrc_t r, uint32_t at)
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS void *)lds, 4, at, 0, 0, 0);
+    }
+
+    // Where the lane's first piece of a tile is; a piece behind the last k is another row's and comes as zeros, in this load and in those
+    // that add a multiple of `step` (below 2^31) to it.
+    __device__ __forceinline__ uint32_t place(int krem) const { return !TR && kpiece >= krem ? 0x80000000u : first; }
+
+    __device__ __forceinline__ void go(int i, char *lds, int wave, __amdgpu_buffer_rsrc_t r, uint32_t at) const
+    {
+        if (TURN && i % 2) at = odd;
+        asm("" : "+v"(at)); // the sum is formed where it is used: held in registers the sums would not fit
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS void *)(lds + (wave + NW * i) * 1024), 16, at + (uint32_t)(TURN ? i / 2 : i) * step, 0, 0, 0);
     }
 };
 
@@ -208,11 +228,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
 {
 #ifdef __HIP_DEVICE_COMPILE__ // the host pass needs the signature alone; given this body it leaves the launch stubs out without a word
     constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
-    static_assert(NI == 4, "a wave has 64 columns");
+    constexpr int NG = DUAL ? NI / 2 : NI; // fragments of a B operand
     constexpr int BR = DUAL ? BN / 2 : BN; // columns of B operand in a tile
     constexpr int ABYTES = BM * 128, BBYTES = BN * 128;
     __shared__ __attribute__((aligned(1024))) char buf0[ABYTES + BBYTES];
     __shared__ __attribute__((aligned(1024))) char buf1[ABYTES + BBYTES];
+    __shared__ __attribute__((aligned(1024))) char unread[NW * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const uint32_t tm = (uint32_t)(g.M + BM - 1) / BM, tn = (uint32_t)(g.N + BR - 1) / BR;
@@ -224,9 +245,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
     la.init(wave, lane, (uint32_t)g.lda);
     lb.init(wave, lane, (uint32_t)g.ldb);
     GrawaFrag<AT, BM, MI> fa;
-    GrawaFrag<BT, BR, NI> fb;
+    GrawaFrag<BT, BR, NG> fb;
     fa.init(lane, wm * TM);
-    fb.init(lane, DUAL ? wn * (TN / 2) : wn * TN); // DUAL: fragments 0, 1 of the first operand, 2, 3 of the second
+    fb.init(lane, wn * NG * 16); // DUAL: the first NG fragments are of the first operand
 
     const int64_t aoff = AT ? (int64_t)m0 * 2 : (int64_t)m0 * g.lda, boff = BT ? (int64_t)n0 * 2 : (int64_t)n0 * g.ldb;
     const int mrows = g.M - m0, nrows = g.N - n0;
@@ -236,97 +257,139 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
     int seg = t0 / kt, skip = t0 - seg * kt, todo = tiles, krem = 0; // of the next tile to load
     const char *pa = nullptr, *pb = nullptr, *pc = nullptr;
     __amdgpu_buffer_rsrc_t ra, rb, rc;
-    int kload = 0; // k that the tile in the descriptors has
-    auto prepare = [&]() {
-        if (krem <= 0 && todo > 0) {
-            pa = g.a[seg].p + tile.k * g.a[seg].worker + aoff + skip * astep;
-            pb = g.b[seg].p + tile.k * g.b[seg].worker + boff + skip * bstep;
-            if (DUAL) pc = g.b[g.nseg + seg].p + tile.k * g.b[g.nseg + seg].worker + boff + skip * bstep;
-            krem = g.len - skip * GRAWA_BK;
-            skip = 0;
-            ++seg;
+    int kload = 0;             // k that the tile in the descriptors has
+    uint32_t oa = 0, ob = 0;   // the lane's places in it
+    // The next tile's descriptors, in steps that find room between matrix instructions.
+    auto prepare = [&](int what) {
+        if (what == 0) {
+            if (krem <= 0 && todo > 0) {
+                pa = g.a[seg].p + tile.k * g.a[seg].worker + aoff + skip * astep;
+                pb = g.b[seg].p + tile.k * g.b[seg].worker + boff + skip * bstep;
+                if (DUAL) pc = g.b[g.nseg + seg].p + tile.k * g.b[g.nseg + seg].worker + boff + skip * bstep;
+                krem = g.len - skip * GRAWA_BK;
+                skip = 0;
+                ++seg;
+            }
+            kload = todo > 0 ? krem : 0;
+            krem -= GRAWA_BK;
+            --todo;
+        } else if (what == 1) {
+            ra = la.rsrc(pa, mrows, kload);
+            oa = la.place(kload);
+            pa += astep;
+        } else if (what == 2) {
+            rb = lb.rsrc(pb, nrows, kload);
+            ob = lb.place(kload);
+            pb += bstep;
+        } else if (DUAL) {
+            rc = lb.rsrc(pc, nrows, kload);
+            pc += bstep;
         }
-        kload = todo > 0 ? krem : 0;
-        ra = la.rsrc(pa, mrows, kload);
-        rb = lb.rsrc(pb, nrows, kload);
-        if constexpr (DUAL) rc = lb.rsrc(pc, nrows, kload);
-        pa += astep;
-        pb += bstep;
-        if (DUAL) pc += bstep;
-        krem -= GRAWA_BK;
-        --todo;
+    };
+    // The tiles behind the one whose loads are under way are asked for a tile early, so that the loads find them in L2: the blocks that
+    // share rows (columns) of an operand take a quarter of its lines each, a dword a line, into a corner that nobody reads.  8 workers,
+    // 2048 x 1024 x 4096, operands not in any cache: 126 us without, 108 with; two or four tiles early 108, 110.
+    const uint32_t line_a = la.line(tile.n & 3, wave, lane, la.ld), line_b = lb.line(tile.m & 3, wave, lane, lb.ld);
+    constexpr int FETCHES = DUAL ? 3 : 2;
+    auto fetch = [&](int what) {
+        const int left = todo > 0 ? kload - GRAWA_BK : 0; // of this segment: its end is not looked beyond
+        if (what == 0)
+            la.fetch(unread + wave * 256, la.rsrc(pa, mrows, left), line_a);
+        else if (what == 1)
+            lb.fetch(unread + wave * 256, lb.rsrc(pb, nrows, left), line_b);
+        else
+            lb.fetch(unread + wave * 256, lb.rsrc(pc, nrows, left), line_b);
     };
     constexpr int LA = GrawaTileLoad<AT, BM, NW>::LOADS, LB = GrawaTileLoad<BT, BR, NW>::LOADS, LOADS = LA + LB * (DUAL ? 2 : 1);
     auto load = [&](char *buf, int i) {
         if (i < LA)
-            la.go(i, buf, wave, ra, kload);
+            la.go(i, buf, wave, ra, oa);
         else if (i < LA + LB)
-            lb.go(i - LA, buf + ABYTES, wave, rb, kload);
+            lb.go(i - LA, buf + ABYTES, wave, rb, ob);
         else
-            lb.go(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, kload);
+            lb.go(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, ob);
     };
     grawa_f32x4 acc[MI][NI] = {};
     constexpr int MH = MI / 2;
     grawa_bf16x8 a0[MH], a1[MH], b0[NI], b1[NI];
-    // Everything but the matrix instructions is issued between them, a little after each row of NI of them.
-    auto row = [&](int mh, int i, const grawa_bf16x8 &a, const grawa_bf16x8 (&b)[NI]) {
-        __builtin_amdgcn_sched_barrier(0);
+    // A group: MH rows of NI matrix instructions, and between them, evenly, n other things to do.
+    auto group = [&](int mh, const grawa_bf16x8 (&a)[MH], const grawa_bf16x8 (&b)[NI], int n, const auto &item) {
+        constexpr int PAIRS = MH * NI / 2;
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
-            mfma_in_place(acc[mh * MH + i][j], b[j], a);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int p = 0; p < PAIRS; ++p) {
+            const int i = 2 * p / NI, j = 2 * p % NI;
+            __builtin_amdgcn_sched_barrier(0);
+            mfma_in_place(acc[mh * MH + i][j], b[j], a[i]);
+            mfma_in_place(acc[mh * MH + i][j + 1], b[j + 1], a[i]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = p * n / PAIRS; x < (p + 1) * n / PAIRS; ++x) item(x);
+        }
     };
-    auto read_b = [&](const char *buf, int j, int ks) {
-        return DUAL ? fb.get(buf + ABYTES + (j >= 2 ? BR * 128 : 0), j & 1, ks) : fb.get(buf + ABYTES, j, ks);
-    };
+    auto read_b = [&](const char *buf, int j, int ks) { return fb.get(buf + ABYTES + (j >= NG ? BR * 128 : 0), j % NG, ks); };
     // One tile of 64 k, two instructions deep (ks), the upper half of the wave's rows (mh = 0) before the lower.  The fragments of its
-    // first 32 k have been read; those of the others are read behind the instructions that use a register last.  The buffer is
-    // free when every wave has read all of it, a quarter of the tile before its end: then the tile after the next goes there, and has
-    // a whole tile's time to arrive.
-    auto step = [&](char *cur, const char *next) {
-#pragma unroll
-        for (int i = 0; i < MH; ++i) {
-            row(0, i, a0[i], b0);
-            a0[i] = fa.get(cur, i, 1);
-#pragma unroll
-            for (int j = i * NI / MH; j < (i + 1) * NI / MH; ++j) b1[j] = read_b(cur, j, 1);
-        }
-#pragma unroll
-        for (int i = 0; i < MH; ++i) {
-            row(1, i, a1[i], b0);
-            a1[i] = fa.get(cur, MH + i, 1);
-        }
-        prepare();
-#pragma unroll
-        for (int i = 0; i < MH; ++i) row(0, i, a0[i], b1);
-        grawa_landed<0>();
-#pragma unroll
-        for (int i = 0; i < MH; ++i) {
-            row(1, i, a1[i], b1);
-            a0[i] = fa.get(next, i, 0);
-#pragma unroll
-            for (int j = i * NI / MH; j < (i + 1) * NI / MH; ++j) b0[j] = read_b(next, j, 0);
-            a1[i] = fa.get(next, MH + i, 0);
-#pragma unroll
-            for (int j = i * LOADS / MH; j < (i + 1) * LOADS / MH; ++j) load(cur, j);
-        }
+    // first 32 k, upper half, have been read; every other fragment is read a group before its use.  The buffer is free when every wave
+    // has read all of it, a quarter of the tile before its end: then the tile after the next goes there.  Its loads are spread over
+    // two groups, since 64 of them keep the path into LDS busy for half a tile's time and a wave that finds it full cannot issue
+    // anything else; the half tile that is left is their time to arrive.  8 workers, 2048 x 1024 x 4096: all loads in one group
+    // 106 us, in two 100 to 102, in three 104.
+    constexpr int LEAD = LOADS / 2; // loads in the first of the groups
+    // n reads and the loads from l0 to l1, evenly mixed
+    auto mixed = [&](int x, int n, int l0, int l1, char *buf, const auto &read) {
+        const int m = l1 - l0, t = n + m, before = x * m / t;
+        if ((x + 1) * m / t > before)
+            load(buf, l0 + before);
+        else
+            read(x - before);
     };
-    prepare();
+    auto step = [&](char *cur, char *next) {
+        group(0, a0, b0, MH + NI + LOADS - LEAD, [&](int x) {
+            mixed(x, MH + NI, LEAD, LOADS, next, [&](int r) {
+                if (r < MH)
+                    a1[r] = fa.get(cur, MH + r, 0);
+                else
+                    b1[r - MH] = read_b(cur, r - MH, 1);
+            });
+        });
+        group(1, a1, b0, 2 * MH + FETCHES, [&](int r) {
+            if (r < MH)
+                a0[r] = fa.get(cur, r, 1);
+            else if (r < MH + FETCHES)
+                fetch(r - MH);
+            else
+                a1[r - MH - FETCHES] = fa.get(cur, r - FETCHES, 1);
+        });
+        group(0, a0, b1, 4, [&](int x) { prepare(x); });
+        grawa_landed<FETCHES>();
+        group(1, a1, b1, MH + NI + LEAD, [&](int x) {
+            mixed(x, MH + NI, 0, LEAD, cur, [&](int r) {
+                if (r < MH)
+                    a0[r] = fa.get(next, r, 0);
+                else
+                    b0[r - MH] = read_b(next, r - MH, 0);
+            });
+        });
+    };
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) load(buf0, j);
-    prepare();
+    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) load(buf1, j);
-    grawa_landed<LOADS>();
+        for (int what = 0; what < 4; ++what) prepare(what);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j)
+            if (t == 0 || j < LEAD) load(t ? buf1 : buf0, j);
+    }
+#pragma unroll
+    for (int what = 0; what < FETCHES; ++what) fetch(what);
+    grawa_landed<LEAD + FETCHES>();
 #pragma unroll
     for (int i = 0; i < MH; ++i) a0[i] = fa.get(buf0, i, 0);
 #pragma unroll
     for (int j = 0; j < NI; ++j) b0[j] = read_b(buf0, j, 0);
-#pragma unroll
-    for (int i = 0; i < MH; ++i) a1[i] = fa.get(buf0, MH + i, 0);
-    for (int t = 0; t < tiles; t += 2) { // tiles that are not there are zeros
+    for (int t = 0;;) { // tiles that are not there are loaded as zeros
         step(buf0, buf1);
+        if (++t >= tiles) break;
         step(buf1, buf0);
+        if (++t >= tiles) break;
     }
     grawa_landed<0>(); // nothing may be on its way into LDS when the block ends
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); // the last sums are written: the compiler does not see which instructions write them
