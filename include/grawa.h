@@ -400,7 +400,8 @@ grawa_status_t grawa_ffn(grawa_sublayer_t *plan, int64_t T, const grawa_rows_t *
 
 /*
  * From dy, the gradient of the product with Wd (of the dropout's input, where there
- * is one): dx, dWg, dWu, dWd.  x and the weights are those of the forward call.
+ * is one): dx, dWg, dWu, dWd.  x and the weights hold what they held in the forward
+ * call (with float32 the copies that it left in save may be read in their place).
  * accumulate != 0 adds to dWg, dWu and dWd instead of replacing them.
  */
 grawa_status_t grawa_ffn_backward(grawa_sublayer_t *plan, int64_t T, const grawa_rows_t *dy,

@@ -9,6 +9,7 @@
 // backward pass in float32 (a rounding of theirs would be a third one on the way to dWg, dWu and dx).  float32: every matrix
 // element is split exactly into three bfloat16 terms and the six largest of the nine products of terms are summed in float32;
 // what is left out is below 2^-24 of a product.  (An infinity times a number that is exactly a bfloat16 gives NaN there.)
+#include "grawa_few.h"
 #include "grawa_gemm.h"
 
 namespace {
@@ -44,25 +45,49 @@ template <int PLANES> __device__ __forceinline__ void store_planes8(char *p, int
     }
 }
 
-// Copies [K][R][C] elements into planes of pitch Cp with zeros behind C.  Eight elements a thread.
-template <bool BF16> __global__ __launch_bounds__(256) void k_planes(const char *src, int64_t worker, int64_t row, char *dst, int64_t plane, int64_t R, int C, int Cp, int wide)
+// Copies of matrices and activations whose rows are not on 16-byte boundaries, and of all in float32: [K][R][C] elements into planes of
+// pitch Cp with zeros behind C.  Up to five in a launch; eight elements a thread, read at any alignment.
+struct CopyJob {
+    const char *src;
+    char *dst;
+    int64_t worker, row, plane; // src in elements; dst in bytes
+    uint32_t R, C, Cp;
+};
+
+struct CopyJobs {
+    CopyJob job[5];
+    int n;
+};
+
+template <bool BF16> __global__ __launch_bounds__(256) void k_planes(CopyJobs jobs)
 {
     constexpr int S = BF16 ? 2 : 4;
-    const int64_t groups = Cp / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int k = blockIdx.y;
-    const int64_t r = i / groups;
-    if (r >= R) return;
-    const int c = (int)(i - r * groups) * 8;
-    const char *p = src + ((int64_t)k * worker + r * row + c) * S;
-    float v[8] = {};
-    if (wide) {
-        load_elements<BF16, 8>(p, v);
-    } else {
+    const CopyJob &j = jobs.job[blockIdx.z];
+    const uint32_t groups = j.Cp / 8, k = blockIdx.y;
+    const uint64_t total = (uint64_t)j.R * groups;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256) {
+        const uint32_t r = total >> 32 ? (uint32_t)(i / groups) : (uint32_t)i / groups, c = (uint32_t)(i - (uint64_t)r * groups) * 8;
+        const char *p = j.src + ((int64_t)k * j.worker + (int64_t)r * j.row + c) * S;
+        float v[8] = {};
+        if (c + 8 <= j.C) {
+            const GrawaAny16 a = *(const GrawaAny16 *)p, b = BF16 ? a : *(const GrawaAny16 *)(p + 16);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c + j < C) load_elements<BF16, 1>(p + j * S, v + j);
+            for (int q = 0; q < 4; ++q) {
+                if (BF16) {
+                    v[2 * q] = bf16_lo(a[q]);
+                    v[2 * q + 1] = bf16_hi(a[q]);
+                } else {
+                    v[q] = __uint_as_float(a[q]);
+                    v[4 + q] = __uint_as_float(b[q]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (c + q < j.C) load_elements<BF16, 1>(p + q * S, v + q);
+        }
+        store_planes8<BF16 ? 1 : 3>(j.dst + (((int64_t)k * j.R + r) * j.Cp + c) * 2, j.plane, v);
     }
-    store_planes8<BF16 ? 1 : 3>(dst + (((int64_t)k * R + r) * Cp + c) * 2, plane, v);
 }
 
 // e^z: for results that are rounded to bfloat16 by the hardware's 2^z, whose argument's rounding costs z 2^-24 of it.
@@ -224,9 +249,9 @@ struct Operand {
 
 constexpr int64_t MAX_LD = ((int64_t)1 << 31) / 256 - 128; // bytes; a tile's offsets have 31 bits
 
-// How a product is cut: tiles of 256 x 256 or 128 x 128, and the parts that its sum over k is split into.
+// How a product is cut: its tiles, and the parts that its sum over k is split into.
 struct Cut {
-    bool large;
+    int kind; // 0: 256 x 256, 1: 128 x 128, 2: 64 x 128
     int splits;
     int64_t tiles;
 };
@@ -234,24 +259,27 @@ struct Cut {
 constexpr int64_t PART_FLOATS = (int64_t)512 * 256 * 256; // most that the parts of a product take
 constexpr int MAX_SPLITS = 16;
 
-// The cut with the least time by what was measured (us): a tile of 64 k takes 1.75 in a block of 256 x 256, of which a CU holds one; in
-// one of 128 x 128 it takes 1.3 where a CU holds two and 0.75 where it has one; a block costs about three such tiles more; parts are
-// written and read at 4 TB/s by a launch more.
-Cut cut_of(int64_t K, int64_t M, int64_t N, int64_t ktiles, bool dual, int64_t part_floats)
+// The cut with the least time by what was measured (us): a tile of 64 k takes 1.6 in a block of 256 x 256, of which a CU holds one; in
+// one of 128 x 128 it takes 1.3 where a CU holds two and 0.8 where it has one; in one of 64 x 128, for products of no more rows than
+// that, 1.2 where a CU holds three, 0.9 with two, 0.7 with one; a block costs about three such tiles more; parts are written and read at 4 TB/s by a
+// launch more.
+Cut cut_of(int64_t K, int64_t M, int64_t N, int64_t ktiles, bool dual, bool short_rows, int64_t part_floats)
 {
+    static const struct { int bm, bn, slots; double us[3]; } kinds[3] = {{256, 256, 256, {1.6, 1.6, 1.6}}, {128, 128, 512, {0.8, 1.3, 1.3}}, {64, 128, 768, {0.7, 0.9, 1.2}}};
     Cut best{};
     double least = 0;
     const int64_t padded = K * grawa_round16(M) * grawa_round16(N) * (dual ? 2 : 1);
-    for (int large = 1; large >= 0; --large) {
-        const int64_t bm = large ? 256 : 128, bn = dual ? bm / 2 : bm;
-        const int64_t tiles = K * ((M + bm - 1) / bm) * ((N + bn - 1) / bn), slots = large ? 256 : 512;
+    for (int kind = short_rows && M <= 64 ? 2 : 0; kind < (short_rows && M <= 64 ? 3 : 2); ++kind) {
+        const auto &c = kinds[kind];
+        const int64_t bn = dual ? c.bn / 2 : c.bn, tiles = K * ((M + c.bm - 1) / c.bm) * ((N + bn - 1) / bn);
         for (int s = 1; s <= MAX_SPLITS; ++s) {
-            if (s > 1 && (s * padded > part_floats || ktiles / s < 4 || s * tiles > 2 * slots)) break;
-            const int64_t rounds = (s * tiles + slots - 1) / slots;
-            double us = (double)rounds * ((double)((ktiles + s - 1) / s) + 3) * (large ? 1.75 : s * tiles <= 256 ? 0.75 : 1.3);
+            if (s > 1 && (s * padded > part_floats || ktiles / s < 4 || s * tiles > 2 * c.slots)) break;
+            const int64_t full = s * tiles / c.slots, rest = s * tiles - full * c.slots;
+            const double tile_us = (double)full * c.us[2] + (rest ? c.us[(rest - 1) / 256] : 0);
+            double us = tile_us * ((double)((ktiles + s - 1) / s) + 3);
             if (s > 1) us += 5 + 8e-6 * (double)(s * padded) / 4;
             if (!best.splits || us < least) {
-                best = Cut{large != 0, s, tiles};
+                best = Cut{kind, s, tiles};
                 least = us;
             }
         }
@@ -262,15 +290,17 @@ Cut cut_of(int64_t K, int64_t M, int64_t N, int64_t ktiles, bool dual, int64_t p
 template <bool AT, bool BT, bool DUAL, class Epi> void launch_tiles(const GrawaGemm &g, const Cut &cut, const Epi &epi, hipStream_t st)
 {
     const dim3 grid((unsigned)(cut.tiles * cut.splits));
-    if (cut.large)
+    if (cut.kind == 0)
         k_gemm<256, 256, 2, 4, AT, BT, DUAL, Epi><<<grid, 512, 0, st>>>(g, epi);
-    else
+    else if (cut.kind == 1)
         k_gemm<128, 128, 2, 2, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
+    else if constexpr (!AT)
+        k_gemm<64, 128, 1, 4, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
 }
 
 template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const grawa_sublayer *s, GrawaGemm g, const Epi &epi, hipStream_t st)
 {
-    const Cut cut = cut_of(g.K, g.M, g.N, (int64_t)((g.len + GRAWA_BK - 1) / GRAWA_BK) * g.nseg, DUAL, s->part_floats);
+    const Cut cut = cut_of(g.K, g.M, g.N, (int64_t)((g.len + GRAWA_BK - 1) / GRAWA_BK) * g.nseg, DUAL, !AT, s->part_floats);
     g.splits = cut.splits;
     if (cut.splits == 1) {
         launch_tiles<AT, BT, DUAL>(g, cut, epi, st);
@@ -280,7 +310,11 @@ template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const g
         launch_tiles<AT, BT, DUAL>(g, cut, EpiParts{parts, nullptr, nullptr}, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        k_join<DUAL, Epi><<<dim3((unsigned)((g.N + 127) / 128), (unsigned)((g.M + 15) / 16), (unsigned)g.K), 256, 0, st>>>(parts, cut.splits, g.M, g.N, epi);
+        const unsigned rows = (unsigned)((g.M + 15) / 16);
+        if (cut.splits >= 4 && (int64_t)((g.N + 127) / 128) * rows * g.K < 512)
+            k_join<DUAL, true, Epi><<<dim3((unsigned)((g.N + 31) / 32), rows, (unsigned)g.K), 256, 0, st>>>(parts, cut.splits, g.M, g.N, epi);
+        else
+            k_join<DUAL, false, Epi><<<dim3((unsigned)((g.N + 127) / 128), rows, (unsigned)g.K), 256, 0, st>>>(parts, cut.splits, g.M, g.N, epi);
     }
     return hipGetLastError();
 }
@@ -308,22 +342,34 @@ struct Sublayer { // one call
     hipError_t err = hipSuccess;
 
     int S() const { return s->dtype == GRAWA_BF16 ? 2 : 4; }
-    // An operand read in place where it can be, else a copy in `room`.
+    CopyJobs copies{};
+    int64_t most = 0; // groups of eight of the largest copy
+
+    // An operand read in place where it can be, else a copy in `room`, which copy_all() makes.
     Operand operand(const char *p, int64_t worker, int64_t row, int64_t R, int64_t C, int64_t Cp, char *room)
     {
-        const bool bf = s->dtype == GRAWA_BF16;
-        if (bf && C % 8 == 0 && !(((uintptr_t)p | (uint64_t)worker * 2 | (uint64_t)row * 2) & 15) && row >= C && row * 2 <= MAX_LD)
+        if (s->planes == 1 && C % 8 == 0 && !(((uintptr_t)p | (uint64_t)worker * 2 | (uint64_t)row * 2) & 15) && row >= C && row * 2 <= MAX_LD)
             return Operand{p, worker * 2, 0, row * 2};
         const Operand o{room, R * Cp * 2, (int64_t)s->K * R * Cp * 2, Cp * 2};
-        const int wide = C % 8 == 0 && !(((uintptr_t)p | (uint64_t)worker * S() | (uint64_t)row * S()) & 15);
-        const dim3 grid((unsigned)((R * (Cp / 8) + 255) / 256), (unsigned)s->K);
-        if (bf)
-            k_planes<true><<<grid, 256, 0, st>>>(p, worker, row, room, o.plane, R, (int)C, (int)Cp, wide);
-        else
-            k_planes<false><<<grid, 256, 0, st>>>(p, worker, row, room, o.plane, R, (int)C, (int)Cp, wide);
-        if (err == hipSuccess) err = hipGetLastError();
+        copies.job[copies.n++] = CopyJob{p, room, worker, row, o.plane, (uint32_t)R, (uint32_t)C, (uint32_t)Cp};
+        most = most > R * (Cp / 8) ? most : R * (Cp / 8);
         return o;
     }
+    void copy_all()
+    {
+        if (!copies.n) return;
+        const int64_t blocks = (most + 255) / 256;
+        const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), (unsigned)s->K, (unsigned)copies.n);
+        run([&] {
+            if (s->planes == 1)
+                k_planes<true><<<grid, 256, 0, st>>>(copies);
+            else
+                k_planes<false><<<grid, 256, 0, st>>>(copies);
+            return hipGetLastError();
+        });
+    }
+    // The same of what a forward pass left in `room`.
+    Operand kept(int64_t R, int64_t Cp, char *room) const { return Operand{room, R * Cp * 2, (int64_t)s->K * R * Cp * 2, Cp * 2}; }
     Operand tokens(const GrawaRows &x, char *room) { return operand(x.p, x.worker, x.row, T, s->d, s->dp, room); }
     Operand up_matrix(const GrawaMat &w, char *room) { return operand(w.p, w.worker, s->d, s->f, s->d, s->dp, room); }
     Operand down_matrix(const GrawaMat &w, char *room) { return operand(w.p, w.worker, s->f, s->d, s->f, s->fp, room); }
@@ -344,25 +390,68 @@ struct Sublayer { // one call
     bool wide(const GrawaRows &r) const { return !(((uintptr_t)r.p | (uint64_t)r.worker * S() | (uint64_t)r.row * S()) & 15); }
 };
 
+// Where the copies of x and of the matrices go: with float32 and more than a few tokens into the buffer that the backward pass gets (it
+// would make the same ones again: 85 of 1150 us with 4 x 512 tokens, 1024 x 4096), else into the workspace.
+struct Kept {
+    char *x, *wg, *wu, *wd;
+};
+
+Kept kept_in(const grawa_sublayer *s, int64_t T, char *save)
+{
+    if (!save || !grawa_keeps_copies(s, T)) return Kept{s->x, s->wg, s->wu, s->wd};
+    const int64_t tokens = 6 * s->K * T * s->dp, up = 6 * s->K * s->f * s->dp;
+    char *p = save + grawa_save_bytes_own(s, T);
+    return Kept{p, p + tokens, p + tokens + up, p + tokens + 2 * up};
+}
+
+// A product of at most GRAWA_FEW tokens.
+template <bool BF16, bool DUAL, bool PLANES, class Epi> hipError_t launch_few(const GrawaFew &g, int K, const Epi &epi, hipStream_t st)
+{
+    const int mt = (g.M + 15) / 16, columns = few_columns(mt, DUAL);
+    const dim3 grid((unsigned)((g.N + columns - 1) / columns), (unsigned)K);
+    // Eight waves share k where the columns alone give few waves.
+    const unsigned threads = (int64_t)grid.x * K < 1024 ? 512 : 256;
+    if (mt == 1) k_few<BF16, 1, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
+    else if (mt == 2) k_few<BF16, 2, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
+    else if (mt == 3) k_few<BF16, 3, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
+    else k_few<BF16, 4, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
+    return hipGetLastError();
+}
+
 template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, GrawaMat wg, GrawaMat wu, GrawaMat wd, GrawaRows residual, GrawaDrop drop, GrawaRows y, char *save)
 {
     const grawa_sublayer *s = c.s;
-    const Operand ox = c.tokens(x, s->x), og = c.up_matrix(wg, s->wg), ou = c.up_matrix(wu, s->wu), od = c.down_matrix(wd, s->wd);
     const int64_t n = c.T * s->fp;
     const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
     float *gate = (float *)save;
     char *h = save ? save + s->K * blocks * 8 : s->h;
+    const EpiGateUp<PLANES, ACT> inner{h, gate, gate ? gate + s->K * blocks : nullptr, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
+    const EpiStore<PLANES == 1, true> outer{y, residual, drop, (int)s->d, (int)c.T, 0, c.wide(y) && (!residual.p || c.wide(residual)), 0};
+    // Few tokens: see grawa_few.h.  To the end in float32, which tiles multiply six times: 4 workers, 1024 x 4096, 64 tokens 189 us, by tiles
+    // 240.  In bfloat16 up to 16, 67 us and 82 with one matrix of 4096 x 11264, and up to 32 while the matrices are small and the
+    // launches count: 38 us and 43 with four of 1024 x 4096, but 97 and 80 with the larger one.
+    constexpr bool BF16 = PLANES == 1;
+    if (c.T <= (!BF16 ? GRAWA_FEW : s->K * s->d * s->f <= (int64_t)1 << 25 ? 32 : 16)) {
+        constexpr int S = BF16 ? 2 : 4;
+        GrawaFew g{(int)c.T, (int)s->f, (int)s->d, {wg.p, wg.worker * S}, {wu.p, wu.worker * S}, x.p, x.worker * S, x.row * S, 0};
+        c.run([&] { return launch_few<BF16, true, false>(g, s->K, inner, c.st); });
+        g = GrawaFew{(int)c.T, (int)s->d, (int)s->f, {wd.p, wd.worker * S}, {}, h, n * 2, s->fp * 2, s->K * n * 2};
+        c.run([&] { return launch_few<BF16, false, !BF16>(g, s->K, outer, c.st); });
+        return c.err;
+    }
+    // The split copies of float32 go to where the backward pass finds them, if one follows.
+    const Kept at = kept_in(s, c.T, save);
+    const Operand ox = c.tokens(x, at.x), og = c.up_matrix(wg, at.wg), ou = c.up_matrix(wu, at.wu), od = c.down_matrix(wd, at.wd);
+    c.copy_all();
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ox, og, &ou);
-        const EpiGateUp<PLANES, ACT> epi{h, gate, gate ? gate + s->K * blocks : nullptr, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
-        c.run([&] { return launch_gemm<false, false, true>(s, g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, false, true>(s, g, inner, c.st); });
     }
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
         add_segments(g, PLANES, c.inner(h), od, nullptr);
-        const EpiStore<PLANES == 1, true> epi{y, residual, drop, (int)s->d, (int)c.T, 0, c.wide(y) && (!residual.p || c.wide(residual)), 0};
-        c.run([&] { return launch_gemm<false, false, false>(s, g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, false, false>(s, g, outer, c.st); });
     }
     return c.err;
 }
@@ -371,8 +460,12 @@ template <int PLANES, int ACT>
 hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat wu, GrawaMat wd, const char *save, GrawaRows dx, GrawaMat dwg, GrawaMat dwu, GrawaMat dwd, int accumulate)
 {
     const grawa_sublayer *s = c.s;
-    const Operand ox = c.tokens(x, s->x), ody = c.tokens(dy, s->dy);
-    const Operand og = c.up_matrix(wg, s->wg), ou = c.up_matrix(wu, s->wu), od = c.down_matrix(wd, s->wd);
+    const bool have = grawa_keeps_copies(s, c.T);
+    const Kept at = kept_in(s, c.T, (char *)save);
+    const Operand ody = c.tokens(dy, s->dy), ox = have ? c.kept(c.T, s->dp, at.x) : c.tokens(x, at.x);
+    const Operand og = have ? c.kept(s->f, s->dp, at.wg) : c.up_matrix(wg, at.wg), ou = have ? c.kept(s->f, s->dp, at.wu) : c.up_matrix(wu, at.wu);
+    const Operand od = have ? c.kept(s->d, s->fp, at.wd) : c.down_matrix(wd, at.wd);
+    c.copy_all();
     const int64_t n = c.T * s->fp;
     const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
     const float *gate = (const float *)save;
