@@ -1,53 +1,65 @@
-// Elements of either type by the one or by the 16 bytes, widened to float32 (device side of the feed-forward sublayer).
+// Elements of either type, one by one or by 16 bytes at any alignment, widened to float32 (device side of the feed-forward sublayer).
 #pragma once
 #include "grawa_device.h"
 
 typedef __bf16 grawa_bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t GrawaAny16 __attribute__((ext_vector_type(4), aligned(2))); // 16 bytes anywhere: one instruction all the same
+typedef uint32_t GrawaAny8 __attribute__((ext_vector_type(2), aligned(2)));
 
-// VEC consecutive elements from p on: 16 bytes at a time where VEC is more than one, p then on a 16-byte boundary.
-template <bool BF16, int VEC> __device__ __forceinline__ void load_elements(const char *p, float *v)
+template <bool BF16> __device__ __forceinline__ float load_one(const char *p) { return BF16 ? bf16_one(*(const uint16_t *)p) : *(const float *)p; }
+
+template <bool BF16> __device__ __forceinline__ void store_one(char *p, float v)
 {
-    if constexpr (VEC == 1) {
-        v[0] = BF16 ? bf16_one(*(const uint16_t *)p) : *(const float *)p;
-    } else if constexpr (BF16) {
-        static_assert(VEC % 8 == 0, "16 bytes");
-#pragma unroll
-        for (int q = 0; q < VEC / 8; ++q) {
-            const uint4 u = ((const uint4 *)p)[q];
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[8 * q + 2 * j] = bf16_lo(w[j]);
-                v[8 * q + 2 * j + 1] = bf16_hi(w[j]);
-            }
-        }
-    } else {
-        static_assert(VEC % 4 == 0, "16 bytes");
-#pragma unroll
-        for (int q = 0; q < VEC / 4; ++q) {
-            const float4 u = ((const float4 *)p)[q];
-            v[4 * q] = u.x, v[4 * q + 1] = u.y, v[4 * q + 2] = u.z, v[4 * q + 3] = u.w;
-        }
-    }
+    if constexpr (BF16)
+        *(__bf16 *)p = (__bf16)v;
+    else
+        *(float *)p = v;
 }
 
-template <bool BF16, int VEC> __device__ __forceinline__ void store_elements(char *p, const float *v)
-{
-    if constexpr (VEC == 1) {
-        if constexpr (BF16)
-            *(__bf16 *)p = (__bf16)v[0];
-        else
-            *(float *)p = v[0];
-    } else if constexpr (BF16) {
+// 16 bytes: eight bfloat16 or four float32.
+template <bool BF16> struct GrawaPiece {
+    static constexpr int N = BF16 ? 8 : 4, S = BF16 ? 2 : 4;
+    uint32_t w[4];
+
+    // n (> 0) elements are left of the row; what it does not have is 0.
+    __device__ __forceinline__ void load(const char *p, int n)
+    {
+        if (n >= N) {
+            const GrawaAny16 v = *(const GrawaAny16 *)p;
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else {
+            w[0] = w[1] = w[2] = w[3] = 0;
 #pragma unroll
-        for (int q = 0; q < VEC / 8; ++q) {
-            grawa_bf16x8 u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = (__bf16)v[8 * q + j];
-            ((grawa_bf16x8 *)p)[q] = u;
+            for (int j = 0; j < N - 1; ++j)
+                if (j < n) {
+                    if constexpr (BF16)
+                        w[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << (j % 2 * 16);
+                    else
+                        w[j] = ((const uint32_t *)p)[j];
+                }
         }
+    }
+    __device__ __forceinline__ float operator[](int j) const { return BF16 ? (j % 2 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2])) : __uint_as_float(w[j]); }
+};
+
+template <bool BF16> __device__ __forceinline__ void store_piece(char *p, int n, const float *v)
+{
+    constexpr int N = GrawaPiece<BF16>::N, S = GrawaPiece<BF16>::S;
+    if (n >= N) {
+        GrawaAny16 u;
+        if constexpr (BF16) {
+            grawa_bf16x8 b;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) b[j] = (__bf16)v[j];
+            u = __builtin_bit_cast(GrawaAny16, b);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = __float_as_uint(v[j]);
+        }
+        *(GrawaAny16 *)p = u;
     } else {
 #pragma unroll
-        for (int q = 0; q < VEC / 4; ++q) ((float4 *)p)[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        for (int j = 0; j < N - 1; ++j)
+            if (j < n) store_one<BF16>(p + j * S, v[j]);
     }
 }

@@ -17,9 +17,6 @@ struct GrawaFew {
 
 namespace {
 
-typedef uint32_t GrawaAny16 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t GrawaAny8 __attribute__((ext_vector_type(2), aligned(2)));
-
 // What a lane holds of a step of 64 bytes of k (of float32 16 k, of bfloat16 32): 16 bytes, k = 16 / S (lane / 16) ... of row lane % 16.
 struct GrawaStep {
     uint32_t w[4];

@@ -30,7 +30,7 @@ __device__ __forceinline__ void split3(float v, uint16_t t[3])
 template <int PLANES> __device__ __forceinline__ void store_planes8(char *p, int64_t plane, const float *v)
 {
     if constexpr (PLANES == 1) {
-        store_elements<true, 8>(p, v);
+        store_piece<true>(p, 8, v);
     } else {
         uint16_t t[8][3];
 #pragma unroll
@@ -84,7 +84,7 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_planes(CopyJobs jo
         } else {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-                if (c + q < j.C) load_elements<BF16, 1>(p + q * S, v + q);
+                if (c + q < j.C) v[q] = load_one<BF16>(p + q * S);
         }
         store_planes8<BF16 ? 1 : 3>(j.dst + (((int64_t)k * j.R + r) * j.Cp + c) * 2, j.plane, v);
     }
@@ -197,7 +197,7 @@ template <bool BF16, bool OUT> struct EpiStore {
     static constexpr int OUTS = 1, VEC = BF16 ? 8 : 4;
     GrawaRows y, res;   // OUT: res.p may be null
     GrawaDrop drop;     // OUT
-    int N, T, accumulate, wide;
+    int N, T, accumulate;
     uint32_t row0;      // of the worker, for the dropout
     __device__ __forceinline__ void tile(int k, int)
     {
@@ -217,26 +217,13 @@ template <bool BF16, bool OUT> struct EpiStore {
         }
         char *p = y.p + ((int64_t)m * y.row + n) * S;
         const char *from = OUT ? (res.p ? res.p + ((int64_t)m * res.row + n) * S : nullptr) : accumulate ? p : nullptr;
-        if (wide && n + VEC <= N) {
-            if (from) {
-                float r[VEC];
-                load_elements<BF16, VEC>(from, r);
+        if (from) {
+            GrawaPiece<BF16> r;
+            r.load(from, N - n);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) v[j] += r[j];
-            }
-            store_elements<BF16, VEC>(p, v);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                if (n + j >= N) break;
-                float r = v[j], old;
-                if (from) {
-                    load_elements<BF16, 1>(from + j * S, &old);
-                    r += old;
-                }
-                store_elements<BF16, 1>(p + j * S, &r);
-            }
+            for (int j = 0; j < VEC; ++j) v[j] += r[j];
         }
+        store_piece<BF16>(p, N - n, v);
     }
 };
 
@@ -387,7 +374,6 @@ struct Sublayer { // one call
     {
         if (err == hipSuccess) err = f();
     }
-    bool wide(const GrawaRows &r) const { return !(((uintptr_t)r.p | (uint64_t)r.worker * S() | (uint64_t)r.row * S()) & 15); }
 };
 
 // Where the copies of x and of the matrices go: with float32 and more than a few tokens into the buffer that the backward pass gets (it
@@ -426,7 +412,7 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
     float *gate = (float *)save;
     char *h = save ? save + s->K * blocks * 8 : s->h;
     const EpiGateUp<PLANES, ACT> inner{h, gate, gate ? gate + s->K * blocks : nullptr, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
-    const EpiStore<PLANES == 1, true> outer{y, residual, drop, (int)s->d, (int)c.T, 0, c.wide(y) && (!residual.p || c.wide(residual)), 0};
+    const EpiStore<PLANES == 1, true> outer{y, residual, drop, (int)s->d, (int)c.T, 0, 0};
     // Few tokens: see grawa_few.h.  To the end in float32, which tiles multiply six times: 4 workers, 1024 x 4096, 64 tokens 189 us, by tiles
     // 240.  In bfloat16 up to 16, 67 us and 82 with one matrix of 4096 x 11264, and up to 32 while the matrices are small and the
     // launches count: 38 us and 43 with four of 1024 x 4096, but 97 and 80 with the larger one.
@@ -480,7 +466,7 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
         GrawaGemm g = c.product(M, N, c.T);
         add_segments(g, PLANES, a, b, nullptr);
         const GrawaRows out{w.p, w.worker, N};
-        const EpiStore<PLANES == 1, false> epi{out, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, c.wide(out), 0};
+        const EpiStore<PLANES == 1, false> epi{out, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, 0};
         c.run([&] { return launch_gemm<true, true, false>(s, g, epi, c.st); });
     };
     store(odg, ox, dwg, s->f, s->d);
@@ -490,7 +476,7 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
         GrawaGemm g = c.product(c.T, s->d, s->f);
         add_segments(g, PLANES, odg, og, nullptr);
         add_segments(g, PLANES, odu, ou, nullptr);
-        const EpiStore<PLANES == 1, false> epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, c.wide(dx), 0};
+        const EpiStore<PLANES == 1, false> epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, 0};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
     return c.err;
@@ -500,9 +486,8 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
 template <bool BF16> __global__ __launch_bounds__(256) void k_zero(GrawaMat w, int64_t n)
 {
     constexpr int S = BF16 ? 2 : 4;
-    const float zero = 0.f;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
-        store_elements<BF16, 1>(w.p + ((int64_t)blockIdx.y * w.worker + i) * S, &zero);
+        store_one<BF16>(w.p + ((int64_t)blockIdx.y * w.worker + i) * S, 0.f);
 }
 
 #define GRAWA_FFN_FORMS(GO)                                                                                        \

@@ -32,52 +32,51 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float *sm)
     return v;
 }
 
-// A block of BLOCK threads holds BLOCK / TPR rows side by side; thread c of a row has elements (j * TPR + c) * VEC ... of it, j < NV.
-template <bool BF16, int VEC, int NV, int TPR, int BLOCK>
+// A block of BLOCK threads holds BLOCK / TPR rows side by side; thread c of a row has the 16-byte pieces j TPR + c of it, j < NV.
+template <bool BF16, int NV, int TPR, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_norm(GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y, float *stats, int64_t T, int d)
 {
-    constexpr int S = BF16 ? 2 : 4;
+    typedef GrawaPiece<BF16> Piece;
+    constexpr int S = Piece::S, N = Piece::N;
     static_assert(TPR == 64 || TPR == BLOCK, "a row is a wave's or the block's");
     __shared__ float sm[2][BLOCK / 64];
     const int c = threadIdx.x % TPR, k = blockIdx.y;
     const int64_t t = (int64_t)blockIdx.x * (BLOCK / TPR) + threadIdx.x / TPR;
     if (t >= T) return; // whole waves of a row that is one wave's, or the whole block
     const char *px = x.p + ((int64_t)k * x.worker + t * x.row) * S;
-    float v[NV][VEC];
-    float sum = 0.f;
+    const char *pw = w.p + (int64_t)k * w.worker * S, *pb = b.p ? b.p + (int64_t)k * b.worker * S : nullptr;
+    Piece v[NV], ww[NV], bb[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int e = (j * TPR + c) * VEC;
-        if (e < d) {
-            load_elements<BF16, VEC>(px + (int64_t)e * S, v[j]);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) sum += v[j][i];
-        }
+    for (int j = 0; j < NV; ++j) { // all on their way before the first is waited for
+        const int e = (j * TPR + c) * N;
+        if (e >= d) continue;
+        v[j].load(px + (int64_t)e * S, d - e);
+        ww[j].load(pw + (int64_t)e * S, d - e);
+        if (pb) bb[j].load(pb + (int64_t)e * S, d - e);
     }
-    const float mean = row_sum<TPR>(sum, sm[0]) / (float)d;
-    float sq = 0.f;
+    float sum = 0.f, sq = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        if ((j * TPR + c) * VEC < d)
+        if ((j * TPR + c) * N < d)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                v[j][i] -= mean;
-                sq += v[j][i] * v[j][i];
-            }
+            for (int i = 0; i < N; ++i) sum += v[j][i];
+    const float mean = row_sum<TPR>(sum, sm[0]) / (float)d;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((j * TPR + c) * N + i < d) sq += (v[j][i] - mean) * (v[j][i] - mean);
     const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, sm[1]) / (float)d + eps);
     if (stats && c == 0) *(float2 *)(stats + 2 * ((int64_t)k * T + t)) = make_float2(mean, rstd);
     char *py = y.p + ((int64_t)k * y.worker + t * y.row) * S;
-    const char *pw = w.p + (int64_t)k * w.worker * S, *pb = b.p ? b.p + (int64_t)k * b.worker * S : nullptr;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int e = (j * TPR + c) * VEC;
+        const int e = (j * TPR + c) * N;
         if (e >= d) continue;
-        float ww[VEC], bb[VEC] = {};
-        load_elements<BF16, VEC>(pw + (int64_t)e * S, ww);
-        if (pb) load_elements<BF16, VEC>(pb + (int64_t)e * S, bb);
+        float r[N];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) ww[i] = v[j][i] * rstd * ww[i] + bb[i];
-        store_elements<BF16, VEC>(py + (int64_t)e * S, ww);
+        for (int i = 0; i < N; ++i) r[i] = (v[j][i] - mean) * rstd * ww[j][i] + (pb ? bb[j][i] : 0.f);
+        store_piece<BF16>(py + (int64_t)e * S, d - e, r);
     }
 }
 
@@ -91,12 +90,12 @@ template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_long(GrawaRo
     const char *px = x.p + ((int64_t)k * x.worker + t * x.row) * S;
     float sum = 0.f, sq = 0.f, v, ww, bb = 0.f;
     for (int e = c; e < d; e += 1024) {
-        load_elements<BF16, 1>(px + (int64_t)e * S, &v);
+        v = load_one<BF16>(px + (int64_t)e * S);
         sum += v;
     }
     const float mean = row_sum<1024>(sum, sm[0]) / (float)d;
     for (int e = c; e < d; e += 1024) {
-        load_elements<BF16, 1>(px + (int64_t)e * S, &v);
+        v = load_one<BF16>(px + (int64_t)e * S);
         sq += (v - mean) * (v - mean);
     }
     const float rstd = 1.f / sqrtf(row_sum<1024>(sq, sm[1]) / (float)d + eps);
@@ -104,63 +103,82 @@ template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_long(GrawaRo
     char *py = y.p + ((int64_t)k * y.worker + t * y.row) * S;
     const char *pw = w.p + (int64_t)k * w.worker * S, *pb = b.p ? b.p + (int64_t)k * b.worker * S : nullptr;
     for (int e = c; e < d; e += 1024) { // y may be x: a thread writes what only it reads again
-        load_elements<BF16, 1>(px + (int64_t)e * S, &v);
-        load_elements<BF16, 1>(pw + (int64_t)e * S, &ww);
-        if (pb) load_elements<BF16, 1>(pb + (int64_t)e * S, &bb);
+        v = load_one<BF16>(px + (int64_t)e * S);
+        ww = load_one<BF16>(pw + (int64_t)e * S);
+        if (pb) bb = load_one<BF16>(pb + (int64_t)e * S);
         v = (v - mean) * rstd * ww + bb;
-        store_elements<BF16, 1>(py + (int64_t)e * S, &v);
+        store_one<BF16>(py + (int64_t)e * S, v);
     }
 }
 
-// The backward pass of rows t0, t0 + step, ... of a worker.  part: [K][gridDim.x][2][d], the block's sums of dw and db.
-template <bool BF16, int VEC, int NV, int TPR, int BLOCK>
+// The backward pass of rows t0, t0 + step, ... of a worker; the next row is on its way while one is worked on.  part:
+// [K][gridDim.x][2][d], the block's sums of dw and db.
+template <bool BF16, int NV, int TPR, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_norm_back(GrawaRows dy, GrawaRows x, GrawaMat w, const float *stats, GrawaRows add, GrawaRows dx,
                                                      float *part, int64_t T, int d)
 {
-    constexpr int S = BF16 ? 2 : 4, ROWS = BLOCK / TPR;
+    typedef GrawaPiece<BF16> Piece;
+    constexpr int S = Piece::S, N = Piece::N, ROWS = BLOCK / TPR;
     static_assert(TPR == 64 || TPR == BLOCK, "a row is a wave's or the block's");
     __shared__ float sm[4][BLOCK / 64];
-    __shared__ float cols[ROWS > 1 ? NV * TPR * VEC : 1];
+    __shared__ float cols[ROWS > 1 ? NV * TPR * N : 1];
     const int c = threadIdx.x % TPR, k = blockIdx.y;
     const char *pw = w.p + (int64_t)k * w.worker * S;
-    float ww[NV][VEC], dw[NV][VEC] = {}, db[NV][VEC] = {};
+    Piece ww[NV], nx[NV], ndy[NV], nadd[NV];
+    float dw[NV][N] = {}, db[NV][N] = {};
+    float2 nst = make_float2(0.f, 0.f);
+    auto fetch = [&](int64_t t) {
+        const char *px = x.p + ((int64_t)k * x.worker + t * x.row) * S, *pdy = dy.p + ((int64_t)k * dy.worker + t * dy.row) * S;
+        const char *padd = add.p ? add.p + ((int64_t)k * add.worker + t * add.row) * S : nullptr;
+        nst = *(const float2 *)(stats + 2 * ((int64_t)k * T + t));
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int e = (j * TPR + c) * N;
+            if (e >= d) continue;
+            nx[j].load(px + (int64_t)e * S, d - e);
+            ndy[j].load(pdy + (int64_t)e * S, d - e);
+            if (padd) nadd[j].load(padd + (int64_t)e * S, d - e);
+        }
+    };
+    const int64_t first = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR, step = (int64_t)gridDim.x * ROWS;
+    if (first < T) fetch(first);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-        if ((j * TPR + c) * VEC < d) load_elements<BF16, VEC>(pw + (int64_t)(j * TPR + c) * VEC * S, ww[j]);
+        if ((j * TPR + c) * N < d) ww[j].load(pw + (int64_t)(j * TPR + c) * N * S, d - (j * TPR + c) * N);
     int turn = 0; // which pair of `sm`: a wave may be one row ahead of another
-    for (int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; t < T; t += (int64_t)gridDim.x * ROWS, turn ^= 2) {
-        const char *px = x.p + ((int64_t)k * x.worker + t * x.row) * S, *pdy = dy.p + ((int64_t)k * dy.worker + t * dy.row) * S;
-        const float2 st = *(const float2 *)(stats + 2 * ((int64_t)k * T + t));
-        float a[NV][VEC], h[NV][VEC];
+    for (int64_t t = first; t < T; t += step, turn ^= 2) {
+        const float2 st = nst;
+        Piece px[NV], pdy[NV], padd[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) px[j] = nx[j], pdy[j] = ndy[j], padd[j] = nadd[j];
+        // dx may be dy or add: a row is read by nobody but those who write it
+        if (t + step < T) fetch(t + step);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int e = (j * TPR + c) * VEC;
-            if (e >= d) continue;
-            load_elements<BF16, VEC>(px + (int64_t)e * S, h[j]);
-            load_elements<BF16, VEC>(pdy + (int64_t)e * S, a[j]);
+            if ((j * TPR + c) * N >= d) continue;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                h[j][i] = (h[j][i] - st.x) * st.y;
-                dw[j][i] += a[j][i] * h[j][i];
-                db[j][i] += a[j][i];
-                a[j][i] *= ww[j][i];
-                s1 += a[j][i];
-                s2 += a[j][i] * h[j][i];
+            for (int i = 0; i < N; ++i) { // behind the row's end dy is 0
+                const float h = (px[j][i] - st.x) * st.y, a = pdy[j][i] * ww[j][i];
+                dw[j][i] += pdy[j][i] * h;
+                db[j][i] += pdy[j][i];
+                s1 += a;
+                s2 += a * h;
             }
         }
         const float m1 = row_sum<TPR>(s1, sm[turn]) / (float)d, m2 = row_sum<TPR>(s2, sm[turn + 1]) / (float)d;
         char *pdx = dx.p + ((int64_t)k * dx.worker + t * dx.row) * S;
-        const char *padd = add.p ? add.p + ((int64_t)k * add.worker + t * add.row) * S : nullptr;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int e = (j * TPR + c) * VEC;
+            const int e = (j * TPR + c) * N;
             if (e >= d) continue;
-            float r[VEC] = {};
-            if (padd) load_elements<BF16, VEC>(padd + (int64_t)e * S, r);
+            float r[N];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) r[i] += st.y * (a[j][i] - m1 - h[j][i] * m2);
-            store_elements<BF16, VEC>(pdx + (int64_t)e * S, r);
+            for (int i = 0; i < N; ++i) {
+                const float h = (px[j][i] - st.x) * st.y, a = pdy[j][i] * ww[j][i];
+                r[i] = st.y * (a - m1 - h * m2) + (add.p ? padd[j][i] : 0.f);
+            }
+            store_piece<BF16>(pdx + (int64_t)e * S, d - e, r);
         }
     }
     float *out = part + ((int64_t)k * gridDim.x + blockIdx.x) * 2 * d;
@@ -173,8 +191,8 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(GrawaRows dy, GrawaRows x, 
 #pragma unroll
                     for (int j = 0; j < NV; ++j)
 #pragma unroll
-                        for (int i = 0; i < VEC; ++i) {
-                            const int e = (j * TPR + c) * VEC + i;
+                        for (int i = 0; i < N; ++i) {
+                            const int e = (j * TPR + c) * N + i;
                             const float v = what ? db[j][i] : dw[j][i];
                             cols[e] = r ? cols[e] + v : v;
                         }
@@ -186,8 +204,8 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(GrawaRows dy, GrawaRows x, 
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const int e = (j * TPR + c) * VEC + i;
+            for (int i = 0; i < N; ++i) {
+                const int e = (j * TPR + c) * N + i;
                 if (e < d) {
                     out[e] = dw[j][i];
                     out[d + e] = db[j][i];
@@ -208,9 +226,9 @@ template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_back_long(Gr
     const float2 st = *(const float2 *)(stats + 2 * ((int64_t)k * T + t));
     float s1 = 0.f, s2 = 0.f, v, a, ww;
     for (int e = c; e < d; e += 1024) {
-        load_elements<BF16, 1>(px + (int64_t)e * S, &v);
-        load_elements<BF16, 1>(pdy + (int64_t)e * S, &a);
-        load_elements<BF16, 1>(pw + (int64_t)e * S, &ww);
+        v = load_one<BF16>(px + (int64_t)e * S);
+        a = load_one<BF16>(pdy + (int64_t)e * S);
+        ww = load_one<BF16>(pw + (int64_t)e * S);
         a *= ww;
         s1 += a;
         s2 += a * (v - st.x) * st.y;
@@ -220,12 +238,12 @@ template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_back_long(Gr
     const char *padd = add.p ? add.p + ((int64_t)k * add.worker + t * add.row) * S : nullptr;
     for (int e = c; e < d; e += 1024) {
         float r = 0.f;
-        load_elements<BF16, 1>(px + (int64_t)e * S, &v);
-        load_elements<BF16, 1>(pdy + (int64_t)e * S, &a);
-        load_elements<BF16, 1>(pw + (int64_t)e * S, &ww);
-        if (padd) load_elements<BF16, 1>(padd + (int64_t)e * S, &r);
+        v = load_one<BF16>(px + (int64_t)e * S);
+        a = load_one<BF16>(pdy + (int64_t)e * S);
+        ww = load_one<BF16>(pw + (int64_t)e * S);
+        if (padd) r = load_one<BF16>(padd + (int64_t)e * S);
         r += st.y * (a * ww - m1 - (v - st.x) * st.y * m2);
-        store_elements<BF16, 1>(pdx + (int64_t)e * S, &r);
+        store_one<BF16>(pdx + (int64_t)e * S, r);
     }
 }
 
@@ -236,8 +254,8 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_norm_back_cols(Gra
     if (e >= d) return;
     float dw = 0.f, db = 0.f, v, a;
     for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-        load_elements<BF16, 1>(x.p + ((int64_t)k * x.worker + t * x.row + e) * S, &v);
-        load_elements<BF16, 1>(dy.p + ((int64_t)k * dy.worker + t * dy.row + e) * S, &a);
+        v = load_one<BF16>(x.p + ((int64_t)k * x.worker + t * x.row + e) * S);
+        a = load_one<BF16>(dy.p + ((int64_t)k * dy.worker + t * dy.row + e) * S);
         const float2 st = *(const float2 *)(stats + 2 * ((int64_t)k * T + t));
         dw += a * (v - st.x) * st.y;
         db += a;
@@ -247,50 +265,49 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_norm_back_cols(Gra
     out[d + e] = db;
 }
 
-// The blocks' sums added up: 64 columns a block, its four waves take every fourth of the n parts.
-template <bool BF16> __global__ __launch_bounds__(256) void k_norm_sums(const float *part, int n, GrawaMat dw, GrawaMat db, int accumulate, int d)
+// The blocks' sums added up: 64 columns a block, its sixteen waves take every sixteenth of the n parts.
+template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_sums(const float *part, int n, GrawaMat dw, GrawaMat db, int accumulate, int d)
 {
     constexpr int S = BF16 ? 2 : 4;
-    __shared__ float sm[4][64];
+    __shared__ float sm[16][64];
     const int c = threadIdx.x % 64, g = threadIdx.x / 64, k = blockIdx.y, what = blockIdx.z;
     const int e = blockIdx.x * 64 + c;
     float s = 0.f;
-    if (e < d)
-        for (int i = g; i < n; i += 4) s += part[(((int64_t)k * n + i) * 2 + what) * d + e];
+    if (e < d) {
+#pragma unroll 8
+        for (int i = g; i < n; i += 16) s += part[(((int64_t)k * n + i) * 2 + what) * d + e];
+    }
     sm[g][c] = s;
     __syncthreads();
     const GrawaMat &m = what ? db : dw;
     if (g || e >= d || !m.p) return;
     char *p = m.p + ((int64_t)k * m.worker + e) * S;
-    float v = (sm[0][c] + sm[1][c]) + (sm[2][c] + sm[3][c]), old;
-    if (accumulate) {
-        load_elements<BF16, 1>(p, &old);
-        v += old;
-    }
-    store_elements<BF16, 1>(p, &v);
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) v += (sm[i][c] + sm[i + 1][c]) + (sm[i + 2][c] + sm[i + 3][c]);
+    if (accumulate) v += load_one<BF16>(p);
+    store_one<BF16>(p, v);
 }
 
-bool aligned(const GrawaRows &r, int S) { return !(((uintptr_t)r.p | (uint64_t)r.worker * S | (uint64_t)r.row * S) & 15); }
-bool aligned(const GrawaMat &r, int S) { return !(((uintptr_t)r.p | (uint64_t)r.worker * S) & 15); }
-
 // What takes a row of d elements: the fewest threads that hold it in at most 32 registers each.
-#define GRAWA_NORM_FORMS(GO, GOLONG, BF, VEC)                              \
+#define GRAWA_NORM_FORMS(GO, GOLONG, BF)                                   \
     do {                                                                   \
-        constexpr int N = 32 / VEC;                                        \
-        if (d <= 8 * 64) GO(BF, VEC, (8 / VEC), 64, 256);                  \
-        else if (d <= 16 * 64) GO(BF, VEC, (16 / VEC), 64, 256);           \
-        else if (d <= 16 * 256) GO(BF, VEC, (16 / VEC), 256, 256);         \
-        else if (d <= 32 * 256) GO(BF, VEC, N, 256, 256);                  \
-        else if (d <= 16 * 1024) GO(BF, VEC, (16 / VEC), 1024, 1024);      \
+        constexpr int N = GrawaPiece<BF>::N;                               \
+        if (d <= 8 * 64) GO(BF, (8 / N), 64, 256);                         \
+        else if (d <= 16 * 64) GO(BF, (16 / N), 64, 256);                  \
+        else if (d <= 16 * 256) GO(BF, (16 / N), 256, 256);                \
+        else if (d <= 32 * 256) GO(BF, (32 / N), 256, 256);                \
+        else if (d <= 16 * 1024) GO(BF, (16 / N), 1024, 1024);             \
         else GOLONG(BF);                                                   \
     } while (0)
 
 } // namespace
 
-// Blocks of a worker in the backward pass: enough for four on every CU over all workers, and each with some rows to add up.
+// Blocks of a worker in the backward pass: at most four for each CU over all workers, and each with rows enough (two for every one
+// that it holds at a time) that its sums are little beside them.
 int grawa_norm_blocks(int K, int64_t T, int64_t d)
 {
-    const int64_t rows = d <= 1024 ? 4 : 1, groups = (T + rows - 1) / rows;
+    const int64_t rows = d <= 1024 ? 4 : 1, groups = (T + 2 * rows - 1) / (2 * rows);
     const int64_t want = 1024 / K > 1 ? 1024 / K : 1;
     const int64_t n = groups < want ? groups : want;
     return (int)(n > 0 ? n : 1);
@@ -300,18 +317,12 @@ hipError_t grawa_launch_layer_norm(const grawa_sublayer *s, int64_t T, GrawaRows
                                    float *stats, hipStream_t st)
 {
     if (!T) return hipSuccess;
-    const int d = (int)s->d, S = s->dtype == GRAWA_BF16 ? 2 : 4;
-    const bool wide = d % (16 / S) == 0 && aligned(x, S) && aligned(y, S) && aligned(w, S) && (!b.p || aligned(b, S));
-#define GO(BF, VEC, NV, TPR, BLOCK)                                                                                      \
-    k_norm<BF, VEC, NV, TPR, BLOCK><<<dim3((unsigned)((T + BLOCK / TPR - 1) / (BLOCK / TPR)), (unsigned)s->K), BLOCK, 0, st>>>(x, w, b, eps, y, stats, T, d)
+    const int d = (int)s->d;
+#define GO(BF, NV, TPR, BLOCK)                                                                                           \
+    k_norm<BF, NV, TPR, BLOCK><<<dim3((unsigned)((T + BLOCK / TPR - 1) / (BLOCK / TPR)), (unsigned)s->K), BLOCK, 0, st>>>(x, w, b, eps, y, stats, T, d)
 #define GOLONG(BF) k_norm_long<BF><<<dim3((unsigned)T, (unsigned)s->K), 1024, 0, st>>>(x, w, b, eps, y, stats, T, d)
-    if (S == 2) {
-        if (wide) GRAWA_NORM_FORMS(GO, GOLONG, true, 8);
-        else GRAWA_NORM_FORMS(GO, GOLONG, true, 1);
-    } else {
-        if (wide) GRAWA_NORM_FORMS(GO, GOLONG, false, 4);
-        else GRAWA_NORM_FORMS(GO, GOLONG, false, 1);
-    }
+    if (s->dtype == GRAWA_BF16) GRAWA_NORM_FORMS(GO, GOLONG, true);
+    else GRAWA_NORM_FORMS(GO, GOLONG, false);
 #undef GO
 #undef GOLONG
     return hipGetLastError();
@@ -320,33 +331,27 @@ hipError_t grawa_launch_layer_norm(const grawa_sublayer *s, int64_t T, GrawaRows
 hipError_t grawa_launch_layer_norm_backward(const grawa_sublayer *s, int64_t T, GrawaRows dy, GrawaRows x, GrawaMat w, const float *stats,
                                             GrawaRows add, GrawaRows dx, GrawaMat dw, GrawaMat db, int accumulate, hipStream_t st)
 {
-    const int d = (int)s->d, S = s->dtype == GRAWA_BF16 ? 2 : 4, nb = T ? grawa_norm_blocks(s->K, T, d) : 0;
+    const int d = (int)s->d, nb = T ? grawa_norm_blocks(s->K, T, d) : 0;
     float *part = s->norm_part;
     if (T) {
-        const bool wide = d % (16 / S) == 0 && aligned(x, S) && aligned(dy, S) && aligned(dx, S) && aligned(w, S) && (!add.p || aligned(add, S));
         const dim3 grid((unsigned)nb, (unsigned)s->K);
-#define GO(BF, VEC, NV, TPR, BLOCK) k_norm_back<BF, VEC, NV, TPR, BLOCK><<<grid, BLOCK, 0, st>>>(dy, x, w, stats, add, dx, part, T, d)
+#define GO(BF, NV, TPR, BLOCK) k_norm_back<BF, NV, TPR, BLOCK><<<grid, BLOCK, 0, st>>>(dy, x, w, stats, add, dx, part, T, d)
 #define GOLONG(BF)                                                                                                               \
     do {                                                                                                                         \
         k_norm_back_cols<BF><<<dim3((unsigned)nb, (unsigned)((d + 255) / 256), (unsigned)s->K), 256, 0, st>>>(dy, x, stats, part, T, d); \
         k_norm_back_long<BF><<<dim3((unsigned)T, (unsigned)s->K), 1024, 0, st>>>(dy, x, w, stats, add, dx, T, d);                \
     } while (0)
-        if (S == 2) {
-            if (wide) GRAWA_NORM_FORMS(GO, GOLONG, true, 8);
-            else GRAWA_NORM_FORMS(GO, GOLONG, true, 1);
-        } else {
-            if (wide) GRAWA_NORM_FORMS(GO, GOLONG, false, 4);
-            else GRAWA_NORM_FORMS(GO, GOLONG, false, 1);
-        }
+        if (s->dtype == GRAWA_BF16) GRAWA_NORM_FORMS(GO, GOLONG, true);
+        else GRAWA_NORM_FORMS(GO, GOLONG, false);
 #undef GO
 #undef GOLONG
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     const dim3 sums((unsigned)((d + 63) / 64), (unsigned)s->K, 2);
-    if (S == 2)
-        k_norm_sums<true><<<sums, 256, 0, st>>>(part, nb, dw, db, accumulate, d);
+    if (s->dtype == GRAWA_BF16)
+        k_norm_sums<true><<<sums, 1024, 0, st>>>(part, nb, dw, db, accumulate, d);
     else
-        k_norm_sums<false><<<sums, 256, 0, st>>>(part, nb, dw, db, accumulate, d);
+        k_norm_sums<false><<<sums, 1024, 0, st>>>(part, nb, dw, db, accumulate, d);
     return hipGetLastError();
 }

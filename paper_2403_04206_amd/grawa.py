@@ -88,7 +88,8 @@ def lib():
         fn = getattr(L, name)
         fn.restype = res
         fn.argtypes = args
-    for name in ("grawa_lgrawa_update", "grawa_local_step_scored", "grawa_local_lgrawa_update", "grawa_local_mgrawa_update"):
+    for name in ("grawa_lgrawa_update", "grawa_local_step_scored", "grawa_local_lgrawa_update", "grawa_local_mgrawa_update", "grawa_layer_norm",
+                 "grawa_layer_norm_backward", "grawa_ffn", "grawa_dropout"):
         _addresses[name] = C.cast(getattr(L, name), vp).value
     _lib = L
     return L
@@ -127,6 +128,7 @@ def _stream_no_tensors(stream=None):
 # The same of whole calls: their status, or None for any argument that is not plainly in order; the Python call follows then.
 try:
     from ._rows import built_for, rows as _native_rows, scored as _native_scored, local as _native_local, lgrawa as _native_lgrawa
+    from ._rows import norm as _native_norm, norm_back as _native_norm_back, feed as _native_feed, drop as _native_drop
     if built_for != buildlib.rows_built_for():
         raise ImportError("_rows.so is for %s" % built_for)
 except Exception:                        # not built, or not for this torch: the Python checks alone
@@ -135,7 +137,7 @@ except Exception:                        # not built, or not for this torch: the
 
     def _native_scored(*args):
         return None
-    _native_local = _native_lgrawa = _native_scored
+    _native_local = _native_lgrawa = _native_norm = _native_norm_back = _native_feed = _native_drop = _native_scored
 
 
 _NULL = C.c_void_p(0)
@@ -622,6 +624,11 @@ class SublayerPlan:
 
     def layer_norm(self, x, weight, bias, out, eps=1e-5, stats_out=None, stream=None):
         """grawa_layer_norm: out = (x - mean) / sqrt(var + eps) * weight + bias; stats_out: float32 [K, T, 2] for the backward pass."""
+        if stream is None:
+            st = _native_norm(_addresses.get("grawa_layer_norm"), self._h.value, self.K, self.T, self.d, _DTYPES[self.dtype], x, weight, bias, out, eps,
+                              stats_out, _stream)
+            if st is not None:
+                return _check(st, "grawa_layer_norm")
         K, d, dt, T = self.K, self.d, self.dtype, self._count(x, "x")
         _check(lib().grawa_layer_norm(self._h, T, _tokens(x, K, T, d, dt, "x"), _mats(weight, (K, d), dt, "weight"),
                                       _mats(bias, (K, d), dt, "bias", True), float(eps), _tokens(out, K, T, d, dt, "out"),
@@ -629,6 +636,11 @@ class SublayerPlan:
 
     def layer_norm_backward(self, dy, x, weight, stats, dx, dweight, dbias, add=None, accumulate=False, stream=None):
         """grawa_layer_norm_backward: dx (plus `add`), dweight and dbias, added to what they hold with accumulate."""
+        if stream is None:
+            st = _native_norm_back(_addresses.get("grawa_layer_norm_backward"), self._h.value, self.K, self.T, self.d, _DTYPES[self.dtype], dy, x, weight,
+                                   stats, dx, dweight, dbias, add, accumulate, _stream)
+            if st is not None:
+                return _check(st, "grawa_layer_norm_backward")
         K, d, dt, T = self.K, self.d, self.dtype, self._count(dy, "dy")
         _check(lib().grawa_layer_norm_backward(
             self._h, T, _tokens(dy, K, T, d, dt, "dy"), _tokens(x, K, T, d, dt, "x"), _mats(weight, (K, d), dt, "weight"),
@@ -638,6 +650,11 @@ class SublayerPlan:
 
     def ffn(self, x, wg, wu, wd, out, save=None, residual=None, p=0.0, rng=None, site=0, stream=None):
         """grawa_ffn: out = residual + dropout((act(x wg^T) * (x wu^T)) wd^T)."""
+        if stream is None and save is None:
+            st = _native_feed(_addresses.get("grawa_ffn"), self._h.value, self.K, self.T, self.d, _DTYPES[self.dtype], x, wg, wu, wd, out, residual, p, rng,
+                              site, self.f, _stream)
+            if st is not None:
+                return _check(st, "grawa_ffn")
         K, d, f, dt, T = self.K, self.d, self.f, self.dtype, self._count(x, "x")
         _check(lib().grawa_ffn(
             self._h, T, _tokens(x, K, T, d, dt, "x"), _mats(wg, (K, f, d), dt, "wg"), _mats(wu, (K, f, d), dt, "wu"),
@@ -656,6 +673,10 @@ class SublayerPlan:
 
 def dropout(x, out, p, rng, site=0, residual=None, stream=None):
     """grawa_dropout: out = residual + keep(x) / (1 - p) for x [K, T, d]; rng: int64 CUDA tensor, the seed and the step."""
+    if stream is None:
+        st = _native_drop(_addresses.get("grawa_dropout"), x, out, p, rng, site, residual, _stream)
+        if st is not None:
+            return _check(st, "grawa_dropout")
     if x is None or x.ndim != 3 or x.dtype not in _DTYPES:
         raise TypeError("x must be a float32 or bfloat16 CUDA tensor [K, T, d]")
     K, T, d = x.shape

@@ -1,0 +1,139 @@
+"""The feed-forward sublayer's calls of the binding in native code (csrc/grawa_rows.cpp) against the Python ones: for every form of an argument
+both pass the library the same values, or the native call leaves it to the Python one, which passes or refuses it as before."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2403_04206_amd import grawa
+
+K, T, d, f = 3, 5, 8, 16
+INT, I64, PTR, F32, U32 = C.c_int, C.c_int64, C.c_void_p, C.c_float, C.c_uint32
+ROWS, MATS = C.POINTER(grawa._RowsArg), C.POINTER(grawa._MatsArg)
+SIGNATURES = {"grawa_layer_norm": [PTR, I64, ROWS, MATS, MATS, F32, ROWS, PTR, PTR],
+              "grawa_layer_norm_backward": [PTR, I64, ROWS, ROWS, MATS, PTR, ROWS, ROWS, MATS, MATS, INT, PTR],
+              "grawa_ffn": [PTR, I64, ROWS, MATS, MATS, MATS, ROWS, F32, PTR, U32, ROWS, PTR, PTR],
+              "grawa_dropout": [INT, I64, I64, INT, ROWS, ROWS, F32, PTR, U32, ROWS, PTR]}
+NATIVE = {n: getattr(grawa, n) for n in ("_native_norm", "_native_norm_back", "_native_feed", "_native_drop")}
+
+
+def plain(v):
+    if isinstance(v, C._Pointer):
+        return tuple(getattr(v.contents, n) for n, _ in v.contents._fields_) if v else None
+    return v
+
+
+class Library:
+    """Functions of the library's signatures that note what they are given.  Their Python calls pass structures by reference, as the
+    library's own signatures take them."""
+    def __init__(self):
+        self.seen = []
+        for name, sig in SIGNATURES.items():
+            fn = C.CFUNCTYPE(INT, *sig)(lambda *a, name=name: self.seen.append((name,) + tuple(plain(v) for v in a)) or grawa.OK)
+            setattr(self, name, fn)
+
+
+def tokens(dev):
+    b = torch.zeros((K + 1, T + 1, d + 4), device=dev, dtype=torch.bfloat16)
+    short = torch.zeros((K, T, d), device=dev, dtype=torch.bfloat16)
+    short.untyped_storage().resize_(short.untyped_storage().nbytes() - 2)
+    return [b[:K, :T, :d], torch.zeros((K, T, d), device=dev, dtype=torch.bfloat16), b[:K, :T - 2, :d], b[:K, :T + 1, :d], b[:K, :T, :d + 1], b[:K, :T, 1:d + 1], b[:1, :T, :d].expand(K, T, d),
+            b[:K, :1, :d].expand(K, T, d), b[:T].permute(1, 0, 2)[:T, :K, :d], b[:K, :T, :d].float(), b[0, :T, :d], short,
+            b[:K, :T, ::2][:, :, :d], b[:K, :0, :d], None, 3]
+
+
+def mats(dev, *shape):
+    n = 1
+    for s in shape:
+        n *= s
+    b = torch.zeros((K, n + 9), device=dev, dtype=torch.bfloat16)
+    return [b[:, 3:3 + n].view(K, *shape), b[:, :n].view(K, *shape).clone(), b[:2, :n].view(2, *shape), b[:1, :n].view(1, *shape).expand(K, *shape), b[:, :n].view(K, *shape).float(), b[:, :n - 1],
+            torch.zeros((K, *shape[:-1], 2 * shape[-1]), device=dev, dtype=torch.bfloat16)[..., ::2], torch.zeros((K, *shape[::-1]), device=dev, dtype=torch.bfloat16).transpose(1, -1), None, "w"]
+
+
+def stats(dev):
+    b = torch.zeros((K, T, 2), device=dev)
+    return [None, b, b.double(), b[:, :, :1], torch.zeros((K, 2, T), device=dev).transpose(1, 2), torch.zeros((K, T + 1, 2), device=dev)]
+
+
+def rngs(dev):
+    b = torch.zeros(4, dtype=torch.int64, device=dev)
+    return [None, b[:2], b[1:], b[:1], b[::2], b.double(), b.view(2, 2), 7]
+
+
+def calls_of(dev):
+    plan = grawa.SublayerPlan.__new__(grawa.SublayerPlan)
+    plan.K, plan.T, plan.d, plan.f, plan.dtype, plan._h = K, T, d, f, torch.bfloat16, PTR(0x1000)
+    x, w, wg, wd, st, rng = tokens(dev), mats(dev, d), mats(dev, f, d), mats(dev, d, f), stats(dev), rngs(dev)
+    X, W, G, D, S = x[0], w[0], wg[0], wd[0], st[1]
+    calls = [lambda a=a: plan.layer_norm(a, W, W, X) for a in x] + [lambda a=a: plan.layer_norm(X, W, None, a, 0.5) for a in x]
+    calls += [lambda a=a: plan.layer_norm(x[2], W, W, a) for a in x]
+    calls += [lambda a=a: plan.layer_norm(X, a, W, X) for a in w] + [lambda a=a: plan.layer_norm(X, W, a, X, stats_out=S) for a in w]
+    calls += [lambda a=a: plan.layer_norm(X, W, W, X, stats_out=a) for a in st] + [lambda e=e: plan.layer_norm(X, W, W, X, eps=e) for e in (0, 1e-5, 1, "e", None)]
+    for i in range(4):
+        calls += [lambda a=a, i=i: plan.layer_norm_backward(*[a if i == j else X for j in range(2)], W, S, a if i == 2 else X, W, W, add=a if i == 3 else None) for a in x]
+    for i in range(3):
+        calls += [lambda a=a, i=i: plan.layer_norm_backward(X, X, a if i == 0 else W, S, X, a if i == 1 else W, a if i == 2 else W) for a in w]
+    calls += [lambda a=a: plan.layer_norm_backward(X, X, W, a, X, W, W) for a in st] + [lambda a=a: plan.layer_norm_backward(X, X, W, S, X, W, None, accumulate=a) for a in (True, False, 1, 0)]
+    for i in range(3):
+        calls += [lambda a=a, i=i: plan.ffn(a if i == 0 else X, G, G, D, a if i == 1 else X, residual=a if i == 2 else None) for a in x]
+    calls += [lambda a=a: plan.ffn(X, a, G, D, X) for a in wg] + [lambda a=a: plan.ffn(X, G, a, D, X) for a in wg] + [lambda a=a: plan.ffn(X, G, G, a, X) for a in wd]
+    calls += [lambda r=r, p=p, s=s: plan.ffn(X, G, G, D, X, p=p, rng=r, site=s) for r in rng for p in (0, 0.0, 0.25, "p") for s in (0, 5, -1, 1 << 32)]
+    for i in range(3):
+        calls += [lambda a=a, i=i: grawa.dropout(a if i == 0 else X, a if i == 1 else X, 0.0, None, residual=a if i == 2 else None) for a in x]
+    calls += [lambda r=r, p=p, s=s: grawa.dropout(X, X, p, r, site=s) for r in rng for p in (0, 0.0, 0.25, "p") for s in (0, (1 << 32) - 1, -1, 1 << 32)]
+    return plan, calls
+
+
+def outcome(call, library, native, monkeypatch):
+    library.seen.clear()
+    for name in NATIVE:
+        monkeypatch.setattr(grawa, name, NATIVE[name] if native else lambda *a: None)
+    try:
+        call()
+        return library.seen[:]
+    except (TypeError, ValueError, AttributeError, C.ArgumentError) as e:
+        return type(e) if not isinstance(e, (AttributeError, C.ArgumentError)) else TypeError
+    finally:
+        for name, fn in NATIVE.items():
+            monkeypatch.setattr(grawa, name, fn)
+
+
+def compare(dev, monkeypatch):
+    library = Library()
+    monkeypatch.setattr(grawa, "lib", lambda: library)
+    for name in SIGNATURES:
+        monkeypatch.setitem(grawa._addresses, name, C.cast(getattr(library, name), PTR).value)
+    plan, calls = calls_of(dev)
+    kinds = set()
+    for i, call in enumerate(calls):
+        got, want = outcome(call, library, True, monkeypatch), outcome(call, library, False, monkeypatch)
+        assert got == want, i
+        kinds.add(type(want))
+    plan._h = PTR()                     # nothing to destroy
+    return kinds
+
+
+def test_host_tensors(monkeypatch):
+    assert compare("cpu", monkeypatch) == {type}
+
+
+@pytest.mark.gpu
+def test_device_tensors(monkeypatch):
+    assert grawa._native_norm.__module__ != grawa.__name__, "the native calls are not built"
+    assert compare("cuda:0", monkeypatch) == {type, list}
+
+
+@pytest.mark.gpu
+def test_the_native_call_is_the_one_that_runs(monkeypatch):
+    monkeypatch.setattr(grawa, "_tokens", None)
+    monkeypatch.setattr(grawa, "_mats", None)
+    dev = "cuda:0"
+    x, w, m, md = torch.zeros((K, T, d), device=dev), torch.ones((K, d), device=dev), torch.ones((K, f, d), device=dev), torch.ones((K, d, f), device=dev)
+    stat, rng = torch.zeros((K, T, 2), device=dev), torch.zeros(2, dtype=torch.int64, device=dev)
+    with grawa.SublayerPlan(K, T, d, f, dtype=torch.float32) as plan:
+        plan.layer_norm(x, w, w, x, stats_out=stat)
+        plan.layer_norm_backward(x, x, w, stat, x, w, w, add=x)
+        plan.ffn(x, m, m, md, x.clone(), residual=x, p=0.5, rng=rng, site=1)
+        grawa.dropout(x, x, 0.5, rng)
+        torch.cuda.synchronize()
