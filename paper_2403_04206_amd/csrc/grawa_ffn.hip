@@ -6,7 +6,7 @@
 // kernel makes dH and from it dG and dU in its epilogue, so that no pass over [T][f] arrays stands between the products.
 //
 // Roundings.  bfloat16: H, dG and dU are rounded to bfloat16, as the matrix instructions take them; G and U are kept for the
-// backward pass in float32 (a rounding of theirs would be a third one on the way to dWg, dWu and dx).  float32: every matrix
+// backward pass with eight bits more than that (a rounding of theirs would be a third one on the way to dWg, dWu and dx).  float32: every matrix
 // element is split exactly into three bfloat16 terms and the six largest of the nine products of terms are summed in float32;
 // what is left out is below 2^-24 of a product.  (An infinity times a number that is exactly a bfloat16 gives NaN there.)
 #include "grawa_few.h"
@@ -117,33 +117,68 @@ template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z,
     }
 }
 
-// Gate and up before the activation are kept for the backward pass as the fragments of the matrix instruction: blocks of 16 x 16, each
-// 64 lanes by 16 bytes, so that both kernels move them by whole KiB straight from and to the registers.
+// Gate and up before the activation are kept for the backward pass as the fragments of the matrix instruction, blocks of 16 x 16 by 64
+// lanes, so that both kernels move them by whole KiB straight from and to the registers.  Float32 keeps them whole: a plane of G, a
+// plane of U.  Bfloat16 keeps the upper 24 bits (a sign, 8 and 15: 2^-16 of a value, a hundredth of what dG and dU are rounded by):
+// a plane of 16 bytes a lane with the upper halves of four G and four U, then one of 8 bytes with the next byte of each.  The forward
+// and the backward kernel of 8 x 2048 tokens, 1024 x 4096, move 270 MB less for it.
+template <int PLANES> struct KeptGateUp {
+    char *p;          // null: not kept
+    int64_t all;      // fragments of all workers, elements of one plane
+    __device__ __forceinline__ void put(int64_t at, const grawa_f32x4 &g, const grawa_f32x4 &u) const
+    {
+        if constexpr (PLANES == 3) {
+            *(grawa_f32x4 *)(p + at * 4) = g;
+            *(grawa_f32x4 *)(p + (all + at) * 4) = u;
+        } else {
+            uint32_t a[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(g[j]), a[4 + j] = __float_as_uint(u[j]);
+            uint32_t hi[4], lo[2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) hi[j] = __builtin_amdgcn_perm(a[2 * j + 1], a[2 * j], 0x07060302);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) lo[j] = __builtin_amdgcn_perm(a[4 * j + 1], a[4 * j], 0x0c0c0501) | __builtin_amdgcn_perm(a[4 * j + 3], a[4 * j + 2], 0x05010c0c);
+            *(uint4 *)(p + at * 4) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *(uint2 *)(p + all * 4 + at * 2) = make_uint2(lo[0], lo[1]);
+        }
+    }
+    __device__ __forceinline__ void get(int64_t at, grawa_f32x4 &g, grawa_f32x4 &u) const
+    {
+        if constexpr (PLANES == 3) {
+            g = *(const grawa_f32x4 *)(p + at * 4);
+            u = *(const grawa_f32x4 *)(p + (all + at) * 4);
+        } else {
+            const uint4 h = *(const uint4 *)(p + at * 4);
+            const uint2 l = *(const uint2 *)(p + all * 4 + at * 2);
+            const uint32_t hi[4] = {h.x, h.y, h.z, h.w}, lo[2] = {l.x, l.y}, which[4] = {0x0504000c, 0x0706010c, 0x0504020c, 0x0706030c};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[j] = __uint_as_float(__builtin_amdgcn_perm(hi[j / 2], lo[0], which[j]));
+                u[j] = __uint_as_float(__builtin_amdgcn_perm(hi[2 + j / 2], lo[1], which[j]));
+            }
+        }
+    }
+};
 
 // Epilogue of gate and up: H, and for a backward pass G and U.
 template <int PLANES, int ACT> struct EpiGateUp {
     static constexpr int OUTS = 1, VEC = 8;
     char *h;            // [PLANES][K][M][pitch]
-    float *gate, *up;   // [K][fragments], or null
+    KeptGateUp<PLANES> kept;
     int64_t plane;      // bytes between the planes of h
     int64_t worker;     // elements of a worker's h
     int64_t blocks;     // fragments of a worker, elements
     int N, pitch;
+    int64_t at0;
     __device__ __forceinline__ void tile(int k, int)
     {
         h += k * worker * 2;
-        if (gate) {
-            gate += k * blocks;
-            up += k * blocks;
-        }
+        at0 = k * blocks;
     }
     __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &g, grawa_f32x4 &u) const
     {
-        if (gate) {
-            const int64_t at = grawa_fragment_at(mb, nb, (N + 15) >> 4, lane);
-            *(grawa_f32x4 *)(gate + at) = g;
-            *(grawa_f32x4 *)(up + at) = u;
-        }
+        if (kept.p) kept.put(at0 + grawa_fragment_at(mb, nb, (N + 15) >> 4, lane), g, u);
 #pragma unroll
         for (int j = 0; j < 4; ++j) g[j] = act_of<PLANES, ACT>(g[j]) * u[j];
     }
@@ -159,21 +194,21 @@ template <int PLANES, int ACT> struct EpiGateUp {
 // Epilogue of dH: dG and dU.
 template <int PLANES, int ACT> struct EpiBack {
     static constexpr int OUTS = 2, VEC = 8;
-    const float *gate, *up;
+    KeptGateUp<PLANES> kept;
     char *dg, *du;
     int64_t plane, worker, blocks;
     int N, pitch;
+    int64_t at0;
     __device__ __forceinline__ void tile(int k, int)
     {
-        gate += k * blocks;
-        up += k * blocks;
+        at0 = k * blocks;
         dg += k * worker * 2;
         du += k * worker * 2;
     }
     __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &dh, grawa_f32x4 &out) const
     {
-        const int64_t at = grawa_fragment_at(mb, nb, (N + 15) >> 4, lane);
-        const grawa_f32x4 g = *(const grawa_f32x4 *)(gate + at), u = *(const grawa_f32x4 *)(up + at);
+        grawa_f32x4 g, u;
+        kept.get(at0 + grawa_fragment_at(mb, nb, (N + 15) >> 4, lane), g, u);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float a, da;
@@ -409,9 +444,8 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
     const grawa_sublayer *s = c.s;
     const int64_t n = c.T * s->fp;
     const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
-    float *gate = (float *)save;
-    char *h = save ? save + s->K * blocks * 8 : s->h;
-    const EpiGateUp<PLANES, ACT> inner{h, gate, gate ? gate + s->K * blocks : nullptr, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
+    char *h = save ? save + s->K * blocks * grawa_kept_bytes(s) : s->h;
+    const EpiGateUp<PLANES, ACT> inner{h, {save, s->K * blocks}, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
     const EpiStore<PLANES == 1, true> outer{y, residual, drop, (int)s->d, (int)c.T, 0, 0};
     // Few tokens: see grawa_few.h.  To the end in float32, which tiles multiply six times: 4 workers, 1024 x 4096, 64 tokens 189 us, by tiles
     // 240.  In bfloat16 up to 16, 67 us and 82 with one matrix of 4096 x 11264, and up to 32 while the matrices are small and the
@@ -454,12 +488,11 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
     c.copy_all();
     const int64_t n = c.T * s->fp;
     const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
-    const float *gate = (const float *)save;
-    const Operand oh = c.inner((char *)save + s->K * blocks * 8), odg = c.inner(s->dg), odu = c.inner(s->du);
+    const Operand oh = c.inner((char *)save + s->K * blocks * grawa_kept_bytes(s)), odg = c.inner(s->dg), odu = c.inner(s->du);
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ody, od, nullptr);
-        const EpiBack<PLANES, ACT> epi{gate, gate + s->K * blocks, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp};
+        const EpiBack<PLANES, ACT> epi{{(char *)save, s->K * blocks}, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
     auto store = [&](const Operand &a, const Operand &b, GrawaMat w, int64_t M, int64_t N) {

@@ -46,12 +46,13 @@ static inline int64_t grawa_round16(int64_t n) { return (n + 15) & ~(int64_t)15;
 
 constexpr int GRAWA_FEW = 64; // tokens of a worker up to which a forward pass may take the kernels of grawa_few.h
 
-// The buffer that a training forward leaves to its backward: gate and up before the activation in float32, in fragments of 16 x 16; then
+// The buffer that a training forward leaves to its backward: gate and up before the activation, in fragments of 16 x 16; then
 // their product in bfloat16 planes, [planes][K][T][fp]; then with float32, unless the tokens are few, the planes of x and of the
 // three matrices, [3][K][T][dp], 2 x [3][K][f][dp], [3][K][d][fp].  All parts are multiples of 16 bytes.
+static inline int64_t grawa_kept_bytes(const grawa_sublayer *s) { return s->planes == 1 ? 6 : 8; } // of a gate and an up, see grawa_ffn.hip
 static inline int64_t grawa_save_bytes_own(const grawa_sublayer *s, int64_t T)
 {
-    return (int64_t)s->K * (grawa_round16(T) * grawa_round16(s->f) * 8 + T * s->fp * 2 * s->planes);
+    return (int64_t)s->K * (grawa_round16(T) * grawa_round16(s->f) * grawa_kept_bytes(s) + T * s->fp * 2 * s->planes);
 }
 static inline bool grawa_keeps_copies(const grawa_sublayer *s, int64_t T) { return s->planes == 3 && T > GRAWA_FEW; }
 static inline int64_t grawa_save_bytes(const grawa_sublayer *s, int64_t T)
