@@ -157,7 +157,8 @@ __global__ __launch_bounds__(GRAWA_FEW_WAVES * 64, 1) void k_few(GrawaFew g, Epi
             v[0] += *(const grawa_f32x4 *)&sums[w][i * NB + j][lane * 4];
             if (DUAL) u[0] += *(const grawa_f32x4 *)&sums[w][i * NB + NF + j][lane * 4];
         }
-        if (i * 16 < g.M && n0 + j * 16 < g.N) grawa_finish<1>(epi, corners[wave], i * 16, n0 + j * 16, lane, g.M, g.N, v, u);
+        typename Epi::Ahead r[1]; // the epilogues of these products read nothing
+        if (i * 16 < g.M && n0 + j * 16 < g.N) grawa_finish<1>(epi, corners[wave], i * 16, n0 + j * 16, lane, g.M, g.N, r, v, u);
     }
 }
 

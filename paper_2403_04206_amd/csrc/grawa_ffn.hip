@@ -90,31 +90,53 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_planes(CopyJobs jo
     }
 }
 
-// e^z: for results that are rounded to bfloat16 by the hardware's 2^z, whose argument's rounding costs z 2^-24 of it.
-template <int PLANES> __device__ __forceinline__ float exp_of(float z) { return PLANES == 1 ? __expf(z) : expf(z); }
-
-// The activation and its derivative.
-template <int PLANES, int ACT> __device__ __forceinline__ float act_of(float z)
+// The activation and its derivative.  Float32 calls the mathematical functions.  For results that are rounded to bfloat16 the hardware's
+// 2^z and 1/z (an ulp each) do, and for the error function formula 7.1.26 of Abramowitz and Stegun, "Handbook of Mathematical
+// Functions" (1964), taken as erfc(x) e^(x^2) so that small values keep a relative error of 1e-6: with division, expf and erff the
+// kernel of dH took 266 us for 8 x 2048 tokens, 1024 x 4096, so it takes 252.
+template <int PLANES> __device__ __forceinline__ float sigmoid_of(float z)
 {
-    if constexpr (ACT == GRAWA_ACT_SILU) return z / (1.f + exp_of<PLANES>(-z));
-    if constexpr (ACT == GRAWA_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    return z * (z > 0.f ? 1.f : 0.f);
+    if constexpr (PLANES == 3) return 1.f / (1.f + expf(-z));
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+}
+
+// The normal distribution's cumulative function at z and its density.
+template <int PLANES> __device__ __forceinline__ void normal_of(float z, float &cdf, float &density)
+{
+    if constexpr (PLANES == 3) {
+        cdf = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        density = expf(-0.5f * z * z) * 0.39894228040143268f;
+    } else {
+        const float x = fabsf(z) * 0.70710678118654752f, e = __builtin_amdgcn_exp2f(x * x * -1.4426950408889634f);
+        const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+        const float half = 0.5f * e * (t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))));
+        cdf = z < 0.f ? half : 1.f - half;
+        density = e * 0.39894228040143268f;
+    }
 }
 
 template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z, float &a, float &da)
 {
     if constexpr (ACT == GRAWA_ACT_SILU) {
-        const float s = 1.f / (1.f + exp_of<PLANES>(-z));
+        const float s = sigmoid_of<PLANES>(z);
         a = z * s;
-        da = s * (1.f + z * (1.f - s));
+        da = s + a * (1.f - s);
     } else if constexpr (ACT == GRAWA_ACT_GELU) {
-        const float cdf = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        float cdf, density;
+        normal_of<PLANES>(z, cdf, density);
         a = z * cdf;
-        da = cdf + z * exp_of<PLANES>(-0.5f * z * z) * 0.39894228040143268f;
+        da = cdf + z * density;
     } else {
         da = z > 0.f ? 1.f : 0.f;
         a = z * da;
     }
+}
+
+template <int PLANES, int ACT> __device__ __forceinline__ float act_of(float z)
+{
+    float a, da;
+    act_both<PLANES, ACT>(z, a, da);
+    return a;
 }
 
 // Gate and up before the activation are kept for the backward pass as the fragments of the matrix instruction, blocks of 16 x 16 by 64
@@ -143,20 +165,28 @@ template <int PLANES> struct KeptGateUp {
             *(uint2 *)(p + all * 4 + at * 2) = make_uint2(lo[0], lo[1]);
         }
     }
-    __device__ __forceinline__ void get(int64_t at, grawa_f32x4 &g, grawa_f32x4 &u) const
+    struct Raw {
+        uint32_t w[PLANES == 3 ? 8 : 6];
+    };
+    __device__ __forceinline__ void get(int64_t at, Raw &r) const
     {
+        const uint4 a = *(const uint4 *)(p + at * 4);
+        r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w;
         if constexpr (PLANES == 3) {
-            g = *(const grawa_f32x4 *)(p + at * 4);
-            u = *(const grawa_f32x4 *)(p + (all + at) * 4);
+            const uint4 b = *(const uint4 *)(p + (all + at) * 4);
+            r.w[4] = b.x, r.w[5] = b.y, r.w[6] = b.z, r.w[7] = b.w;
         } else {
-            const uint4 h = *(const uint4 *)(p + at * 4);
-            const uint2 l = *(const uint2 *)(p + all * 4 + at * 2);
-            const uint32_t hi[4] = {h.x, h.y, h.z, h.w}, lo[2] = {l.x, l.y}, which[4] = {0x0504000c, 0x0706010c, 0x0504020c, 0x0706030c};
+            const uint2 b = *(const uint2 *)(p + all * 4 + at * 2);
+            r.w[4] = b.x, r.w[5] = b.y;
+        }
+    }
+    static __device__ __forceinline__ void values(const Raw &r, grawa_f32x4 &g, grawa_f32x4 &u)
+    {
+        constexpr uint32_t which[4] = {0x0504000c, 0x0706010c, 0x0504020c, 0x0706030c};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                g[j] = __uint_as_float(__builtin_amdgcn_perm(hi[j / 2], lo[0], which[j]));
-                u[j] = __uint_as_float(__builtin_amdgcn_perm(hi[2 + j / 2], lo[1], which[j]));
-            }
+        for (int j = 0; j < 4; ++j) {
+            g[j] = __uint_as_float(PLANES == 3 ? r.w[j] : __builtin_amdgcn_perm(r.w[j / 2], r.w[4], which[j]));
+            u[j] = __uint_as_float(PLANES == 3 ? r.w[4 + j] : __builtin_amdgcn_perm(r.w[2 + j / 2], r.w[5], which[j]));
         }
     }
 };
@@ -176,7 +206,9 @@ template <int PLANES, int ACT> struct EpiGateUp {
         h += k * worker * 2;
         at0 = k * blocks;
     }
-    __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &g, grawa_f32x4 &u) const
+    typedef GrawaNothing Ahead;
+    __device__ __forceinline__ void ahead(int, int, int, Ahead &) const {}
+    __device__ __forceinline__ void fragment(int mb, int nb, int lane, const Ahead &, grawa_f32x4 &g, grawa_f32x4 &u) const
     {
         if (kept.p) kept.put(at0 + grawa_fragment_at(mb, nb, (N + 15) >> 4, lane), g, u);
 #pragma unroll
@@ -184,9 +216,10 @@ template <int PLANES, int ACT> struct EpiGateUp {
     }
     __device__ __forceinline__ void put(int, int m, int n, float *v) const
     {
+        if (n + 8 > N)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (n + j >= N) v[j] = 0.f;
+            for (int j = 0; j < 8; ++j)
+                if (n + j >= N) v[j] = 0.f;
         store_planes8<PLANES>(h + ((int64_t)m * pitch + n) * 2, plane, v);
     }
 };
@@ -205,10 +238,12 @@ template <int PLANES, int ACT> struct EpiBack {
         dg += k * worker * 2;
         du += k * worker * 2;
     }
-    __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &dh, grawa_f32x4 &out) const
+    typedef typename KeptGateUp<PLANES>::Raw Ahead;
+    __device__ __forceinline__ void ahead(int mb, int nb, int lane, Ahead &r) const { kept.get(at0 + grawa_fragment_at(mb, nb, (N + 15) >> 4, lane), r); }
+    __device__ __forceinline__ void fragment(int, int, int, const Ahead &r, grawa_f32x4 &dh, grawa_f32x4 &out) const
     {
         grawa_f32x4 g, u;
-        kept.get(at0 + grawa_fragment_at(mb, nb, (N + 15) >> 4, lane), g, u);
+        kept.values(r, g, u);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float a, da;
@@ -219,9 +254,10 @@ template <int PLANES, int ACT> struct EpiBack {
     }
     __device__ __forceinline__ void put(int o, int m, int n, float *v) const
     {
+        if (n + 8 > N)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (n + j >= N) v[j] = 0.f;
+            for (int j = 0; j < 8; ++j)
+                if (n + j >= N) v[j] = 0.f;
         store_planes8<PLANES>((o ? du : dg) + ((int64_t)m * pitch + n) * 2, plane, v);
     }
 };
@@ -241,7 +277,9 @@ template <bool BF16, bool OUT> struct EpiStore {
         if (OUT && res.p) res.p += (int64_t)k * res.worker * S;
         row0 = (uint32_t)k * (uint32_t)T;
     }
-    __device__ __forceinline__ void fragment(int, int, int, grawa_f32x4 &, grawa_f32x4 &) const {}
+    typedef GrawaNothing Ahead;
+    __device__ __forceinline__ void ahead(int, int, int, Ahead &) const {}
+    __device__ __forceinline__ void fragment(int, int, int, const Ahead &, grawa_f32x4 &, grawa_f32x4 &) const {}
     __device__ __forceinline__ void put(int, int m, int n, float *v) const
     {
         constexpr int S = BF16 ? 2 : 4;
@@ -489,27 +527,27 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
     const int64_t n = c.T * s->fp;
     const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
     const Operand oh = c.inner((char *)save + s->K * blocks * grawa_kept_bytes(s)), odg = c.inner(s->dg), odu = c.inner(s->du);
+    typedef EpiStore<PLANES == 1, false> Store;
+    auto weight_product = [&](const Operand &a, const Operand &b, int64_t M, int64_t N) {
+        GrawaGemm g = c.product(M, N, c.T);
+        add_segments(g, PLANES, a, b, nullptr);
+        return g;
+    };
+    auto weight_store = [&](GrawaMat w, int64_t N) { return Store{GrawaRows{w.p, w.worker, N}, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, 0}; };
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ody, od, nullptr);
         const EpiBack<PLANES, ACT> epi{{(char *)save, s->K * blocks}, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
-    auto store = [&](const Operand &a, const Operand &b, GrawaMat w, int64_t M, int64_t N) {
-        GrawaGemm g = c.product(M, N, c.T);
-        add_segments(g, PLANES, a, b, nullptr);
-        const GrawaRows out{w.p, w.worker, N};
-        const EpiStore<PLANES == 1, false> epi{out, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, 0};
-        c.run([&] { return launch_gemm<true, true, false>(s, g, epi, c.st); });
-    };
-    store(odg, ox, dwg, s->f, s->d);
-    store(odu, ox, dwu, s->f, s->d);
-    store(ody, oh, dwd, s->d, s->f);
+    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(odg, ox, s->f, s->d), weight_store(dwg, s->d), c.st); });
+    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(odu, ox, s->f, s->d), weight_store(dwu, s->d), c.st); });
+    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(ody, oh, s->d, s->f), weight_store(dwd, s->f), c.st); });
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
         add_segments(g, PLANES, odg, og, nullptr);
         add_segments(g, PLANES, odu, ou, nullptr);
-        const EpiStore<PLANES == 1, false> epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, 0};
+        const Store epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, 0};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
     return c.err;

@@ -169,7 +169,9 @@ template <int N> __device__ __forceinline__ void grawa_landed()
 }
 
 // c += a b with the sums where they are.  The builtin leaves it to the register allocator whether a sum stays in its registers; it moves
-// them about, and the fragments then do not fit beside them.  The operands are waited for as any others' are.
+// them about, and the fragments then do not fit beside them.  The operands are waited for as any others' are.  What the compiler does
+// not see is that c is still being written when the next instruction starts: between the first of these and the wait behind the last
+// nothing else may touch a sum, a spill to memory least of all, and tests/test_product_kernels.py looks for that in what is built.
 __device__ __forceinline__ void mfma_in_place(grawa_f32x4 &c, const grawa_bf16x8 &a, const grawa_bf16x8 &b)
 {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
@@ -177,19 +179,31 @@ __device__ __forceinline__ void mfma_in_place(grawa_f32x4 &c, const grawa_bf16x8
 
 // What becomes of the sums is up to an epilogue, see grawa_ffn.hip:
 //   epi.tile(worker, split)              once
-//   epi.fragment(mb, nb, lane, v, u)     a fragment of 16 x 16 sums, rows 16 mb ..., columns 16 nb ...: the lane has row lane % 16, columns
+//   epi.ahead(mb, nb, lane, r)           asks for what the epilogue needs for a fragment, which is sixteen rows (and more) from its turn
+//   epi.fragment(mb, nb, lane, r, v, u)  a fragment of 16 x 16 sums, rows 16 mb ..., columns 16 nb ...: the lane has row lane % 16, columns
 //                                        4 (lane / 16) ...; v the product, u the second one where there are two.  Leaves in v, and
 //                                        with OUTS = 2 in u, what goes on to
 //   epi.put(o, m, n, v)                  VEC columns from n on of row m of output o; m < M, n < N
 // Sixteen rows of NJ fragments of a wave.  A lane has four consecutive columns of one row of every fragment.  What goes to rows in memory
 // passes through a corner of LDS of the wave's own, so that a store instruction writes whole runs of a row: straight from the
 // fragments it would write 64 separate pieces of 16 bytes.  The 16-byte piece c of row r stands at place c ^ r.
+struct GrawaNothing {};
+
 template <int NJ, class Epi>
-__device__ __forceinline__ void grawa_finish(const Epi &epi, float *corner, int m1, int n1, int lane, int M, int N, grawa_f32x4 (&v)[NJ], grawa_f32x4 (&u)[NJ])
+__device__ __forceinline__ void grawa_ahead(const Epi &epi, int m1, int n1, int lane, int M, int N, typename Epi::Ahead (&r)[NJ])
 {
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
-        if (n1 + j * 16 < N) epi.fragment(m1 >> 4, (n1 >> 4) + j, lane, v[j], u[j]);
+        if (m1 < M && n1 + j * 16 < N) epi.ahead(m1 >> 4, (n1 >> 4) + j, lane, r[j]);
+}
+
+template <int NJ, class Epi>
+__device__ __forceinline__ void grawa_finish(const Epi &epi, float *corner, int m1, int n1, int lane, int M, int N, const typename Epi::Ahead (&r)[NJ],
+                                             grawa_f32x4 (&v)[NJ], grawa_f32x4 (&u)[NJ])
+{
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+        if (n1 + j * 16 < N) epi.fragment(m1 >> 4, (n1 >> 4) + j, lane, r[j], v[j], u[j]);
     if constexpr (Epi::OUTS > 0) {
         constexpr int COLS = NJ * 16, PIECES = COLS / 4, LPR = COLS / Epi::VEC, ROWS = 64 / LPR < 16 ? 64 / LPR : 16;
 #pragma unroll
@@ -220,11 +234,11 @@ __device__ __forceinline__ void grawa_finish(const Epi &epi, float *corner, int 
     }
 }
 
-// The kernel.  DUAL: B is two operands, BN / 2 columns of each.
 namespace {
 
+// The kernel: a tile a block.  DUAL: B is two operands, BN / 2 columns of each.
 template <int BM, int BN, int WM, int WN, bool AT, bool BT, bool DUAL, class Epi>
-__global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
+__global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm([[maybe_unused]] GrawaGemm g, [[maybe_unused]] Epi epi)
 {
 #ifdef __HIP_DEVICE_COMPILE__ // the host pass needs the signature alone; given this body it leaves the launch stubs out without a word
     constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
@@ -233,7 +247,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
     constexpr int ABYTES = BM * 128, BBYTES = BN * 128;
     __shared__ __attribute__((aligned(1024))) char buf0[ABYTES + BBYTES];
     __shared__ __attribute__((aligned(1024))) char buf1[ABYTES + BBYTES];
-    __shared__ __attribute__((aligned(1024))) char unread[NW * 256];
+    __shared__ __attribute__((aligned(1024))) char unread[NW * 256]; // where lines that are only asked for go
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const uint32_t tm = (uint32_t)(g.M + BM - 1) / BM, tn = (uint32_t)(g.N + BR - 1) / BR;
@@ -310,6 +324,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
             lb.go(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, ob);
     };
     grawa_f32x4 acc[MI][NI] = {};
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(acc[i][j])); // zero from here on, two instructions at least before the first use
     constexpr int MH = MI / 2;
     grawa_bf16x8 a0[MH], a1[MH], b0[NI], b1[NI];
     // A group: MH rows of NI matrix instructions, and between them, evenly, n other things to do.
@@ -397,21 +415,23 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm(GrawaGemm g, Epi epi)
     epi.tile(tile.k, tile.split);
     constexpr int NJ = DUAL ? NI / 2 : NI, COLS = NJ * 16;
     static_assert(NW * Epi::OUTS * 16 * COLS * 4 <= ABYTES + BBYTES, "the corners fit a buffer");
+    constexpr int DEEP = sizeof(typename Epi::Ahead) <= 24 ? 2 : 1; // rows of fragments that are asked for ahead of their turn
+    typename Epi::Ahead r[DEEP + 1][NJ];
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) grawa_ahead<NJ>(epi, m0 + wm * TM + i * 16, n0 + wn * COLS, lane, g.M, g.N, r[i]);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         const int m1 = m0 + wm * TM + i * 16;
         if (m1 >= g.M) break;
+        if (i + DEEP < MI) grawa_ahead<NJ>(epi, m1 + DEEP * 16, n0 + wn * COLS, lane, g.M, g.N, r[(i + DEEP) % (DEEP + 1)]);
         grawa_f32x4 v[NJ], u[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             v[j] = acc[i][j];
             u[j] = DUAL ? acc[i][j + NI - NJ] : grawa_f32x4{};
         }
-        grawa_finish<NJ>(epi, (float *)buf0 + wave * (Epi::OUTS * 16 * COLS), m1, n0 + wn * COLS, lane, g.M, g.N, v, u);
+        grawa_finish<NJ>(epi, (float *)buf0 + wave * (Epi::OUTS * 16 * COLS), m1, n0 + wn * COLS, lane, g.M, g.N, r[i % (DEEP + 1)], v, u);
     }
-#else
-    (void)g;
-    (void)epi;
 #endif
 }
 
@@ -434,7 +454,9 @@ struct EpiParts {
         v0 = const_cast<float *>(parts.at(k, split, 0));
         u0 = const_cast<float *>(parts.at(k, split, parts.products - 1));
     }
-    __device__ __forceinline__ void fragment(int mb, int nb, int lane, grawa_f32x4 &v, grawa_f32x4 &u) const
+    typedef GrawaNothing Ahead;
+    __device__ __forceinline__ void ahead(int, int, int, Ahead &) const {}
+    __device__ __forceinline__ void fragment(int mb, int nb, int lane, const Ahead &, grawa_f32x4 &v, grawa_f32x4 &u) const
     {
         const int64_t at = grawa_fragment_at(mb, nb, parts.nb, lane);
         *(grawa_f32x4 *)(v0 + at) = v;
@@ -453,6 +475,9 @@ template <bool DUAL, bool SHARED, class Epi> __global__ __launch_bounds__(256) v
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = blockIdx.z;
     const int m1 = blockIdx.y * 16, n1 = (SHARED ? blockIdx.x : blockIdx.x * 4 + wave) * NJ * 16;
     if (n1 >= N) return; // the whole block where it is shared
+    epi.tile(k, 0);
+    typename Epi::Ahead r[NJ];
+    if (!SHARED || !wave) grawa_ahead<NJ>(epi, m1, n1, lane, M, N, r);
     grawa_f32x4 v[NJ] = {}, u[NJ] = {};
     const int s0 = SHARED ? splits * wave / 4 : 0, s1 = SHARED ? splits * (wave + 1) / 4 : splits;
 #pragma unroll 4
@@ -480,8 +505,7 @@ template <bool DUAL, bool SHARED, class Epi> __global__ __launch_bounds__(256) v
                 u[j] += *(const grawa_f32x4 *)&sums[w][NJ + j][lane * 4];
             }
     }
-    epi.tile(k, 0);
-    grawa_finish<NJ>(epi, corners[wave], m1, n1, lane, M, N, v, u);
+    grawa_finish<NJ>(epi, corners[wave], m1, n1, lane, M, N, r, v, u);
 }
 
 } // namespace
