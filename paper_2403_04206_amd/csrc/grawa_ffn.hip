@@ -46,7 +46,7 @@ template <int PLANES> __device__ __forceinline__ void store_planes8(char *p, int
 }
 
 // Copies of matrices and activations whose rows are not on 16-byte boundaries, and of all in float32: [K][R][C] elements into planes of
-// pitch Cp with zeros behind C.  Up to five in a launch; eight elements a thread, read at any alignment.
+// pitch Cp with zeros behind C to the next multiple of 8.  Up to five in a launch; eight elements a thread, read at any alignment.
 struct CopyJob {
     const char *src;
     char *dst;
@@ -63,7 +63,7 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_planes(CopyJobs jo
 {
     constexpr int S = BF16 ? 2 : 4;
     const CopyJob &j = jobs.job[blockIdx.z];
-    const uint32_t groups = j.Cp / 8, k = blockIdx.y;
+    const uint32_t groups = (j.C + 7) / 8, k = blockIdx.y;
     const uint64_t total = (uint64_t)j.R * groups;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256) {
         const uint32_t r = total >> 32 ? (uint32_t)(i / groups) : (uint32_t)i / groups, c = (uint32_t)(i - (uint64_t)r * groups) * 8;
@@ -412,7 +412,7 @@ struct Sublayer { // one call
             return Operand{p, worker * 2, 0, row * 2};
         const Operand o{room, R * Cp * 2, (int64_t)s->K * R * Cp * 2, Cp * 2};
         copies.job[copies.n++] = CopyJob{p, room, worker, row, o.plane, (uint32_t)R, (uint32_t)C, (uint32_t)Cp};
-        most = most > R * (Cp / 8) ? most : R * (Cp / 8);
+        most = most > R * ((C + 7) / 8) ? most : R * ((C + 7) / 8);
         return o;
     }
     void copy_all()

@@ -100,8 +100,8 @@ grawa_status_t grawa_sublayer_create(grawa_sublayer_t **out, int K, int64_t T, i
     s->T = T;
     s->d = d;
     s->f = f;
-    s->dp = grawa_round8(d);
-    s->fp = grawa_round8(f);
+    s->dp = grawa_round64(d);
+    s->fp = grawa_round64(f);
     s->dtype = dtype;
     s->act = act;
     s->planes = dtype == GRAWA_BF16 ? 1 : 3;

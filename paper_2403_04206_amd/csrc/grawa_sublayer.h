@@ -13,7 +13,7 @@ struct grawa_sublayer {
     int K, device;
     int64_t T;          // most tokens of a worker
     int64_t d, f;       // model width; inner width of the feed-forward block, 0: none
-    int64_t dp, fp;     // rounded up to 8 elements: pitches of what the library lays out itself
+    int64_t dp, fp;     // rounded up to 64 elements: pitches of what the library lays out itself, so that a row's tiles are whole lines
     grawa_dtype_t dtype;
     grawa_act_t act;
     int planes;         // bfloat16 terms that a matrix element is held in: 1, or 3 for float32
@@ -40,7 +40,7 @@ struct GrawaMat {
     int64_t worker;
 };
 
-static inline int64_t grawa_round8(int64_t n) { return (n + 7) & ~(int64_t)7; }
+static inline int64_t grawa_round64(int64_t n) { return (n + 63) & ~(int64_t)63; }
 
 static inline int64_t grawa_round16(int64_t n) { return (n + 15) & ~(int64_t)15; }
 

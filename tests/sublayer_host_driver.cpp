@@ -78,7 +78,7 @@ int main()
     EXPECT(grawa_sublayer_create(&q, K, T, d, 0, GRAWA_F32, GRAWA_ACT_RELU) == OK && q); // the layer norm alone
     device = 0;
     int64_t bytes = 0;
-    EXPECT(grawa_sublayer_save_bytes(p, T, &bytes) == OK && bytes == K * (16 * 16 * (3 + 3) + T * f * 2)); // 5 tokens take a fragment of 16
+    EXPECT(grawa_sublayer_save_bytes(p, T, &bytes) == OK && bytes == K * (16 * 16 * (3 + 3) + T * 64 * 2)); // 5 tokens take a fragment of 16, rows are 64 wide
     EXPECT(grawa_sublayer_save_bytes(p, T + 1, &bytes) == ARG && grawa_sublayer_save_bytes(p, -1, &bytes) == ARG);
     EXPECT(grawa_sublayer_save_bytes(p, T, nullptr) == ARG && grawa_sublayer_save_bytes(nullptr, T, &bytes) == ARG && grawa_sublayer_save_bytes(q, T, &bytes) == ARG);
 
