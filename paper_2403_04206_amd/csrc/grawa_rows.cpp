@@ -324,11 +324,25 @@ PyObject *norm_back(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
-// feed(function, plan, K, T, d, dtype, x, wg, wu, wd, out, residual, p, rng, site, f, current): grawa_ffn without a buffer for a backward pass
+// None where it may be, or a contiguous uint8 tensor of at least what `size`, grawa_sublayer_save_bytes, says.
+bool save_of(PyObject *o, void *size, void *plan, int64_t T, bool optional, void *&p)
+{
+    p = nullptr;
+    if (o == Py_None) return optional;
+    const at::Tensor *t = plain_tensor(o);
+    int64_t need = 0;
+    if (!t || t->scalar_type() != at::kByte || t->dim() != 1 || !t->is_contiguous() || reinterpret_cast<int (*)(const void *, int64_t, int64_t *)>(size)(plan, T, &need) != 0)
+        return false;
+    if (t->size(0) < need || !holds(*t, need, 1)) return false;
+    p = t->data_ptr();
+    return true;
+}
+
+// feed(function, size, plan, K, T, d, dtype, f, x, wg, wu, wd, out, save, residual, p, rng, site, current): grawa_ffn
 PyObject *feed(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     typedef int (*Function)(void *, int64_t, const RowsArg *, const MatsArg *, const MatsArg *, const MatsArg *, const RowsArg *, float, const int64_t *, uint32_t, const RowsArg *, void *, void *);
-    void *function, *plan;
+    void *function, *size, *plan, *save;
     long long K, T, d, dt, f;
     float p;
     int64_t *rng;
@@ -336,16 +350,42 @@ PyObject *feed(PyObject *, PyObject *const *args, Py_ssize_t n)
     RowsArg x, out, residual{};
     MatsArg wg, wu, wd;
     try {
-        if (n != 17 || !pointer_of(args[0], function) || !pointer_of(args[1], plan) || !plan_of(args + 2, K, T, d, dt, args[6]) || !integer_of(args[15], f) || f < 1 ||
-            !tokens_of(args[6], K, T, d, dt, x) || !mats_of(args[7], K, f, d, dt, wg) || !mats_of(args[8], K, f, d, dt, wu) || !mats_of(args[9], K, d, f, dt, wd) ||
-            !tokens_of(args[10], K, T, d, dt, out) || (args[11] != Py_None && !tokens_of(args[11], K, T, d, dt, residual)) || !number_of(args[12], p) ||
-            !rng_of(args[13], p, rng) || !site_of(args[14], site))
+        if (n != 19 || !pointer_of(args[0], function) || !pointer_of(args[1], size) || !pointer_of(args[2], plan) || !plan_of(args + 3, K, T, d, dt, args[8]) ||
+            !integer_of(args[7], f) || f < 1 || !tokens_of(args[8], K, T, d, dt, x) || !mats_of(args[9], K, f, d, dt, wg) || !mats_of(args[10], K, f, d, dt, wu) ||
+            !mats_of(args[11], K, d, f, dt, wd) || !tokens_of(args[12], K, T, d, dt, out) || !save_of(args[13], size, plan, T, true, save) ||
+            (args[14] != Py_None && !tokens_of(args[14], K, T, d, dt, residual)) || !number_of(args[15], p) || !rng_of(args[16], p, rng) || !site_of(args[17], site))
             Py_RETURN_NONE;
     } catch (...) {
         Py_RETURN_NONE;
     }
-    return status_of(args[16], [&](void *stream) {
-        return reinterpret_cast<Function>(function)(plan, T, &x, &wg, &wu, &wd, args[11] == Py_None ? nullptr : &residual, p, rng, site, &out, nullptr, stream);
+    return status_of(args[18], [&](void *stream) {
+        return reinterpret_cast<Function>(function)(plan, T, &x, &wg, &wu, &wd, args[14] == Py_None ? nullptr : &residual, p, rng, site, &out, save, stream);
+    });
+}
+
+// feed_back(function, size, plan, K, T, d, dtype, f, dy, x, wg, wu, wd, save, dx, dwg, dwu, dwd, accumulate, current): grawa_ffn_backward
+PyObject *feed_back(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    typedef int (*Function)(void *, int64_t, const RowsArg *, const RowsArg *, const MatsArg *, const MatsArg *, const MatsArg *, const void *, const RowsArg *, const MatsArg *, const MatsArg *,
+                            const MatsArg *, int, void *);
+    void *function, *size, *plan, *save;
+    long long K, T, d, dt, f;
+    RowsArg dy, x, dx;
+    MatsArg m[6];
+    try {
+        if (n != 20 || !pointer_of(args[0], function) || !pointer_of(args[1], size) || !pointer_of(args[2], plan) || !plan_of(args + 3, K, T, d, dt, args[8]) ||
+            !integer_of(args[7], f) || f < 1 || !tokens_of(args[8], K, T, d, dt, dy) || !tokens_of(args[9], K, T, d, dt, x) ||
+            !save_of(args[13], size, plan, T, false, save) || !tokens_of(args[14], K, T, d, dt, dx) || !PyBool_Check(args[18]))
+            Py_RETURN_NONE;
+        for (int i = 0; i < 6; ++i) {
+            const bool down = i % 3 == 2;
+            if (!mats_of(args[i < 3 ? 10 + i : 12 + i], K, down ? d : f, down ? f : d, dt, m[i])) Py_RETURN_NONE;
+        }
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return status_of(args[19], [&](void *stream) {
+        return reinterpret_cast<Function>(function)(plan, T, &dy, &x, &m[0], &m[1], &m[2], save, &dx, &m[3], &m[4], &m[5], args[18] == Py_True, stream);
     });
 }
 
@@ -377,7 +417,7 @@ PyObject *drop(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 #define GRAWA_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {GRAWA_METHOD(rows), GRAWA_METHOD(scored), GRAWA_METHOD(local), GRAWA_METHOD(lgrawa), GRAWA_METHOD(norm), GRAWA_METHOD(norm_back),
-                         GRAWA_METHOD(feed), GRAWA_METHOD(drop), {nullptr, nullptr, 0, nullptr}};
+                         GRAWA_METHOD(feed), GRAWA_METHOD(feed_back), GRAWA_METHOD(drop), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace

@@ -89,7 +89,7 @@ def lib():
         fn.restype = res
         fn.argtypes = args
     for name in ("grawa_lgrawa_update", "grawa_local_step_scored", "grawa_local_lgrawa_update", "grawa_local_mgrawa_update", "grawa_layer_norm",
-                 "grawa_layer_norm_backward", "grawa_ffn", "grawa_dropout"):
+                 "grawa_layer_norm_backward", "grawa_sublayer_save_bytes", "grawa_ffn", "grawa_ffn_backward", "grawa_dropout"):
         _addresses[name] = C.cast(getattr(L, name), vp).value
     _lib = L
     return L
@@ -128,7 +128,7 @@ def _stream_no_tensors(stream=None):
 # The same of whole calls: their status, or None for any argument that is not plainly in order; the Python call follows then.
 try:
     from ._rows import built_for, rows as _native_rows, scored as _native_scored, local as _native_local, lgrawa as _native_lgrawa
-    from ._rows import norm as _native_norm, norm_back as _native_norm_back, feed as _native_feed, drop as _native_drop
+    from ._rows import norm as _native_norm, norm_back as _native_norm_back, feed as _native_feed, feed_back as _native_feed_back, drop as _native_drop
     if built_for != buildlib.rows_built_for():
         raise ImportError("_rows.so is for %s" % built_for)
 except Exception:                        # not built, or not for this torch: the Python checks alone
@@ -137,7 +137,7 @@ except Exception:                        # not built, or not for this torch: the
 
     def _native_scored(*args):
         return None
-    _native_local = _native_lgrawa = _native_norm = _native_norm_back = _native_feed = _native_drop = _native_scored
+    _native_local = _native_lgrawa = _native_norm = _native_norm_back = _native_feed = _native_feed_back = _native_drop = _native_scored
 
 
 _NULL = C.c_void_p(0)
@@ -650,9 +650,9 @@ class SublayerPlan:
 
     def ffn(self, x, wg, wu, wd, out, save=None, residual=None, p=0.0, rng=None, site=0, stream=None):
         """grawa_ffn: out = residual + dropout((act(x wg^T) * (x wu^T)) wd^T)."""
-        if stream is None and save is None:
-            st = _native_feed(_addresses.get("grawa_ffn"), self._h.value, self.K, self.T, self.d, _DTYPES[self.dtype], x, wg, wu, wd, out, residual, p, rng,
-                              site, self.f, _stream)
+        if stream is None:
+            st = _native_feed(_addresses.get("grawa_ffn"), _addresses.get("grawa_sublayer_save_bytes"), self._h.value, self.K, self.T, self.d,
+                              _DTYPES[self.dtype], self.f, x, wg, wu, wd, out, save, residual, p, rng, site, _stream)
             if st is not None:
                 return _check(st, "grawa_ffn")
         K, d, f, dt, T = self.K, self.d, self.f, self.dtype, self._count(x, "x")
@@ -663,6 +663,11 @@ class SublayerPlan:
 
     def ffn_backward(self, dy, x, wg, wu, wd, save, dx, dwg, dwu, dwd, accumulate=False, stream=None):
         """grawa_ffn_backward: from dy, the gradient of the product with wd, the gradients of x and of the weights."""
+        if stream is None:
+            st = _native_feed_back(_addresses.get("grawa_ffn_backward"), _addresses.get("grawa_sublayer_save_bytes"), self._h.value, self.K, self.T, self.d,
+                                   _DTYPES[self.dtype], self.f, dy, x, wg, wu, wd, save, dx, dwg, dwu, dwd, accumulate, _stream)
+            if st is not None:
+                return _check(st, "grawa_ffn_backward")
         K, d, f, dt, T = self.K, self.d, self.f, self.dtype, self._count(dy, "dy")
         _check(lib().grawa_ffn_backward(
             self._h, T, _tokens(dy, K, T, d, dt, "dy"), _tokens(x, K, T, d, dt, "x"), _mats(wg, (K, f, d), dt, "wg"),

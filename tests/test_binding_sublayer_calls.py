@@ -13,8 +13,9 @@ ROWS, MATS = C.POINTER(grawa._RowsArg), C.POINTER(grawa._MatsArg)
 SIGNATURES = {"grawa_layer_norm": [PTR, I64, ROWS, MATS, MATS, F32, ROWS, PTR, PTR],
               "grawa_layer_norm_backward": [PTR, I64, ROWS, ROWS, MATS, PTR, ROWS, ROWS, MATS, MATS, INT, PTR],
               "grawa_ffn": [PTR, I64, ROWS, MATS, MATS, MATS, ROWS, F32, PTR, U32, ROWS, PTR, PTR],
+              "grawa_ffn_backward": [PTR, I64, ROWS, ROWS, MATS, MATS, MATS, PTR, ROWS, MATS, MATS, MATS, INT, PTR],
               "grawa_dropout": [INT, I64, I64, INT, ROWS, ROWS, F32, PTR, U32, ROWS, PTR]}
-NATIVE = {n: getattr(grawa, n) for n in ("_native_norm", "_native_norm_back", "_native_feed", "_native_drop")}
+NATIVE = {n: getattr(grawa, n) for n in ("_native_norm", "_native_norm_back", "_native_feed", "_native_feed_back", "_native_drop")}
 
 
 def plain(v):
@@ -31,6 +32,11 @@ class Library:
         for name, sig in SIGNATURES.items():
             fn = C.CFUNCTYPE(INT, *sig)(lambda *a, name=name: self.seen.append((name,) + tuple(plain(v) for v in a)) or grawa.OK)
             setattr(self, name, fn)
+
+        def size(plan, T, n):
+            n[0] = 100 * T
+            return grawa.OK
+        self.grawa_sublayer_save_bytes = C.CFUNCTYPE(INT, PTR, I64, C.POINTER(I64))(size)
 
 
 def tokens(dev):
@@ -56,6 +62,11 @@ def stats(dev):
     return [None, b, b.double(), b[:, :, :1], torch.zeros((K, 2, T), device=dev).transpose(1, 2), torch.zeros((K, T + 1, 2), device=dev)]
 
 
+def saves(dev):
+    b = torch.zeros(1000, dtype=torch.uint8, device=dev)
+    return [None, b, b[:100 * T], b[:100 * T - 1], b[::2][:100 * T], b.view(10, 100), b.to(torch.int8), b[4:], 5]
+
+
 def rngs(dev):
     b = torch.zeros(4, dtype=torch.int64, device=dev)
     return [None, b[:2], b[1:], b[:1], b[::2], b.double(), b.view(2, 2), 7]
@@ -79,6 +90,14 @@ def calls_of(dev):
         calls += [lambda a=a, i=i: plan.ffn(a if i == 0 else X, G, G, D, a if i == 1 else X, residual=a if i == 2 else None) for a in x]
     calls += [lambda a=a: plan.ffn(X, a, G, D, X) for a in wg] + [lambda a=a: plan.ffn(X, G, a, D, X) for a in wg] + [lambda a=a: plan.ffn(X, G, G, a, X) for a in wd]
     calls += [lambda r=r, p=p, s=s: plan.ffn(X, G, G, D, X, p=p, rng=r, site=s) for r in rng for p in (0, 0.0, 0.25, "p") for s in (0, 5, -1, 1 << 32)]
+    V = saves(dev)[1]
+    calls += [lambda a=a: plan.ffn(X, G, G, D, X, save=a) for a in saves(dev)] + [lambda a=a: plan.ffn_backward(X, X, G, G, D, a, X, G, G, D) for a in saves(dev)]
+    for i in range(3):
+        calls += [lambda a=a, i=i: plan.ffn_backward(*[a if i == j else X for j in range(2)], G, G, D, V, a if i == 2 else X, G, G, D) for a in x]
+    for i in range(6):
+        calls += [lambda a=a, i=i: plan.ffn_backward(X, X, *[a if i == j else (D if j == 2 else G) for j in range(3)], V, X, *[a if i == j else (D if j == 5 else G) for j in range(3, 6)])
+                  for a in (wd if i % 3 == 2 else wg)]
+    calls += [lambda a=a: plan.ffn_backward(X, X, G, G, D, V, X, G, G, D, accumulate=a) for a in (True, False, 1, 0)]
     for i in range(3):
         calls += [lambda a=a, i=i: grawa.dropout(a if i == 0 else X, a if i == 1 else X, 0.0, None, residual=a if i == 2 else None) for a in x]
     calls += [lambda r=r, p=p, s=s: grawa.dropout(X, X, p, r, site=s) for r in rng for p in (0, 0.0, 0.25, "p") for s in (0, (1 << 32) - 1, -1, 1 << 32)]
@@ -102,7 +121,7 @@ def outcome(call, library, native, monkeypatch):
 def compare(dev, monkeypatch):
     library = Library()
     monkeypatch.setattr(grawa, "lib", lambda: library)
-    for name in SIGNATURES:
+    for name in list(SIGNATURES) + ["grawa_sublayer_save_bytes"]:
         monkeypatch.setitem(grawa._addresses, name, C.cast(getattr(library, name), PTR).value)
     plan, calls = calls_of(dev)
     kinds = set()
@@ -135,5 +154,8 @@ def test_the_native_call_is_the_one_that_runs(monkeypatch):
         plan.layer_norm(x, w, w, x, stats_out=stat)
         plan.layer_norm_backward(x, x, w, stat, x, w, w, add=x)
         plan.ffn(x, m, m, md, x.clone(), residual=x, p=0.5, rng=rng, site=1)
+        save = torch.zeros(plan.save_bytes(T), dtype=torch.uint8, device=dev)
+        plan.ffn(x, m, m, md, x.clone(), save=save)
+        plan.ffn_backward(x, x, m, m, md, save, x.clone(), m.clone(), m.clone(), md.clone())
         grawa.dropout(x, x, 0.5, rng)
         torch.cuda.synchronize()
