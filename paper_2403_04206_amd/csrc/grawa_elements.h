@@ -42,7 +42,8 @@ template <bool BF16> struct GrawaPiece {
     __device__ __forceinline__ float operator[](int j) const { return BF16 ? (j % 2 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2])) : __uint_as_float(w[j]); }
 };
 
-template <bool BF16> __device__ __forceinline__ void store_piece(char *p, int n, const float *v)
+// NT: for what nobody reads again soon.
+template <bool BF16, bool NT = false> __device__ __forceinline__ void store_piece(char *p, int n, const float *v)
 {
     constexpr int N = GrawaPiece<BF16>::N, S = GrawaPiece<BF16>::S;
     if (n >= N) {
@@ -56,7 +57,10 @@ template <bool BF16> __device__ __forceinline__ void store_piece(char *p, int n,
 #pragma unroll
             for (int j = 0; j < 4; ++j) u[j] = __float_as_uint(v[j]);
         }
-        *(GrawaAny16 *)p = u;
+        if (NT)
+            __builtin_nontemporal_store(u, (GrawaAny16 *)p);
+        else
+            *(GrawaAny16 *)p = u;
     } else {
 #pragma unroll
         for (int j = 0; j < N - 1; ++j)

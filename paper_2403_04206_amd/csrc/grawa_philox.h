@@ -9,14 +9,17 @@ struct GrawaWords {
     uint32_t w[4];
 };
 
+// The compiler makes two instructions of a ^ b ^ c.
+__device__ __forceinline__ uint32_t grawa_xor3(uint32_t a, uint32_t b, uint32_t c) { return (uint32_t)__builtin_amdgcn_bitop3_b32((int)a, (int)b, (int)c, 0x96); }
+
 __device__ __forceinline__ GrawaWords grawa_philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1)
 {
 #pragma unroll
     for (int r = 0; r < 7; ++r) {
         const uint64_t p = (uint64_t)0xD2511F53u * c0, q = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
+        c0 = grawa_xor3((uint32_t)(q >> 32), c1, k0);
         c1 = (uint32_t)q;
-        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
+        c2 = grawa_xor3((uint32_t)(p >> 32), c3, k1);
         c3 = (uint32_t)p;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
