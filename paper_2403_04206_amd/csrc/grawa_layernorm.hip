@@ -76,7 +76,7 @@ __global__ __launch_bounds__(BLOCK) void k_norm(GrawaRows x, GrawaMat w, GrawaMa
         float r[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) r[i] = (v[j][i] - mean) * rstd * ww[j][i] + (pb ? bb[j][i] : 0.f);
-        store_piece<BF16>(py + (int64_t)e * S, d - e, r);
+        store_piece<BF16, true>(py + (int64_t)e * S, d - e, r);
     }
 }
 
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(GrawaRows dy, GrawaRows x, 
                 const float h = (px[j][i] - st.x) * st.y, a = pdy[j][i] * ww[j][i];
                 r[i] = st.y * (a - m1 - h * m2) + (add.p ? padd[j][i] : 0.f);
             }
-            store_piece<BF16>(pdx + (int64_t)e * S, d - e, r);
+            store_piece<BF16, true>(pdx + (int64_t)e * S, d - e, r);
         }
     }
     float *out = part + ((int64_t)k * gridDim.x + blockIdx.x) * 2 * d;
