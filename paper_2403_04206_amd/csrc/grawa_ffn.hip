@@ -300,7 +300,7 @@ template <bool BF16, bool OUT> struct EpiStore {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) v[j] += r[j];
         }
-        store_piece<BF16>(p, N - n, v);
+        store_piece<BF16, true>(p, N - n, v);
     }
 };
 
