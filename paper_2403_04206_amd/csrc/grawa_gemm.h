@@ -100,11 +100,11 @@ template <bool TR, int R, int NW> struct GrawaTileLoad {
     // that add a multiple of `step` (below 2^31) to it.
     __device__ __forceinline__ uint32_t place(int krem) const { return !TR && kpiece >= krem ? 0x80000000u : first; }
 
-    __device__ __forceinline__ void go(int i, char *lds, int wave, __amdgpu_buffer_rsrc_t r, uint32_t at) const
+    template <int AUX = 0> __device__ __forceinline__ void go(int i, char *lds, int wave, __amdgpu_buffer_rsrc_t r, uint32_t at) const
     {
         if (TURN && i % 2) at = odd;
         asm("" : "+v"(at)); // the sum is formed where it is used: held in registers the sums would not fit
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS void *)(lds + (wave + NW * i) * 1024), 16, at + (uint32_t)(TURN ? i / 2 : i) * step, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS void *)(lds + (wave + NW * i) * 1024), 16, at + (uint32_t)(TURN ? i / 2 : i) * step, 0, 0, AUX);
     }
 };
 
@@ -319,9 +319,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm([[maybe_unused]] GrawaG
         if (i < LA)
             la.go(i, buf, wave, ra, oa);
         else if (i < LA + LB)
-            lb.go(i - LA, buf + ABYTES, wave, rb, ob);
+            lb.template go<BM == 64 ? 2 : 0>(i - LA, buf + ABYTES, wave, rb, ob);
         else
-            lb.go(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, ob);
+            lb.template go<BM == 64 ? 2 : 0>(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, ob);
     };
     grawa_f32x4 acc[MI][NI] = {};
 #pragma unroll
