@@ -351,15 +351,24 @@ Cut cut_of(int64_t K, int64_t M, int64_t N, int64_t ktiles, bool dual, bool shor
     return best;
 }
 
-template <bool AT, bool BT, bool DUAL, class Epi> void launch_tiles(const GrawaGemm &g, const Cut &cut, const Epi &epi, hipStream_t st)
+// A product of one row of tiles reads its matrix once.  If the block's three matrices are more than the last-level cache holds, nothing of
+// them is there at the next call, and they are read past it: 48 tokens, 4096 x 11264 (277 MB), 79.6 us by cached loads, 69.3 so, but
+// four workers' 1024 x 4096 (101 MB) 28.6 us again and again by cached loads and 35.8 past them.
+constexpr int64_t CACHED = (int64_t)256 << 20;
+
+template <bool AT, bool BT, bool DUAL, class Epi> void launch_tiles(const grawa_sublayer *s, const GrawaGemm &g, const Cut &cut, const Epi &epi, hipStream_t st)
 {
     const dim3 grid((unsigned)(cut.tiles * cut.splits));
     if (cut.kind == 0)
-        k_gemm<256, 256, 2, 4, AT, BT, DUAL, Epi><<<grid, 512, 0, st>>>(g, epi);
+        k_gemm<256, 256, 2, 4, false, AT, BT, DUAL, Epi><<<grid, 512, 0, st>>>(g, epi);
     else if (cut.kind == 1)
-        k_gemm<128, 128, 2, 2, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
-    else if constexpr (!AT)
-        k_gemm<64, 128, 1, 4, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
+        k_gemm<128, 128, 2, 2, false, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
+    else if constexpr (!AT) {
+        if (6 * s->planes * (int64_t)s->K * s->d * s->f > CACHED)
+            k_gemm<64, 128, 1, 4, true, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
+        else
+            k_gemm<64, 128, 1, 4, false, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
+    }
 }
 
 template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const grawa_sublayer *s, GrawaGemm g, const Epi &epi, hipStream_t st)
@@ -367,11 +376,11 @@ template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const g
     const Cut cut = cut_of(g.K, g.M, g.N, (int64_t)((g.len + GRAWA_BK - 1) / GRAWA_BK) * g.nseg, DUAL, !AT, s->part_floats);
     g.splits = cut.splits;
     if (cut.splits == 1) {
-        launch_tiles<AT, BT, DUAL>(g, cut, epi, st);
+        launch_tiles<AT, BT, DUAL>(s, g, cut, epi, st);
     } else {
         const int64_t blocks = grawa_round16(g.M) * grawa_round16(g.N);
         const GrawaParts parts{s->part, blocks, g.K, DUAL ? 2 : 1, (g.N + 15) >> 4};
-        launch_tiles<AT, BT, DUAL>(g, cut, EpiParts{parts, nullptr, nullptr}, st);
+        launch_tiles<AT, BT, DUAL>(s, g, cut, EpiParts{parts, nullptr, nullptr}, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const unsigned rows = (unsigned)((g.M + 15) / 16);

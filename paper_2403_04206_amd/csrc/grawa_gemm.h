@@ -236,8 +236,8 @@ __device__ __forceinline__ void grawa_finish(const Epi &epi, float *corner, int 
 
 namespace {
 
-// The kernel: a tile a block.  DUAL: B is two operands, BN / 2 columns of each.
-template <int BM, int BN, int WM, int WN, bool AT, bool BT, bool DUAL, class Epi>
+// The kernel: a tile a block.  DUAL: B is two operands, BN / 2 columns of each.  PAST: B is read past the caches.
+template <int BM, int BN, int WM, int WN, bool PAST, bool AT, bool BT, bool DUAL, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm([[maybe_unused]] GrawaGemm g, [[maybe_unused]] Epi epi)
 {
 #ifdef __HIP_DEVICE_COMPILE__ // the host pass needs the signature alone; given this body it leaves the launch stubs out without a word
@@ -315,16 +315,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm([[maybe_unused]] GrawaG
             lb.fetch(unread + wave * 256, lb.rsrc(pc, nrows, left), line_b);
     };
     constexpr int LA = GrawaTileLoad<AT, BM, NW>::LOADS, LB = GrawaTileLoad<BT, BR, NW>::LOADS, LOADS = LA + LB * (DUAL ? 2 : 1);
-    // A matrix that one row of tiles reads is read by nobody else and goes past the caches: 48 tokens, 4096 x 11264, 79.6 us by cached loads,
-    // 69.3 so.
-    constexpr int AUX_B = BM == 64 ? 2 : 0;
     auto load = [&](char *buf, int i) {
         if (i < LA)
             la.go(i, buf, wave, ra, oa);
         else if (i < LA + LB)
-            lb.template go<AUX_B>(i - LA, buf + ABYTES, wave, rb, ob);
+            lb.template go<PAST ? 2 : 0>(i - LA, buf + ABYTES, wave, rb, ob);
         else
-            lb.template go<AUX_B>(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, ob);
+            lb.template go<PAST ? 2 : 0>(i - LA - LB, buf + ABYTES + BR * 128, wave, rc, ob);
     };
     grawa_f32x4 acc[MI][NI] = {};
 #pragma unroll
