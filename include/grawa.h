@@ -322,6 +322,11 @@ grawa_status_t grawa_lgrawa_update_static(int K, int64_t P, int L, const int64_t
  * accumulation are float32.  With bfloat16 the inner activations H, dG and dU are
  * rounded to bfloat16 once; with float32 the products are formed from exact
  * three-term bfloat16 splittings with an error of a float32 product's order.
+ * What passes from call to call has the plan's type as well.  Normalised tokens
+ * rounded to bfloat16 move a gate by up to about 2^-8 of its size; relu, whose
+ * derivative jumps at 0, then counts some gates near 0 on the other side, and the
+ * gradients of a whole bfloat16 sublayer with relu are 2 to 4 % from those of unrounded
+ * tokens (silu and gelu 0.4 %, float32 1e-6).
  *
  * Layouts.  grawa_rows_t is K x T rows of `width` elements: worker k's row t starts
  * at data + k * worker + t * row elements; elements of a row are adjacent.  Strides

@@ -2,7 +2,8 @@
 //   mean = sum x / d;  rstd = (sum (x - mean)^2 / d + eps)^(-1/2);  xhat = (x - mean) rstd;  y = xhat w + b
 //   a = dy w;  dx = rstd (a - mean(a) - xhat mean(a xhat)) [+ add];  dw = sum_t dy xhat;  db = sum_t dy
 // Both passes are bound by memory.  A row is read once and stays in registers, so that the variance is that of the centered
-// values (no difference of large sums).  Everything is summed in float32; the sums over tokens are split over blocks, each block's
+// values (no difference of large sums).  Results are stored past the caches, whose place the second reading of x then has:
+// 8 x 2048 x 1024 in bfloat16, forward and backward, 43.4 us by cached stores, 37.7 so.  Everything is summed in float32; the sums over tokens are split over blocks, each block's
 // kept in registers, left in a workspace and added in a fixed order by a second launch: results do not depend on timing.
 #include "grawa_elements.h"
 #include "grawa_sublayer.h"
