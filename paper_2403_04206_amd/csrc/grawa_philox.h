@@ -10,7 +10,14 @@ struct GrawaWords {
 };
 
 // The compiler makes two instructions of a ^ b ^ c.
-__device__ __forceinline__ uint32_t grawa_xor3(uint32_t a, uint32_t b, uint32_t c) { return (uint32_t)__builtin_amdgcn_bitop3_b32((int)a, (int)b, (int)c, 0x96); }
+__device__ __forceinline__ uint32_t grawa_xor3(uint32_t a, uint32_t b, uint32_t c)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    return (uint32_t)__builtin_amdgcn_bitop3_b32((int)a, (int)b, (int)c, 0x96);
+#else
+    return a ^ b ^ c; // plain C++ includes this header for its types
+#endif
+}
 
 __device__ __forceinline__ GrawaWords grawa_philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1)
 {
