@@ -3,6 +3,8 @@
 // from L2 again for every wave, do not outweigh B), goes straight from memory to the matrix instructions, and asks for the next
 // piece of each row before it works on the one it has; the waves of a block share k and add their sums in LDS, in order.
 // Elements are read where they are, at any alignment: no copy of a matrix is made, and float32 is multiplied as float32.
+// One token of each of four workers, 1024 x 4096 in bfloat16, 101 MB of matrices: 12.3 and 8.4 us, 5.4 and 4.0 TB/s.  Loads past the caches
+// make it 22.9 us instead of 20.9 as a whole, and are no faster where other data has passed through the caches in between (26.4, 24.6).
 #pragma once
 #include "grawa_gemm.h"
 

