@@ -275,9 +275,16 @@ template <bool BF16, bool OUT> struct EpiStore {
     GrawaDrop drop;     // OUT
     int N, T, accumulate;
     uint32_t row0;      // of the worker, for the dropout
+    GrawaMat second;    // !OUT: what the workers from `one` on, a second product's, write to
+    int one;
     __device__ __forceinline__ void tile(int k, int)
     {
         constexpr int S = BF16 ? 2 : 4;
+        if (!OUT && k >= one) {
+            k -= one;
+            y.p = second.p;
+            y.worker = second.worker;
+        }
         y.p += (int64_t)k * y.worker * S;
         if (OUT && res.p) res.p += (int64_t)k * res.worker * S;
         row0 = (uint32_t)k * (uint32_t)T;
@@ -451,7 +458,7 @@ struct Sublayer { // one call
     GrawaGemm product(int64_t M, int64_t N, int64_t len) const
     {
         GrawaGemm g{};
-        g.K = s->K;
+        g.K = g.one = s->K;
         g.M = (int)M;
         g.N = (int)N;
         g.len = (int)len;
@@ -498,7 +505,7 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
     const int64_t blocks = grawa_round16(c.T) * grawa_round16(s->f);
     char *h = save ? save + s->K * blocks * grawa_kept_bytes(s) : s->h;
     const EpiGateUp<PLANES, ACT> inner{h, {save, s->K * blocks}, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
-    const EpiStore<PLANES == 1, true> outer{y, residual, drop, (int)s->d, (int)c.T, 0, 0};
+    const EpiStore<PLANES == 1, true> outer{y, residual, drop, (int)s->d, (int)c.T, 0, 0, GrawaMat{}, s->K};
     // Few tokens: see grawa_few.h.  To the end in float32, which tiles multiply six times: 4 workers, 1024 x 4096, 64 tokens 189 us, by tiles
     // 240.  In bfloat16 up to 16, 67 us and 82 with one matrix of 4096 x 11264, and up to 32 while the matrices are small and the
     // launches count: 38 us and 43 with four of 1024 x 4096, but 97 and 80 with the larger one.
@@ -547,21 +554,31 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
         add_segments(g, PLANES, a, b, nullptr);
         return g;
     };
-    auto weight_store = [&](GrawaMat w, int64_t N) { return Store{GrawaRows{w.p, w.worker, N}, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, 0}; };
+    auto weight_store = [&](GrawaMat w, int64_t N, GrawaMat second) { return Store{GrawaRows{w.p, w.worker, N}, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, 0, second, s->K}; };
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
         add_segments(g, PLANES, ody, od, nullptr);
         const EpiBack<PLANES, ACT> epi{{(char *)save, s->K * blocks}, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
-    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(odg, ox, s->f, s->d), weight_store(dwg, s->d), c.st); });
-    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(odu, ox, s->f, s->d), weight_store(dwu, s->d), c.st); });
-    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(ody, oh, s->d, s->f), weight_store(dwd, s->f), c.st); });
+    // dWg and dWu: in one launch while one of them gives a CU no more than a tile: 2 x 54 tokens, 192 x 64, 48 -> 42 us for a whole
+    // training pass.  One after the other beyond: 8192 tokens, 4096 x 11264, 5225 us, side by side 5275.
+    GrawaGemm gate = weight_product(odg, ox, s->f, s->d);
+    const GrawaGemm up = weight_product(odu, ox, s->f, s->d);
+    if (s->K * ((s->f + 255) / 256) * ((s->d + 255) / 256) <= 256) {
+        for (int i = 0; i < up.nseg; ++i) gate.a[gate.nseg + i] = up.a[i];
+        gate.K = 2 * s->K;
+        c.run([&] { return launch_gemm<true, true, false>(s, gate, weight_store(dwg, s->d, dwu), c.st); });
+    } else {
+        c.run([&] { return launch_gemm<true, true, false>(s, gate, weight_store(dwg, s->d, GrawaMat{}), c.st); });
+        c.run([&] { return launch_gemm<true, true, false>(s, up, weight_store(dwu, s->d, GrawaMat{}), c.st); });
+    }
+    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(ody, oh, s->d, s->f), weight_store(dwd, s->f, GrawaMat{}), c.st); });
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
         add_segments(g, PLANES, odg, og, nullptr);
         add_segments(g, PLANES, odu, ou, nullptr);
-        const Store epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, 0};
+        const Store epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, 0, GrawaMat{}, s->K};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
     return c.err;

@@ -30,13 +30,14 @@ struct GrawaSeg {
 };
 
 struct GrawaGemm {
-    int K;            // workers
+    int K;            // workers; from `one` on those of a second product of the same shape with the same B
+    int one;
     int M, N;         // of one worker; with two B operands N counts the columns of one
     int len;          // k of a segment, > 0; where k is contiguous a row holds zeros from there to the next multiple of 8
     int nseg;
     int splits;       // blocks that share a tile's sum, each a run of its tiles of 64 k
     int64_t lda, ldb; // bytes between rows as stored, times 256 below 2^31
-    GrawaSeg a[GRAWA_MAX_SEGS], b[GRAWA_MAX_SEGS]; // two B operands: the second's segments from nseg on
+    GrawaSeg a[GRAWA_MAX_SEGS], b[GRAWA_MAX_SEGS]; // a second product's A, two B operands: the second's segments from nseg on
 };
 
 #define GRAWA_LDS __attribute__((address_space(3)))
@@ -257,6 +258,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm([[maybe_unused]] GrawaG
     const uint32_t tm = (uint32_t)(g.M + BM - 1) / BM, tn = (uint32_t)(g.N + BR - 1) / BR;
     const GrawaTile2 tile = grawa_tile_of(blockIdx.x, gridDim.x, tm, tn, (uint32_t)g.K);
     const int m0 = tile.m * BM, n0 = tile.n * BR;
+    const int worker = tile.k < g.one ? tile.k : tile.k - g.one, a_seg = tile.k < g.one ? 0 : g.nseg;
 
     GrawaTileLoad<AT, BM, NW> la;
     GrawaTileLoad<BT, BR, NW> lb; // of each B operand
@@ -281,9 +283,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_gemm([[maybe_unused]] GrawaG
     auto prepare = [&](int what) {
         if (what == 0) {
             if (krem <= 0 && todo > 0) {
-                pa = g.a[seg].p + tile.k * g.a[seg].worker + aoff + skip * astep;
-                pb = g.b[seg].p + tile.k * g.b[seg].worker + boff + skip * bstep;
-                if (DUAL) pc = g.b[g.nseg + seg].p + tile.k * g.b[g.nseg + seg].worker + boff + skip * bstep;
+                pa = g.a[a_seg + seg].p + worker * g.a[a_seg + seg].worker + aoff + skip * astep;
+                pb = g.b[seg].p + worker * g.b[seg].worker + boff + skip * bstep;
+                if (DUAL) pc = g.b[g.nseg + seg].p + worker * g.b[g.nseg + seg].worker + boff + skip * bstep;
                 krem = g.len - skip * GRAWA_BK;
                 skip = 0;
                 ++seg;

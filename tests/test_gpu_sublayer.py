@@ -148,6 +148,13 @@ def test_ffn_shared_batch_and_larger_plan():
 
 def test_ffn_large_tiles():
     run_ffn(600, 32, 530, 520, 530, BF, shift=8)
+
+
+@pytest.mark.parametrize("K,T,d,f,dtype", [(1, 40, 6704, 6712, BF),      # matrices that no cache holds, more tiles than CUs
+                                           (17, 70, 1000, 1032, BF), (1, 70, 4104, 4099, F)])
+def test_ffn_large_matrices(K, T, d, f, dtype):
+    run_ffn(700, K, T, d, f, dtype)
+    torch.cuda.empty_cache()
     run_ffn(610, 16, 600, 264, 1056, F, act="gelu")
 
 
