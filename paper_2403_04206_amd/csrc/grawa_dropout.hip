@@ -61,7 +61,7 @@ hipError_t grawa_launch_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype
     while (lanes < 256 && lanes < groups) lanes *= 2;
     const int64_t across = (groups + lanes - 1) / lanes, down = (T + 256 / lanes - 1) / (256 / lanes);
     // A block for every row group up to what fills the card many times over; beyond, blocks walk on.
-    const int64_t most = across * K < 65535 ? 65535 / (across * K) + 1 : 1;
+    const int64_t most = across * K < 65535 ? 65535 / (across * K) : 1;
     const dim3 grid((unsigned)across, (unsigned)(down < most ? down : most), (unsigned)K);
 #define GO(B, R) k_dropout<B, R><<<grid, 256, 0, st>>>(x, residual, drop, y, (uint32_t)T, (uint32_t)d, lanes)
     if (dtype == GRAWA_BF16) {

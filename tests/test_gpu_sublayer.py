@@ -281,6 +281,20 @@ def test_dropout_keeps_as_many_as_it_should():
         assert abs(kept - n * (1 - p)) < 6 * (n * p * (1 - p)) ** 0.5        # six standard deviations
 
 
+def test_dropout_of_more_rows_than_a_grid_has():
+    T, d = 65535 * 256 + 300, 8                       # a thread a row: blocks walk on
+    x, res = make(31, 1, T, d, dtype=BF), make(32, 1, T, d, dtype=BF)
+    y, tail = torch.empty_like(x), torch.empty((1, T, d), device=DEV, dtype=BF)
+    grawa.dropout(x, y, 0.0, rng_of(6, 2), residual=res)
+    grawa.dropout(x, tail, 0.5, rng_of(6, 2), site=1)
+    torch.cuda.synchronize()
+    assert torch.equal(y, (x.float() + res.float()).to(BF))
+    assert torch.logical_or(tail == 0, tail == 2 * x).all()
+    assert abs((tail[0, -300:] != 0).double().mean().item() - 0.5) < 0.1
+    del x, res, y, tail
+    torch.cuda.empty_cache()
+
+
 def test_ffn_with_dropout_and_residual_equals_the_two_calls():
     for dtype, T in ((BF, 140), (F, 140), (BF, 5), (F, 5), (BF, 40)):
         K, d, f = 2, 72, 136
