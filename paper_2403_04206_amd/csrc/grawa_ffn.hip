@@ -400,9 +400,10 @@ template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const g
     return hipGetLastError();
 }
 
-// Segments of A B, small products first.
-void add_segments(GrawaGemm &g, int planes, const Operand &a, const Operand &b, const Operand *b2)
+// Segments of A B, small products first.  A product has one pitch for all its A and one for all its B: operands that do not agree are refused.
+hipError_t add_segments(GrawaGemm &g, int planes, const Operand &a, const Operand &b, const Operand *b2)
 {
+    if ((b2 && b2->ld != b.ld) || (g.nseg && (g.lda != a.ld || g.ldb != b.ld))) return hipErrorInvalidValue;
     static const int pairs[6][2] = {{0, 2}, {2, 0}, {1, 1}, {0, 1}, {1, 0}, {0, 0}};
     const int n = planes == 1 ? 1 : 6;
     for (int i = 0; i < n; ++i) {
@@ -414,6 +415,7 @@ void add_segments(GrawaGemm &g, int planes, const Operand &a, const Operand &b, 
     }
     g.lda = a.ld;
     g.ldb = b.ld;
+    return hipSuccess;
 }
 
 struct Sublayer { // one call
@@ -427,10 +429,13 @@ struct Sublayer { // one call
     int64_t most = 0; // groups of eight of the largest copy
 
     // An operand read in place where it can be, else a copy in `room`, which copy_all() makes.
-    Operand operand(const char *p, int64_t worker, int64_t row, int64_t R, int64_t C, int64_t Cp, char *room)
+    bool in_place(const char *p, int64_t worker, int64_t row, int64_t C) const
     {
-        if (s->planes == 1 && C % 8 == 0 && !(((uintptr_t)p | (uint64_t)worker * 2 | (uint64_t)row * 2) & 15) && row >= C && row * 2 <= MAX_LD)
-            return Operand{p, worker * 2, 0, row * 2};
+        return s->planes == 1 && C % 8 == 0 && !(((uintptr_t)p | (uint64_t)worker * 2 | (uint64_t)row * 2) & 15) && row >= C && row * 2 <= MAX_LD;
+    }
+    Operand operand(const char *p, int64_t worker, int64_t row, int64_t R, int64_t C, int64_t Cp, char *room, bool here)
+    {
+        if (here) return Operand{p, worker * 2, 0, row * 2};
         const Operand o{room, R * Cp * 2, (int64_t)s->K * R * Cp * 2, Cp * 2};
         copies.job[copies.n++] = CopyJob{p, room, worker, row, o.plane, (uint32_t)R, (uint32_t)C, (uint32_t)Cp};
         most = most > R * ((C + 7) / 8) ? most : R * ((C + 7) / 8);
@@ -451,9 +456,15 @@ struct Sublayer { // one call
     }
     // The same of what a forward pass left in `room`.
     Operand kept(int64_t R, int64_t Cp, char *room) const { return Operand{room, R * Cp * 2, (int64_t)s->K * R * Cp * 2, Cp * 2}; }
-    Operand tokens(const GrawaRows &x, char *room) { return operand(x.p, x.worker, x.row, T, s->d, s->dp, room); }
-    Operand up_matrix(const GrawaMat &w, char *room) { return operand(w.p, w.worker, s->d, s->f, s->d, s->dp, room); }
-    Operand down_matrix(const GrawaMat &w, char *room) { return operand(w.p, w.worker, s->f, s->d, s->f, s->fp, room); }
+    Operand tokens(const GrawaRows &x, char *room) { return operand(x.p, x.worker, x.row, T, s->d, s->dp, room, in_place(x.p, x.worker, x.row, s->d)); }
+    // Wg and Wu are operands of one product, which has one pitch: both are read in place, or both are copied.
+    void up_matrices(const GrawaMat &wg, const GrawaMat &wu, char *room_g, char *room_u, Operand &g, Operand &u)
+    {
+        const bool here = in_place(wg.p, wg.worker, s->d, s->d) && in_place(wu.p, wu.worker, s->d, s->d);
+        g = operand(wg.p, wg.worker, s->d, s->f, s->d, s->dp, room_g, here);
+        u = operand(wu.p, wu.worker, s->d, s->f, s->d, s->dp, room_u, here);
+    }
+    Operand down_matrix(const GrawaMat &w, char *room) { return operand(w.p, w.worker, s->f, s->d, s->f, s->fp, room, in_place(w.p, w.worker, s->f, s->f)); }
     Operand inner(char *p) const { return Operand{p, T * s->fp * 2, s->K * T * s->fp * 2, s->fp * 2}; }
     GrawaGemm product(int64_t M, int64_t N, int64_t len) const
     {
@@ -520,16 +531,18 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
     }
     // The split copies of float32 go to where the backward pass finds them, if one follows.
     const Kept at = kept_in(s, c.T, save);
-    const Operand ox = c.tokens(x, at.x), og = c.up_matrix(wg, at.wg), ou = c.up_matrix(wu, at.wu), od = c.down_matrix(wd, at.wd);
+    const Operand ox = c.tokens(x, at.x), od = c.down_matrix(wd, at.wd);
+    Operand og, ou;
+    c.up_matrices(wg, wu, at.wg, at.wu, og, ou);
     c.copy_all();
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
-        add_segments(g, PLANES, ox, og, &ou);
+        c.run([&] { return add_segments(g, PLANES, ox, og, &ou); });
         c.run([&] { return launch_gemm<false, false, true>(s, g, inner, c.st); });
     }
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
-        add_segments(g, PLANES, c.inner(h), od, nullptr);
+        c.run([&] { return add_segments(g, PLANES, c.inner(h), od, nullptr); });
         c.run([&] { return launch_gemm<false, false, false>(s, g, outer, c.st); });
     }
     return c.err;
@@ -542,7 +555,8 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
     const bool have = grawa_keeps_copies(s, c.T);
     const Kept at = kept_in(s, c.T, (char *)save);
     const Operand ody = c.tokens(dy, s->dy), ox = have ? c.kept(c.T, s->dp, at.x) : c.tokens(x, at.x);
-    const Operand og = have ? c.kept(s->f, s->dp, at.wg) : c.up_matrix(wg, at.wg), ou = have ? c.kept(s->f, s->dp, at.wu) : c.up_matrix(wu, at.wu);
+    Operand og = c.kept(s->f, s->dp, at.wg), ou = c.kept(s->f, s->dp, at.wu);
+    if (!have) c.up_matrices(wg, wu, at.wg, at.wu, og, ou);
     const Operand od = have ? c.kept(s->d, s->fp, at.wd) : c.down_matrix(wd, at.wd);
     c.copy_all();
     const int64_t n = c.T * s->fp;
@@ -551,13 +565,13 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
     typedef EpiStore<PLANES == 1, false> Store;
     auto weight_product = [&](const Operand &a, const Operand &b, int64_t M, int64_t N) {
         GrawaGemm g = c.product(M, N, c.T);
-        add_segments(g, PLANES, a, b, nullptr);
+        c.run([&] { return add_segments(g, PLANES, a, b, nullptr); });
         return g;
     };
     auto weight_store = [&](GrawaMat w, int64_t N, GrawaMat second) { return Store{GrawaRows{w.p, w.worker, N}, GrawaRows{}, GrawaDrop{}, (int)N, 0, accumulate, 0, second, s->K}; };
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
-        add_segments(g, PLANES, ody, od, nullptr);
+        c.run([&] { return add_segments(g, PLANES, ody, od, nullptr); });
         const EpiBack<PLANES, ACT> epi{{(char *)save, s->K * blocks}, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
@@ -573,11 +587,12 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
         c.run([&] { return launch_gemm<true, true, false>(s, gate, weight_store(dwg, s->d, GrawaMat{}), c.st); });
         c.run([&] { return launch_gemm<true, true, false>(s, up, weight_store(dwu, s->d, GrawaMat{}), c.st); });
     }
-    c.run([&] { return launch_gemm<true, true, false>(s, weight_product(ody, oh, s->d, s->f), weight_store(dwd, s->f, GrawaMat{}), c.st); });
+    const GrawaGemm down = weight_product(ody, oh, s->d, s->f);
+    c.run([&] { return launch_gemm<true, true, false>(s, down, weight_store(dwd, s->f, GrawaMat{}), c.st); });
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
-        add_segments(g, PLANES, odg, og, nullptr);
-        add_segments(g, PLANES, odu, ou, nullptr);
+        c.run([&] { return add_segments(g, PLANES, odg, og, nullptr); });
+        c.run([&] { return add_segments(g, PLANES, odu, ou, nullptr); });
         const Store epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, 0, GrawaMat{}, s->K};
         c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
     }
