@@ -116,8 +116,10 @@ template <int PLANES> __device__ __forceinline__ void normal_of(float z, float &
     }
 }
 
-template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z, float &a, float &da)
+// a = act(z) and back = v act'(z).  What relu closes is 0 whatever stands beside it: a gate of -infinity, an infinite v; a NaN stays one.
+template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z, float v, float &a, float &back)
 {
+    float da;
     if constexpr (ACT == GRAWA_ACT_SILU) {
         const float s = sigmoid_of<PLANES>(z);
         a = z * s;
@@ -128,15 +130,17 @@ template <int PLANES, int ACT> __device__ __forceinline__ void act_both(float z,
         a = z * cdf;
         da = cdf + z * density;
     } else {
-        da = z > 0.f ? 1.f : 0.f;
-        a = z * da;
+        a = z <= 0.f ? 0.f : z;
+        back = z > 0.f ? v : 0.f;
+        return;
     }
+    back = v * da;
 }
 
 template <int PLANES, int ACT> __device__ __forceinline__ float act_of(float z)
 {
-    float a, da;
-    act_both<PLANES, ACT>(z, a, da);
+    float a, back;
+    act_both<PLANES, ACT>(z, 0.f, a, back);
     return a;
 }
 
@@ -251,10 +255,10 @@ template <int PLANES, int ACT> struct EpiBack {
         kept.values(r, g, u);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float a, da;
-            act_both<PLANES, ACT>(g[j], a, da);
+            float a, back;
+            act_both<PLANES, ACT>(g[j], dh[j] * u[j], a, back);
             out[j] = dh[j] * a;
-            dh[j] = dh[j] * u[j] * da;
+            dh[j] = back;
         }
     }
     __device__ __forceinline__ void put(int o, int m, int n, float *v) const

@@ -1,0 +1,53 @@
+"""The gated feed-forward block at the ends of its numbers: gates that are infinite or far out, values whose bits are all in use, infinities."""
+import pytest
+import torch
+
+from paper_2403_04206_amd import grawa
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F = torch.bfloat16, torch.float32
+
+
+def tensor(values, dtype):
+    return torch.tensor(values, device=DEV, dtype=torch.float64).to(dtype)
+
+
+def forward_and_back(x, wg, wu, wd, dy, act):
+    """One worker's y, dx, dWg, dWu, dWd: x, dy [T, d], wg, wu [f, d], wd [d, f]."""
+    (T, d), f, dtype = x.shape, wg.shape[0], x.dtype
+    x, wg, wu, wd, dy = (t.unsqueeze(0).contiguous() for t in (x, wg, wu, wd, dy))
+    y, dx, dwg, dwu, dwd = (torch.full_like(t, 7.0) for t in (x, x, wg, wu, wd))
+    with grawa.SublayerPlan(1, T, d, f, dtype=dtype, activation=act) as plan:
+        save = torch.empty(plan.save_bytes(), dtype=torch.uint8, device=DEV)
+        plan.ffn(x, wg, wu, wd, y, save=save)
+        plan.ffn_backward(dy, x, wg, wu, wd, save, dx, dwg, dwu, dwd)
+        torch.cuda.synchronize()
+    return tuple(t[0].double() for t in (y, dx, dwg, dwu, dwd))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("T", [3, 40, 140])
+def test_relu_closes_a_gate_whatever_stands_beside_it(dtype, T):
+    print("[case] relu", dtype, T, flush=True)
+    big = 2.0 ** 70                                    # its square is no float32
+    x, one = tensor([[big]] * T, dtype), tensor([[1.0]], dtype)
+    # a gate of -infinity: relu gives 0, and so do the block and its gradients
+    y, dx, dwg, dwu, dwd = forward_and_back(x, -one * big, one / big, one, torch.ones_like(x), "relu")
+    for t in (y, dx, dwg, dwu, dwd):
+        assert (t == 0).all()
+    # gates of -1: what comes back through them is 0 beside an infinite up, and under an infinite gradient
+    y, dx, dwg, dwu, dwd = forward_and_back(x, -one / big, one * big, one, torch.ones_like(x), "relu")
+    assert (dwg == 0).all()
+    y, dx, dwg, dwu, dwd = forward_and_back(x, -one / big, one / big, one * big, x, "relu")
+    assert (y == 0).all() and (dwg == 0).all()
+    # a gate that is no number is none afterwards, an infinite one stays
+    nan = x.clone()
+    nan[T - 1, 0] = float("nan")
+    y = forward_and_back(nan, one / big, one / big, one, torch.ones_like(x), "relu")[0]
+    assert torch.isnan(y[T - 1]).all() and (y[:T - 1] == 1).all()
+    y = forward_and_back(x, one * big, one / big, one, torch.ones_like(x), "relu")[0]
+    if dtype is BF or T <= 64:
+        assert (y == float("inf")).all()
+    else:                                              # terms of a float32 that are 0 make a NaN of it
+        assert not torch.isfinite(y).any()
