@@ -8,22 +8,24 @@
 // Roundings.  bfloat16: H, dG and dU are rounded to bfloat16, as the matrix instructions take them; G and U are kept for the
 // backward pass with eight bits more than that (a rounding of theirs would be a third one on the way to dWg, dWu and dx).  float32: every matrix
 // element is split exactly into three bfloat16 terms and the six largest of the nine products of terms are summed in float32;
-// what is left out is below 2^-24 of a product.  (An infinity times a number that is exactly a bfloat16 gives NaN there.)
+// what is left out is at most 2^-24 of a product.  (An infinity times a number that is exactly a bfloat16 gives NaN there.)
 #include "grawa_few.h"
 #include "grawa_gemm.h"
 
 namespace {
 
-// The three terms, each the number's upper 16 bits after the terms before it: the remainders are exact, and nothing can overflow.
+// The three terms, each what the terms before it left, rounded to nearest; the last takes all that is left.  Rounded, and not cut off: the second
+// and the third term are then at most 2^-8 and 2^-17 of the number's leading bit, and of either sign.  Cut off, they reach 2^-7 and 2^-15 and have
+// the number's own sign, so that what a sum of products leaves out is up to 2^-21 of it and always on one side.  A number that
+// would round to infinity is cut off.
 __device__ __forceinline__ void split3(float v, uint16_t t[3])
 {
-    uint32_t u = __float_as_uint(v);
-    if ((u & 0x7fffffffu) > 0x7f800000u) u = 0x7fc00000u; // a NaN whose mark stands in the lower bits
-    t[0] = (uint16_t)(u >> 16);
-    const float r = (u & 0x7f800000u) == 0x7f800000u ? 0.f : v - __uint_as_float(u & 0xffff0000u);
-    const uint32_t w = __float_as_uint(r);
-    t[1] = (uint16_t)(w >> 16);
-    t[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(w & 0xffff0000u)) >> 16);
+    const uint32_t u = __float_as_uint(v);
+    t[0] = __builtin_bit_cast(uint16_t, (__bf16)v);
+    if ((t[0] & 0x7fff) == 0x7f80) t[0] = (uint16_t)(u >> 16);
+    const float r = (u & 0x7f800000u) == 0x7f800000u ? 0.f : v - bf16_one(t[0]);
+    t[1] = __builtin_bit_cast(uint16_t, (__bf16)r);
+    t[2] = __builtin_bit_cast(uint16_t, (__bf16)(r - bf16_one(t[1])));
 }
 
 // Eight numbers to the planes at p, p + plane, p + 2 plane (bytes): 16 bytes each.

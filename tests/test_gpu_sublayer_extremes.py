@@ -51,3 +51,25 @@ def test_relu_closes_a_gate_whatever_stands_beside_it(dtype, T):
         assert (y == float("inf")).all()
     else:                                              # terms of a float32 that are 0 make a NaN of it
         assert not torch.isfinite(y).any()
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_float32_products_of_numbers_with_all_their_bits(T):
+    """One product after the other, (x wg) (x wu) wd with positive numbers, against 64 bits.  Each of the three products may lack 2^-24 of
+    itself, and its terms are added with an error of 2^-23, whichever way a sum is rounded; the gate times the up and the result are rounded
+    once more, 2^-24 each: 3 * 3 + 2 times 2^-24, and one for what is of second order."""
+    print("[case] bits", T, flush=True)
+    g = torch.Generator().manual_seed(3)
+    worst = [1 + 2.0 ** -7 - 2.0 ** -23, 1 + 2.0 ** -8 - 2.0 ** -23, 1 + 2.0 ** -7 + 2.0 ** -15 - 2.0 ** -23, 2 - 2.0 ** -23]
+    for weights in [[w] * 3 for w in worst] + (1 + torch.rand((20, 3), generator=g)).tolist():
+        x = (1 + torch.rand((T, 1), generator=g)).to(DEV)
+        x[0, 0], x[-1, 0] = weights[0], worst[0]
+        wg, wu, wd = (tensor([[w]], F) for w in weights)
+        y, dx, dwg, dwu, dwd = forward_and_back(x, wg, wu, wd, torch.ones_like(x), "relu")
+        x, wg, wu, wd = (t.double() for t in (x, wg, wu, wd))
+        want = (x * wg) * (x * wu) * wd
+        off = ((y - want) / want).abs().max().item() * 2.0 ** 24
+        assert off <= 12, (weights, off)
+        # dx = 2 x wg wu wd: three products one after the other in each of two that are added, a rounding more
+        off = ((dx - 2 * x * wg * wu * wd) / (2 * x * wg * wu * wd)).abs().max().item() * 2.0 ** 24
+        assert off <= 14, (weights, off)
