@@ -73,3 +73,19 @@ def test_float32_products_of_numbers_with_all_their_bits(T):
         # dx = 2 x wg wu wd: three products one after the other in each of two that are added, a rounding more
         off = ((dx - 2 * x * wg * wu * wd) / (2 * x * wg * wu * wd)).abs().max().item() * 2.0 ** 24
         assert off <= 14, (weights, off)
+
+
+@pytest.mark.parametrize("T", [3, 40, 140])
+def test_gate_and_up_go_to_the_backward_pass_rounded_to_nearest(T):
+    """bfloat16.  An up (a gate) a little above the middle between two bfloat16 numbers, by less than one part in 2^15: dG (dU) is the up (the gate) rounded
+    to bfloat16 here, the upper of the two."""
+    print("[case] kept", T, flush=True)
+    x, dy = torch.zeros((T, 3), device=DEV, dtype=BF), torch.zeros((T, 3), device=DEV, dtype=BF)
+    x[T - 1] = 1
+    dy[T - 1, 0] = 1
+    one, wd = tensor([[1.0, 0.0, 0.0]], BF), tensor([[1.0], [0.0], [0.0]], BF)
+    for sign, at in ((1, 0), (-1, 0), (1, 1)):
+        odd = tensor([[1.0, 2.0 ** -8, 29 * 2.0 ** -20]], BF) * sign
+        y, dx, dwg, dwu, dwd = forward_and_back(x, odd if at else one, one if at else odd, wd, dy, "relu")
+        got = dwu if at else dwg
+        assert (got == sign * (1 + 2.0 ** -7)).all(), (sign, at, got)
