@@ -89,3 +89,26 @@ def test_gate_and_up_go_to_the_backward_pass_rounded_to_nearest(T):
         y, dx, dwg, dwu, dwd = forward_and_back(x, odd if at else one, one if at else odd, wd, dy, "relu")
         got = dwu if at else dwg
         assert (got == sign * (1 + 2.0 ** -7)).all(), (sign, at, got)
+
+
+@pytest.mark.parametrize("T", [30, 481])
+@pytest.mark.parametrize("act,low", [("gelu", -12.5), ("silu", -80.0)])
+def test_activations_far_out(act, low, T):
+    """bfloat16.  The activation of x and its derivative, which the block gives as they are with an up of 1 and matrices of 0 and 1, against 64 bits: one
+    rounding to bfloat16, 2^-8, and 2^-11 for the function; the derivative's two terms may cancel, with 2^-18 of them left."""
+    print("[case] tails", act, T, flush=True)
+    z = torch.linspace(low, 12.5, T, device=DEV, dtype=torch.float64).to(BF)
+    x = torch.stack((z, torch.ones_like(z)), 1)
+    dy = torch.zeros_like(x)
+    dy[:, 0] = 1
+    y, dx, _, _, _ = forward_and_back(x, tensor([[1.0, 0.0]], BF), tensor([[0.0, 1.0]], BF), tensor([[1.0], [0.0]], BF), dy, act)
+    z = z.double()
+    if act == "gelu":
+        first, second = 0.5 * torch.erfc(-z / 2 ** 0.5), z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+    else:
+        first = torch.sigmoid(z)
+        second = z * first * torch.sigmoid(-z)
+    for what, got, want, slack in (("value", y[:, 0], z * first, 0), ("derivative", dx[:, 0], first + second, 2.0 ** -18 * (first + second.abs()))):
+        over = (got - want).abs() - (2.0 ** -8 + 2.0 ** -11) * want.abs() - slack
+        i = over.argmax().item()
+        assert over[i] <= 0, (what, z[i].item(), got[i].item(), want[i].item())
