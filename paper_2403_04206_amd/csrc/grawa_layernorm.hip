@@ -36,14 +36,14 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float *sm)
 // A block of BLOCK threads holds BLOCK / TPR rows side by side; thread c of a row has the 16-byte pieces j TPR + c of it, j < NV.
 // Rows up to 1024 elements are a wave's, which needs no barrier.  8 x 2048 x 1024 in bfloat16: 12.5 us, 5.4 TB/s.
 template <bool BF16, int NV, int TPR, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void k_norm(GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y, float *stats, int64_t T, int d)
+__global__ __launch_bounds__(BLOCK) void k_norm(GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y, float *stats, int64_t t0, int64_t T, int d)
 {
     typedef GrawaPiece<BF16> Piece;
     constexpr int S = Piece::S, N = Piece::N;
     static_assert(TPR == 64 || TPR == BLOCK, "a row is a wave's or the block's");
     __shared__ float sm[2][BLOCK / 64];
     const int c = threadIdx.x % TPR, k = blockIdx.y;
-    const int64_t t = (int64_t)blockIdx.x * (BLOCK / TPR) + threadIdx.x / TPR;
+    const int64_t t = t0 + (int64_t)blockIdx.x * (BLOCK / TPR) + threadIdx.x / TPR;
     if (t >= T) return; // whole waves of a row that is one wave's, or the whole block
     const char *px = x.p + ((int64_t)k * x.worker + t * x.row) * S;
     const char *pw = w.p + (int64_t)k * w.worker * S, *pb = b.p ? b.p + (int64_t)k * b.worker * S : nullptr;
@@ -83,12 +83,12 @@ __global__ __launch_bounds__(BLOCK) void k_norm(GrawaRows x, GrawaMat w, GrawaMa
 }
 
 // Rows that no block holds: they are read three times.
-template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_long(GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y, float *stats, int64_t T, int d)
+template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_long(GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y, float *stats, int64_t t0, int64_t T, int d)
 {
     constexpr int S = BF16 ? 2 : 4;
     __shared__ float sm[2][16];
     const int c = threadIdx.x, k = blockIdx.y;
-    const int64_t t = blockIdx.x;
+    const int64_t t = t0 + blockIdx.x;
     const char *px = x.p + ((int64_t)k * x.worker + t * x.row) * S;
     float sum = 0.f, sq = 0.f, v, ww, bb = 0.f;
     for (int e = c; e < d; e += 1024) {
@@ -217,12 +217,12 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(GrawaRows dy, GrawaRows x, 
 }
 
 // Rows that no block holds: dx by a block for each row, dw and db by a thread for each column of a range of rows.
-template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_back_long(GrawaRows dy, GrawaRows x, GrawaMat w, const float *stats, GrawaRows add, GrawaRows dx, int64_t T, int d)
+template <bool BF16> __global__ __launch_bounds__(1024) void k_norm_back_long(GrawaRows dy, GrawaRows x, GrawaMat w, const float *stats, GrawaRows add, GrawaRows dx, int64_t t0, int64_t T, int d)
 {
     constexpr int S = BF16 ? 2 : 4;
     __shared__ float sm[2][16];
     const int c = threadIdx.x, k = blockIdx.y;
-    const int64_t t = blockIdx.x;
+    const int64_t t = t0 + blockIdx.x;
     const char *px = x.p + ((int64_t)k * x.worker + t * x.row) * S, *pdy = dy.p + ((int64_t)k * dy.worker + t * dy.row) * S;
     const char *pw = w.p + (int64_t)k * w.worker * S;
     const float2 st = *(const float2 *)(stats + 2 * ((int64_t)k * T + t));
@@ -315,14 +315,25 @@ int grawa_norm_blocks(int K, int64_t T, int64_t d)
     return (int)(n > 0 ? n : 1);
 }
 
+// T rows by blocks that hold `rows` each: a launch has fewer than 2^32 threads along x, so very many rows take several.
+template <class F> static void launch_rows(int64_t T, int rows, int threads, const F &launch)
+{
+    const int64_t most = ((int64_t)1 << 31) / threads * rows;
+    for (int64_t t0 = 0; t0 < T; t0 += most) {
+        const int64_t n = T - t0 < most ? T - t0 : most;
+        launch((unsigned)((n + rows - 1) / rows), t0);
+    }
+}
+
 hipError_t grawa_launch_layer_norm(const grawa_sublayer *s, int64_t T, GrawaRows x, GrawaMat w, GrawaMat b, float eps, GrawaRows y,
                                    float *stats, hipStream_t st)
 {
     if (!T) return hipSuccess;
     const int d = (int)s->d;
+    const unsigned K = (unsigned)s->K;
 #define GO(BF, NV, TPR, BLOCK)                                                                                           \
-    k_norm<BF, NV, TPR, BLOCK><<<dim3((unsigned)((T + BLOCK / TPR - 1) / (BLOCK / TPR)), (unsigned)s->K), BLOCK, 0, st>>>(x, w, b, eps, y, stats, T, d)
-#define GOLONG(BF) k_norm_long<BF><<<dim3((unsigned)T, (unsigned)s->K), 1024, 0, st>>>(x, w, b, eps, y, stats, T, d)
+    launch_rows(T, BLOCK / TPR, BLOCK, [&](unsigned n, int64_t t0) { k_norm<BF, NV, TPR, BLOCK><<<dim3(n, K), BLOCK, 0, st>>>(x, w, b, eps, y, stats, t0, T, d); })
+#define GOLONG(BF) launch_rows(T, 1, 1024, [&](unsigned n, int64_t t0) { k_norm_long<BF><<<dim3(n, K), 1024, 0, st>>>(x, w, b, eps, y, stats, t0, T, d); })
     if (s->dtype == GRAWA_BF16) GRAWA_NORM_FORMS(GO, GOLONG, true);
     else GRAWA_NORM_FORMS(GO, GOLONG, false);
 #undef GO
@@ -341,7 +352,7 @@ hipError_t grawa_launch_layer_norm_backward(const grawa_sublayer *s, int64_t T, 
 #define GOLONG(BF)                                                                                                               \
     do {                                                                                                                         \
         k_norm_back_cols<BF><<<dim3((unsigned)nb, (unsigned)((d + 255) / 256), (unsigned)s->K), 256, 0, st>>>(dy, x, stats, part, T, d); \
-        k_norm_back_long<BF><<<dim3((unsigned)T, (unsigned)s->K), 1024, 0, st>>>(dy, x, w, stats, add, dx, T, d);                \
+        launch_rows(T, 1, 1024, [&](unsigned n, int64_t t0) { k_norm_back_long<BF><<<dim3(n, (unsigned)s->K), 1024, 0, st>>>(dy, x, w, stats, add, dx, t0, T, d); }); \
     } while (0)
         if (s->dtype == GRAWA_BF16) GRAWA_NORM_FORMS(GO, GOLONG, true);
         else GRAWA_NORM_FORMS(GO, GOLONG, false);

@@ -1,6 +1,7 @@
 // What the feed-forward sublayer launches, without a GPU: the host side of its files is linked with a runtime of stubs, which notes every
 // launch and its arguments.  Addresses are numbers here and nothing is read through them.
 //   sublayer_launch_driver operands    every operand of every product: its pitch is that of the matrix it points to, and no row leaves it
+//   sublayer_launch_driver grids       every launch is one that a card takes, at the largest shapes too
 #include <cstdio>
 #include <cstring>
 #include <string>
@@ -186,10 +187,65 @@ static int operands()
     return 0;
 }
 
+// -- grids ------------------------------------------------------------------------------
+
+static int64_t launches;
+
+static void grid_launch(const std::string &name, dim3 grid, dim3 block, void **)
+{
+    ++launches;
+    const bool takes = grid.x && grid.y && grid.z && grid.y <= 65535 && grid.z <= 65535 && block.x * block.y * block.z <= 1024 && (uint64_t)grid.x * block.x <= UINT32_MAX;
+    expect(takes, (name.substr(0, 60) + " of " + std::to_string(grid.x) + " x " + std::to_string(grid.y) + " x " + std::to_string(grid.z) + " blocks of " + std::to_string(block.x)).c_str());
+}
+
+static int grids()
+{
+    launched = grid_launch;
+    const int64_t card = (int64_t)288 << 30; // what the arrays of a call may take together
+    const int64_t tokens_max = (int64_t)1 << 30, width_max = ((int64_t)1 << 20) - 1;
+    int norms = 0, blocks = 0;
+    for (int dt = 0; dt < 2; ++dt)
+        for (const int64_t K : {1, 2, 7, 64, 1024})
+            for (int64_t T = 1; T <= tokens_max / K; T = T * 2 < tokens_max / K || T == tokens_max / K ? T * 2 : tokens_max / K)
+                for (const int64_t d : {(int64_t)1, (int64_t)8, (int64_t)64, (int64_t)512, (int64_t)1024, (int64_t)1032, (int64_t)4096, (int64_t)8192, (int64_t)16384, (int64_t)16390, width_max}) {
+                    const int S = dt ? 2 : 4;
+                    const int64_t bytes = K * T * d * S;
+                    what = "dtype " + std::to_string(dt) + " K " + std::to_string(K) + " T " + std::to_string(T) + " d " + std::to_string(d);
+                    if (bytes > card / 2) continue;
+                    const grawa_dtype_t type = dt ? GRAWA_BF16 : GRAWA_F32;
+                    char *const at = (char *)((uintptr_t)1 << 50);
+                    const grawa_rows_t x{at, T * d, d}, y{at + ((int64_t)1 << 45), T * d, d};
+                    const grawa_mats_t w{at, width_max};
+                    const int64_t rng[2] = {};
+                    expect(grawa_dropout((int)K, T, d, type, &x, &x, 0.5f, rng, 0, &y, nullptr) == GRAWA_OK, "a dropout's status");
+                    grawa_sublayer_t *p = nullptr;
+                    if (grawa_sublayer_create(&p, (int)K, T, d, 0, type, GRAWA_ACT_SILU) != GRAWA_OK) return 1;
+                    ++norms;
+                    expect(grawa_layer_norm(p, T, &x, &w, &w, 0.f, &y, (float *)at, nullptr) == GRAWA_OK, "a norm's status");
+                    expect(grawa_layer_norm_backward(p, T, &x, &x, &w, (const float *)at, nullptr, &y, &w, &w, 0, nullptr) == GRAWA_OK, "a norm's status");
+                    grawa_sublayer_destroy(p);
+                    for (const int64_t f : {(int64_t)1, (int64_t)64, (int64_t)1024, (int64_t)11264, width_max}) {
+                        const int64_t matrix = K * d * f * S, rows = (dt ? 2 : 6) * K * T * f; // of an inner array
+                        if (matrix > card / 6 || rows > card / 4) continue;
+                        next_address = (uintptr_t)1 << 44;
+                        if (grawa_sublayer_create(&p, (int)K, T, d, f, type, GRAWA_ACT_SILU) != GRAWA_OK) return 1;
+                        if ((int64_t)(next_address - ((uintptr_t)1 << 44)) + 3 * matrix + 2 * bytes <= card) {
+                            ++blocks;
+                            const grawa_mats_t m{at, d * f};
+                            expect(grawa_ffn(p, T, &x, &m, &m, &m, nullptr, 0.f, nullptr, 0, &y, at, nullptr) == GRAWA_OK, "a block's status");
+                            expect(grawa_ffn_backward(p, T, &x, &x, &m, &m, &m, at, &y, &m, &m, &m, 0, nullptr) == GRAWA_OK, "a block's status");
+                        }
+                        grawa_sublayer_destroy(p);
+                    }
+                }
+    expect(norms > 1000 && blocks > 1000 && launches > 10000, "shapes were looked at");
+    return 0;
+}
+
 int main(int n, char **args)
 {
     if (n != 2) return 2;
-    const int rc = !std::strcmp(args[1], "operands") ? operands() : 2;
+    const int rc = !std::strcmp(args[1], "operands") ? operands() : !std::strcmp(args[1], "grids") ? grids() : 2;
     if (rc || failures) {
         std::printf("%d failures\n", failures);
         return 1;

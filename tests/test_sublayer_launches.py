@@ -38,3 +38,8 @@ def test_products_read_their_matrices_by_their_own_pitch(driver):
     """Every operand of every product, with each of x, dy, Wg, Wu and Wd on and off 16 bytes: the matrix that it points to has the pitch that the
     product walks it with, and the rows that the product reads are that matrix's."""
     run(driver, "operands")
+
+
+def test_every_launch_fits_a_grid(driver):
+    """Up to the limits that the calls take, and what a card's memory holds: fewer than 2^32 threads along x, at most 65535 blocks along y and z."""
+    run(driver, "grids")
