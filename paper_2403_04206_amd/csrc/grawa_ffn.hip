@@ -372,14 +372,15 @@ Cut cut_of(int64_t K, int64_t M, int64_t N, int64_t ktiles, bool dual, bool shor
 // four workers' 1024 x 4096 (101 MB) 28.6 us again and again by cached loads and 35.8 past them.
 constexpr int64_t CACHED = (int64_t)256 << 20;
 
-template <bool AT, bool BT, bool DUAL, class Epi> void launch_tiles(const grawa_sublayer *s, const GrawaGemm &g, const Cut &cut, const Epi &epi, hipStream_t st)
+// SHORT: products of no more rows than the lowest tile has come here at all.
+template <bool AT, bool BT, bool DUAL, bool SHORT, class Epi> void launch_tiles(const grawa_sublayer *s, const GrawaGemm &g, const Cut &cut, const Epi &epi, hipStream_t st)
 {
     const dim3 grid((unsigned)(cut.tiles * cut.splits));
     if (cut.kind == 0)
         k_gemm<256, 256, 2, 4, false, AT, BT, DUAL, Epi><<<grid, 512, 0, st>>>(g, epi);
     else if (cut.kind == 1)
         k_gemm<128, 128, 2, 2, false, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
-    else if constexpr (!AT) {
+    else if constexpr (SHORT) {
         if (6 * s->planes * (int64_t)s->K * s->d * s->f > CACHED)
             k_gemm<64, 128, 1, 4, true, AT, BT, DUAL, Epi><<<grid, 256, 0, st>>>(g, epi);
         else
@@ -387,16 +388,16 @@ template <bool AT, bool BT, bool DUAL, class Epi> void launch_tiles(const grawa_
     }
 }
 
-template <bool AT, bool BT, bool DUAL, class Epi> hipError_t launch_gemm(const grawa_sublayer *s, GrawaGemm g, const Epi &epi, hipStream_t st)
+template <bool AT, bool BT, bool DUAL, bool SHORT, class Epi> hipError_t launch_gemm(const grawa_sublayer *s, GrawaGemm g, const Epi &epi, hipStream_t st)
 {
-    const Cut cut = cut_of(g.K, g.M, g.N, (int64_t)((g.len + GRAWA_BK - 1) / GRAWA_BK) * g.nseg, DUAL, !AT, s->part_floats);
+    const Cut cut = cut_of(g.K, g.M, g.N, (int64_t)((g.len + GRAWA_BK - 1) / GRAWA_BK) * g.nseg, DUAL, SHORT, s->part_floats);
     g.splits = cut.splits;
     if (cut.splits == 1) {
-        launch_tiles<AT, BT, DUAL>(s, g, cut, epi, st);
+        launch_tiles<AT, BT, DUAL, SHORT>(s, g, cut, epi, st);
     } else {
         const int64_t blocks = grawa_round16(g.M) * grawa_round16(g.N);
         const GrawaParts parts{s->part, blocks, g.K, DUAL ? 2 : 1, (g.N + 15) >> 4};
-        launch_tiles<AT, BT, DUAL>(s, g, cut, EpiParts{parts, nullptr, nullptr}, st);
+        launch_tiles<AT, BT, DUAL, SHORT>(s, g, cut, EpiParts{parts, nullptr, nullptr}, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const unsigned rows = (unsigned)((g.M + 15) / 16);
@@ -512,6 +513,7 @@ template <bool BF16, bool DUAL, bool PLANES, class Epi> hipError_t launch_few(co
     const unsigned threads = (int64_t)grid.x * K < 1024 ? 512 : 256;
     if (mt == 1) k_few<BF16, 1, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
     else if (mt == 2) k_few<BF16, 2, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
+    else if constexpr (BF16) return hipErrorInvalidValue; // more than 32 tokens do not come here
     else if (mt == 3) k_few<BF16, 3, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
     else k_few<BF16, 4, DUAL, PLANES, Epi><<<grid, threads, 0, st>>>(g, epi);
     return hipGetLastError();
@@ -546,12 +548,12 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
     {
         GrawaGemm g = c.product(c.T, s->f, s->d);
         c.run([&] { return add_segments(g, PLANES, ox, og, &ou); });
-        c.run([&] { return launch_gemm<false, false, true>(s, g, inner, c.st); });
+        c.run([&] { return launch_gemm<false, false, true, BF16>(s, g, inner, c.st); });
     }
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
         c.run([&] { return add_segments(g, PLANES, c.inner(h), od, nullptr); });
-        c.run([&] { return launch_gemm<false, false, false>(s, g, outer, c.st); });
+        c.run([&] { return launch_gemm<false, false, false, BF16>(s, g, outer, c.st); });
     }
     return c.err;
 }
@@ -581,7 +583,7 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
         GrawaGemm g = c.product(c.T, s->f, s->d);
         c.run([&] { return add_segments(g, PLANES, ody, od, nullptr); });
         const EpiBack<PLANES, ACT> epi{{(char *)save, s->K * blocks}, s->dg, s->du, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
-        c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, true, false, true>(s, g, epi, c.st); });
     }
     // dWg and dWu: in one launch while one of them gives a CU no more than a tile: 2 x 54 tokens, 192 x 64, 48 -> 42 us for a whole
     // training pass.  One after the other beyond: 8192 tokens, 4096 x 11264, 5225 us, side by side 5275.
@@ -590,19 +592,19 @@ hipError_t backward(Sublayer c, GrawaRows dy, GrawaRows x, GrawaMat wg, GrawaMat
     if (s->K * ((s->f + 255) / 256) * ((s->d + 255) / 256) <= 256) {
         for (int i = 0; i < up.nseg; ++i) gate.a[gate.nseg + i] = up.a[i];
         gate.K = 2 * s->K;
-        c.run([&] { return launch_gemm<true, true, false>(s, gate, weight_store(dwg, s->d, dwu), c.st); });
+        c.run([&] { return launch_gemm<true, true, false, false>(s, gate, weight_store(dwg, s->d, dwu), c.st); });
     } else {
-        c.run([&] { return launch_gemm<true, true, false>(s, gate, weight_store(dwg, s->d, GrawaMat{}), c.st); });
-        c.run([&] { return launch_gemm<true, true, false>(s, up, weight_store(dwu, s->d, GrawaMat{}), c.st); });
+        c.run([&] { return launch_gemm<true, true, false, false>(s, gate, weight_store(dwg, s->d, GrawaMat{}), c.st); });
+        c.run([&] { return launch_gemm<true, true, false, false>(s, up, weight_store(dwu, s->d, GrawaMat{}), c.st); });
     }
     const GrawaGemm down = weight_product(ody, oh, s->d, s->f);
-    c.run([&] { return launch_gemm<true, true, false>(s, down, weight_store(dwd, s->f, GrawaMat{}), c.st); });
+    c.run([&] { return launch_gemm<true, true, false, false>(s, down, weight_store(dwd, s->f, GrawaMat{}), c.st); });
     {
         GrawaGemm g = c.product(c.T, s->d, s->f);
         c.run([&] { return add_segments(g, PLANES, odg, og, nullptr); });
         c.run([&] { return add_segments(g, PLANES, odu, ou, nullptr); });
         const Store epi{dx, GrawaRows{}, GrawaDrop{}, (int)s->d, 0, 0, 0, GrawaMat{}, s->K};
-        c.run([&] { return launch_gemm<false, true, false>(s, g, epi, c.st); });
+        c.run([&] { return launch_gemm<false, true, false, true>(s, g, epi, c.st); });
     }
     return c.err;
 }

@@ -2,8 +2,10 @@
 // launch and its arguments.  Addresses are numbers here and nothing is read through them.
 //   sublayer_launch_driver operands    every operand of every product: its pitch is that of the matrix it points to, and no row leaves it
 //   sublayer_launch_driver grids       every launch is one that a card takes, at the largest shapes too
+//   sublayer_launch_driver reached     every kernel that is built is launched by some call
 #include <cstdio>
 #include <cstring>
+#include <set>
 #include <string>
 #include <unordered_map>
 #include <vector>
@@ -242,10 +244,50 @@ static int grids()
     return 0;
 }
 
+// -- reached ----------------------------------------------------------------------------
+
+static std::set<std::string> seen;
+
+static int reached()
+{
+    launched = [](const std::string &name, dim3, dim3, void **) { seen.insert(name); };
+    char *const at = (char *)((uintptr_t)1 << 50);
+    const int64_t rng[2] = {};
+    const struct { int64_t d, f; } widths[] = {{8, 0}, {600, 0}, {1032, 0}, {5000, 0}, {9000, 0}, {20000, 0}, {64, 72}, {1024, 4096}, {4096, 11264}, {8192, 256}, {256, 8192}, {1000, 2731}};
+    for (int dt = 0; dt < 2; ++dt)
+        for (const grawa_act_t act : {GRAWA_ACT_SILU, GRAWA_ACT_GELU, GRAWA_ACT_RELU})
+            for (const int K : {1, 2, 16, 1024})
+                for (const int64_t T : {0, 1, 16, 20, 32, 40, 60, 64, 100, 300, 1000, 2048, 8192, 40000})
+                    for (const auto &c : widths) {
+                        what = "dtype " + std::to_string(dt) + " K " + std::to_string(K) + " T " + std::to_string(T) + " d " + std::to_string(c.d);
+                        const grawa_dtype_t type = dt ? GRAWA_BF16 : GRAWA_F32;
+                        const grawa_rows_t x{at, T * c.d, c.d}, y{at + ((int64_t)1 << 45), T * c.d, c.d};
+                        const grawa_mats_t w{at, c.d}, m{at, c.d * c.f};
+                        grawa_sublayer_t *p = nullptr;
+                        if (K * c.f * (c.d + T) >= (int64_t)1 << 31) continue; // more than a card holds
+                        if (grawa_sublayer_create(&p, K, T, c.d, c.f, type, act) != GRAWA_OK) return 1;
+                        bool ok = grawa_dropout(K, T, c.d, type, &x, &x, 0.5f, rng, 0, &y, nullptr) == GRAWA_OK && grawa_dropout(K, T, c.d, type, &x, nullptr, 0.5f, rng, 0, &y, nullptr) == GRAWA_OK;
+                        ok = ok && grawa_layer_norm(p, T, &x, &w, &w, 0.f, &y, (float *)at, nullptr) == GRAWA_OK;
+                        ok = ok && grawa_layer_norm_backward(p, T, &x, &x, &w, (const float *)at, nullptr, &y, &w, &w, 0, nullptr) == GRAWA_OK;
+                        if (c.f) {
+                            ok = ok && grawa_ffn(p, T, &x, &m, &m, &m, nullptr, 0.f, nullptr, 0, &y, at, nullptr) == GRAWA_OK;
+                            ok = ok && grawa_ffn_backward(p, T, &x, &x, &m, &m, &m, at, &y, &m, &m, &m, 0, nullptr) == GRAWA_OK;
+                        }
+                        expect(ok, "a call's status");
+                        grawa_sublayer_destroy(p);
+                    }
+    for (const auto &n : names()) {
+        what = n.second;
+        expect(seen.count(n.second), "no call launches it");
+    }
+    expect(names().size() > 100, "kernels were looked at");
+    return 0;
+}
+
 int main(int n, char **args)
 {
     if (n != 2) return 2;
-    const int rc = !std::strcmp(args[1], "operands") ? operands() : !std::strcmp(args[1], "grids") ? grids() : 2;
+    const int rc = !std::strcmp(args[1], "operands") ? operands() : !std::strcmp(args[1], "grids") ? grids() : !std::strcmp(args[1], "reached") ? reached() : 2;
     if (rc || failures) {
         std::printf("%d failures\n", failures);
         return 1;

@@ -43,3 +43,8 @@ def test_products_read_their_matrices_by_their_own_pitch(driver):
 def test_every_launch_fits_a_grid(driver):
     """Up to the limits that the calls take, and what a card's memory holds: fewer than 2^32 threads along x, at most 65535 blocks along y and z."""
     run(driver, "grids")
+
+
+def test_every_kernel_is_launched_by_some_call(driver):
+    """No form of a kernel is built that no call comes to."""
+    run(driver, "reached")
