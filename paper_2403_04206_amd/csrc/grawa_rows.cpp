@@ -50,13 +50,18 @@ bool vector_of(PyObject *o, int64_t n, float *&p)
     return true;
 }
 
+bool holds(const at::Tensor &t, int64_t elements, int64_t size) // from the view's start on
+{
+    return (int64_t)(t.storage().nbytes() / (size_t)size) - t.storage_offset() >= elements;
+}
+
 // None, or a contiguous float32 tensor [K, L], with L = 0 [K].
 bool table_of(PyObject *o, int64_t K, int64_t L, float *&p)
 {
     p = nullptr;
     if (o == Py_None) return true;
     const at::Tensor *t = plain_tensor(o);
-    if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous() || t->dim() != (L ? 2 : 1) || t->size(0) != K || (L && t->size(1) != L))
+    if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous() || t->dim() != (L ? 2 : 1) || t->size(0) != K || (L && t->size(1) != L) || !holds(*t, t->numel(), 4))
         return false;
     p = static_cast<float *>(t->data_ptr());
     return true;
@@ -205,11 +210,6 @@ struct MatsArg { // grawa_mats_t
     int64_t worker;
 };
 
-bool holds(const at::Tensor &t, int64_t elements, int64_t size) // from the view's start on
-{
-    return (int64_t)(t.storage().nbytes() / (size_t)size) - t.storage_offset() >= elements;
-}
-
 at::ScalarType type_of(long long dt) { return dt ? at::kBFloat16 : at::kFloat; }
 
 // [K, T, d] with unit stride in the last axis.  The strides of what passes fit the storage, so no product overflows.
@@ -245,7 +245,8 @@ bool stats_of(PyObject *o, int64_t K, int64_t T, float *&p)
     p = nullptr;
     if (o == Py_None) return true;
     const at::Tensor *t = plain_tensor(o);
-    if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous() || t->dim() != 3 || t->size(0) != K || t->size(1) != T || t->size(2) != 2) return false;
+    if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous() || t->dim() != 3 || t->size(0) != K || t->size(1) != T || t->size(2) != 2 || !holds(*t, t->numel(), 4))
+        return false;
     p = static_cast<float *>(t->data_ptr());
     return true;
 }

@@ -240,6 +240,7 @@ def _table(t, shape, what: str):
         raise TypeError("%s must be a contiguous float32 CUDA tensor" % what)
     if tuple(t.shape) != tuple(shape):
         raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), tuple(shape)))
+    _covers(t, t.numel(), what)
     return C.c_void_p(t.data_ptr())
 
 
