@@ -528,10 +528,15 @@ template <int PLANES, int ACT> hipError_t forward(Sublayer c, GrawaRows x, Grawa
     const EpiGateUp<PLANES, ACT> inner{h, {save, s->K * blocks}, s->K * n * 2, n, blocks, (int)s->f, (int)s->fp, 0};
     const EpiStore<PLANES == 1, true> outer{y, residual, drop, (int)s->d, (int)c.T, 0, 0, GrawaMat{}, s->K};
     // Few tokens: see grawa_few.h.  To the end in float32, which tiles multiply six times: 4 workers, 1024 x 4096, 64 tokens 189 us, by tiles
-    // 240.  In bfloat16 up to 16, 67 us and 82 with one matrix of 4096 x 11264, and up to 32 while the matrices are small and the
-    // launches count: 38 us and 43 with four of 1024 x 4096, but 97 and 80 with the larger one.
+    // 240.  In bfloat16 up to 16 tokens, and up to 32 while no axis is long (one block then goes along it by itself) and the matrices are small.  us
+    // by k_few and by tiles, the matrices in no cache, K x (d x f).  16 tokens: 4 x (1024 x 4096) 25.6 and 35.2, 1 x (4096 x 11264) 61.3 and 58.1, 1 x (1024 x
+    // 16384) 45.3 and 40.8.  17 and 32 tokens: 1 x (4096 x 4096) 32.7, 36.9 and 36.1, 36.1; 4 x (1024 x 4096) 32.0, 37.8 and 36.5, 36.7; 4 x (2048 x
+    // 2048) 27.8, 31.9 and 36.0, 36.4; 256 x (256 x 256) 35.7, 39.7 and 32.3, 33.2; beyond: 8 x (1024 x 4096) 48.5, 56.3 and 50.4, 51.0; 1 x (1536
+    // x 6144) 34.9, 40.4 and 30.2, 29.8; 1 x (8192 x 1024) 33.4, 38.8 and 29.6, 29.6; 1 x (1024 x 16384) 66.7, 78.2 and 41.1, 41.3.  With the matrices
+    // in a cache tiles gain up to 8 us on these figures, k_few 2.
     constexpr bool BF16 = PLANES == 1;
-    if (c.T <= (!BF16 ? GRAWA_FEW : s->K * s->d * s->f <= (int64_t)1 << 25 ? 32 : 16)) {
+    const bool small = s->d <= 4096 && s->f <= 4096 && s->K * s->d * s->f <= (int64_t)1 << 24;
+    if (c.T <= (!BF16 ? GRAWA_FEW : small ? 32 : 16)) {
         constexpr int S = BF16 ? 2 : 4;
         GrawaFew g{(int)c.T, (int)s->f, (int)s->d, {wg.p, wg.worker * S}, {wu.p, wu.worker * S}, x.p, x.worker * S, x.row * S, 0};
         c.run([&] { return launch_few<BF16, true, false>(g, s->K, inner, c.st); });
