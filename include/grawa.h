@@ -321,7 +321,11 @@ grawa_status_t grawa_lgrawa_update_static(int K, int64_t P, int L, const int64_t
  * gradients are all float32 or all bfloat16.  Sums, statistics and the products'
  * accumulation are float32.  With bfloat16 the inner activations H, dG and dU are
  * rounded to bfloat16 once; with float32 the products are formed from exact
- * three-term bfloat16 splittings with an error of a float32 product's order.
+ * three-term bfloat16 splittings, of whose nine products the three smallest, at most
+ * 2^-24 of a product, are left out.  There (float32, any backward call and a forward
+ * call of more than 64 tokens) an infinity times a number with a term that is 0
+ * gives NaN: what an infinity reaches is not finite, but may be NaN where IEEE
+ * arithmetic has an infinity.  bfloat16 and few tokens follow IEEE arithmetic.
  * What passes from call to call has the plan's type as well.  Normalised tokens
  * rounded to bfloat16 move a gate by up to about 2^-8 of its size; relu, whose
  * derivative jumps at 0, then counts some gates near 0 on the other side, and the
@@ -335,7 +339,7 @@ grawa_status_t grawa_lgrawa_update_static(int K, int64_t P, int L, const int64_t
  * without gaps inside, `worker` elements apart (the views of a flat row).  Any
  * alignment to whole elements is accepted; matrices whose bases, strides and widths
  * are multiples of 16 bytes are read in place, others are copied to the plan's
- * workspace first.  Outputs must not overlap inputs except where a call says so.
+ * workspace first (Wg and Wu both where one has to be).  Outputs must not overlap inputs except where a call says so.
  *
  * Limits: 1 <= K <= GRAWA_MAX_WORKERS, 0 <= T, K T <= 2^30, 1 <= d < 2^20,
  * 0 <= f < 2^20; UNSUPPORTED beyond.  T = 0 is no error: gradients of parameters are
@@ -365,12 +369,21 @@ typedef struct grawa_sublayer grawa_sublayer_t; /* opaque */
  * workspace is allocated here, on the current device, and freed by
  * grawa_sublayer_destroy (the caller must have synchronised the streams that used
  * it; NULL is accepted).  Two calls on one plan must be ordered on one stream.
+ * With f > 0 it has room for copies of x, dy and the matrices, whether a call makes
+ * them or not (bfloat16 at 16-byte places needs none), for H, dG and dU and for split
+ * sums: 2 n K (2 T d' + 3 T f' + 2 f d' + d f') bytes and up to 128 MiB, with d' and f'
+ * the widths rounded up to 64, n = 1 for bfloat16 and 3 for float32.
  */
 grawa_status_t grawa_sublayer_create(grawa_sublayer_t **out, int K, int64_t T, int64_t d, int64_t f,
                                      grawa_dtype_t dtype, grawa_act_t act);
 grawa_status_t grawa_sublayer_destroy(grawa_sublayer_t *plan);
 
-/* Bytes of the buffer that grawa_ffn leaves to grawa_ffn_backward for T tokens (host pointer). */
+/*
+ * Bytes of the buffer that grawa_ffn leaves to grawa_ffn_backward for T tokens (host
+ * pointer): 8 (float32: 14) for each of K T f inner elements, T and f rounded up; with
+ * float32 and more than 64 tokens 6 more for each element of x and of the three
+ * matrices, so one and a half copies of the weights until the backward call.
+ */
 grawa_status_t grawa_sublayer_save_bytes(const grawa_sublayer_t *plan, int64_t T, int64_t *bytes);
 
 /*

@@ -71,8 +71,8 @@ template <bool BF16> __device__ __forceinline__ void few_mfma(grawa_f32x4 &c, co
     }
 }
 
-// Columns of a product that a wave takes, and steps that it has in flight twice: up to sixteen rows one fragment and 256 bytes of each row
-// of B; above, four fragments of B and 128 bytes.
+// Columns of a product that a wave takes, and steps that it has in flight twice: up to sixteen rows, and of two matrices, one fragment of each
+// matrix, else two; 256 bytes of each row up to 32 rows, 128 above.
 constexpr int few_columns(int mt, bool dual) { return mt == 1 || dual ? 16 : 32; }
 constexpr int few_chunk(int mt) { return mt <= 2 ? 4 : 2; }
 
@@ -81,7 +81,8 @@ __global__ __launch_bounds__(GRAWA_FEW_WAVES * 64, 1) void k_few(GrawaFew g, Epi
 {
     constexpr int S = BF16 ? 2 : 4, KS = 64 / S, CHUNK = few_chunk(MT); // k of a step, steps of a chunk
     constexpr int NF = few_columns(MT, DUAL) / 16, NB = DUAL ? 2 * NF : NF; // fragments of a product and of B a step
-    __shared__ __attribute__((aligned(16))) float sums[GRAWA_FEW_WAVES][MT * NB][256]; // 128 KiB at most
+    __shared__ __attribute__((aligned(16))) float sums[GRAWA_FEW_WAVES][MT * NB][256];
+    static_assert(MT * NB <= 8, "64 KiB at most");
     __shared__ __attribute__((aligned(16))) float corners[GRAWA_FEW_WAVES][Epi::OUTS * 256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, k = blockIdx.y;
     const int q = lane >> 4, n0 = blockIdx.x * (16 * NF);
