@@ -112,3 +112,28 @@ def test_activations_far_out(act, low, T):
         over = (got - want).abs() - (2.0 ** -8 + 2.0 ** -11) * want.abs() - slack
         i = over.argmax().item()
         assert over[i] <= 0, (what, z[i].item(), got[i].item(), want[i].item())
+
+
+@pytest.mark.parametrize("T", [30, 481])
+@pytest.mark.parametrize("act,low", [("gelu", -12.5), ("silu", -80.0)])
+def test_activations_far_out_in_float32(act, low, T):
+    """The same in float32, with numbers that are exact in one term: 2^-19 for the functions and the sums, and what roundings of the functions' arguments, 2^-24
+    each, come to: z^2 2^-23 (silu: |z| 2^-23) of each term."""
+    print("[case] tails in float32", act, T, flush=True)
+    z = torch.linspace(low, 12.5, T, device=DEV, dtype=torch.float64).to(BF).to(F)
+    x = torch.stack((z, torch.ones_like(z)), 1)
+    dy = torch.zeros_like(x)
+    dy[:, 0] = 1
+    y, dx, _, _, _ = forward_and_back(x, tensor([[1.0, 0.0]], F), tensor([[0.0, 1.0]], F), tensor([[1.0], [0.0]], F), dy, act)
+    z = z.double()
+    if act == "gelu":
+        first, second = 0.5 * torch.erfc(-z / 2 ** 0.5), z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+        share = 2.0 ** -19 + z * z * 2.0 ** -23
+    else:
+        first = torch.sigmoid(z)
+        second = z * first * torch.sigmoid(-z)
+        share = 2.0 ** -19 + z.abs() * 2.0 ** -23
+    for what, got, want, size in (("value", y[:, 0], z * first, (z * first).abs()), ("derivative", dx[:, 0], first + second, first + second.abs())):
+        over = (got - want).abs() - share * size
+        i = over.argmax().item()
+        assert over[i] <= 0, (what, z[i].item(), got[i].item(), want[i].item())
