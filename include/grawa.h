@@ -444,6 +444,128 @@ grawa_status_t grawa_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype, c
                              const grawa_rows_t *y, void *stream);
 
 /*
+ * The attention of a transformer block, forward and backward, for all K workers of a
+ * GPU in one call each: what stands beside the feed-forward sublayer.  As there, every
+ * worker's parameters are read from its row of a flat array and its gradients are
+ * written to its row of another.
+ *
+ *   head norm   y = rotate(x / sqrt(mean(x^2) + eps) * weight)   each head of q and of k
+ *   attention   o_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij)
+ *               s_ij = scale q_i . k_j + bias[bucket_of[p_i - j]]
+ *
+ * Positions.  Each of a worker's N sequences has Sq new tokens (queries) and room for
+ * Sk tokens (keys and values).  Query i stands at position p_i = start + i, key j at
+ * position j.  It sees the keys j <= p_i with p_i - j < window or j < sinks: a window
+ * that ends at itself, and first tokens that stay visible.  A sequence has `length`
+ * tokens; keys from there on are not read, and queries at positions from there on, or
+ * below 0, see nothing.  Training and prompts: Sq = Sk, start 0, shorter sequences
+ * padded behind.  Single tokens and chunks over a cache: start = length - Sq.
+ * A row that sees nothing, or whose visible scores are all -infinity, gives 0 and passes no
+ * gradient on.  What a row does not see does not reach it, infinities and NaN included.
+ *
+ * Types.  One type a plan, as in the sublayer.  Scores, softmax statistics, sums and
+ * angles are float32 (angles are reduced in 64 bits).  With bfloat16 exp(s_ij - max)
+ * and the gradient of s_ij are rounded to bfloat16 once, as the matrix instructions
+ * take them, and the gradients use o as rounded; with float32 products are float32.
+ *
+ * Layouts.  grawa_heads_t is K x N x S x heads rows of D elements: worker k's sequence
+ * n, token s, head h starts at data + k * worker + n * sequence + s * token + h * head
+ * elements; elements of a row are adjacent.  Strides of inputs are not negative (0
+ * shares); rows of outputs must not overlap.  For the attention every row has to start
+ * at a multiple of 16 bytes (ALIGNMENT otherwise), and the strides of tokens are below
+ * 2^24 bytes; the head norm takes any alignment to whole elements.  H / G heads of
+ * queries, one after the other, share a head of keys and values.
+ *
+ * Limits: 1 <= K <= GRAWA_MAX_WORKERS, K N H <= 2^20, K N H S <= 2^30, S <= 2^28, D a multiple of 8
+ * up to 128, H a multiple of G, at most GRAWA_MAX_DISTANCES distances and
+ * GRAWA_MAX_BUCKETS buckets; UNSUPPORTED beyond.  N = 0 and tokens = 0 are no errors.
+ */
+#define GRAWA_MAX_DISTANCES 1024
+#define GRAWA_MAX_BUCKETS 256
+
+typedef struct {
+    int K;                    /* workers */
+    int64_t sequences, length; /* most sequences of a worker, most tokens of one */
+    int heads, kv_heads, width; /* H, G, D */
+    grawa_dtype_t dtype;
+    float scale;              /* > 0; of q . k */
+    int64_t window;           /* tokens that a query sees up to itself; 0: all before it */
+    int64_t sinks;            /* first tokens that stay visible */
+    int rotary;               /* elements of a head that are turned, even; 0: none */
+    int interleaved;          /* pairs are (2 e, 2 e + 1), else (e, e + rotary / 2) */
+    const double *frequencies; /* [rotary / 2], radians a position (host) */
+    int buckets;              /* entries of a head's bias; 0: no bias */
+    int64_t distances;        /* entries of bucket_of */
+    const int32_t *bucket_of; /* [distances] (host); longer distances are in the last one's */
+} grawa_attention_shape_t;
+
+typedef struct {
+    void *data;
+    int64_t worker, sequence, token, head; /* strides in elements */
+} grawa_heads_t;
+
+typedef struct grawa_attention_plan grawa_attention_plan_t; /* opaque */
+
+/*
+ * Shape, tables and device workspace of the calls below; the workspace is allocated
+ * here, on the current device.  The rules for grawa_sublayer_create hold: two calls on
+ * one plan must be ordered on one stream (graphs captured from them too), and destroy
+ * wants the streams synchronised.  It has 8 K N H S bytes, S rounded up to 256, room for the
+ * sums of the parameters' gradients, and up to 64 MiB for blocks that share a sum.
+ */
+grawa_status_t grawa_attention_create(grawa_attention_plan_t **out, const grawa_attention_shape_t *shape);
+grawa_status_t grawa_attention_destroy(grawa_attention_plan_t *plan);
+
+/*
+ * Norm and rotation of N sequences of S tokens.  qweight, kweight: vectors of D for
+ * each worker, shared by its heads.  starts: device int32 [K][N], position of each
+ * sequence's first token, or NULL for 0; any value.  q_out may be q and k_out k.
+ */
+grawa_status_t grawa_head_norm(grawa_attention_plan_t *plan, int64_t N, int64_t S, const grawa_heads_t *q,
+                               const grawa_heads_t *k, const grawa_mats_t *qweight,
+                               const grawa_mats_t *kweight, float eps, const int32_t *starts,
+                               const grawa_heads_t *q_out, const grawa_heads_t *k_out, void *stream);
+
+/*
+ * Its backward pass from the gradients of q_out and k_out; q and k are what the forward call was
+ * given.  dq may be dq_out and dk dk_out.  accumulate != 0 adds to dqweight and dkweight.
+ */
+grawa_status_t grawa_head_norm_backward(grawa_attention_plan_t *plan, int64_t N, int64_t S,
+                                        const grawa_heads_t *dq_out, const grawa_heads_t *dk_out,
+                                        const grawa_heads_t *q, const grawa_heads_t *k,
+                                        const grawa_mats_t *qweight, const grawa_mats_t *kweight, float eps,
+                                        const int32_t *starts, const grawa_heads_t *dq,
+                                        const grawa_heads_t *dk, const grawa_mats_t *dqweight,
+                                        const grawa_mats_t *dkweight, int accumulate, void *stream);
+
+/*
+ * Attention of N sequences, Sq queries and room for Sk keys each, both up to the plan's
+ * length.  bias: [H][buckets] for each worker; NULL if and only if the plan has no
+ * buckets.  lengths, starts: device int32 [K][N] or NULL for Sk and Sk - Sq; lengths
+ * outside 0 ... Sk count as the nearer of the two.  lse: float32 [K][N][H][Sq], the
+ * logarithms of the sums of exponentials for the backward pass (-infinity for a row
+ * that sees nothing), or NULL.  o must not overlap an input.
+ */
+grawa_status_t grawa_attention(grawa_attention_plan_t *plan, int64_t N, int64_t Sq, int64_t Sk,
+                               const grawa_heads_t *q, const grawa_heads_t *k, const grawa_heads_t *v,
+                               const grawa_mats_t *bias, const int32_t *lengths, const int32_t *starts,
+                               const grawa_heads_t *o, float *lse, void *stream);
+
+/*
+ * Its gradients: dq, dk, dv, and dbias where the plan has buckets.  Inputs, o and lse
+ * are those of the forward call.  Padding gets 0.  accumulate != 0 adds to dbias instead
+ * of replacing it.  Sums are formed in a fixed order.
+ */
+grawa_status_t grawa_attention_backward(grawa_attention_plan_t *plan, int64_t N, int64_t Sq, int64_t Sk,
+                                        const grawa_heads_t *d_o, const grawa_heads_t *q,
+                                        const grawa_heads_t *k, const grawa_heads_t *v,
+                                        const grawa_mats_t *bias, const int32_t *lengths,
+                                        const int32_t *starts, const grawa_heads_t *o, const float *lse,
+                                        const grawa_heads_t *dq, const grawa_heads_t *dk,
+                                        const grawa_heads_t *dv, const grawa_mats_t *dbias,
+                                        int accumulate, void *stream);
+
+/*
  * Measurement aids (not part of the method).
  *
  * grawa_plan_profile: with enable != 0 the plan attaches a start and a stop

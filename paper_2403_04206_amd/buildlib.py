@@ -16,10 +16,12 @@ ROWS = os.path.join(PKG, "_rows.so")
 ROWS_SOURCE = os.path.join(CSRC, "grawa_rows.cpp")
 SOURCES = [os.path.join(CSRC, n) for n in ("grawa_api.cpp", "grawa_maps.cpp", "grawa_norms.hip", "grawa_pull.hip",
                                             "grawa_local.hip", "grawa_static.hip", "grawa_sublayer.cpp", "grawa_layernorm.hip",
-                                            "grawa_dropout.hip", "grawa_ffn.hip")]
+                                            "grawa_dropout.hip", "grawa_ffn.hip", "grawa_attention.cpp", "grawa_heads.hip", "grawa_attend.hip",
+                                            "grawa_attend_back.hip")]
 HEADERS = [os.path.join(CSRC, "grawa_internal.h"), os.path.join(CSRC, "grawa_device.h"), os.path.join(CSRC, "grawa_scores.h"), os.path.join(CSRC, "grawa_fold.h"),
            os.path.join(CSRC, "grawa_maps.h"), os.path.join(CSRC, "grawa_route.h"), os.path.join(CSRC, "grawa_offsets.h"),
            os.path.join(CSRC, "grawa_sublayer.h"), os.path.join(CSRC, "grawa_philox.h"), os.path.join(CSRC, "grawa_elements.h"), os.path.join(CSRC, "grawa_gemm.h"), os.path.join(CSRC, "grawa_few.h"),
+           os.path.join(CSRC, "grawa_attention.h"), os.path.join(CSRC, "grawa_attend.h"),
            os.path.join(ROOT, "include", "grawa.h")]
 
 # Packed fp32 instructions are switched off for all device code (a hipcc flag, not a host one;

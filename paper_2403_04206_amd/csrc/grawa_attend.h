@@ -1,0 +1,243 @@
+// Tiles of heads in LDS and their fragments for the matrix instructions of 32 x 32, in bfloat16 or float32 (device side of the attention).
+//
+// A tile is ROWS tokens (keys or queries) of one head, DP elements each, zeros where the head has fewer elements or the sequence no
+// more tokens.  It goes from memory straight into LDS, 16 bytes a lane, bounded by its buffer descriptor.  The 16-byte piece c of row r
+// stands at place c ^ key(r), key(r) = 2 (r % 4) + r / 4 % 2: the eight rows that a fragment by rows is read from at a time fall on
+// different banks, and so do the four rows of the transposing load, each by two neighbouring pieces.
+//
+// A fragment is 32 x 16: the lane has line lane % 32 and eight k of it.  By rows those are k = 8 (lane / 32) + j.  By columns the lines
+// are elements of the head and k runs over tokens in the order in which a product's sums stand in registers: for sums of 32 x 32 the
+// lane has column lane % 32 and rows j % 4 + 8 (j / 4) + 4 (lane / 32) in register j, so registers 8 t ... 8 t + 7 are, without any
+// exchange, the second operand of a product over tokens 16 t + 4 (lane / 32) + j % 4 + 8 (j / 4).
+// float32 goes through the same fragments by eight instructions of 32 x 32 x 2, each of which takes register j of both halves.
+#pragma once
+#include "grawa_attention.h"
+#include "grawa_elements.h"
+
+typedef float grawa_f32x16 __attribute__((ext_vector_type(16)));
+typedef float grawa_f32x8 __attribute__((ext_vector_type(8)));
+typedef float grawa_f32x4v __attribute__((ext_vector_type(4)));
+typedef short grawa_s16x4v __attribute__((ext_vector_type(4)));
+typedef short grawa_s16x8v __attribute__((ext_vector_type(8)));
+
+#define GRAWA_LDS_AT __attribute__((address_space(3)))
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+template <bool BF16> struct Frag;
+template <> struct Frag<true> {
+    typedef grawa_bf16x8 V;
+};
+template <> struct Frag<false> {
+    typedef grawa_f32x8 V;
+};
+
+#ifdef __HIP_DEVICE_COMPILE__
+__device__ __forceinline__ grawa_f32x16 mfma(const grawa_bf16x8 &a, const grawa_bf16x8 &b, const grawa_f32x16 &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ grawa_f32x16 mfma(const grawa_f32x8 &a, const grawa_f32x8 &b, grawa_f32x16 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// Registers 8 t ... 8 t + 7 of sums as an operand.
+__device__ __forceinline__ void as_operand(const grawa_f32x16 &s, int t, grawa_bf16x8 &f)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = (__bf16)s[8 * t + j];
+}
+__device__ __forceinline__ void as_operand(const grawa_f32x16 &s, int t, grawa_f32x8 &f)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = s[8 * t + j];
+}
+
+// What the other half of the wave has.
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
+    typedef typename Frag<BF16>::V V;
+    static constexpr int ES = BF16 ? 2 : 4, RB = DP * ES, PPR = RB / 16, BYTES = ROWS * RB, LOADS = BYTES / 1024 / NW;
+    static constexpr bool TURN = NW * 64 / PPR == 4; // a wave's loads are four rows apart: every other one has the other half of the keys
+    static_assert(LOADS * NW * 1024 == BYTES && (TURN || NW * 64 / PPR % 8 == 0), "whole loads of whole groups of rows");
+
+    static __device__ __forceinline__ int key(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+
+    // Loads: the lane's offset in the wave's first one (two where they take turns), and from one to the next.
+    uint32_t first, odd, step;
+    __device__ __forceinline__ void init(int wave, int lane, uint32_t token, int D)
+    {
+        const int id = wave * 64 + lane, row = id / PPR, c = (id % PPR) ^ key(row), c4 = (id % PPR) ^ key(row + 4);
+        first = c * 16 < D * ES ? (uint32_t)row * token + (uint32_t)c * 16 : 0x80000000u;
+        odd = !TURN ? 0 : c4 * 16 < D * ES ? (uint32_t)(row + 4) * token + (uint32_t)c4 * 16 : 0x80000000u;
+        step = (TURN ? 8 : NW * 64 / PPR) * token;
+    }
+    // rows: what the sequence has from the tile's first token on; none: nothing is read and all comes as zeros.
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const char *p, int rows, uint32_t token, int D)
+    {
+        const int n = rows < ROWS ? rows : ROWS;
+        return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, n > 0 ? (uint32_t)(n - 1) * token + (uint32_t)(D * ES) : 0, 0x00020000);
+    }
+    __device__ __forceinline__ void load(char *lds, int wave, __amdgpu_buffer_rsrc_t r) const
+    {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS_AT void *)(lds + (wave + NW * i) * 1024), 16,
+                                                     TURN && i % 2 ? odd + (uint32_t)(i / 2) * step : first + (uint32_t)(TURN ? i / 2 : i) * step, 0, 0, 0);
+    }
+
+    // Lines row0 ... row0 + 31 (a multiple of 32), elements 16 ks ... of the head.
+    static __device__ __forceinline__ V by_rows(const char *lds, int lane, int row0, int ks)
+    {
+        const int row = lane & 31, half = lane >> 5;
+        const char *p = lds + (row0 + row) * RB;
+        if constexpr (BF16) {
+            return *(const V *)(p + (((2 * ks + half) ^ key(row)) << 4));
+        } else {
+            const grawa_f32x4v a = *(const grawa_f32x4v *)(p + (((4 * ks + 2 * half) ^ key(row)) << 4));
+            const grawa_f32x4v b = *(const grawa_f32x4v *)(p + (((4 * ks + 2 * half + 1) ^ key(row)) << 4));
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    // Lines: elements 32 dt ... of the head, k: tokens row0 ... row0 + 15 (a multiple of 16) in the order of a product's registers.
+    static __device__ __forceinline__ V by_columns(const char *lds, int lane, int row0, int dt)
+    {
+        if constexpr (BF16) {
+            const int s = lane & 15, half = lane >> 5, row = 4 * half + (s >> 2);
+            const char *p = lds + (row0 + row) * RB + (((4 * dt + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1)) ^ key(row)) << 4) + (s & 1) * 8;
+            const grawa_s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)p);
+            const grawa_s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)(p + 8 * RB));
+            return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int m = lane & 31, half = lane >> 5;
+            V v;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int row = 4 * half + (j & 3) + 8 * (j >> 2);
+                v[j] = *(const float *)(lds + (row0 + row) * RB + (((8 * dt + (m >> 2)) ^ key(row)) << 4) + (m & 3) * 4);
+            }
+            return v;
+        }
+    }
+};
+
+// All loads into LDS have landed and all reads from it are done, the wave's own and then the other waves'.
+__device__ __forceinline__ void landed()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// What the wave's lanes have written to LDS, its other lanes read from here on.
+__device__ __forceinline__ void wave_order()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Takes what is not finite out of an operand and marks it: 1 where it was plus (minus) infinity, both where it was no number.
+template <class V> __device__ __forceinline__ void take_out(V &v, V &plus, V &minus, bool signs)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float f = (float)v[j];
+        const bool odd = !(fabsf(f) < __builtin_inff());
+        plus[j] = odd && !(signs && f < 0.f) ? 1.f : 0.f;
+        minus[j] = odd && !(signs && f > 0.f) ? 1.f : 0.f;
+        v[j] = odd ? 0.f : f;
+    }
+}
+
+// sums += a w for a tile of which only some pairs count: a pair that does not count has w = 0, but an infinity or no number in its line
+// of a must not reach the sum.  `counts` has 1 for pairs that count.  signs: an infinity keeps its sign (else all become no number).
+template <class V> __device__ __forceinline__ void product_of_some(grawa_f32x16 &sums, V a, const V &w, const V &counts, bool signs)
+{
+    V plus, minus;
+    take_out(a, plus, minus, signs);
+    sums = mfma(a, w, sums);
+    __builtin_amdgcn_sched_barrier(0); // one at a time: this is not where speed counts, and registers are few
+    const grawa_f32x16 p = mfma(plus, counts, grawa_f32x16{});
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sums[j] += p[j] > 0.f ? __builtin_inff() : 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+    const grawa_f32x16 m = mfma(minus, counts, grawa_f32x16{});
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sums[j] -= m[j] > 0.f ? __builtin_inff() : 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <bool B> struct Is {
+    static constexpr bool value = B;
+};
+
+__device__ __forceinline__ int clamp_int(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// Which tokens a sequence has and where its new ones begin; whatever the caller's numbers are, positions stay far from 32 bits.
+struct Place {
+    int start, length;
+};
+__device__ __forceinline__ Place place_of(const GrawaAttend &a, int kn)
+{
+    Place p;
+    p.start = a.starts ? clamp_int(a.starts[kn], -(1 << 29), 1 << 29) : a.Sk - a.Sq;
+    p.length = a.lengths ? clamp_int(a.lengths[kn], 0, a.Sk) : a.Sk;
+    return p;
+}
+
+// One column of queries: its 32 x 16 fragments straight from memory, zeros where there is nothing.
+template <bool BF16> __device__ __forceinline__ typename Frag<BF16>::V load_line(const char *row, int e, int D, bool there)
+{
+    typedef typename Frag<BF16>::V V;
+    V v = {};
+    if (there && e < D) {
+        if constexpr (BF16) {
+            v = *(const V *)(row + e * 2);
+        } else {
+            const grawa_f32x4v a = *(const grawa_f32x4v *)(row + e * 4), b = *(const grawa_f32x4v *)(row + e * 4 + 16);
+            v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    return v;
+}
+
+// Sixteen sums of a column, elements 32 dt + 8 q + 4 (lane / 32) ... of the head, to memory.
+template <bool BF16> __device__ __forceinline__ void store_column(char *row, int lane, int dt, int D, const grawa_f32x16 &s, float f)
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int e = 32 * dt + 8 * q + 4 * (lane >> 5);
+        if (e >= D) continue;
+        if constexpr (BF16) {
+            typedef __bf16 B4 __attribute__((ext_vector_type(4)));
+            B4 b;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = (__bf16)(s[4 * q + j] * f);
+            *(B4 *)(row + e * 2) = b;
+        } else {
+            grawa_f32x4v b;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = s[4 * q + j] * f;
+            *(grawa_f32x4v *)(row + e * 4) = b;
+        }
+    }
+}
+
+// Blocks go round the eight XCDs; each gets a run of consecutive numbers, so that blocks that read the same keys share its L2.
+__device__ __forceinline__ uint32_t run_of(uint32_t id, uint32_t total)
+{
+    const uint32_t q = total / 8, r = total % 8, xcd = id % 8;
+    return xcd * q + (xcd < r ? xcd : r) + id / 8;
+}
+#endif // __HIP_DEVICE_COMPILE__
+
+} // namespace

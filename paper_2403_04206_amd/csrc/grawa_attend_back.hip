@@ -1,0 +1,465 @@
+// Gradients of the attention of grawa_attend.hip:
+//   P_ij = exp(s_ij - lse_i), dP = do v^T, delta_i = do_i . o_i, dS = P (dP - delta)
+//   dq = scale dS k,  dk = scale dS^T q,  dv = P^T do,  dbias[b] = sum of dS over the pairs whose distance is in bucket b
+// Two kernels form P and dS tile by tile, one for blocks of queries (dq, dbias, delta), one for blocks of keys (dk and dv of all heads
+// that share them): nothing is added up in an order that depends on timing.
+#include "grawa_attend.h"
+
+namespace {
+
+// A block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.
+template <bool BF16, int DP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_attend_dq(GrawaAttend a)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int BK = 64, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
+    typedef HeadTile<BF16, DP, BK, 4> Tile;
+    typedef typename Tile::V V;
+    __shared__ __attribute__((aligned(1024))) char lds[BUFS * 2 * Tile::BYTES]; // keys and values
+    __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];              // the bias by distance
+    __shared__ float by_distance[BIAS ? 4 : 1][BIAS ? GRAWA_MAX_DISTANCES : 1]; // of each wave: sums of dS
+    __shared__ float square[BIAS ? 4 : 1][BIAS ? 32 * 33 : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int t = (int)run_of(blockIdx.x, gridDim.x), hd = t / a.blocks, qb = a.blocks - 1 - (t - hd * a.blocks);
+    const int kn = hd / a.H, head = hd - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
+    const Place at = place_of(a, kn);
+    const int i = qb * 128 + wave * 32 + (lane & 31), pos = at.start + i;
+    const bool there = i < a.Sq, counts = there && pos >= 0 && pos < at.length;
+    const int64_t row = ((int64_t)kn * a.H + head) * a.Sq + i, row2 = ((int64_t)kn * a.H + head) * a.row_pitch + i;
+
+    V q[KS], go[KS];
+    float delta = 0.f;
+    {
+        const char *pq = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i * a.q.token + (int64_t)head * a.q.head;
+        const char *pg = a.go.p + (int64_t)k * a.go.worker + (int64_t)n * a.go.seq + (int64_t)i * a.go.token + (int64_t)head * a.go.head;
+        const char *po = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i * a.o.token + (int64_t)head * a.o.head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            q[ks] = load_line<BF16>(pq, 16 * ks + 8 * half, a.D, counts);
+            go[ks] = load_line<BF16>(pg, 16 * ks + 8 * half, a.D, counts);
+            const V o = load_line<BF16>(po, 16 * ks + 8 * half, a.D, counts);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) delta += (float)o[j] * (float)go[ks][j];
+        }
+        delta += other_half(delta);
+    }
+    float lse = counts ? a.lse[row] * LOG2E : __builtin_inff();
+    if (lse == -__builtin_inff()) lse = __builtin_inff(); // the row sees nothing
+    if (half == 0 && i < a.row_pitch) a.row_lse[row2] = lse, a.row_dot[row2] = delta;
+
+    const float c2 = a.scale * LOG2E;
+    float far = 0.f;
+    if constexpr (BIAS) {
+        const char *bias = a.bias.p + (int64_t)k * a.bias.worker * ES + (int64_t)head * a.buckets * ES;
+        far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
+        for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
+    }
+
+    const int p0 = at.start + qb * 128, p1 = at.start + min((qb + 1) * 128, a.Sq) - 1, w0 = p0 + wave * 32, w1 = w0 + 31;
+    const int end = min(p1, at.length - 1) + 1, begin = max(0, max(p0, 0) - a.window + 1);
+    const bool any = p1 >= 0 && p0 < at.length;
+    const int t0 = begin / BK, first_tiles = any ? min(t0, (min(a.sinks, end) + BK - 1) / BK) : 0, tiles = any ? first_tiles + (end + BK - 1) / BK - t0 : 0;
+    const char *kp = a.k.p + (int64_t)k * a.k.worker + (int64_t)n * a.k.seq + (int64_t)g * a.k.head;
+    const char *vp = a.v.p + (int64_t)k * a.v.worker + (int64_t)n * a.v.seq + (int64_t)g * a.v.head;
+    Tile lk, lv;
+    lk.init(wave, lane, (uint32_t)a.k.token, a.D);
+    lv.init(wave, lane, (uint32_t)a.v.token, a.D);
+    const auto load = [&](int it, char *buf) {
+        const int j0 = (it < first_tiles ? it : it - first_tiles + t0) * BK;
+        lk.load(buf, wave, Tile::rsrc(kp + (int64_t)j0 * a.k.token, at.length - j0, (uint32_t)a.k.token, a.D));
+        lv.load(buf + Tile::BYTES, wave, Tile::rsrc(vp + (int64_t)j0 * a.v.token, at.length - j0, (uint32_t)a.v.token, a.D));
+    };
+
+    grawa_f32x16 dq[DT];
+    float far_sum = 0.f; // of dS from the last distance of the table on
+    const auto run = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
+        if constexpr (BIAS) {
+            far_sum = 0.f;
+            for (int d = lane; d < a.distances; d += 64) by_distance[wave][d] = 0.f;
+        }
+        if (BUFS == 2 && tiles) load(0, lds);
+        for (int it = 0; it < tiles; ++it) {
+            char *buf = lds + (BUFS == 2 ? it & 1 : 0) * 2 * Tile::BYTES;
+            if (BUFS == 1) {
+                landed();
+                load(it, buf);
+            }
+            landed();
+            if (BUFS == 2 && it + 1 < tiles) load(it + 1, lds + ((it + 1) & 1) * 2 * Tile::BYTES);
+            const int tile0 = (it < first_tiles ? it : it - first_tiles + t0) * BK;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int j0 = tile0 + 32 * u, j1 = j0 + 31;
+                if (j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks)) continue;
+                const bool all = j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks);
+                grawa_f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), q[ks], s);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), go[ks], dp);
+                const bool is_far = BIAS && w0 - j1 >= a.distances - 1;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float b = 0.f;
+                    if constexpr (BIAS) b = is_far ? far : table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
+                    s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, b - lse)) * (dp[r] - delta);
+                }
+                if (!all)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + (r & 3) + 8 * (r >> 2) + 4 * half, d = pos - j;
+                        s[r] = d >= 0 && (d < a.window || j < a.sinks) ? s[r] : 0.f;
+                    }
+                if constexpr (BIAS) {
+                    if (is_far) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) far_sum += s[r];
+                    } else { // along the diagonals of the square: lane x has those that are x - 31 above the first
+                        float *sq = square[wave];
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sq[((r & 3) + 8 * (r >> 2) + 4 * half) * 33 + (lane & 31)] = s[r];
+                        wave_order();
+                        float sum = 0.f;
+                        const int x = lane - 31;
+                        for (int r = 0; r < 32; ++r)
+                            if (r + x >= 0 && r + x < 32) sum += sq[r * 33 + r + x];
+                        const int d = w0 - j0 + x;
+                        if (d >= a.distances - 1)
+                            far_sum += sum;
+                        else if (d >= 0 && lane < 63)
+                            by_distance[wave][d] += sum;
+                        wave_order();
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    V w;
+                    as_operand(s, h, w);
+                    if (careful.value && !all) {
+                        V seen;
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            const int j = j0 + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, d = pos - j;
+                            seen[r] = d >= 0 && (d < a.window || j < a.sinks) ? 1.f : 0.f;
+                        }
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) product_of_some(dq[d], Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, seen, false);
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) dq[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, dq[d]);
+                    }
+                }
+            }
+        }
+        bool odd = false;
+        if (!careful.value && counts)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) odd |= dq[d][r] != dq[d][r];
+        return __syncthreads_or(odd);
+    };
+    // What is no number may come from a token that the query does not see: once more, with care.
+    if (__builtin_expect(run(Is<false>()), 0)) run(Is<true>());
+
+    if (there) {
+        char *out = a.dq.p + (int64_t)k * a.dq.worker + (int64_t)n * a.dq.seq + (int64_t)i * a.dq.token + (int64_t)head * a.dq.head;
+        if (!counts)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
+#pragma unroll
+        for (int d = 0; d < DT; ++d) store_column<BF16>(out, lane, d, a.D, dq[d], a.scale);
+    }
+    if constexpr (BIAS) {
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) far_sum += __shfl_xor(far_sum, m, 64);
+        if (lane == 0) by_distance[wave][a.distances - 1] = far_sum;
+        __syncthreads();
+        for (int b = threadIdx.x; b < a.buckets; b += 256) {
+            float sum = 0.f;
+            for (int d = 0; d < a.distances; ++d)
+                if (a.bucket_of[d] == b) sum += (by_distance[0][d] + by_distance[1][d]) + (by_distance[2][d] + by_distance[3][d]);
+            a.bias_part[(((int64_t)kn * a.H + head) * a.blocks + qb) * a.buckets + b] = sum;
+        }
+    }
+#endif
+}
+
+// dbias of a head: the sums of its blocks, in order.
+template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums(GrawaAttend a)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    const int head = blockIdx.x, k = blockIdx.y, b = threadIdx.x;
+    if (b >= a.buckets) return;
+    float sum = 0.f;
+    for (int n = 0; n < a.N; ++n) {
+        const float *p = a.bias_part + ((int64_t)(k * a.N + n) * a.H + head) * a.blocks * a.buckets + b;
+        for (int i = 0; i < a.blocks; ++i) sum += p[(int64_t)i * a.buckets];
+    }
+    char *out = a.dbias.p + ((int64_t)k * a.dbias.worker + (int64_t)head * a.buckets + b) * (BF16 ? 2 : 4);
+    store_one<BF16>(out, a.accumulate ? load_one<BF16>(out) + sum : sum);
+#endif
+}
+
+// A block has 128 keys, a wave 32 of them; all waves share tiles of 64 queries and the gradients of their outputs, of one head after
+// the other.  splits > 1 (sink_splits for the keys that all queries see): that many blocks share the queries of a block of keys.
+template <bool BF16, int DP, bool BIAS>
+__global__ __launch_bounds__(256, BF16 && DP == 64 ? 2 : 1) void k_attend_dkv(GrawaAttend a)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int BQ = 64, BKV = 128, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
+    typedef HeadTile<BF16, DP, BQ, 4> Tile;
+    typedef typename Tile::V V;
+    __shared__ __attribute__((aligned(1024))) char lds[BUFS * 2 * Tile::BYTES]; // queries and gradients of outputs
+    __shared__ __attribute__((aligned(1024))) float of_rows[2][2][BQ];          // log2 of the sums of exponentials, do . o
+    __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int per = a.sink_blocks * a.sink_splits + (a.key_blocks - a.sink_blocks) * a.splits;
+    const int t = (int)run_of(blockIdx.x, gridDim.x), hd = t / per, item = t - hd * per, sink_items = a.sink_blocks * a.sink_splits;
+    const bool sink = item < sink_items;
+    const int splits = sink ? a.sink_splits : a.splits, kb = sink ? item / a.sink_splits : a.sink_blocks + (item - sink_items) / a.splits;
+    const int split = sink ? item % a.sink_splits : (item - sink_items) % a.splits;
+    const int kn = hd / a.G, g = hd - kn * a.G, k = kn / a.N, n = kn - k * a.N;
+    const Place at = place_of(a, kn);
+    const int b0 = kb * BKV, w0 = b0 + wave * 32, w1 = w0 + 31, j = w0 + (lane & 31);
+    const bool there = j < a.Sk, counts = j < at.length;
+
+    V kf[KS], vf[KS];
+    {
+        const char *pk = a.k.p + (int64_t)k * a.k.worker + (int64_t)n * a.k.seq + (int64_t)j * a.k.token + (int64_t)g * a.k.head;
+        const char *pv = a.v.p + (int64_t)k * a.v.worker + (int64_t)n * a.v.seq + (int64_t)j * a.v.token + (int64_t)g * a.v.head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            kf[ks] = load_line<BF16>(pk, 16 * ks + 8 * half, a.D, counts);
+            vf[ks] = load_line<BF16>(pv, 16 * ks + 8 * half, a.D, counts);
+        }
+    }
+    const float c2 = a.scale * LOG2E;
+
+    // Queries that see any of the block's keys: rows i0 ... i1 of the call, by tiles, of each head.
+    const int last = min(at.length - 1 - at.start, a.Sq - 1);
+    const int i0 = max(0, max(b0, 0) - at.start), i1 = sink ? last : min(last, b0 + BKV - 1 + a.window - 1 - at.start);
+    const int t0 = i0 / BQ, tiles = b0 < at.length && i1 >= i0 ? i1 / BQ - t0 + 1 : 0, all_tiles = tiles * a.share;
+    const int from = (int)((int64_t)all_tiles * split / splits), to = (int)((int64_t)all_tiles * (split + 1) / splits);
+    Tile lq, lg;
+    lq.init(wave, lane, (uint32_t)a.q.token, a.D);
+    lg.init(wave, lane, (uint32_t)a.go.token, a.D);
+    const auto load = [&](int it, int buf) {
+        const int h = it / tiles, head = g * a.share + h, i = (t0 + it - h * tiles) * BQ;
+        char *to_lds = lds + (BUFS == 2 ? buf : 0) * 2 * Tile::BYTES;
+        const char *pq = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i * a.q.token + (int64_t)head * a.q.head;
+        const char *pg = a.go.p + (int64_t)k * a.go.worker + (int64_t)n * a.go.seq + (int64_t)i * a.go.token + (int64_t)head * a.go.head;
+        lq.load(to_lds, wave, Tile::rsrc(pq, last + 1 - i, (uint32_t)a.q.token, a.D));
+        lg.load(to_lds + Tile::BYTES, wave, Tile::rsrc(pg, last + 1 - i, (uint32_t)a.go.token, a.D));
+        if (wave < 2) { // rows up to the pitch, a multiple of a tile, are there
+            const float *p = (wave ? a.row_dot : a.row_lse) + ((int64_t)kn * a.H + head) * a.row_pitch + i;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, BQ * 4, 0x00020000),
+                                                     (GRAWA_LDS_AT void *)of_rows[buf][wave], 4, (uint32_t)lane * 4, 0, 0, 0);
+        }
+    };
+
+    grawa_f32x16 dk[DT], dv[DT];
+    const auto run = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dk[d] = dv[d] = grawa_f32x16{};
+        int table_of = -1;
+        if (BUFS == 2 && from < to) load(from, 0);
+        for (int it = from; it < to; ++it) {
+            const int b = BUFS == 2 ? (it - from) & 1 : 0, h = it / tiles, tile0 = (t0 + it - h * tiles) * BQ;
+            const char *buf = lds + b * 2 * Tile::BYTES;
+            if (BUFS == 1) {
+                landed();
+                load(it, 0);
+            }
+            landed();
+            if (BUFS == 2 && it + 1 < to) load(it + 1, b ^ 1);
+            if constexpr (BIAS)
+                if (h != table_of) { // the other waves are behind their last look at the table of the head before
+                    const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + (int64_t)(g * a.share + h) * a.buckets) * ES;
+                    for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
+                    table_of = h;
+                    __syncthreads();
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int p0 = at.start + tile0 + 32 * u, p1 = p0 + 31; // positions of the queries
+                if (w0 > p1 || w0 >= at.length || (w1 <= p0 - a.window && w0 >= a.sinks)) continue;
+                const bool all = w1 <= p0 && (p1 - w0 < a.window || w1 < a.sinks);
+                grawa_f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), kf[ks], s);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), vf[ks], dp);
+                const bool is_far = BIAS && p0 - w1 >= a.distances - 1;
+                V pw[2], dw[2];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int x = (r & 3) + 8 * (r >> 2) + 4 * half, d = p0 + x - j;
+                    float bias = 0.f;
+                    if constexpr (BIAS) bias = is_far ? table[a.distances - 1] : table[clamp_int(d, 0, a.distances - 1)];
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, bias - of_rows[b][0][32 * u + x]));
+                    dp[r] = p * (dp[r] - of_rows[b][1][32 * u + x]);
+                    s[r] = p;
+                    if (!all) {
+                        const bool seen = d >= 0 && (d < a.window || j < a.sinks);
+                        s[r] = seen ? s[r] : 0.f;
+                        dp[r] = seen ? dp[r] : 0.f;
+                    }
+                }
+                as_operand(s, 0, pw[0]);
+                as_operand(s, 1, pw[1]);
+                as_operand(dp, 0, dw[0]);
+                as_operand(dp, 1, dw[1]);
+#pragma unroll
+                for (int h2 = 0; h2 < 2; ++h2) {
+                    if (careful.value && !all) {
+                        V seen;
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            const int d = p0 + 16 * h2 + (r & 3) + 8 * (r >> 2) + 4 * half - j;
+                            seen[r] = d >= 0 && (d < a.window || j < a.sinks) ? 1.f : 0.f;
+                        }
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            product_of_some(dv[d], Tile::by_columns(buf + Tile::BYTES, lane, 32 * u + 16 * h2, d), pw[h2], seen, true);
+                            product_of_some(dk[d], Tile::by_columns(buf, lane, 32 * u + 16 * h2, d), dw[h2], seen, false);
+                        }
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            dv[d] = mfma(Tile::by_columns(buf + Tile::BYTES, lane, 32 * u + 16 * h2, d), pw[h2], dv[d]);
+                            dk[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h2, d), dw[h2], dk[d]);
+                        }
+                    }
+                }
+            }
+        }
+        bool odd = false;
+        if (!careful.value && counts)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) odd |= dk[d][r] != dk[d][r] || dv[d][r] != dv[d][r];
+        return __syncthreads_or(odd);
+    };
+    if (__builtin_expect(run(Is<false>()), 0)) run(Is<true>());
+
+    if (!there) return;
+    if (!counts)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dk[d] = dv[d] = grawa_f32x16{};
+    if (splits > 1) {
+        float *p = a.part + (((int64_t)hd * per + item) * BKV + (j - b0)) * 2 * DP;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            store_column<false>((char *)p, lane, d, DP, dk[d], a.scale);
+            store_column<false>((char *)(p + DP), lane, d, DP, dv[d], 1.f);
+        }
+        return;
+    }
+    char *pk = a.dk.p + (int64_t)k * a.dk.worker + (int64_t)n * a.dk.seq + (int64_t)j * a.dk.token + (int64_t)g * a.dk.head;
+    char *pv = a.dv.p + (int64_t)k * a.dv.worker + (int64_t)n * a.dv.seq + (int64_t)j * a.dv.token + (int64_t)g * a.dv.head;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+        store_column<BF16>(pk, lane, d, a.D, dk[d], a.scale);
+        store_column<BF16>(pv, lane, d, a.D, dv[d], 1.f);
+    }
+#endif
+}
+
+// dk and dv of the keys whose queries several blocks shared: their sums, in order.
+template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_dkv_join(GrawaAttend a, int first, int blocks)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int LPR = 2 * DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N; // threads of a key: half have dk, half dv
+    const int64_t id = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;    // [K N][G][blocks][128]
+    const int x = threadIdx.x % LPR, which = x / (LPR / 2), e0 = x % (LPR / 2) * 8;
+    const int per = a.sink_blocks * a.sink_splits + (a.key_blocks - a.sink_blocks) * a.splits;
+    const int key = (int)(id % 128), kb = first + (int)(id / 128 % blocks);
+    const int64_t hd = id / 128 / blocks;
+    const int j = kb * 128 + key;
+    if (hd >= (int64_t)a.K * a.N * a.G || j >= a.Sk) return;
+    const bool sink = kb < a.sink_blocks;
+    const int splits = sink ? a.sink_splits : a.splits, item = sink ? kb * a.sink_splits : a.sink_blocks * a.sink_splits + (kb - a.sink_blocks) * a.splits;
+    float v[8] = {};
+    for (int s = 0; s < splits; ++s) {
+        const grawa_f32x4v *p = (const grawa_f32x4v *)(a.part + ((hd * per + item + s) * 128 + key) * 2 * DP + which * DP + e0);
+        const grawa_f32x4v b = p[0], c = p[1];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += b[q], v[4 + q] += c[q];
+    }
+    const int kn = (int)(hd / a.G), g = (int)(hd - (int64_t)kn * a.G), k = kn / a.N, n = kn - k * a.N;
+    const GrawaHeads &to = which ? a.dv : a.dk;
+    char *out = to.p + (int64_t)k * to.worker + (int64_t)n * to.seq + (int64_t)j * to.token + (int64_t)g * to.head;
+#pragma unroll
+    for (int q = 0; q < 8; q += PN)
+        if (e0 + q < a.D) store_piece<BF16>(out + (e0 + q) * ES, PN, v + q);
+#endif
+}
+
+template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t part_floats, hipStream_t st)
+{
+    const int64_t kn = (int64_t)a.K * a.N;
+    hipError_t e;
+    if (a.Sq > 0) {
+        a.blocks = (a.Sq + 127) / 128;
+        hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3((uint32_t)(kn * a.H * a.blocks)), dim3(256), 0, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (BIAS) {
+        if (a.Sq == 0) a.blocks = 0;
+        hipLaunchKernelGGL((k_bias_sums<BF16>), dim3((uint32_t)a.H, (uint32_t)a.K), dim3(256), 0, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    a.key_blocks = (a.Sk + 127) / 128;
+    // Blocks of keys that all later queries see, and not only those that the window lets through.
+    const int64_t window_tiles = ((int64_t)a.window + 128 + 63) / 64, tiles = (a.Sq + 63) / 64;
+    a.sink_blocks = a.window == GRAWA_NO_WINDOW ? 0 : (int)(((int64_t)a.sinks + 127) / 128 < a.key_blocks ? ((int64_t)a.sinks + 127) / 128 : a.key_blocks);
+    const int64_t groups = kn * a.G, slot = (int64_t)128 * 2 * DP, room = part_floats / slot / groups;
+    const int64_t regular = a.key_blocks - a.sink_blocks, most = (tiles < window_tiles ? tiles : window_tiles) * a.share;
+    int64_t splits = regular ? 512 / (groups * regular) : 1;
+    if (splits > most / 2) splits = most / 2;
+    if (regular && splits > room / 2 / regular) splits = room / 2 / regular;
+    a.splits = splits < 1 ? 1 : (int)splits;
+    int64_t sink_splits = 1;
+    if (a.sink_blocks) {
+        sink_splits = (tiles * a.share + most - 1) / most * a.splits;
+        if (sink_splits > room / 2 / a.sink_blocks) sink_splits = room / 2 / a.sink_blocks;
+    }
+    a.sink_splits = sink_splits < 1 ? 1 : (int)sink_splits;
+    // what is written for joining: all items have a place
+    if ((a.splits > 1 || a.sink_splits > 1) && (int64_t)a.sink_blocks * a.sink_splits + regular * a.splits > room) a.splits = a.sink_splits = 1;
+    const int64_t per = (int64_t)a.sink_blocks * a.sink_splits + regular * a.splits;
+    hipLaunchKernelGGL((k_attend_dkv<BF16, DP, BIAS>), dim3((uint32_t)(groups * per)), dim3(256), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int first = a.sink_splits > 1 ? 0 : a.sink_blocks, end = a.splits > 1 ? a.key_blocks : a.sink_blocks;
+    if (end <= first) return hipSuccess;
+    const int64_t ids = groups * (end - first) * 128;
+    hipLaunchKernelGGL((k_attend_dkv_join<BF16, DP>), dim3((uint32_t)(ids * (DP / 4) / 256)), dim3(256), 0, st, a, first, end - first);
+    return hipGetLastError();
+}
+
+} // namespace
+
+hipError_t grawa_launch_attend_backward(const grawa_attention_plan *s, GrawaAttend a, hipStream_t st)
+{
+    if (a.N == 0 && !a.buckets) return hipSuccess;
+    if (a.N == 0 || a.Sk == 0) { // nothing but the bias's gradient, of no pairs
+        if (!a.buckets) return hipSuccess;
+        a.blocks = 0;
+        if (s->dtype == GRAWA_BF16)
+            hipLaunchKernelGGL((k_bias_sums<true>), dim3((uint32_t)a.H, (uint32_t)a.K), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((k_bias_sums<false>), dim3((uint32_t)a.H, (uint32_t)a.K), dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
+    const bool bias = a.buckets > 0, wide = grawa_padded_width(a.D) == 128;
+    if (s->dtype == GRAWA_BF16) {
+        if (wide) return bias ? launch<true, 128, true>(a, s->part_floats, st) : launch<true, 128, false>(a, s->part_floats, st);
+        return bias ? launch<true, 64, true>(a, s->part_floats, st) : launch<true, 64, false>(a, s->part_floats, st);
+    }
+    if (wide) return bias ? launch<false, 128, true>(a, s->part_floats, st) : launch<false, 128, false>(a, s->part_floats, st);
+    return bias ? launch<false, 64, true>(a, s->part_floats, st) : launch<false, 64, false>(a, s->part_floats, st);
+}

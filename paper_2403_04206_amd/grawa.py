@@ -83,6 +83,12 @@ def lib():
         "grawa_ffn": (it, [vp, i64, vp, vp, vp, vp, vp, fl, vp, C.c_uint32, vp, vp, vp]),
         "grawa_ffn_backward": (it, [vp, i64] + [vp] * 10 + [it, vp]),
         "grawa_dropout": (it, [it, i64, i64, it, vp, vp, fl, vp, C.c_uint32, vp, vp]),
+        "grawa_attention_create": (it, [C.POINTER(vp), vp]),
+        "grawa_attention_destroy": (it, [vp]),
+        "grawa_head_norm": (it, [vp, i64, i64, vp, vp, vp, vp, fl, vp, vp, vp, vp]),
+        "grawa_head_norm_backward": (it, [vp, i64, i64, vp, vp, vp, vp, vp, vp, fl, vp, vp, vp, vp, vp, it, vp]),
+        "grawa_attention": (it, [vp, i64, i64, i64] + [vp] * 9),
+        "grawa_attention_backward": (it, [vp, i64, i64, i64] + [vp] * 13 + [it, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -689,3 +695,179 @@ def dropout(x, out, p, rng, site=0, residual=None, stream=None):
     dt = x.dtype
     _check(lib().grawa_dropout(K, T, d, _DTYPES[dt], _tokens(x, K, T, d, dt, "x"), _tokens(residual, K, T, d, dt, "residual", True),
                                float(p), _rng(rng, p), _site(site), _tokens(out, K, T, d, dt, "out"), _stream(stream)), "grawa_dropout")
+
+
+# -- attention ------------------------------------------------------------------------
+
+MAX_DISTANCES, MAX_BUCKETS = 1024, 256
+
+
+class _HeadsArg(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("worker", C.c_int64), ("sequence", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class _ShapeArg(C.Structure):
+    _fields_ = [("K", C.c_int), ("sequences", C.c_int64), ("length", C.c_int64), ("heads", C.c_int), ("kv_heads", C.c_int), ("width", C.c_int),
+                ("dtype", C.c_int), ("scale", C.c_float), ("window", C.c_int64), ("sinks", C.c_int64), ("rotary", C.c_int), ("interleaved", C.c_int),
+                ("frequencies", C.c_void_p), ("buckets", C.c_int), ("distances", C.c_int64), ("bucket_of", C.c_void_p)]
+
+
+def rotary_frequencies(dims, base=10000.0):
+    """base^(-2 i / dims), i < dims / 2: radians a position of the pairs of a rotation of `dims` elements."""
+    dims = int(dims)
+    if dims < 0 or dims % 2 or not base > 0:
+        raise ValueError("dims must be even and base positive")
+    return [float(base) ** (-2.0 * i / dims) for i in range(dims // 2)]
+
+
+def log_buckets(buckets, far):
+    """The bucket of every distance up to the first in the last bucket: half the buckets hold a distance each, the others grow by a
+    common factor up to `far`, from which on all distances share the last one (at the latest).  Found in whole numbers: bucket half + j
+    begins at the first n with (n / half)^(buckets - half) >= (far / half)^j."""
+    buckets, far = int(buckets), int(far)
+    half = buckets // 2
+    if buckets < 2 or far <= half:
+        raise ValueError("at least two buckets, and far above half their number")
+    e, out, j = buckets - half, list(range(half)), 0
+    while not out or out[-1] < buckets - 1:
+        n = len(out)
+        while j < e - 1 and far ** (j + 1) * half ** e <= n ** e * half ** (j + 1):
+            j += 1
+        out.append(half + j)
+    return out
+
+
+def _heads(t, shape, dtype, what):
+    """[K, N, S, heads, D] with unit stride in the last axis, for the C call."""
+    if t is None or t.dtype is not dtype or t.ndim != 5 or not _on_device(t):
+        raise TypeError("%s must be a %s CUDA tensor [K, N, S, heads, D]" % (what, str(dtype).replace("torch.", "")))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), shape))
+    stride = t.stride()
+    if shape[4] > 1 and stride[4] != 1:
+        raise TypeError("%s: elements of a row must be adjacent" % what)
+    if t.numel():
+        _covers(t, sum((n - 1) * s for n, s in zip(shape[:4], stride)) + shape[4], what)
+    return C.byref(_HeadsArg(t.data_ptr(), *stride[:4]))
+
+
+class AttentionPlan:
+    """grawa_attention_plan_t: the attention of K workers (norms of heads with rotation, attention through a window with first tokens
+    that stay visible, learned bias by buckets), its shape, tables and device workspace.  `sequences` and `length` are the most that a
+    call may have; `heads` of queries share `kv_heads` of keys and values; `width` is a head's.  scale is width^-0.5 by default, window 0
+    none; frequencies (radians a position, host) turn 2 len(frequencies) elements of a head; bucket_of (host) has the bucket of every
+    distance, the last one's for longer ones.  Activations are [K, N, S, heads, D] at any strides (rows of the attention at 16 bytes),
+    parameters views of the workers' flat rows: qweight, kweight [K, D], bias [K, heads, buckets]."""
+
+    def __init__(self, K, sequences, length, heads, kv_heads, width, dtype=torch.bfloat16, scale=None, window=0, sinks=0, frequencies=None,
+                 interleaved=False, buckets=0, bucket_of=None):
+        if dtype not in _DTYPES:
+            raise TypeError("dtype must be torch.float32 or torch.bfloat16")
+        self.K, self.N, self.S, self.H, self.G, self.D = (int(x) for x in (K, sequences, length, heads, kv_heads, width))
+        self.dtype, self.buckets = dtype, int(buckets)
+        if (bucket_of is None) != (self.buckets == 0):
+            raise ValueError("buckets and bucket_of go together")
+        freq = np.ascontiguousarray([] if frequencies is None else frequencies, dtype=np.float64)
+        of = np.ascontiguousarray([] if bucket_of is None else bucket_of, dtype=np.int32)
+        if freq.ndim != 1 or of.ndim != 1:
+            raise ValueError("frequencies and bucket_of are lists of numbers")
+        scale = self.D ** -0.5 if scale is None and self.D > 0 else float(0.0 if scale is None else scale)
+        shape = _ShapeArg(self.K, self.N, self.S, self.H, self.G, self.D, _DTYPES[dtype], scale, int(window), int(sinks), 2 * freq.size,
+                          1 if interleaved else 0, freq.ctypes.data, self.buckets, of.size, of.ctypes.data)
+        self._h = C.c_void_p()
+        _check(lib().grawa_attention_create(C.byref(self._h), C.byref(shape)), "grawa_attention_create")
+
+    def destroy(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            torch.cuda.synchronize()
+            st = lib().grawa_attention_destroy(self._h)
+            self._h = C.c_void_p()
+            _check(st, "grawa_attention_destroy")
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.destroy()
+
+    def _tokens_of(self, t, what):
+        """Sequences and tokens of a call's tensor."""
+        if t is None or t.ndim != 5:
+            raise TypeError("%s must be a CUDA tensor [K, N, S, heads, D]" % what)
+        N, S = t.shape[1], t.shape[2]
+        if N > self.N or S > self.S:
+            raise ValueError("%s has %d sequences of %d tokens, the plan takes %d of %d" % (what, N, S, self.N, self.S))
+        return N, S
+
+    def _places(self, t, N, what):
+        if t is None:
+            return _NULL
+        if t.dtype is not torch.int32 or not t.is_contiguous() or not _on_device(t):
+            raise TypeError("%s must be a contiguous int32 CUDA tensor" % what)
+        if tuple(t.shape) != (self.K, N):
+            raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), (self.K, N)))
+        _covers(t, t.numel(), what)
+        return C.c_void_p(t.data_ptr())
+
+    def _bias(self, t, what):
+        if self.buckets:
+            return _mats(t, (self.K, self.H, self.buckets), self.dtype, what)
+        if t is not None:
+            raise ValueError("%s: the plan has no buckets" % what)
+        return None
+
+    def head_norm(self, q, k, qweight, kweight, q_out, k_out, eps=1e-6, starts=None, stream=None):
+        """grawa_head_norm: each head divided by its root mean square, times the weight, turned by its position (start + index)."""
+        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
+        N, S = self._tokens_of(q, "q")
+        sq, sk = (K, N, S, H, D), (K, N, S, G, D)
+        _check(lib().grawa_head_norm(
+            self._h, N, S, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _mats(qweight, (K, D), dt, "qweight"), _mats(kweight, (K, D), dt, "kweight"),
+            float(eps), self._places(starts, N, "starts"), _heads(q_out, sq, dt, "q_out"), _heads(k_out, sk, dt, "k_out"), _stream(stream)),
+            "grawa_head_norm")
+
+    def head_norm_backward(self, dq_out, dk_out, q, k, qweight, kweight, dq, dk, dqweight, dkweight, eps=1e-6, starts=None, accumulate=False, stream=None):
+        """grawa_head_norm_backward: dq, dk and the gradients of the weights, added to what those hold with accumulate."""
+        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
+        N, S = self._tokens_of(q, "q")
+        sq, sk = (K, N, S, H, D), (K, N, S, G, D)
+        _check(lib().grawa_head_norm_backward(
+            self._h, N, S, _heads(dq_out, sq, dt, "dq_out"), _heads(dk_out, sk, dt, "dk_out"), _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"),
+            _mats(qweight, (K, D), dt, "qweight"), _mats(kweight, (K, D), dt, "kweight"), float(eps), self._places(starts, N, "starts"),
+            _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"), _mats(dqweight, (K, D), dt, "dqweight"), _mats(dkweight, (K, D), dt, "dkweight"),
+            1 if accumulate else 0, _stream(stream)), "grawa_head_norm_backward")
+
+    def _lse(self, t, N, Sq, what, optional):
+        if t is None and optional:
+            return _NULL
+        if t is None:
+            raise TypeError("%s is required" % what)
+        return _table(t, (self.K, N, self.H, Sq), what)
+
+    def attention(self, q, k, v, out, lse_out=None, bias=None, lengths=None, starts=None, stream=None):
+        """grawa_attention: out = softmax(scale q k^T + bias) v over the keys that each query sees; lse_out: float32 [K, N, heads, Sq] for
+        the backward pass."""
+        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
+        (N, Sq), Sk = self._tokens_of(q, "q"), self._tokens_of(k, "k")[1]
+        sq, sk = (K, N, Sq, H, D), (K, N, Sk, G, D)
+        _check(lib().grawa_attention(
+            self._h, N, Sq, Sk, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"), self._bias(bias, "bias"),
+            self._places(lengths, N, "lengths"), self._places(starts, N, "starts"), _heads(out, sq, dt, "out"), self._lse(lse_out, N, Sq, "lse_out", True),
+            _stream(stream)), "grawa_attention")
+
+    def attention_backward(self, dout, q, k, v, out, lse, dq, dk, dv, bias=None, dbias=None, lengths=None, starts=None, accumulate=False, stream=None):
+        """grawa_attention_backward: dq, dk, dv and, with buckets, dbias, added to what it holds with accumulate."""
+        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
+        (N, Sq), Sk = self._tokens_of(q, "q"), self._tokens_of(k, "k")[1]
+        sq, sk = (K, N, Sq, H, D), (K, N, Sk, G, D)
+        _check(lib().grawa_attention_backward(
+            self._h, N, Sq, Sk, _heads(dout, sq, dt, "dout"), _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
+            self._bias(bias, "bias"), self._places(lengths, N, "lengths"), self._places(starts, N, "starts"), _heads(out, sq, dt, "out"),
+            self._lse(lse, N, Sq, "lse", False), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"), _heads(dv, sk, dt, "dv"),
+            self._bias(dbias, "dbias"), 1 if accumulate else 0, _stream(stream)), "grawa_attention_backward")
