@@ -2,8 +2,9 @@
 //
 // A tile is ROWS tokens (keys or queries) of one head, DP elements each, zeros where the head has fewer elements or the sequence no
 // more tokens.  It goes from memory straight into LDS, 16 bytes a lane, bounded by its buffer descriptor.  The 16-byte piece c of row r
-// stands at place c ^ key(r), key(r) = 2 (r % 4) + r / 4 % 2: the eight rows that a fragment by rows is read from at a time fall on
-// different banks, and so do the four rows of the transposing load, each by two neighbouring pieces.
+// stands at place c ^ key(r).  LDS has 64 banks, a load of 16 bytes a lane takes sixteen lanes at a time and the transposing load of 8
+// bytes thirty-two: the sixteen rows of the one, the four rows and four pieces of the other (float32 by columns: two rows four apart and
+// eight pieces) fall on different banks.  Keys that only told eight rows apart cost four cycles more a load.
 //
 // A fragment is 32 x 16: the lane has line lane % 32 and eight k of it.  By rows those are k = 8 (lane / 32) + j.  By columns the lines
 // are elements of the head and k runs over tokens in the order in which a product's sums stand in registers: for sums of 32 x 32 the
@@ -64,19 +65,27 @@ __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 
 template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
     typedef typename Frag<BF16>::V V;
     static constexpr int ES = BF16 ? 2 : 4, RB = DP * ES, PPR = RB / 16, BYTES = ROWS * RB, LOADS = BYTES / 1024 / NW;
-    static constexpr bool TURN = NW * 64 / PPR == 4; // a wave's loads are four rows apart: every other one has the other half of the keys
-    static_assert(LOADS * NW * 1024 == BYTES && (TURN || NW * 64 / PPR % 8 == 0), "whole loads of whole groups of rows");
+    static constexpr int RPL = NW * 64 / PPR, TURNS = RPL < 16 ? 16 / RPL : 1; // rows that the waves load at a time; loads until the keys repeat
+    static_assert(LOADS * NW * 1024 == BYTES && LOADS % TURNS == 0, "whole loads of whole groups of rows");
 
-    static __device__ __forceinline__ int key(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+    static __device__ __forceinline__ int key(int row)
+    {
+        if constexpr (!BF16) return (((row >> 2) & 1) << 3) | ((row & 3) << 1) | ((row >> 3) & 1);
+        if constexpr (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+        return (((row >> 1) & 1) << 2) | ((row >> 2) & 1) | (((row >> 3) & 1) << 1); // rows of 128 bytes: their lowest bit is a bank's
+    }
 
-    // Loads: the lane's offset in the wave's first one (two where they take turns), and from one to the next.
-    uint32_t first, odd, step;
+    // Loads: the lane's offset in the wave's first ones, until the keys repeat.
+    uint32_t first[TURNS], step;
     __device__ __forceinline__ void init(int wave, int lane, uint32_t token, int D)
     {
-        const int id = wave * 64 + lane, row = id / PPR, c = (id % PPR) ^ key(row), c4 = (id % PPR) ^ key(row + 4);
-        first = c * 16 < D * ES ? (uint32_t)row * token + (uint32_t)c * 16 : 0x80000000u;
-        odd = !TURN ? 0 : c4 * 16 < D * ES ? (uint32_t)(row + 4) * token + (uint32_t)c4 * 16 : 0x80000000u;
-        step = (TURN ? 8 : NW * 64 / PPR) * token;
+        const int id = wave * 64 + lane;
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            const int row = id / PPR + i * RPL, c = (id % PPR) ^ key(row);
+            first[i] = c * 16 < D * ES ? (uint32_t)row * token + (uint32_t)c * 16 : 0x80000000u;
+        }
+        step = RPL * TURNS * token;
     }
     // rows: what the sequence has from the tile's first token on; none: nothing is read and all comes as zeros.
     static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const char *p, int rows, uint32_t token, int D)
@@ -88,39 +97,43 @@ template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
     {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS_AT void *)(lds + (wave + NW * i) * 1024), 16,
-                                                     TURN && i % 2 ? odd + (uint32_t)(i / 2) * step : first + (uint32_t)(TURN ? i / 2 : i) * step, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS_AT void *)(lds + (wave + NW * i) * 1024), 16, first[i % TURNS] + (uint32_t)(i / TURNS) * step, 0, 0, 0);
     }
+
+    // Fragments: an address that all of a tile's share, of which a fragment's differs by some of its low bits and by a constant.
+    static __device__ __forceinline__ uint32_t address(const char *lds) { return (uint32_t)(uintptr_t)(GRAWA_LDS_AT const char *)lds; }
 
     // Lines row0 ... row0 + 31 (a multiple of 32), elements 16 ks ... of the head.
     static __device__ __forceinline__ V by_rows(const char *lds, int lane, int row0, int ks)
     {
         const int row = lane & 31, half = lane >> 5;
-        const char *p = lds + (row0 + row) * RB;
+        const uint32_t at = address(lds) + row * RB + (((BF16 ? half : 2 * half) ^ key(row)) << 4);
         if constexpr (BF16) {
-            return *(const V *)(p + (((2 * ks + half) ^ key(row)) << 4));
+            return *(GRAWA_LDS_AT const V *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (ks << 5)) + row0 * RB);
         } else {
-            const grawa_f32x4v a = *(const grawa_f32x4v *)(p + (((4 * ks + 2 * half) ^ key(row)) << 4));
-            const grawa_f32x4v b = *(const grawa_f32x4v *)(p + (((4 * ks + 2 * half + 1) ^ key(row)) << 4));
+            const grawa_f32x4v a = *(GRAWA_LDS_AT const grawa_f32x4v *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (ks << 6)) + row0 * RB);
+            const grawa_f32x4v b = *(GRAWA_LDS_AT const grawa_f32x4v *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (ks << 6) ^ 16) + row0 * RB);
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
     // Lines: elements 32 dt ... of the head, k: tokens row0 ... row0 + 15 (a multiple of 16) in the order of a product's registers.
     static __device__ __forceinline__ V by_columns(const char *lds, int lane, int row0, int dt)
     {
+        const int half = lane >> 5;
         if constexpr (BF16) {
-            const int s = lane & 15, half = lane >> 5, row = 4 * half + (s >> 2);
-            const char *p = lds + (row0 + row) * RB + (((4 * dt + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1)) ^ key(row)) << 4) + (s & 1) * 8;
-            const grawa_s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)p);
-            const grawa_s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)(p + 8 * RB));
+            const int s = lane & 15, row = 4 * half + (s >> 2);
+            const uint32_t at = (address(lds) + row * RB + (((2 * ((lane >> 4) & 1) + ((s & 3) >> 1)) ^ key(row)) << 4) + (s & 1) * 8) ^ (dt << 6);
+            const grawa_s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)at + row0 * RB));
+            const grawa_s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)(at ^ 32) + (row0 + 8) * RB)); // eight rows on, the key's second bit is another
             return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const int m = lane & 31, half = lane >> 5;
+            const int m = lane & 31;
             V v;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int row = 4 * half + (j & 3) + 8 * (j >> 2);
-                v[j] = *(const float *)(lds + (row0 + row) * RB + (((8 * dt + (m >> 2)) ^ key(row)) << 4) + (m & 3) * 4);
+                const uint32_t at = address(lds) + row * RB + (((m >> 2) ^ key(row)) << 4) + (m & 3) * 4;
+                v[j] = *(GRAWA_LDS_AT const float *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (dt << 7)) + row0 * RB);
             }
             return v;
         }
@@ -232,12 +245,40 @@ template <bool BF16> __device__ __forceinline__ void store_column(char *row, int
     }
 }
 
-// Blocks go round the eight XCDs; each gets a run of consecutive numbers, so that blocks that read the same keys share its L2.
-__device__ __forceinline__ uint32_t run_of(uint32_t id, uint32_t total)
+__device__ __forceinline__ bool sees(const GrawaAttend &a, int pos, int j)
 {
-    const uint32_t q = total / 8, r = total % 8, xcd = id % 8;
-    return xcd * q + (xcd < r ? xcd : r) + id / 8;
+    const int d = pos - j;
+    return d >= 0 && (d < a.window || j < a.sinks);
+}
+
+// Marks of the tokens j0 + ... that a column sees, in the order of an operand.
+template <class V> __device__ __forceinline__ V marks(const GrawaAttend &a, int pos, int j0, int half)
+{
+    V v;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? 1.f : 0.f;
+    return v;
+}
+
+// Which head and which of its blocks a workgroup has.  Workgroups go round the eight XCDs; each XCD gets heads of its own, so that
+// blocks that read the same keys share its L2, and takes the first block of all of them, then the second: blocks are numbered from the
+// longest on, and the short ones fill the end.  Few heads that eight does not divide are dealt out one by one.
+struct Turn {
+    int head, block;
+};
+__device__ __forceinline__ Turn turn_of(uint32_t id, uint32_t heads, int by_xcd)
+{
+    if (!by_xcd) return Turn{(int)(id % heads), (int)(id / heads)};
+    const uint32_t each = (heads + 7) / 8, r = id / 8;
+    return Turn{(int)(id % 8 * each + r % each), (int)(r / each)};
 }
 #endif // __HIP_DEVICE_COMPILE__
+
+// The grid for turn_of; heads that are not there have workgroups that end at once.
+inline uint32_t grid_of(int64_t heads, int64_t blocks, int &by_xcd)
+{
+    by_xcd = heads % 8 == 0 || heads >= 64;
+    return (uint32_t)((by_xcd ? (heads + 7) / 8 * 8 : heads) * blocks);
+}
 
 } // namespace

@@ -6,58 +6,83 @@
 
 namespace {
 
-// KEYS = false: a block has 128 CT queries of one head, a wave 32 CT of them, and all waves share a tile of 64 keys.
-// KEYS = true, for few queries: a block has up to 32 columns, which are the queries of all heads that share their keys, and its waves
-// have 32 keys each of a tile; their sums are joined at the end.
+#ifdef __HIP_DEVICE_COMPILE__
+// The running maximum (of scores times log2 e) and sum of a column's softmax.
+struct Running {
+    float m, l;
+};
+
+// Exponentials of a column's scores against its running maximum, in place.  SCALED: the scores are in units of log2 already.
+template <bool SCALED, int NS, int DT>
+__device__ __forceinline__ void soften(grawa_f32x16 (&s)[NS], float c2, Running &run, grawa_f32x16 (&o)[DT])
+{
+    float top = s[0][0];
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+    top = fmaxf(top, other_half(top));
+    if (!SCALED) top *= c2;
+    // The maximum moves only where it would grow by more than 2^8: until then the sums are of exponentials up to 2^8.
+    if (__any(top > run.m + 8.f)) {
+        const float m2 = fmaxf(run.m, top), f = m2 == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(run.m - m2);
+        run.m = m2;
+        run.l *= f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= f;
+    }
+    const float base = run.m == -__builtin_inff() ? 0.f : run.m;
+#pragma unroll
+    for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[u][r] = __builtin_amdgcn_exp2f(SCALED ? s[u][r] - base : __builtin_fmaf(s[u][r], c2, -base));
+            run.l += s[u][r]; // before it is rounded: the gradients start from this sum
+        }
+}
+#endif
+
+// A block has 128 CT queries of one head, a wave 32 CT of them, and all waves share tiles of 64 keys and values, two in LDS.
 // splits > 1: that many blocks share the keys, and k_attend_join puts their results together.
-template <bool BF16, int DP, int CT, bool KEYS, bool BIAS, int NW>
-__global__ __launch_bounds__(NW * 64, KEYS ? 1 : 2) void k_attend(GrawaAttend a)
+template <bool BF16, int DP, int CT, bool BIAS>
+__global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int BK = KEYS ? 32 * NW : 64, NS = KEYS ? 1 : 2, COLS = KEYS ? 32 : 32 * CT * NW, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32;
-    static_assert(!KEYS || CT == 1, "one set of columns");
-    typedef HeadTile<BF16, DP, BK, NW> Tile;
+    constexpr int BK = 64, COLS = 128 * CT, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32;
+    typedef HeadTile<BF16, DP, BK, 4> Tile;
     typedef typename Tile::V V;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES]; // two buffers of keys and values
-    __shared__ float table[BIAS && !KEYS ? GRAWA_MAX_DISTANCES : 1];     // the bias by distance
+    __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];              // the bias by distance
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int groups = KEYS ? a.G : a.H, per = a.blocks * a.splits;
-    const int t = (int)run_of(blockIdx.x, gridDim.x), hd = t / per, rest = t - hd * per, split = rest % a.splits, qb = a.blocks - 1 - rest / a.splits;
-    const int kn = hd / groups, k = kn / a.N, n = kn - k * a.N, g = KEYS ? hd - kn * groups : (hd - kn * groups) / a.share;
+    const int heads = a.K * a.N * a.H;
+    const Turn turn = turn_of(blockIdx.x, heads, a.by_xcd);
+    if (turn.head >= heads) return;
+    const int qb = a.blocks - 1 - turn.block / a.splits, split = turn.block % a.splits;
+    const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
     const Place at = place_of(a, kn);
 
     // The lane's columns.
-    int head[CT], i[CT], pos[CT];
-    bool there[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const int col = qb * COLS + (KEYS ? 0 : wave * 32 * CT) + 32 * c + (lane & 31);
-        head[c] = KEYS ? g * a.share + col / a.Sq : hd - kn * groups;
-        i[c] = KEYS ? col % a.Sq : col;
-        there[c] = KEYS ? col < a.share * a.Sq : col < a.Sq;
-        pos[c] = at.start + i[c];
-    }
-    const auto counts = [&](int c) { return there[c] && pos[c] >= 0 && pos[c] < at.length; };
+    const int i0 = qb * COLS + wave * 32 * CT + (lane & 31), pos0 = at.start + i0; // column c: 32 c more
+    const auto there = [&](int c) { return i0 + 32 * c < a.Sq; };
+    const auto counts = [&](int c) { return there(c) && pos0 + 32 * c >= 0 && pos0 + 32 * c < at.length; };
     V q[CT][KS];
+    {
+        const char *row = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i0 * a.q.token + (int64_t)head * a.q.head;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const char *row = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i[c] * a.q.token + (int64_t)head[c] * a.q.head;
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[c][ks] = load_line<BF16>(row, 16 * ks + 8 * half, a.D, counts(c));
+            for (int ks = 0; ks < KS; ++ks) q[c][ks] = load_line<BF16>(row + (int64_t)(32 * c) * a.q.token, 16 * ks + 8 * half, a.D, counts(c));
     }
     const float c2 = a.scale * LOG2E;
-    const char *bias = BIAS ? a.bias.p + (int64_t)k * a.bias.worker * ES : nullptr;
-    float far[CT];
+    float far = 0.f;
     if constexpr (BIAS) {
-#pragma unroll
-        for (int c = 0; c < CT; ++c) far[c] = there[c] ? load_one<BF16>(bias + (head[c] * a.buckets + a.bucket_of[a.distances - 1]) * ES) * LOG2E : 0.f;
-        if constexpr (!KEYS)
-            for (int d = threadIdx.x; d < a.distances; d += NW * 64) table[d] = load_one<BF16>(bias + (head[0] * a.buckets + a.bucket_of[d]) * ES) * LOG2E;
+        const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + head * a.buckets) * ES;
+        far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
+        for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
     }
 
     // Tiles: those with first tokens, then those of the window.
-    const int p0 = KEYS ? at.start : at.start + qb * COLS, p1 = KEYS ? at.start + a.Sq - 1 : at.start + min((qb + 1) * COLS, a.Sq) - 1;
-    const int w0 = KEYS ? p0 : p0 + wave * 32 * CT, w1 = KEYS ? p1 : w0 + 32 * CT - 1; // of the wave
+    const int p0 = at.start + qb * COLS, p1 = at.start + min((qb + 1) * COLS, a.Sq) - 1, w0 = p0 + wave * 32 * CT, w1 = w0 + 32 * CT - 1;
     const int end = min(p1, at.length - 1) + 1, begin = max(0, max(p0, 0) - a.window + 1);
     const bool any = p1 >= 0 && p0 < at.length;
     const int t0 = begin / BK, first_tiles = any ? min(t0, (min(a.sinks, end) + BK - 1) / BK) : 0, tiles = any ? first_tiles + (end + BK - 1) / BK - t0 : 0;
@@ -67,222 +92,312 @@ __global__ __launch_bounds__(NW * 64, KEYS ? 1 : 2) void k_attend(GrawaAttend a)
     Tile lk, lv;
     lk.init(wave, lane, (uint32_t)a.k.token, a.D);
     lv.init(wave, lane, (uint32_t)a.v.token, a.D);
+    const auto tile_of = [&](int it) { return (it < first_tiles ? it : it - first_tiles + t0) * BK; };
     const auto load = [&](int it, char *buf) {
-        const int j0 = (it < first_tiles ? it : it - first_tiles + t0) * BK;
+        const int j0 = tile_of(it);
+        lk.load(buf, wave, Tile::rsrc(kp + (int64_t)j0 * a.k.token, at.length - j0, (uint32_t)a.k.token, a.D));
+        lv.load(buf + Tile::BYTES, wave, Tile::rsrc(vp + (int64_t)j0 * a.v.token, at.length - j0, (uint32_t)a.v.token, a.D));
+    };
+    const auto none = [&](int j0, int j1) { return j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
+    const auto all = [&](int j0, int j1) { return j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks); };
+    // Scores of 32 keys and a set of columns: masked, with a bias in units of log2.
+    const auto scores = [&](int j0, int c, grawa_f32x16 &s) __attribute__((always_inline)) {
+        if constexpr (BIAS) {
+            const bool is_far = w0 - (j0 + 31) >= a.distances - 1;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int d = pos0 + 32 * c - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half);
+                s[r] = s[r] * c2 + (is_far ? far : table[clamp_int(d, 0, a.distances - 1)]);
+            }
+        }
+        if (!all(j0, j0 + 31))
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = sees(a, pos0 + 32 * c, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : -__builtin_inff();
+    };
+
+    grawa_f32x16 o[CT][DT];
+    Running run[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        run[c] = Running{-__builtin_inff(), 0.f};
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[c][d] = grawa_f32x16{};
+    }
+    const auto step = [&](const char *buf, int j0) __attribute__((always_inline)) {
+        grawa_f32x16 s[CT][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) s[c][u] = grawa_f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const V f = Tile::by_rows(buf, lane, 32 * u, ks);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) s[c][u] = mfma(f, q[c][ks], s[c][u]);
+            }
+        }
+        V p[CT][4];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) scores(j0 + 32 * u, c, s[c][u]);
+            soften<BIAS>(s[c], c2, run[c], o[c]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) as_operand(s[c][u], h, p[c][2 * u + h]);
+        }
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const V f = Tile::by_columns(buf + Tile::BYTES, lane, 16 * h, d);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) o[c][d] = mfma(f, p[c][h], o[c][d]);
+            }
+    };
+    if (from < to) load(from, lds);
+    for (int it = from; it < to; ++it) {
+        const char *buf = lds + ((it - from) & 1) * 2 * Tile::BYTES;
+        landed();
+        if (it + 1 < to) load(it + 1, lds + ((it + 1 - from) & 1) * 2 * Tile::BYTES);
+        const int j0 = tile_of(it), j1 = j0 + BK - 1;
+        if (!none(j0, j1)) step(buf, j0);
+    }
+
+    const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row0 = ((int64_t)kn * a.H + head) * a.Sq + i0;
+    float *part = a.part + (int64_t)split * rows * DP + row0 * DP, *part_lse = a.part + (int64_t)a.splits * rows * DP + (int64_t)split * rows + row0;
+    char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i0 * a.o.token + (int64_t)head * a.o.head;
+    float f[CT]; // what the sums are divided by
+    bool odd = false;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const float l = run[c].l + other_half(run[c].l);
+        const bool sum = counts(c) && !(l == 0.f);
+        const float lse2 = sum ? run[c].m + __builtin_amdgcn_logf(l) : -__builtin_inff();
+        f[c] = sum ? 1.f / l : 0.f;
+        if (half == 0 && there(c)) {
+            if (a.splits > 1)
+                part_lse[32 * c] = lse2;
+            else if (a.lse)
+                a.lse[row0 + 32 * c] = lse2 * LN2;
+        }
+        if (sum)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) odd |= o[c][d][r] != o[c][d][r];
+    }
+    const auto put = [&](int c, int d, const grawa_f32x16 &sums) {
+        if (!there(c)) return;
+        grawa_f32x16 v;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[r] = f[c] == 0.f ? 0.f : sums[r] * f[c];
+        if (a.splits > 1)
+            store_column<false>((char *)(part + 32 * c * DP), lane, d, DP, v, 1.f);
+        else
+            store_column<BF16>(out + (int64_t)(32 * c) * a.o.token, lane, d, a.D, v, 1.f);
+    };
+    // What is no number may come from a token that the column does not see: once more then, with care.
+    if (__builtin_expect(!__syncthreads_or(odd), 1)) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) put(c, d, o[c][d]);
+        return;
+    }
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            const float base = run[c].m == -__builtin_inff() ? 0.f : run[c].m;
+            grawa_f32x16 sums = {};
+            for (int it = from; it < to; ++it) {
+                landed();
+                load(it, lds);
+                landed();
+                for (int u = 0; u < 2; ++u) {
+                    const int j0 = tile_of(it) + 32 * u, j1 = j0 + 31;
+                    if (none(j0, j1)) continue;
+                    grawa_f32x16 s = {};
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(lds, lane, 32 * u, ks), q[c][ks], s);
+                    scores(j0, c, s);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(BIAS ? s[r] - base : __builtin_fmaf(s[r], c2, -base));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        V p;
+                        as_operand(s, h, p);
+                        const V v = Tile::by_columns(lds + Tile::BYTES, lane, 32 * u + 16 * h, d);
+                        if (all(j0, j1))
+                            sums = mfma(v, p, sums);
+                        else
+                            product_of_some(sums, v, p, marks<V>(a, pos0 + 32 * c, j0 + 16 * h, half), true);
+                    }
+                }
+            }
+            put(c, d, sums);
+        }
+#endif
+}
+
+// The same for few queries: a block has up to 32 columns, which are the queries of all heads that share their keys, and its NW waves
+// have 32 keys each of a tile; their sums are joined at the end.
+template <bool BF16, int DP, bool BIAS, int NW>
+__global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAttend a)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int BK = 32 * NW, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32;
+    typedef HeadTile<BF16, DP, BK, NW> Tile;
+    typedef typename Tile::V V;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES]; // two buffers of keys and values
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int groups = a.K * a.N * a.G;
+    const Turn turn = turn_of(blockIdx.x, groups, a.by_xcd);
+    if (turn.head >= groups) return;
+    const int cb = turn.block / a.splits, split = turn.block % a.splits;
+    const int kn = turn.head / a.G, g = turn.head - kn * a.G, k = kn / a.N, n = kn - k * a.N;
+    const Place at = place_of(a, kn);
+
+    // The lane's column.
+    const int col = cb * 32 + (lane & 31), head = g * a.share + col / a.Sq, i = col % a.Sq, pos = at.start + i;
+    const bool there = col < a.share * a.Sq, counts = there && pos >= 0 && pos < at.length;
+    V q[KS];
+    {
+        const char *row = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i * a.q.token + (int64_t)head * a.q.head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = load_line<BF16>(row, 16 * ks + 8 * half, a.D, counts);
+    }
+    const float c2 = a.scale * LOG2E;
+    const char *bias = BIAS ? a.bias.p + ((int64_t)k * a.bias.worker + (there ? head : 0) * a.buckets) * ES : nullptr;
+    float far = 0.f;
+    if constexpr (BIAS) far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
+
+    const int w0 = at.start, w1 = at.start + a.Sq - 1; // positions
+    const int end = min(w1, at.length - 1) + 1, begin = max(0, max(w0, 0) - a.window + 1);
+    const bool any = w1 >= 0 && w0 < at.length;
+    const int t0 = begin / BK, first_tiles = any ? min(t0, (min(a.sinks, end) + BK - 1) / BK) : 0, tiles = any ? first_tiles + (end + BK - 1) / BK - t0 : 0;
+    const int from = (int)((int64_t)tiles * split / a.splits), to = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const char *kp = a.k.p + (int64_t)k * a.k.worker + (int64_t)n * a.k.seq + (int64_t)g * a.k.head;
+    const char *vp = a.v.p + (int64_t)k * a.v.worker + (int64_t)n * a.v.seq + (int64_t)g * a.v.head;
+    Tile lk, lv;
+    lk.init(wave, lane, (uint32_t)a.k.token, a.D);
+    lv.init(wave, lane, (uint32_t)a.v.token, a.D);
+    const auto tile_of = [&](int it) { return (it < first_tiles ? it : it - first_tiles + t0) * BK; };
+    const auto load = [&](int it, char *buf) {
+        const int j0 = tile_of(it);
         lk.load(buf, wave, Tile::rsrc(kp + (int64_t)j0 * a.k.token, at.length - j0, (uint32_t)a.k.token, a.D));
         lv.load(buf + Tile::BYTES, wave, Tile::rsrc(vp + (int64_t)j0 * a.v.token, at.length - j0, (uint32_t)a.v.token, a.D));
     };
 
-    grawa_f32x16 o[CT][DT];
-    float m[CT], l[CT];
-    const auto run = [&](auto careful) __attribute__((always_inline)) {
+    grawa_f32x16 o[DT];
+    Running run;
+    const auto go = [&](auto careful) __attribute__((always_inline)) {
+        run = Running{-__builtin_inff(), 0.f};
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            m[c] = -__builtin_inff();
-            l[c] = 0.f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[c][d] = grawa_f32x16{};
-        }
+        for (int d = 0; d < DT; ++d) o[d] = grawa_f32x16{};
         if (from < to) load(from, lds);
         for (int it = from; it < to; ++it) {
-            char *buf = lds + ((it - from) & 1) * 2 * Tile::BYTES;
+            const char *buf = lds + ((it - from) & 1) * 2 * Tile::BYTES;
             landed();
             if (it + 1 < to) load(it + 1, lds + ((it + 1 - from) & 1) * 2 * Tile::BYTES);
-            const int j0 = (it < first_tiles ? it : it - first_tiles + t0) * BK + (KEYS ? wave * 32 : 0), j1 = j0 + 32 * NS - 1;
+            const int j0 = tile_of(it) + wave * 32, j1 = j0 + 31;
             if (j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks)) continue; // none of the wave's pairs count
             const bool all = j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks);
-            grawa_f32x16 s[CT][NS];
+            grawa_f32x16 s[1] = {};
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int u = 0; u < NS; ++u) s[c][u] = grawa_f32x16{};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int u = 0; u < NS; ++u) {
-                    const V f = Tile::by_rows(buf, lane, (KEYS ? wave * 32 : 0) + 32 * u, ks);
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) s[c][u] = mfma(f, q[c][ks], s[c][u]);
-                }
+            for (int ks = 0; ks < KS; ++ks) s[0] = mfma(Tile::by_rows(buf, lane, wave * 32, ks), q[ks], s[0]);
             if constexpr (BIAS) {
-                const bool is_far = w0 - j1 >= a.distances - 1;
+                if (w0 - j1 >= a.distances - 1) {
 #pragma unroll
-                for (int c = 0; c < CT; ++c)
-#pragma unroll
-                    for (int u = 0; u < NS; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            float b = far[c];
-                            if (!is_far) {
-                                const int d = clamp_int(pos[c] - (j0 + 32 * u + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1);
-                                b = !KEYS ? table[d] : there[c] ? load_one<BF16>(bias + (head[c] * a.buckets + a.bucket_of[d]) * ES) * LOG2E : 0.f;
-                            }
-                            s[c][u][r] = s[c][u][r] * c2 + b;
-                        }
-            }
-            if (!all) {
-#pragma unroll
-                for (int c = 0; c < CT; ++c)
-#pragma unroll
-                    for (int u = 0; u < NS; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int j = j0 + 32 * u + (r & 3) + 8 * (r >> 2) + 4 * half, d = pos[c] - j;
-                            const bool seen = d >= 0 && (d < a.window || j < a.sinks);
-                            s[c][u][r] = seen ? s[c][u][r] : -__builtin_inff();
-                        }
-            }
-            V p[CT][NS][2];
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                float top = s[c][0][0];
-#pragma unroll
-                for (int u = 0; u < NS; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[c][u][r]);
-                top = fmaxf(top, other_half(top));
-                if (!BIAS) top *= c2;
-                // The running maximum moves only where it would grow by more than 2^8: until then the sums are of exponentials up to 2^8.
-                if (__any(top > m[c] + 8.f)) {
-                    const float m2 = fmaxf(m[c], top), f = m2 == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[c] - m2);
-                    m[c] = m2;
-                    l[c] *= f;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[c][d] *= f;
-                }
-                const float base = m[c] == -__builtin_inff() ? 0.f : m[c];
-#pragma unroll
-                for (int u = 0; u < NS; ++u) {
+                    for (int r = 0; r < 16; ++r) s[0][r] = s[0][r] * c2 + far;
+                } else {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        s[c][u][r] = __builtin_amdgcn_exp2f(BIAS ? s[c][u][r] - base : __builtin_fmaf(s[c][u][r], c2, -base));
-                        l[c] += s[c][u][r];
+                        const int d = clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1);
+                        s[0][r] = s[0][r] * c2 + load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
                     }
-                    as_operand(s[c][u], 0, p[c][u][0]);
-                    as_operand(s[c][u], 1, p[c][u][1]);
                 }
             }
-            const char *vt = buf + Tile::BYTES;
-            if (careful.value && !all) {
+            if (!all)
 #pragma unroll
-                for (int u = 0; u < NS; ++u)
+                for (int r = 0; r < 16; ++r) s[0][r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[0][r] : -__builtin_inff();
+            soften<BIAS>(s, c2, run, o);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+                V p;
+                as_operand(s[0], h, p);
 #pragma unroll
-                        for (int c = 0; c < CT; ++c) {
-                            V seen;
-#pragma unroll
-                            for (int r = 0; r < 8; ++r) {
-                                const int j = j0 + 32 * u + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, d = pos[c] - j;
-                                seen[r] = d >= 0 && (d < a.window || j < a.sinks) ? 1.f : 0.f;
-                            }
-#pragma unroll
-                            for (int d = 0; d < DT; ++d)
-                                product_of_some(o[c][d], Tile::by_columns(vt, lane, (KEYS ? wave * 32 : 0) + 32 * u + 16 * h, d), p[c][u][h], seen, true);
-                        }
-            } else {
-#pragma unroll
-                for (int u = 0; u < NS; ++u)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            const V f = Tile::by_columns(vt, lane, (KEYS ? wave * 32 : 0) + 32 * u + 16 * h, d);
-#pragma unroll
-                            for (int c = 0; c < CT; ++c) o[c][d] = mfma(f, p[c][u][h], o[c][d]);
-                        }
+                for (int d = 0; d < DT; ++d) {
+                    const V v = Tile::by_columns(buf + Tile::BYTES, lane, wave * 32 + 16 * h, d);
+                    if (careful.value && !all)
+                        product_of_some(o[d], v, p, marks<V>(a, pos, j0 + 16 * h, half), true);
+                    else
+                        o[d] = mfma(v, p, o[d]);
+                }
             }
         }
         bool odd = false;
-        if (!careful.value)
+        if (!careful.value && counts)
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
-                if (counts(c))
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) odd |= o[c][d][r] != o[c][d][r];
+                for (int r = 0; r < 16; ++r) odd |= o[d][r] != o[d][r];
         return __syncthreads_or(odd); // every wave is behind its last read of a tile
     };
-    // Where that left something that is no number it may come from a token that the column does not see: once more, with care.
-    if (__builtin_expect(run(Is<false>()), 0)) run(Is<true>());
-#pragma unroll
-    for (int c = 0; c < CT; ++c) l[c] += other_half(l[c]);
+    // What is no number may come from a token that the column does not see: once more then, with care.
+    if (__builtin_expect(go(Is<false>()), 0)) go(Is<true>());
 
-    const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq;
-    float *part = a.part + (int64_t)split * rows * DP, *part_lse = a.part + (int64_t)a.splits * rows * DP + (int64_t)split * rows;
-    if constexpr (!KEYS) {
+    const float l = run.l + other_half(run.l);
+    constexpr int PITCH = DP + 4;
+    float *sums = (float *)lds, *ml = sums + NW * 32 * PITCH;
+    static_assert((NW * 32 * PITCH + NW * 64) * 4 <= 4 * Tile::BYTES, "room for the waves' sums");
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            if (!there[c]) continue;
-            const float lse2 = counts(c) && !(l[c] == 0.f) ? m[c] + __builtin_amdgcn_logf(l[c]) : -__builtin_inff();
-            const float f = counts(c) && !(l[c] == 0.f) ? 1.f / l[c] : 0.f;
-            const int64_t row = ((int64_t)kn * a.H + head[c]) * a.Sq + i[c];
-            if (!counts(c))
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[c][d] = grawa_f32x16{};
-            if (a.splits > 1) {
+        for (int r = 0; r < 4; ++r)
+            *(grawa_f32x4v *)(sums + (wave * 32 + (lane & 31)) * PITCH + 32 * d + 8 * r + 4 * half) = grawa_f32x4v{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+    if (half == 0) ml[wave * 64 + lane] = run.m, ml[wave * 64 + 32 + lane] = l;
+    __syncthreads();
+    constexpr int LPC = NW * 2, EPL = DP / LPC; // threads of a column, elements of each
+    const int cl = threadIdx.x / LPC, e0 = threadIdx.x % LPC * EPL, c = cb * 32 + cl;
+    if (c >= a.share * a.Sq) return;
+    const int h = g * a.share + c / a.Sq, ii = c % a.Sq, p = at.start + ii;
+    float top = -__builtin_inff(), total = 0.f, v[EPL];
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[w * 64 + cl]);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) store_column<false>((char *)(part + row * DP), lane, d, DP, o[c][d], f);
-                if (half == 0) part_lse[row] = lse2;
-                continue;
-            }
-            char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i[c] * a.o.token + (int64_t)head[c] * a.o.head;
+    for (int e = 0; e < EPL; ++e) v[e] = 0.f;
+    for (int w = 0; w < NW; ++w) {
+        const float mw = ml[w * 64 + cl], lw = ml[w * 64 + 32 + cl];
+        if (lw == 0.f) continue;
+        const float f = __builtin_amdgcn_exp2f(mw - top);
+        total += lw * f;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) store_column<BF16>(out, lane, d, a.D, o[c][d], f);
-            if (a.lse && half == 0) a.lse[row] = lse2 * LN2;
-        }
-    } else {
-        constexpr int PITCH = DP + 4;
-        float *sums = (float *)lds, *ml = sums + NW * 32 * PITCH; // every wave is behind its last read of a tile
-        static_assert((NW * 32 * PITCH + NW * 64) * 4 <= 4 * Tile::BYTES, "room for the waves' sums");
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *(grawa_f32x4v *)(sums + (wave * 32 + (lane & 31)) * PITCH + 32 * d + 8 * r + 4 * half) =
-                    grawa_f32x4v{o[0][d][4 * r], o[0][d][4 * r + 1], o[0][d][4 * r + 2], o[0][d][4 * r + 3]};
-        if (half == 0) ml[wave * 64 + lane] = m[0], ml[wave * 64 + 32 + lane] = l[0];
-        __syncthreads();
-        constexpr int LPC = NW * 2, EPL = DP / LPC; // threads of a column, elements of each
-        const int cl = threadIdx.x / LPC, e0 = threadIdx.x % LPC * EPL, col = qb * 32 + cl;
-        if (col < a.share * a.Sq) {
-            const int h = g * a.share + col / a.Sq, ii = col % a.Sq, p = at.start + ii;
-            float top = -__builtin_inff(), total = 0.f, v[EPL];
-            for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[w * 64 + cl]);
-#pragma unroll
-            for (int e = 0; e < EPL; ++e) v[e] = 0.f;
-            for (int w = 0; w < NW; ++w) {
-                const float mw = ml[w * 64 + cl], f = mw == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-                if (f == 0.f && ml[w * 64 + 32 + cl] == 0.f) continue;
-                total += ml[w * 64 + 32 + cl] * f;
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) v[e] += sums[(w * 32 + cl) * PITCH + e0 + e] * f;
-            }
-            const bool row_counts = p >= 0 && p < at.length && !(total == 0.f);
-            const float f = row_counts ? 1.f / total : 0.f, lse2 = row_counts ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
-            const int64_t row = ((int64_t)kn * a.H + h) * a.Sq + ii;
-            char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)ii * a.o.token + (int64_t)h * a.o.head;
-#pragma unroll
-            for (int e = 0; e < EPL; ++e) v[e] = row_counts ? v[e] * f : 0.f;
-            if (a.splits > 1) {
-#pragma unroll
-                for (int e = 0; e < EPL; e += 4) *(grawa_f32x4v *)(part + row * DP + e0 + e) = grawa_f32x4v{v[e], v[e + 1], v[e + 2], v[e + 3]};
-                if (e0 == 0) part_lse[row] = lse2;
-            } else {
-                constexpr int PN = GrawaPiece<BF16>::N;
-#pragma unroll
-                for (int e = 0; e < EPL; e += PN)
-                    if (e0 + e < a.D) store_piece<BF16>(out + (e0 + e) * ES, PN, v + e);
-                if (a.lse && e0 == 0) a.lse[row] = lse2 * LN2;
-            }
-        }
+        for (int e = 0; e < EPL; ++e) v[e] += sums[(w * 32 + cl) * PITCH + e0 + e] * f;
     }
+    const bool sum = p >= 0 && p < at.length && !(total == 0.f);
+    const float f = sum ? 1.f / total : 0.f, lse2 = sum ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
+    const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row = ((int64_t)kn * a.H + h) * a.Sq + ii;
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) v[e] = sum ? v[e] * f : 0.f;
+    if (a.splits > 1) {
+        float *part = a.part + ((int64_t)split * rows + row) * DP + e0;
+#pragma unroll
+        for (int e = 0; e < EPL; e += 4) *(grawa_f32x4v *)(part + e) = grawa_f32x4v{v[e], v[e + 1], v[e + 2], v[e + 3]};
+        if (e0 == 0) a.part[(int64_t)a.splits * rows * DP + (int64_t)split * rows + row] = lse2;
+        return;
+    }
+    char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)ii * a.o.token + (int64_t)h * a.o.head;
+    constexpr int PN = GrawaPiece<BF16>::N;
+#pragma unroll
+    for (int e = 0; e < EPL; e += PN)
+        if (e0 + e < a.D) store_piece<BF16>(out + (e0 + e) * ES, PN, v + e);
+    if (a.lse && e0 == 0) a.lse[row] = lse2 * LN2;
 #endif
 }
 
 // o = sum over the splits of o_s exp(lse_s - lse): a wave has 64 / (DP / 8) rows.
-template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_join(GrawaAttend a)
+template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_join([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int LPR = DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N;
@@ -339,16 +454,17 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     if ((int64_t)a.share * a.Sq <= KEYS_COLUMNS) {
         a.blocks = (a.share * a.Sq + 31) / 32;
         a.splits = splits_of(kn * a.G * a.blocks, rows, DP, (seen + 32 * KW - 1) / (32 * KW), part_floats);
-        hipLaunchKernelGGL((k_attend<BF16, DP, 1, true, BIAS, KW>), dim3((uint32_t)(kn * a.G * a.blocks * a.splits)), dim3(KW * 64), 0, st, a);
+        const uint32_t grid = grid_of(kn * a.G, (int64_t)a.blocks * a.splits, a.by_xcd);
+        hipLaunchKernelGGL((k_attend_few<BF16, DP, BIAS, KW>), dim3(grid), dim3(KW * 64), 0, st, a);
     } else {
-        const bool wide = BF16 && kn * a.H * ((a.Sq + 255) / 256) >= 512;
+        const bool wide = BF16 && DP == 64 && kn * a.H * ((a.Sq + 255) / 256) >= 512;
         a.blocks = wide ? (a.Sq + 255) / 256 : (a.Sq + 127) / 128;
         a.splits = splits_of(kn * a.H * a.blocks, rows, DP, (seen + 63) / 64, part_floats);
-        const dim3 grid((uint32_t)(kn * a.H * a.blocks * a.splits));
-        if (BF16 && wide)
-            hipLaunchKernelGGL((k_attend<BF16, DP, BF16 ? 2 : 1, false, BIAS, 4>), grid, dim3(256), 0, st, a);
+        const uint32_t grid = grid_of(kn * a.H, (int64_t)a.blocks * a.splits, a.by_xcd);
+        if (wide)
+            hipLaunchKernelGGL((k_attend<BF16, DP, BF16 && DP == 64 ? 2 : 1, BIAS>), dim3(grid), dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL((k_attend<BF16, DP, 1, false, BIAS, 4>), grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL((k_attend<BF16, DP, 1, BIAS>), dim3(grid), dim3(256), 0, st, a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

@@ -9,23 +9,25 @@ namespace {
 
 // A block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.
 template <bool BF16, int DP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_attend_dq(GrawaAttend a)
+__global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int BK = 64, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
     typedef HeadTile<BF16, DP, BK, 4> Tile;
     typedef typename Tile::V V;
     __shared__ __attribute__((aligned(1024))) char lds[BUFS * 2 * Tile::BYTES]; // keys and values
-    __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];              // the bias by distance
+    __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];                     // the bias by distance
     __shared__ float by_distance[BIAS ? 4 : 1][BIAS ? GRAWA_MAX_DISTANCES : 1]; // of each wave: sums of dS
     __shared__ float square[BIAS ? 4 : 1][BIAS ? 32 * 33 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int t = (int)run_of(blockIdx.x, gridDim.x), hd = t / a.blocks, qb = a.blocks - 1 - (t - hd * a.blocks);
-    const int kn = hd / a.H, head = hd - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
+    const int heads = a.K * a.N * a.H;
+    const Turn turn = turn_of(blockIdx.x, heads, a.by_xcd);
+    if (turn.head >= heads) return;
+    const int qb = a.blocks - 1 - turn.block;
+    const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
     const Place at = place_of(a, kn);
     const int i = qb * 128 + wave * 32 + (lane & 31), pos = at.start + i;
     const bool there = i < a.Sq, counts = there && pos >= 0 && pos < at.length;
-    const int64_t row = ((int64_t)kn * a.H + head) * a.Sq + i, row2 = ((int64_t)kn * a.H + head) * a.row_pitch + i;
 
     V q[KS], go[KS];
     float delta = 0.f;
@@ -43,16 +45,21 @@ __global__ __launch_bounds__(256, 2) void k_attend_dq(GrawaAttend a)
         }
         delta += other_half(delta);
     }
-    float lse = counts ? a.lse[row] * LOG2E : __builtin_inff();
+    float lse = counts ? a.lse[((int64_t)kn * a.H + head) * a.Sq + i] * LOG2E : __builtin_inff();
     if (lse == -__builtin_inff()) lse = __builtin_inff(); // the row sees nothing
-    if (half == 0 && i < a.row_pitch) a.row_lse[row2] = lse, a.row_dot[row2] = delta;
+    if (half == 0 && i < a.row_pitch) {
+        const int64_t row = ((int64_t)kn * a.H + head) * a.row_pitch + i;
+        a.row_lse[row] = lse;
+        a.row_dot[row] = delta;
+    }
 
     const float c2 = a.scale * LOG2E;
     float far = 0.f;
     if constexpr (BIAS) {
-        const char *bias = a.bias.p + (int64_t)k * a.bias.worker * ES + (int64_t)head * a.buckets * ES;
+        const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + head * a.buckets) * ES;
         far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
         for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
+        for (int d = lane; d < a.distances; d += 64) by_distance[wave][d] = 0.f;
     }
 
     const int p0 = at.start + qb * 128, p1 = at.start + min((qb + 1) * 128, a.Sq) - 1, w0 = p0 + wave * 32, w1 = w0 + 31;
@@ -64,113 +71,126 @@ __global__ __launch_bounds__(256, 2) void k_attend_dq(GrawaAttend a)
     Tile lk, lv;
     lk.init(wave, lane, (uint32_t)a.k.token, a.D);
     lv.init(wave, lane, (uint32_t)a.v.token, a.D);
+    const auto tile_of = [&](int it) { return (it < first_tiles ? it : it - first_tiles + t0) * BK; };
     const auto load = [&](int it, char *buf) {
-        const int j0 = (it < first_tiles ? it : it - first_tiles + t0) * BK;
+        const int j0 = tile_of(it);
         lk.load(buf, wave, Tile::rsrc(kp + (int64_t)j0 * a.k.token, at.length - j0, (uint32_t)a.k.token, a.D));
         lv.load(buf + Tile::BYTES, wave, Tile::rsrc(vp + (int64_t)j0 * a.v.token, at.length - j0, (uint32_t)a.v.token, a.D));
+    };
+    const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
+    const auto all = [&](int j0) { return j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
+    // dS of 32 keys.
+    const auto slopes = [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
+        grawa_f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), q[ks], s);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), go[ks], dp);
+        const bool is_far = BIAS && w0 - (j0 + 31) >= a.distances - 1;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float b = -lse;
+            if constexpr (BIAS) b += is_far ? far : table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, b)) * (dp[r] - delta);
+        }
+        if (!all(j0))
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : 0.f;
+        return s;
     };
 
     grawa_f32x16 dq[DT];
     float far_sum = 0.f; // of dS from the last distance of the table on
-    const auto run = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
+    for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
+    const auto step = [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
+        const grawa_f32x16 s = slopes(buf, u, j0);
         if constexpr (BIAS) {
-            far_sum = 0.f;
-            for (int d = lane; d < a.distances; d += 64) by_distance[wave][d] = 0.f;
-        }
-        if (BUFS == 2 && tiles) load(0, lds);
-        for (int it = 0; it < tiles; ++it) {
-            char *buf = lds + (BUFS == 2 ? it & 1 : 0) * 2 * Tile::BYTES;
-            if (BUFS == 1) {
-                landed();
-                load(it, buf);
-            }
-            landed();
-            if (BUFS == 2 && it + 1 < tiles) load(it + 1, lds + ((it + 1) & 1) * 2 * Tile::BYTES);
-            const int tile0 = (it < first_tiles ? it : it - first_tiles + t0) * BK;
+            if (w0 - (j0 + 31) >= a.distances - 1) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int j0 = tile0 + 32 * u, j1 = j0 + 31;
-                if (j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks)) continue;
-                const bool all = j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks);
-                grawa_f32x16 s = {}, dp = {};
+                for (int r = 0; r < 16; ++r) far_sum += s[r];
+            } else { // along the diagonals of the square: lane x has those that are x - 31 above the first
+                float *sq = square[wave];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), q[ks], s);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), go[ks], dp);
-                const bool is_far = BIAS && w0 - j1 >= a.distances - 1;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float b = 0.f;
-                    if constexpr (BIAS) b = is_far ? far : table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
-                    s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, b - lse)) * (dp[r] - delta);
-                }
-                if (!all)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + (r & 3) + 8 * (r >> 2) + 4 * half, d = pos - j;
-                        s[r] = d >= 0 && (d < a.window || j < a.sinks) ? s[r] : 0.f;
-                    }
-                if constexpr (BIAS) {
-                    if (is_far) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) far_sum += s[r];
-                    } else { // along the diagonals of the square: lane x has those that are x - 31 above the first
-                        float *sq = square[wave];
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) sq[((r & 3) + 8 * (r >> 2) + 4 * half) * 33 + (lane & 31)] = s[r];
-                        wave_order();
-                        float sum = 0.f;
-                        const int x = lane - 31;
-                        for (int r = 0; r < 32; ++r)
-                            if (r + x >= 0 && r + x < 32) sum += sq[r * 33 + r + x];
-                        const int d = w0 - j0 + x;
-                        if (d >= a.distances - 1)
-                            far_sum += sum;
-                        else if (d >= 0 && lane < 63)
-                            by_distance[wave][d] += sum;
-                        wave_order();
-                    }
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    V w;
-                    as_operand(s, h, w);
-                    if (careful.value && !all) {
-                        V seen;
-#pragma unroll
-                        for (int r = 0; r < 8; ++r) {
-                            const int j = j0 + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, d = pos - j;
-                            seen[r] = d >= 0 && (d < a.window || j < a.sinks) ? 1.f : 0.f;
-                        }
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) product_of_some(dq[d], Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, seen, false);
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) dq[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, dq[d]);
-                    }
-                }
+                for (int r = 0; r < 16; ++r) sq[((r & 3) + 8 * (r >> 2) + 4 * half) * 33 + (lane & 31)] = s[r];
+                wave_order();
+                float sum = 0.f;
+                const int x = lane - 31;
+                for (int r = 0; r < 32; ++r)
+                    if (r + x >= 0 && r + x < 32) sum += sq[r * 33 + r + x];
+                const int d = w0 - j0 + x;
+                if (d >= a.distances - 1)
+                    far_sum += sum;
+                else if (d >= 0 && lane < 63)
+                    by_distance[wave][d] += sum;
+                wave_order();
             }
         }
-        bool odd = false;
-        if (!careful.value && counts)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+        for (int h = 0; h < 2; ++h) {
+            V w;
+            as_operand(s, h, w);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) odd |= dq[d][r] != dq[d][r];
-        return __syncthreads_or(odd);
+            for (int d = 0; d < DT; ++d) dq[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, dq[d]);
+        }
     };
-    // What is no number may come from a token that the query does not see: once more, with care.
-    if (__builtin_expect(run(Is<false>()), 0)) run(Is<true>());
-
-    if (there) {
-        char *out = a.dq.p + (int64_t)k * a.dq.worker + (int64_t)n * a.dq.seq + (int64_t)i * a.dq.token + (int64_t)head * a.dq.head;
-        if (!counts)
+    if (BUFS == 2 && tiles) load(0, lds);
+    for (int it = 0; it < tiles; ++it) {
+        char *buf = lds + (BUFS == 2 ? it & 1 : 0) * 2 * Tile::BYTES;
+        if (BUFS == 1) {
+            landed();
+            load(it, buf);
+        }
+        landed();
+        if (BUFS == 2 && it + 1 < tiles) load(it + 1, lds + ((it + 1) & 1) * 2 * Tile::BYTES);
+        for (int u = 0; u < 2; ++u) {
+            const int j0 = tile_of(it) + 32 * u;
+            if (!none(j0)) step(buf, u, j0);
+        }
+    }
+    bool odd = false;
+    if (counts)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) store_column<BF16>(out, lane, d, a.D, dq[d], a.scale);
+            for (int r = 0; r < 16; ++r) odd |= dq[d][r] != dq[d][r];
+    char *out = a.dq.p + (int64_t)k * a.dq.worker + (int64_t)n * a.dq.seq + (int64_t)i * a.dq.token + (int64_t)head * a.dq.head;
+    const auto put = [&](int d, const grawa_f32x16 &sums) {
+        if (!there) return;
+        grawa_f32x16 v;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[r] = counts ? sums[r] : 0.f;
+        store_column<BF16>(out, lane, d, a.D, v, a.scale);
+    };
+    // What is no number may come from a token that the query does not see: once more then, with care.
+    if (__builtin_expect(!__syncthreads_or(odd), 1)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) put(d, dq[d]);
+    } else {
+        for (int d = 0; d < DT; ++d) {
+            grawa_f32x16 sums = {};
+            for (int it = 0; it < tiles; ++it) {
+                landed();
+                load(it, lds);
+                landed();
+                for (int u = 0; u < 2; ++u) {
+                    const int j0 = tile_of(it) + 32 * u;
+                    if (none(j0)) continue;
+                    const grawa_f32x16 s = slopes(lds, u, j0);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        V w;
+                        as_operand(s, h, w);
+                        const V c = Tile::by_columns(lds, lane, 32 * u + 16 * h, d);
+                        if (all(j0))
+                            sums = mfma(c, w, sums);
+                        else
+                            product_of_some(sums, c, w, marks<V>(a, pos, j0 + 16 * h, half), false);
+                    }
+                }
+            }
+            put(d, sums);
+        }
     }
     if constexpr (BIAS) {
 #pragma unroll
@@ -188,7 +208,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_dq(GrawaAttend a)
 }
 
 // dbias of a head: the sums of its blocks, in order.
-template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums(GrawaAttend a)
+template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     const int head = blockIdx.x, k = blockIdx.y, b = threadIdx.x;
@@ -203,21 +223,27 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums(GrawaAtt
 #endif
 }
 
-// A block has 128 keys, a wave 32 of them; all waves share tiles of 64 queries and the gradients of their outputs, of one head after
-// the other.  splits > 1 (sink_splits for the keys that all queries see): that many blocks share the queries of a block of keys.
-template <bool BF16, int DP, bool BIAS>
-__global__ __launch_bounds__(256, BF16 && DP == 64 ? 2 : 1) void k_attend_dkv(GrawaAttend a)
+// A block has 32 keys for each of its NW waves; all waves share tiles of 64 queries and the gradients of their outputs, of one head
+// after the other.  Keys and the sums of dk and dv stay in registers, values too where heads have 64 elements; with 128 they do not fit
+// and are read from LDS (in registers all the same, 8 heads of 32 x 16384 tokens spilled and took 22.6 ms).  splits > 1 (sink_splits for the keys that all queries see): that many blocks share the queries of a block of keys.
+template <bool BF16, int DP, bool BIAS, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_dkv([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int BQ = 64, BKV = 128, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
-    typedef HeadTile<BF16, DP, BQ, 4> Tile;
+    constexpr int BQ = 64, BKV = 32 * NW, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
+    constexpr bool KEEP = DP == 64; // values in registers
+    typedef HeadTile<BF16, DP, BQ, NW> Tile;
+    typedef HeadTile<BF16, DP, BKV, NW> Values;
     typedef typename Tile::V V;
     __shared__ __attribute__((aligned(1024))) char lds[BUFS * 2 * Tile::BYTES]; // queries and gradients of outputs
     __shared__ __attribute__((aligned(1024))) float of_rows[2][2][BQ];          // log2 of the sums of exponentials, do . o
+    __shared__ __attribute__((aligned(1024))) char values[KEEP ? 16 : Values::BYTES];
     __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int per = a.sink_blocks * a.sink_splits + (a.key_blocks - a.sink_blocks) * a.splits;
-    const int t = (int)run_of(blockIdx.x, gridDim.x), hd = t / per, item = t - hd * per, sink_items = a.sink_blocks * a.sink_splits;
+    const int sink_items = a.sink_blocks * a.sink_splits, per = sink_items + (a.key_blocks - a.sink_blocks) * a.splits, groups = a.K * a.N * a.G;
+    const Turn turn = turn_of(blockIdx.x, groups, a.by_xcd);
+    if (turn.head >= groups) return;
+    const int hd = turn.head, item = turn.block;
     const bool sink = item < sink_items;
     const int splits = sink ? a.sink_splits : a.splits, kb = sink ? item / a.sink_splits : a.sink_blocks + (item - sink_items) / a.splits;
     const int split = sink ? item % a.sink_splits : (item - sink_items) % a.splits;
@@ -226,166 +252,230 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 2 : 1) void k_attend_dkv(Gr
     const int b0 = kb * BKV, w0 = b0 + wave * 32, w1 = w0 + 31, j = w0 + (lane & 31);
     const bool there = j < a.Sk, counts = j < at.length;
 
-    V kf[KS], vf[KS];
+    V kf[KS], vf[KEEP ? KS : 1];
     {
         const char *pk = a.k.p + (int64_t)k * a.k.worker + (int64_t)n * a.k.seq + (int64_t)j * a.k.token + (int64_t)g * a.k.head;
         const char *pv = a.v.p + (int64_t)k * a.v.worker + (int64_t)n * a.v.seq + (int64_t)j * a.v.token + (int64_t)g * a.v.head;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             kf[ks] = load_line<BF16>(pk, 16 * ks + 8 * half, a.D, counts);
-            vf[ks] = load_line<BF16>(pv, 16 * ks + 8 * half, a.D, counts);
+            if constexpr (KEEP) vf[ks] = load_line<BF16>(pv, 16 * ks + 8 * half, a.D, counts);
         }
     }
+    if constexpr (!KEEP) { // lands before the first tile does
+        Values lv;
+        lv.init(wave, lane, (uint32_t)a.v.token, a.D);
+        lv.load(values, wave, Values::rsrc(a.v.p + (int64_t)k * a.v.worker + (int64_t)n * a.v.seq + (int64_t)b0 * a.v.token + (int64_t)g * a.v.head,
+                                           at.length - b0, (uint32_t)a.v.token, a.D));
+    }
+    const auto value = [&](int ks) {
+        if constexpr (KEEP)
+            return vf[ks];
+        else
+            return Values::by_rows(values, lane, wave * 32, ks);
+    };
     const float c2 = a.scale * LOG2E;
 
     // Queries that see any of the block's keys: rows i0 ... i1 of the call, by tiles, of each head.
     const int last = min(at.length - 1 - at.start, a.Sq - 1);
-    const int i0 = max(0, max(b0, 0) - at.start), i1 = sink ? last : min(last, b0 + BKV - 1 + a.window - 1 - at.start);
+    const int i0 = max(0, b0 - at.start), i1 = sink ? last : min(last, b0 + BKV - 1 + a.window - 1 - at.start);
     const int t0 = i0 / BQ, tiles = b0 < at.length && i1 >= i0 ? i1 / BQ - t0 + 1 : 0, all_tiles = tiles * a.share;
     const int from = (int)((int64_t)all_tiles * split / splits), to = (int)((int64_t)all_tiles * (split + 1) / splits);
     Tile lq, lg;
     lq.init(wave, lane, (uint32_t)a.q.token, a.D);
     lg.init(wave, lane, (uint32_t)a.go.token, a.D);
-    const auto load = [&](int it, int buf) {
-        const int h = it / tiles, head = g * a.share + h, i = (t0 + it - h * tiles) * BQ;
-        char *to_lds = lds + (BUFS == 2 ? buf : 0) * 2 * Tile::BYTES;
-        const char *pq = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i * a.q.token + (int64_t)head * a.q.head;
-        const char *pg = a.go.p + (int64_t)k * a.go.worker + (int64_t)n * a.go.seq + (int64_t)i * a.go.token + (int64_t)head * a.go.head;
-        lq.load(to_lds, wave, Tile::rsrc(pq, last + 1 - i, (uint32_t)a.q.token, a.D));
-        lg.load(to_lds + Tile::BYTES, wave, Tile::rsrc(pg, last + 1 - i, (uint32_t)a.go.token, a.D));
+    const char *qp = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq, *gp = a.go.p + (int64_t)k * a.go.worker + (int64_t)n * a.go.seq;
+    struct At {
+        int h, tile; // head of the group, first query of the tile
+    };
+    const auto place = [&](int it) {
+        const int h = it / tiles;
+        return At{h, (t0 + it - h * tiles) * BQ};
+    };
+    const auto load = [&](At t, int b) {
+        const int head = g * a.share + t.h;
+        char *buf = lds + b * 2 * Tile::BYTES;
+        lq.load(buf, wave, Tile::rsrc(qp + (int64_t)t.tile * a.q.token + (int64_t)head * a.q.head, last + 1 - t.tile, (uint32_t)a.q.token, a.D));
+        lg.load(buf + Tile::BYTES, wave, Tile::rsrc(gp + (int64_t)t.tile * a.go.token + (int64_t)head * a.go.head, last + 1 - t.tile, (uint32_t)a.go.token, a.D));
         if (wave < 2) { // rows up to the pitch, a multiple of a tile, are there
-            const float *p = (wave ? a.row_dot : a.row_lse) + ((int64_t)kn * a.H + head) * a.row_pitch + i;
+            const float *p = (wave ? a.row_dot : a.row_lse) + ((int64_t)kn * a.H + head) * a.row_pitch + t.tile;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, BQ * 4, 0x00020000),
-                                                     (GRAWA_LDS_AT void *)of_rows[buf][wave], 4, (uint32_t)lane * 4, 0, 0, 0);
+                                                     (GRAWA_LDS_AT void *)of_rows[b][wave], 4, (uint32_t)lane * 4, 0, 0, 0);
         }
+    };
+    const auto next = [&](At t) {
+        t.tile += BQ;
+        if (t.tile >= (t0 + tiles) * BQ) t.tile = t0 * BQ, ++t.h;
+        return t;
+    };
+    int table_of = -1;
+    const auto tabulate = [&](int h) {
+        if constexpr (BIAS) {
+            if (h == table_of) return;
+            // the other waves are behind their last look at the table of the head before
+            const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + (int64_t)(g * a.share + h) * a.buckets) * ES;
+            for (int d = threadIdx.x; d < a.distances; d += NW * 64) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
+            table_of = h;
+            __syncthreads();
+        }
+    };
+    // Between the parts of a step nothing is moved where registers are few: fragments asked for early would push others out.
+    const auto few_registers = []() __attribute__((always_inline)) {
+        if (DP == 128) __builtin_amdgcn_sched_barrier(0);
+    };
+    // p0: position of the first of 32 queries
+    const auto none = [&](int p0) { return w0 > p0 + 31 || w0 >= at.length || (w1 <= p0 - a.window && w0 >= a.sinks); }; // of the wave's pairs count
+    const auto all = [&](int p0) { return w1 <= p0 && (p0 + 31 - w0 < a.window || w1 < a.sinks); };
+    // P and dS of 32 queries.
+    const auto slopes = [&](const char *buf, int b, int u, int p0, grawa_f32x16 &s, grawa_f32x16 &dp) __attribute__((always_inline)) {
+        s = grawa_f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), kf[ks], s);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const grawa_f32x4v dot = *(const grawa_f32x4v *)(of_rows[b][1] + 32 * u + 8 * x + 4 * half);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) dp[4 * x + y] = -dot[y];
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), value(ks), dp);
+        few_registers();
+        const bool is_far = BIAS && p0 - w1 >= a.distances - 1;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const grawa_f32x4v lse = *(const grawa_f32x4v *)(of_rows[b][0] + 32 * u + 8 * x + 4 * half);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int r = 4 * x + y;
+                float c = -lse[y];
+                if constexpr (BIAS) c += table[is_far ? a.distances - 1 : clamp_int(p0 + 8 * x + 4 * half + y - j, 0, a.distances - 1)];
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, c));
+                dp[r] *= s[r];
+            }
+        }
+        if (!all(p0))
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const bool seen = sees(a, p0 + (r & 3) + 8 * (r >> 2) + 4 * half, j);
+                s[r] = seen ? s[r] : 0.f;
+                dp[r] = seen ? dp[r] : 0.f;
+            }
+        few_registers();
     };
 
     grawa_f32x16 dk[DT], dv[DT];
-    const auto run = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dk[d] = dv[d] = grawa_f32x16{};
-        int table_of = -1;
-        if (BUFS == 2 && from < to) load(from, 0);
-        for (int it = from; it < to; ++it) {
-            const int b = BUFS == 2 ? (it - from) & 1 : 0, h = it / tiles, tile0 = (t0 + it - h * tiles) * BQ;
+    for (int d = 0; d < DT; ++d) dk[d] = dv[d] = grawa_f32x16{};
+    if (from < to) {
+        At t = place(from), ahead = t;
+        if (BUFS == 2) load(t, 0);
+        for (int it = from; it < to; ++it, t = next(t)) {
+            const int b = BUFS == 2 ? (it - from) & 1 : 0;
             const char *buf = lds + b * 2 * Tile::BYTES;
             if (BUFS == 1) {
                 landed();
-                load(it, 0);
+                load(t, 0);
             }
             landed();
-            if (BUFS == 2 && it + 1 < to) load(it + 1, b ^ 1);
-            if constexpr (BIAS)
-                if (h != table_of) { // the other waves are behind their last look at the table of the head before
-                    const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + (int64_t)(g * a.share + h) * a.buckets) * ES;
-                    for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
-                    table_of = h;
-                    __syncthreads();
-                }
-#pragma unroll
+            if (BUFS == 2 && it + 1 < to) load(ahead = next(ahead), b ^ 1);
+            tabulate(t.h);
+            // One way through the step, masked or not: with two the sums change their registers between them.
             for (int u = 0; u < 2; ++u) {
-                const int p0 = at.start + tile0 + 32 * u, p1 = p0 + 31; // positions of the queries
-                if (w0 > p1 || w0 >= at.length || (w1 <= p0 - a.window && w0 >= a.sinks)) continue;
-                const bool all = w1 <= p0 && (p1 - w0 < a.window || w1 < a.sinks);
-                grawa_f32x16 s = {}, dp = {};
+                const int p0 = at.start + t.tile + 32 * u;
+                if (none(p0)) continue;
+                grawa_f32x16 s, dp;
+                slopes(buf, b, u, p0, s, dp);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), kf[ks], s);
+                for (int h = 0; h < 2; ++h) {
+                    V w;
+                    as_operand(s, h, w);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), vf[ks], dp);
-                const bool is_far = BIAS && p0 - w1 >= a.distances - 1;
-                V pw[2], dw[2];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int x = (r & 3) + 8 * (r >> 2) + 4 * half, d = p0 + x - j;
-                    float bias = 0.f;
-                    if constexpr (BIAS) bias = is_far ? table[a.distances - 1] : table[clamp_int(d, 0, a.distances - 1)];
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, bias - of_rows[b][0][32 * u + x]));
-                    dp[r] = p * (dp[r] - of_rows[b][1][32 * u + x]);
-                    s[r] = p;
-                    if (!all) {
-                        const bool seen = d >= 0 && (d < a.window || j < a.sinks);
-                        s[r] = seen ? s[r] : 0.f;
-                        dp[r] = seen ? dp[r] : 0.f;
-                    }
+                    for (int d = 0; d < DT; ++d) dv[d] = mfma(Tile::by_columns(buf + Tile::BYTES, lane, 32 * u + 16 * h, d), w, dv[d]);
+                    few_registers();
                 }
-                as_operand(s, 0, pw[0]);
-                as_operand(s, 1, pw[1]);
-                as_operand(dp, 0, dw[0]);
-                as_operand(dp, 1, dw[1]);
 #pragma unroll
-                for (int h2 = 0; h2 < 2; ++h2) {
-                    if (careful.value && !all) {
-                        V seen;
+                for (int h = 0; h < 2; ++h) {
+                    V w;
+                    as_operand(dp, h, w);
 #pragma unroll
-                        for (int r = 0; r < 8; ++r) {
-                            const int d = p0 + 16 * h2 + (r & 3) + 8 * (r >> 2) + 4 * half - j;
-                            seen[r] = d >= 0 && (d < a.window || j < a.sinks) ? 1.f : 0.f;
-                        }
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            product_of_some(dv[d], Tile::by_columns(buf + Tile::BYTES, lane, 32 * u + 16 * h2, d), pw[h2], seen, true);
-                            product_of_some(dk[d], Tile::by_columns(buf, lane, 32 * u + 16 * h2, d), dw[h2], seen, false);
-                        }
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            dv[d] = mfma(Tile::by_columns(buf + Tile::BYTES, lane, 32 * u + 16 * h2, d), pw[h2], dv[d]);
-                            dk[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h2, d), dw[h2], dk[d]);
-                        }
-                    }
+                    for (int d = 0; d < DT; ++d) dk[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, dk[d]);
+                    few_registers();
                 }
             }
         }
-        bool odd = false;
-        if (!careful.value && counts)
+    }
+    bool odd = false;
+    if (counts)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) odd |= dk[d][r] != dk[d][r] || dv[d][r] != dv[d][r];
-        return __syncthreads_or(odd);
-    };
-    if (__builtin_expect(run(Is<false>()), 0)) run(Is<true>());
-
-    if (!there) return;
-    if (!counts)
+            for (int r = 0; r < 16; ++r) odd |= dk[d][r] != dk[d][r] || dv[d][r] != dv[d][r];
+    const auto put = [&](int d, const grawa_f32x16 &k_sums, const grawa_f32x16 &v_sums) {
+        if (!there) return;
+        grawa_f32x16 x, y;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dk[d] = dv[d] = grawa_f32x16{};
-    if (splits > 1) {
-        float *p = a.part + (((int64_t)hd * per + item) * BKV + (j - b0)) * 2 * DP;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            store_column<false>((char *)p, lane, d, DP, dk[d], a.scale);
-            store_column<false>((char *)(p + DP), lane, d, DP, dv[d], 1.f);
+        for (int r = 0; r < 16; ++r) x[r] = counts ? k_sums[r] : 0.f, y[r] = counts ? v_sums[r] : 0.f;
+        if (splits > 1) {
+            float *p = a.part + (((int64_t)hd * per + item) * BKV + (j - b0)) * 2 * DP;
+            store_column<false>((char *)p, lane, d, DP, x, a.scale);
+            store_column<false>((char *)(p + DP), lane, d, DP, y, 1.f);
+        } else {
+            store_column<BF16>(a.dk.p + (int64_t)k * a.dk.worker + (int64_t)n * a.dk.seq + (int64_t)j * a.dk.token + (int64_t)g * a.dk.head, lane, d, a.D, x, a.scale);
+            store_column<BF16>(a.dv.p + (int64_t)k * a.dv.worker + (int64_t)n * a.dv.seq + (int64_t)j * a.dv.token + (int64_t)g * a.dv.head, lane, d, a.D, y, 1.f);
         }
+    };
+    if (__builtin_expect(!__syncthreads_or(odd), 1)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) put(d, dk[d], dv[d]);
         return;
     }
-    char *pk = a.dk.p + (int64_t)k * a.dk.worker + (int64_t)n * a.dk.seq + (int64_t)j * a.dk.token + (int64_t)g * a.dk.head;
-    char *pv = a.dv.p + (int64_t)k * a.dv.worker + (int64_t)n * a.dv.seq + (int64_t)j * a.dv.token + (int64_t)g * a.dv.head;
-#pragma unroll
     for (int d = 0; d < DT; ++d) {
-        store_column<BF16>(pk, lane, d, a.D, dk[d], a.scale);
-        store_column<BF16>(pv, lane, d, a.D, dv[d], 1.f);
+        grawa_f32x16 k_sums = {}, v_sums = {};
+        for (int it = from; it < to; ++it) {
+            const At t = place(it);
+            landed();
+            load(t, 0);
+            landed();
+            tabulate(t.h);
+            for (int u = 0; u < 2; ++u) {
+                const int p0 = at.start + t.tile + 32 * u;
+                if (none(p0)) continue;
+                grawa_f32x16 s, dp;
+                slopes(lds, 0, u, p0, s, dp);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    V w, seen;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) seen[r] = sees(a, p0 + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, j) ? 1.f : 0.f;
+                    as_operand(s, h, w);
+                    product_of_some(v_sums, Tile::by_columns(lds + Tile::BYTES, lane, 32 * u + 16 * h, d), w, seen, true);
+                    as_operand(dp, h, w);
+                    product_of_some(k_sums, Tile::by_columns(lds, lane, 32 * u + 16 * h, d), w, seen, false);
+                }
+            }
+        }
+        put(d, k_sums, v_sums);
     }
 #endif
 }
 
 // dk and dv of the keys whose queries several blocks shared: their sums, in order.
-template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_dkv_join(GrawaAttend a, int first, int blocks)
+template <bool BF16, int DP, int BKV> __global__ __launch_bounds__(256) void k_attend_dkv_join([[maybe_unused]] GrawaAttend a, [[maybe_unused]] int first, [[maybe_unused]] int blocks)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int LPR = 2 * DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N; // threads of a key: half have dk, half dv
-    const int64_t id = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;    // [K N][G][blocks][128]
+    const int64_t id = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;    // [K N][G][blocks][BKV]
     const int x = threadIdx.x % LPR, which = x / (LPR / 2), e0 = x % (LPR / 2) * 8;
     const int per = a.sink_blocks * a.sink_splits + (a.key_blocks - a.sink_blocks) * a.splits;
-    const int key = (int)(id % 128), kb = first + (int)(id / 128 % blocks);
-    const int64_t hd = id / 128 / blocks;
-    const int j = kb * 128 + key;
+    const int key = (int)(id % BKV), kb = first + (int)(id / BKV % blocks);
+    const int64_t hd = id / BKV / blocks;
+    const int j = kb * BKV + key;
     if (hd >= (int64_t)a.K * a.N * a.G || j >= a.Sk) return;
     const bool sink = kb < a.sink_blocks;
     const int splits = sink ? a.sink_splits : a.splits, item = sink ? kb * a.sink_splits : a.sink_blocks * a.sink_splits + (kb - a.sink_blocks) * a.splits;
     float v[8] = {};
     for (int s = 0; s < splits; ++s) {
-        const grawa_f32x4v *p = (const grawa_f32x4v *)(a.part + ((hd * per + item + s) * 128 + key) * 2 * DP + which * DP + e0);
+        const grawa_f32x4v *p = (const grawa_f32x4v *)(a.part + ((hd * per + item + s) * BKV + key) * 2 * DP + which * DP + e0);
         const grawa_f32x4v b = p[0], c = p[1];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] += b[q], v[4 + q] += c[q];
@@ -405,7 +495,8 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     hipError_t e;
     if (a.Sq > 0) {
         a.blocks = (a.Sq + 127) / 128;
-        hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3((uint32_t)(kn * a.H * a.blocks)), dim3(256), 0, st, a);
+        const uint32_t grid = grid_of(kn * a.H, a.blocks, a.by_xcd);
+        hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3(grid), dim3(256), 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (BIAS) {
@@ -413,11 +504,12 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
         hipLaunchKernelGGL((k_bias_sums<BF16>), dim3((uint32_t)a.H, (uint32_t)a.K), dim3(256), 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    a.key_blocks = (a.Sk + 127) / 128;
+    constexpr int NW = BF16 && DP == 128 ? 8 : 4, BKV = 32 * NW;
+    a.key_blocks = (a.Sk + BKV - 1) / BKV;
     // Blocks of keys that all later queries see, and not only those that the window lets through.
-    const int64_t window_tiles = ((int64_t)a.window + 128 + 63) / 64, tiles = (a.Sq + 63) / 64;
-    a.sink_blocks = a.window == GRAWA_NO_WINDOW ? 0 : (int)(((int64_t)a.sinks + 127) / 128 < a.key_blocks ? ((int64_t)a.sinks + 127) / 128 : a.key_blocks);
-    const int64_t groups = kn * a.G, slot = (int64_t)128 * 2 * DP, room = part_floats / slot / groups;
+    const int64_t window_tiles = ((int64_t)a.window + BKV + 63) / 64, tiles = (a.Sq + 63) / 64, sink_blocks = ((int64_t)a.sinks + BKV - 1) / BKV;
+    a.sink_blocks = a.window == GRAWA_NO_WINDOW ? 0 : (int)(sink_blocks < a.key_blocks ? sink_blocks : a.key_blocks);
+    const int64_t groups = kn * a.G, slot = (int64_t)BKV * 2 * DP, room = part_floats / slot / groups;
     const int64_t regular = a.key_blocks - a.sink_blocks, most = (tiles < window_tiles ? tiles : window_tiles) * a.share;
     int64_t splits = regular ? 512 / (groups * regular) : 1;
     if (splits > most / 2) splits = most / 2;
@@ -432,12 +524,13 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     // what is written for joining: all items have a place
     if ((a.splits > 1 || a.sink_splits > 1) && (int64_t)a.sink_blocks * a.sink_splits + regular * a.splits > room) a.splits = a.sink_splits = 1;
     const int64_t per = (int64_t)a.sink_blocks * a.sink_splits + regular * a.splits;
-    hipLaunchKernelGGL((k_attend_dkv<BF16, DP, BIAS>), dim3((uint32_t)(groups * per)), dim3(256), 0, st, a);
+    const uint32_t grid = grid_of(groups, per, a.by_xcd);
+    hipLaunchKernelGGL((k_attend_dkv<BF16, DP, BIAS, NW>), dim3(grid), dim3(NW * 64), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int first = a.sink_splits > 1 ? 0 : a.sink_blocks, end = a.splits > 1 ? a.key_blocks : a.sink_blocks;
     if (end <= first) return hipSuccess;
-    const int64_t ids = groups * (end - first) * 128;
-    hipLaunchKernelGGL((k_attend_dkv_join<BF16, DP>), dim3((uint32_t)(ids * (DP / 4) / 256)), dim3(256), 0, st, a, first, end - first);
+    const int64_t ids = groups * (end - first) * BKV;
+    hipLaunchKernelGGL((k_attend_dkv_join<BF16, DP, BKV>), dim3((uint32_t)(ids * (DP / 4) / 256)), dim3(256), 0, st, a, first, end - first);
     return hipGetLastError();
 }
 

@@ -52,7 +52,7 @@ struct GrawaAttend {
     int window, sinks, buckets, distances;
     float scale;
     int blocks, splits;          // blocks of queries of a head; blocks that share one's keys
-    int accumulate;
+    int accumulate, by_xcd;
     int key_blocks, sink_blocks, sink_splits; // blocks of keys, and the first of them, that all queries see (dk and dv only)
 };
 
