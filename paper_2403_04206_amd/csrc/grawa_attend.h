@@ -100,45 +100,57 @@ template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS_AT void *)(lds + (wave + NW * i) * 1024), 16, first[i % TURNS] + (uint32_t)(i / TURNS) * step, 0, 0, 0);
     }
 
-    // Fragments: an address that all of a tile's share, of which a fragment's differs by some of its low bits and by a constant.
-    static __device__ __forceinline__ uint32_t address(const char *lds) { return (uint32_t)(uintptr_t)(GRAWA_LDS_AT const char *)lds; }
-
-    // Lines row0 ... row0 + 31 (a multiple of 32), elements 16 ks ... of the head.
-    static __device__ __forceinline__ V by_rows(const char *lds, int lane, int row0, int ks)
+    // Fragments: an address of the lane's that all of a tile's share, of which a fragment's differs by some of its low bits and by a constant.
+    static __device__ __forceinline__ uint32_t rows_of(const char *lds, int lane)
     {
         const int row = lane & 31, half = lane >> 5;
-        const uint32_t at = address(lds) + row * RB + (((BF16 ? half : 2 * half) ^ key(row)) << 4);
+        return (uint32_t)(uintptr_t)(GRAWA_LDS_AT const char *)lds + row * RB + (((BF16 ? half : 2 * half) ^ key(row)) << 4);
+    }
+    static __device__ __forceinline__ uint32_t columns_of(const char *lds, int lane)
+    {
+        const int half = lane >> 5, s = lane & 15, row = 4 * half + (s >> 2), m = lane & 31;
+        const uint32_t at = (uint32_t)(uintptr_t)(GRAWA_LDS_AT const char *)lds;
+        if constexpr (BF16) return at + row * RB + (((2 * ((lane >> 4) & 1) + ((s & 3) >> 1)) ^ key(row)) << 4) + (s & 1) * 8;
+        return at + 4 * half * RB + (((m >> 2) ^ key(4 * half)) << 4) + (m & 3) * 4;
+    }
+    template <class T> static __device__ __forceinline__ T read(uint32_t at, int constant) { return *(GRAWA_LDS_AT const T *)((GRAWA_LDS_AT const char *)(uintptr_t)at + constant); }
+
+    // Lines row0 ... row0 + 31 (a multiple of 32), elements 16 ks ... of the head.
+    static __device__ __forceinline__ V by_rows(uint32_t at, int row0, int ks)
+    {
         if constexpr (BF16) {
-            return *(GRAWA_LDS_AT const V *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (ks << 5)) + row0 * RB);
+            return read<V>(at ^ (ks << 5), row0 * RB);
         } else {
-            const grawa_f32x4v a = *(GRAWA_LDS_AT const grawa_f32x4v *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (ks << 6)) + row0 * RB);
-            const grawa_f32x4v b = *(GRAWA_LDS_AT const grawa_f32x4v *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (ks << 6) ^ 16) + row0 * RB);
+            const grawa_f32x4v a = read<grawa_f32x4v>(at ^ (ks << 6), row0 * RB), b = read<grawa_f32x4v>(at ^ (ks << 6) ^ 16, row0 * RB);
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
     // Lines: elements 32 dt ... of the head, k: tokens row0 ... row0 + 15 (a multiple of 16) in the order of a product's registers.
-    static __device__ __forceinline__ V by_columns(const char *lds, int lane, int row0, int dt)
+    static __device__ __forceinline__ V by_columns(uint32_t at, int row0, int dt)
     {
-        const int half = lane >> 5;
         if constexpr (BF16) {
-            const int s = lane & 15, row = 4 * half + (s >> 2);
-            const uint32_t at = (address(lds) + row * RB + (((2 * ((lane >> 4) & 1) + ((s & 3) >> 1)) ^ key(row)) << 4) + (s & 1) * 8) ^ (dt << 6);
-            const grawa_s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)at + row0 * RB));
-            const grawa_s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)(at ^ 32) + (row0 + 8) * RB)); // eight rows on, the key's second bit is another
+            const uint32_t lower = at ^ (dt << 6), upper = lower ^ 32; // eight rows on, the key's second bit is another
+            const grawa_s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)lower + row0 * RB));
+            const grawa_s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)upper + (row0 + 8) * RB));
             return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const int m = lane & 31;
             V v;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int row = 4 * half + (j & 3) + 8 * (j >> 2);
-                const uint32_t at = address(lds) + row * RB + (((m >> 2) ^ key(row)) << 4) + (m & 3) * 4;
-                v[j] = *(GRAWA_LDS_AT const float *)((GRAWA_LDS_AT const char *)(uintptr_t)(at ^ (dt << 7)) + row0 * RB);
+            for (int j = 0; j < 8; ++j) { // rows 4 (lane / 32) + j % 4 + 8 (j / 4): what their keys differ in
+                const int row = (j & 3) + 8 * (j >> 2);
+                v[j] = read<float>(at ^ (dt << 7) ^ (key(row) << 4), (row0 + row) * RB);
             }
             return v;
         }
     }
 };
+
+// Keeps what an address differs in from being formed ahead for all fragments and held in registers.
+__device__ __forceinline__ uint32_t here(uint32_t at)
+{
+    asm volatile("" : "+v"(at));
+    return at;
+}
 
 // All loads into LDS have landed and all reads from it are done, the wave's own and then the other waves'.
 __device__ __forceinline__ void landed()
@@ -150,6 +162,26 @@ __device__ __forceinline__ void landed()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// A run of N matrix instructions whose fragments from LDS are asked for AHEAD before they are used; f holds the first ones (asked for
+// by `ask`, early).  Nothing is moved across: left to itself the compiler reads a fragment, waits, uses it and reads the next one as
+// soon as registers are few.
+template <int AHEAD, class V, class L> __device__ __forceinline__ void ask(V (&f)[AHEAD], L &&load)
+{
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) f[i] = load(i);
+    __builtin_amdgcn_sched_barrier(0);
+}
+template <int N, int AHEAD, class V, class L, class U> __device__ __forceinline__ void flow(V (&f)[AHEAD], L &&load, U &&use)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        use(i, f[i % AHEAD]);
+        if (i + AHEAD < N) f[i % AHEAD] = load(i + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // What the wave's lanes have written to LDS, its other lanes read from here on.
 __device__ __forceinline__ void wave_order()
 {
@@ -158,34 +190,26 @@ __device__ __forceinline__ void wave_order()
     asm volatile("" ::: "memory");
 }
 
-// Takes what is not finite out of an operand and marks it: 1 where it was plus (minus) infinity, both where it was no number.
-template <class V> __device__ __forceinline__ void take_out(V &v, V &plus, V &minus, bool signs)
+// sums += a w for a tile of which only some pairs count: a pair that does not count has w = 0, but an infinity or no number in its line
+// of a must not reach the sum.  `counts` has 1 for pairs that count; what they bring that is not finite makes the sum no number.  One
+// at a time: this is not where speed counts, and registers are few.
+template <class V> __device__ __forceinline__ void product_of_some(grawa_f32x16 &sums, V a, const V &w, const V &counts)
 {
+    V odd;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float f = (float)v[j];
-        const bool odd = !(fabsf(f) < __builtin_inff());
-        plus[j] = odd && !(signs && f < 0.f) ? 1.f : 0.f;
-        minus[j] = odd && !(signs && f > 0.f) ? 1.f : 0.f;
-        v[j] = odd ? 0.f : f;
+        const float f = (float)a[j];
+        const bool finite = fabsf(f) < __builtin_inff();
+        odd[j] = finite ? 0.f : 1.f;
+        a[j] = finite ? f : 0.f;
     }
-}
-
-// sums += a w for a tile of which only some pairs count: a pair that does not count has w = 0, but an infinity or no number in its line
-// of a must not reach the sum.  `counts` has 1 for pairs that count.  signs: an infinity keeps its sign (else all become no number).
-template <class V> __device__ __forceinline__ void product_of_some(grawa_f32x16 &sums, V a, const V &w, const V &counts, bool signs)
-{
-    V plus, minus;
-    take_out(a, plus, minus, signs);
-    sums = mfma(a, w, sums);
-    __builtin_amdgcn_sched_barrier(0); // one at a time: this is not where speed counts, and registers are few
-    const grawa_f32x16 p = mfma(plus, counts, grawa_f32x16{});
-#pragma unroll
-    for (int j = 0; j < 16; ++j) sums[j] += p[j] > 0.f ? __builtin_inff() : 0.f;
     __builtin_amdgcn_sched_barrier(0);
-    const grawa_f32x16 m = mfma(minus, counts, grawa_f32x16{});
+    sums = mfma(a, w, sums);
+    __builtin_amdgcn_sched_barrier(0);
+    grawa_f32x16 n = {};
+    n = mfma(odd, counts, n);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) sums[j] -= m[j] > 0.f ? __builtin_inff() : 0.f;
+    for (int j = 0; j < 16; ++j) sums[j] = n[j] > 0.f ? __builtin_nanf("") : sums[j];
     __builtin_amdgcn_sched_barrier(0);
 }
 

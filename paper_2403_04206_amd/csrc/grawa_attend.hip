@@ -124,18 +124,20 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
         for (int d = 0; d < DT; ++d) o[c][d] = grawa_f32x16{};
     }
     const auto step = [&](const char *buf, int j0) __attribute__((always_inline)) {
+        constexpr int A = BF16 ? 4 : 2;
+        V f[A];
+        const uint32_t rows = Tile::rows_of(buf, lane), columns = Tile::columns_of(buf + Tile::BYTES, lane);
+        const auto key = [&](int i) { return Tile::by_rows(rows, i % 2 * 32, i / 2); };
+        const auto value = [&](int i) { return Tile::by_columns(columns, i / DT * 16, i % DT); };
         grawa_f32x16 s[CT][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int c = 0; c < CT; ++c) s[c][0] = s[c][1] = grawa_f32x16{};
+        ask(f, key);
+        flow<2 * KS>(f, key, [&](int i, const V &x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c) s[c][u] = grawa_f32x16{};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const V f = Tile::by_rows(buf, lane, 32 * u, ks);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) s[c][u] = mfma(f, q[c][ks], s[c][u]);
-            }
-        }
+            for (int c = 0; c < CT; ++c) s[c][i % 2] = mfma(x, q[c][i / 2], s[c][i % 2]);
+        });
+        ask(f, value);
         V p[CT][4];
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
@@ -147,14 +149,11 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
 #pragma unroll
                 for (int h = 0; h < 2; ++h) as_operand(s[c][u], h, p[c][2 * u + h]);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        flow<4 * DT>(f, value, [&](int i, const V &x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < 4; ++h)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const V f = Tile::by_columns(buf + Tile::BYTES, lane, 16 * h, d);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) o[c][d] = mfma(f, p[c][h], o[c][d]);
-            }
+            for (int c = 0; c < CT; ++c) o[c][i % DT] = mfma(x, p[c][i / DT], o[c][i % DT]);
+        });
     };
     if (from < to) load(from, lds);
     for (int it = from; it < to; ++it) {
@@ -206,6 +205,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
             for (int d = 0; d < DT; ++d) put(c, d, o[c][d]);
         return;
     }
+#pragma unroll 1
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
@@ -215,12 +215,13 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
                 landed();
                 load(it, lds);
                 landed();
+#pragma unroll 1
                 for (int u = 0; u < 2; ++u) {
                     const int j0 = tile_of(it) + 32 * u, j1 = j0 + 31;
                     if (none(j0, j1)) continue;
                     grawa_f32x16 s = {};
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(lds, lane, 32 * u, ks), q[c][ks], s);
+                    for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(Tile::rows_of(lds + 32 * u * Tile::RB, lane), 0, ks), q[c][ks], s);
                     scores(j0, c, s);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(BIAS ? s[r] - base : __builtin_fmaf(s[r], c2, -base));
@@ -228,11 +229,11 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
                     for (int h = 0; h < 2; ++h) {
                         V p;
                         as_operand(s, h, p);
-                        const V v = Tile::by_columns(lds + Tile::BYTES, lane, 32 * u + 16 * h, d);
+                        const V v = Tile::by_columns(Tile::columns_of(lds + Tile::BYTES + (32 * u + 16 * h) * Tile::RB, lane), 0, d);
                         if (all(j0, j1))
                             sums = mfma(v, p, sums);
                         else
-                            product_of_some(sums, v, p, marks<V>(a, pos0 + 32 * c, j0 + 16 * h, half), true);
+                            product_of_some(sums, v, p, marks<V>(a, pos0 + 32 * c, j0 + 16 * h, half));
                     }
                 }
             }
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
             const bool all = j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks);
             grawa_f32x16 s[1] = {};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[0] = mfma(Tile::by_rows(buf, lane, wave * 32, ks), q[ks], s[0]);
+            for (int ks = 0; ks < KS; ++ks) s[0] = mfma(Tile::by_rows(Tile::rows_of(buf + wave * 32 * Tile::RB, lane), 0, ks), q[ks], s[0]);
             if constexpr (BIAS) {
                 if (w0 - j1 >= a.distances - 1) {
 #pragma unroll
@@ -329,9 +330,9 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
                 as_operand(s[0], h, p);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    const V v = Tile::by_columns(buf + Tile::BYTES, lane, wave * 32 + 16 * h, d);
+                    const V v = Tile::by_columns(Tile::columns_of(buf + Tile::BYTES + wave * 32 * Tile::RB, lane), 16 * h, d);
                     if (careful.value && !all)
-                        product_of_some(o[d], v, p, marks<V>(a, pos, j0 + 16 * h, half), true);
+                        product_of_some(o[d], v, p, marks<V>(a, pos, j0 + 16 * h, half));
                     else
                         o[d] = mfma(v, p, o[d]);
                 }

@@ -79,13 +79,20 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     };
     const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0) { return j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
-    // dS of 32 keys.
-    const auto slopes = [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
+    constexpr int A = BF16 ? 4 : 2;
+    // dS of 32 keys; leaves the first fragments of `then` in f.
+    const auto slopes = [&](const char *buf, int u, int j0, V (&f)[A], auto &&then) __attribute__((always_inline)) {
         grawa_f32x16 s = {}, dp = {};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), q[ks], s);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), go[ks], dp);
+        const uint32_t rows[2] = {Tile::rows_of(buf + 32 * u * Tile::RB, lane), Tile::rows_of(buf + Tile::BYTES + 32 * u * Tile::RB, lane)};
+        const auto both = [&](int i) { return Tile::by_rows(rows[i % 2], 0, i / 2); };
+        ask(f, both);
+        flow<2 * KS>(f, both, [&](int i, const V &x) __attribute__((always_inline)) {
+            if (i % 2)
+                dp = mfma(x, go[i / 2], dp);
+            else
+                s = mfma(x, q[i / 2], s);
+        });
+        ask(f, then);
         const bool is_far = BIAS && w0 - (j0 + 31) >= a.distances - 1;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -104,7 +111,10 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
 #pragma unroll
     for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
     const auto step = [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
-        const grawa_f32x16 s = slopes(buf, u, j0);
+        V f[A];
+        const uint32_t at = Tile::columns_of(buf + 32 * u * Tile::RB, lane);
+        const auto columns = [&](int i) { return Tile::by_columns(at, i / DT * 16, i % DT); };
+        const grawa_f32x16 s = slopes(buf, u, j0, f, columns);
         if constexpr (BIAS) {
             if (w0 - (j0 + 31) >= a.distances - 1) {
 #pragma unroll
@@ -126,13 +136,11 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
                 wave_order();
             }
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            V w;
-            as_operand(s, h, w);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) dq[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, dq[d]);
-        }
+        V w[2];
+        as_operand(s, 0, w[0]);
+        as_operand(s, 1, w[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        flow<2 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) { dq[i % DT] = mfma(x, w[i / DT], dq[i % DT]); });
     };
     if (BUFS == 2 && tiles) load(0, lds);
     for (int it = 0; it < tiles; ++it) {
@@ -167,25 +175,28 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
 #pragma unroll
         for (int d = 0; d < DT; ++d) put(d, dq[d]);
     } else {
+#pragma unroll 1
         for (int d = 0; d < DT; ++d) {
             grawa_f32x16 sums = {};
             for (int it = 0; it < tiles; ++it) {
                 landed();
                 load(it, lds);
                 landed();
+#pragma unroll 1
                 for (int u = 0; u < 2; ++u) {
                     const int j0 = tile_of(it) + 32 * u;
                     if (none(j0)) continue;
-                    const grawa_f32x16 s = slopes(lds, u, j0);
+                    V f[A];
+                    const grawa_f32x16 s = slopes(lds, u, j0, f, [&](int) { return V{}; });
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         V w;
                         as_operand(s, h, w);
-                        const V c = Tile::by_columns(lds, lane, 32 * u + 16 * h, d);
+                        const V c = Tile::by_columns(Tile::columns_of(lds + (32 * u + 16 * h) * Tile::RB, lane), 0, d);
                         if (all(j0))
                             sums = mfma(c, w, sums);
                         else
-                            product_of_some(sums, c, w, marks<V>(a, pos, j0 + 16 * h, half), false);
+                            product_of_some(sums, c, w, marks<V>(a, pos, j0 + 16 * h, half));
                     }
                 }
             }
@@ -246,7 +257,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     const int hd = turn.head, item = turn.block;
     const bool sink = item < sink_items;
     const int splits = sink ? a.sink_splits : a.splits, kb = sink ? item / a.sink_splits : a.sink_blocks + (item - sink_items) / a.splits;
-    const int split = sink ? item % a.sink_splits : (item - sink_items) % a.splits;
+    const int split = sink ? item % a.sink_splits : (item - sink_items) % a.splits, slot = sink || a.sink_splits > 1 ? item : item - sink_items;
     const int kn = hd / a.G, g = hd - kn * a.G, k = kn / a.N, n = kn - k * a.N;
     const Place at = place_of(a, kn);
     const int b0 = kb * BKV, w0 = b0 + wave * 32, w1 = w0 + 31, j = w0 + (lane & 31);
@@ -268,11 +279,12 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
         lv.load(values, wave, Values::rsrc(a.v.p + (int64_t)k * a.v.worker + (int64_t)n * a.v.seq + (int64_t)b0 * a.v.token + (int64_t)g * a.v.head,
                                            at.length - b0, (uint32_t)a.v.token, a.D));
     }
+    const uint32_t values_at = Values::rows_of(values + (KEEP ? 0 : wave * 32 * Values::RB), lane);
     const auto value = [&](int ks) {
         if constexpr (KEEP)
             return vf[ks];
         else
-            return Values::by_rows(values, lane, wave * 32, ks);
+            return Values::by_rows(here(values_at), 0, ks);
     };
     const float c2 = a.scale * LOG2E;
 
@@ -319,27 +331,35 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
             __syncthreads();
         }
     };
-    // Between the parts of a step nothing is moved where registers are few: fragments asked for early would push others out.
-    const auto few_registers = []() __attribute__((always_inline)) {
-        if (DP == 128) __builtin_amdgcn_sched_barrier(0);
-    };
     // p0: position of the first of 32 queries
     const auto none = [&](int p0) { return w0 > p0 + 31 || w0 >= at.length || (w1 <= p0 - a.window && w0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int p0) { return w1 <= p0 && (p0 + 31 - w0 < a.window || w1 < a.sinks); };
-    // P and dS of 32 queries.
-    const auto slopes = [&](const char *buf, int b, int u, int p0, grawa_f32x16 &s, grawa_f32x16 &dp) __attribute__((always_inline)) {
+    constexpr int A = BF16 ? 4 : 2;
+    // P and dS of 32 queries; leaves the first fragments of `then` in f.
+    const auto slopes = [&](const char *buf, int b, int u, int p0, grawa_f32x16 &s, grawa_f32x16 &dp, V (&f)[A], auto &&then) __attribute__((always_inline)) {
+        const uint32_t at = Tile::rows_of(buf + 32 * u * Tile::RB, lane);
+        const auto rows = [&](int i) { return Tile::by_rows(KEEP ? at : here(at), i / KS * (Tile::BYTES / Tile::RB), i % KS); };
         s = grawa_f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf, lane, 32 * u, ks), kf[ks], s);
+        ask(f, rows);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const grawa_f32x4v dot = *(const grawa_f32x4v *)(of_rows[b][1] + 32 * u + 8 * x + 4 * half);
 #pragma unroll
             for (int y = 0; y < 4; ++y) dp[4 * x + y] = -dot[y];
         }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma(Tile::by_rows(buf + Tile::BYTES, lane, 32 * u, ks), value(ks), dp);
-        few_registers();
+        V v[KEEP ? 1 : 2]; // values, asked for two before they are used
+        if constexpr (!KEEP) v[0] = value(0), v[1] = value(1);
+        flow<2 * KS>(f, rows, [&](int i, const V &x) __attribute__((always_inline)) {
+            if (i < KS) {
+                s = mfma(x, kf[i], s);
+            } else if constexpr (KEEP) {
+                dp = mfma(x, value(i - KS), dp);
+            } else {
+                dp = mfma(x, v[i % 2], dp);
+                if (i + 2 < 2 * KS) v[i % 2] = value(i + 2 - KS);
+            }
+        });
+        ask(f, then);
         const bool is_far = BIAS && p0 - w1 >= a.distances - 1;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -360,7 +380,6 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
                 s[r] = seen ? s[r] : 0.f;
                 dp[r] = seen ? dp[r] : 0.f;
             }
-        few_registers();
     };
 
     grawa_f32x16 dk[DT], dv[DT];
@@ -380,27 +399,26 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
             if (BUFS == 2 && it + 1 < to) load(ahead = next(ahead), b ^ 1);
             tabulate(t.h);
             // One way through the step, masked or not: with two the sums change their registers between them.
+#pragma unroll 1
             for (int u = 0; u < 2; ++u) {
                 const int p0 = at.start + t.tile + 32 * u;
                 if (none(p0)) continue;
                 grawa_f32x16 s, dp;
-                slopes(buf, b, u, p0, s, dp);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    V w;
-                    as_operand(s, h, w);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) dv[d] = mfma(Tile::by_columns(buf + Tile::BYTES, lane, 32 * u + 16 * h, d), w, dv[d]);
-                    few_registers();
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    V w;
-                    as_operand(dp, h, w);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) dk[d] = mfma(Tile::by_columns(buf, lane, 32 * u + 16 * h, d), w, dk[d]);
-                    few_registers();
-                }
+                V f[A], w[4];
+                const uint32_t at = Tile::columns_of(buf + 32 * u * Tile::RB, lane);
+                const auto columns = [&](int i) { return Tile::by_columns(KEEP ? at : here(at), (1 - i / (2 * DT)) * (Tile::BYTES / Tile::RB) + i / DT % 2 * 16, i % DT); };
+                slopes(buf, b, u, p0, s, dp, f, columns);
+                as_operand(s, 0, w[0]);
+                as_operand(s, 1, w[1]);
+                as_operand(dp, 0, w[2]);
+                as_operand(dp, 1, w[3]);
+                __builtin_amdgcn_sched_barrier(0);
+                flow<4 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) {
+                    if (i < 2 * DT)
+                        dv[i % DT] = mfma(x, w[i / DT], dv[i % DT]);
+                    else
+                        dk[i % DT] = mfma(x, w[i / DT], dk[i % DT]);
+                });
             }
         }
     }
@@ -410,51 +428,55 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) odd |= dk[d][r] != dk[d][r] || dv[d][r] != dv[d][r];
-    const auto put = [&](int d, const grawa_f32x16 &k_sums, const grawa_f32x16 &v_sums) {
+    const auto put = [&](bool keys, int d, const grawa_f32x16 &sums) {
         if (!there) return;
-        grawa_f32x16 x, y;
+        grawa_f32x16 x;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = counts ? k_sums[r] : 0.f, y[r] = counts ? v_sums[r] : 0.f;
-        if (splits > 1) {
-            float *p = a.part + (((int64_t)hd * per + item) * BKV + (j - b0)) * 2 * DP;
-            store_column<false>((char *)p, lane, d, DP, x, a.scale);
-            store_column<false>((char *)(p + DP), lane, d, DP, y, 1.f);
-        } else {
-            store_column<BF16>(a.dk.p + (int64_t)k * a.dk.worker + (int64_t)n * a.dk.seq + (int64_t)j * a.dk.token + (int64_t)g * a.dk.head, lane, d, a.D, x, a.scale);
-            store_column<BF16>(a.dv.p + (int64_t)k * a.dv.worker + (int64_t)n * a.dv.seq + (int64_t)j * a.dv.token + (int64_t)g * a.dv.head, lane, d, a.D, y, 1.f);
-        }
+        for (int r = 0; r < 16; ++r) x[r] = counts ? sums[r] : 0.f;
+        const GrawaHeads &to = keys ? a.dk : a.dv;
+        if (splits > 1)
+            store_column<false>((char *)(a.part + (((int64_t)hd * a.slots + slot) * BKV + (j - b0)) * 2 * DP + (keys ? 0 : DP)), lane, d, DP, x, keys ? a.scale : 1.f);
+        else
+            store_column<BF16>(to.p + (int64_t)k * to.worker + (int64_t)n * to.seq + (int64_t)j * to.token + (int64_t)g * to.head, lane, d, a.D, x, keys ? a.scale : 1.f);
     };
+    // What is no number may come from a query that does not see the key: once more then, with care.
     if (__builtin_expect(!__syncthreads_or(odd), 1)) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) put(d, dk[d], dv[d]);
+        for (int d = 0; d < DT; ++d) put(false, d, dv[d]), put(true, d, dk[d]);
         return;
     }
-    for (int d = 0; d < DT; ++d) {
-        grawa_f32x16 k_sums = {}, v_sums = {};
+#pragma unroll 1
+    for (int x = 0; x < 2 * DT; ++x) {
+        const bool keys = x >= DT;
+        const int d = x % DT;
+        grawa_f32x16 sums = {};
+#pragma unroll 1
         for (int it = from; it < to; ++it) {
             const At t = place(it);
             landed();
             load(t, 0);
             landed();
             tabulate(t.h);
+#pragma unroll 1
             for (int u = 0; u < 2; ++u) {
                 const int p0 = at.start + t.tile + 32 * u;
                 if (none(p0)) continue;
                 grawa_f32x16 s, dp;
-                slopes(lds, 0, u, p0, s, dp);
+                V f[A];
+                slopes(lds, 0, u, p0, s, dp, f, [&](int) { return V{}; });
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = keys ? dp[r] : s[r];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     V w, seen;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) seen[r] = sees(a, p0 + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, j) ? 1.f : 0.f;
                     as_operand(s, h, w);
-                    product_of_some(v_sums, Tile::by_columns(lds + Tile::BYTES, lane, 32 * u + 16 * h, d), w, seen, true);
-                    as_operand(dp, h, w);
-                    product_of_some(k_sums, Tile::by_columns(lds, lane, 32 * u + 16 * h, d), w, seen, false);
+                    product_of_some(sums, Tile::by_columns(Tile::columns_of(lds + (keys ? 0 : Tile::BYTES) + (32 * u + 16 * h) * Tile::RB, lane), 0, d), w, seen);
                 }
             }
         }
-        put(d, k_sums, v_sums);
+        put(keys, d, sums);
     }
 #endif
 }
@@ -466,16 +488,16 @@ template <bool BF16, int DP, int BKV> __global__ __launch_bounds__(256) void k_a
     constexpr int LPR = 2 * DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N; // threads of a key: half have dk, half dv
     const int64_t id = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;    // [K N][G][blocks][BKV]
     const int x = threadIdx.x % LPR, which = x / (LPR / 2), e0 = x % (LPR / 2) * 8;
-    const int per = a.sink_blocks * a.sink_splits + (a.key_blocks - a.sink_blocks) * a.splits;
     const int key = (int)(id % BKV), kb = first + (int)(id / BKV % blocks);
     const int64_t hd = id / BKV / blocks;
     const int j = kb * BKV + key;
     if (hd >= (int64_t)a.K * a.N * a.G || j >= a.Sk) return;
     const bool sink = kb < a.sink_blocks;
-    const int splits = sink ? a.sink_splits : a.splits, item = sink ? kb * a.sink_splits : a.sink_blocks * a.sink_splits + (kb - a.sink_blocks) * a.splits;
+    const int splits = sink ? a.sink_splits : a.splits;
+    const int slot = sink ? kb * a.sink_splits : (a.sink_splits > 1 ? a.sink_blocks * a.sink_splits : 0) + (kb - a.sink_blocks) * a.splits;
     float v[8] = {};
     for (int s = 0; s < splits; ++s) {
-        const grawa_f32x4v *p = (const grawa_f32x4v *)(a.part + ((hd * per + item + s) * BKV + key) * 2 * DP + which * DP + e0);
+        const grawa_f32x4v *p = (const grawa_f32x4v *)(a.part + ((hd * a.slots + slot + s) * BKV + key) * 2 * DP + which * DP + e0);
         const grawa_f32x4v b = p[0], c = p[1];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] += b[q], v[4 + q] += c[q];
@@ -509,20 +531,21 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     // Blocks of keys that all later queries see, and not only those that the window lets through.
     const int64_t window_tiles = ((int64_t)a.window + BKV + 63) / 64, tiles = (a.Sq + 63) / 64, sink_blocks = ((int64_t)a.sinks + BKV - 1) / BKV;
     a.sink_blocks = a.window == GRAWA_NO_WINDOW ? 0 : (int)(sink_blocks < a.key_blocks ? sink_blocks : a.key_blocks);
-    const int64_t groups = kn * a.G, slot = (int64_t)BKV * 2 * DP, room = part_floats / slot / groups;
+    const int64_t groups = kn * a.G, room = part_floats / ((int64_t)BKV * 2 * DP) / groups; // for so many blocks of a group
     const int64_t regular = a.key_blocks - a.sink_blocks, most = (tiles < window_tiles ? tiles : window_tiles) * a.share;
-    int64_t splits = regular ? 512 / (groups * regular) : 1;
+    int64_t splits = regular ? 512 / (groups * regular) : 1, sink_splits = 1;
     if (splits > most / 2) splits = most / 2;
-    if (regular && splits > room / 2 / regular) splits = room / 2 / regular;
-    a.splits = splits < 1 ? 1 : (int)splits;
-    int64_t sink_splits = 1;
-    if (a.sink_blocks) {
-        sink_splits = (tiles * a.share + most - 1) / most * a.splits;
-        if (sink_splits > room / 2 / a.sink_blocks) sink_splits = room / 2 / a.sink_blocks;
+    if (splits > 1 && splits > room / 2 / regular) splits = room / 2 / regular;
+    if (splits < 1) splits = 1;
+    if (a.sink_blocks) { // as long as the others
+        sink_splits = (tiles * a.share + most - 1) / most * splits;
+        const int64_t left = room - (splits > 1 ? regular * splits : 0);
+        if (sink_splits > left / a.sink_blocks) sink_splits = left / a.sink_blocks;
+        if (sink_splits < 1) sink_splits = 1;
     }
-    a.sink_splits = sink_splits < 1 ? 1 : (int)sink_splits;
-    // what is written for joining: all items have a place
-    if ((a.splits > 1 || a.sink_splits > 1) && (int64_t)a.sink_blocks * a.sink_splits + regular * a.splits > room) a.splits = a.sink_splits = 1;
+    a.splits = (int)splits;
+    a.sink_splits = (int)sink_splits;
+    a.slots = (int)((sink_splits > 1 ? a.sink_blocks * sink_splits : 0) + (splits > 1 ? regular * splits : 0));
     const int64_t per = (int64_t)a.sink_blocks * a.sink_splits + regular * a.splits;
     const uint32_t grid = grid_of(groups, per, a.by_xcd);
     hipLaunchKernelGGL((k_attend_dkv<BF16, DP, BIAS, NW>), dim3(grid), dim3(NW * 64), 0, st, a);

@@ -53,7 +53,9 @@ struct GrawaAttend {
     float scale;
     int blocks, splits;          // blocks of queries of a head; blocks that share one's keys
     int accumulate, by_xcd;
-    int key_blocks, sink_blocks, sink_splits; // blocks of keys, and the first of them, that all queries see (dk and dv only)
+    // dk and dv: blocks of keys; the first of them, which all queries see, and how many blocks share their queries; places in `part` for
+    // a group's blocks that share
+    int key_blocks, sink_blocks, sink_splits, slots;
 };
 
 static inline int64_t grawa_round256(int64_t n) { return (n + 255) & ~(int64_t)255; }
