@@ -9,6 +9,9 @@
 
 namespace {
 
+// How the elements of a rotation go in pairs.
+enum Pairs { HALVES, NEIGHBOURS, APART };
+
 struct HeadNorm {
     GrawaHeads q, k, yq, yk, gq, gk; // forward: x and y; backward: x, dx (in yq, yk) and dy
     GrawaMat wq, wk, dwq, dwk;
@@ -16,149 +19,172 @@ struct HeadNorm {
     const double *turns;
     float *part;
     float eps;
-    int N, S, H, G, D, rotary, interleaved;
+    int N, S, H, G, D, rotary;
     int heads; // of an item: so many rows share a token's angles
     int accumulate;
 };
 
 #ifdef __HIP_DEVICE_COMPILE__
+// Eight elements of a row, four from `lo` on and four from `hi` on, at any alignment.
 template <bool BF16> struct Eight {
     float v[8];
-    __device__ __forceinline__ void load(const char *p, bool there)
+    __device__ __forceinline__ void load(const char *p, int lo, int hi, bool there)
     {
-        constexpr int N = GrawaPiece<BF16>::N;
-        GrawaPiece<BF16> piece;
+        if constexpr (BF16) {
+            GrawaAny8 x = {0, 0}, y = {0, 0};
+            if (there) x = *(const GrawaAny8 *)(p + lo * 2), y = *(const GrawaAny8 *)(p + hi * 2);
+            v[0] = bf16_lo(x.x), v[1] = bf16_hi(x.x), v[2] = bf16_lo(x.y), v[3] = bf16_hi(x.y);
+            v[4] = bf16_lo(y.x), v[5] = bf16_hi(y.x), v[6] = bf16_lo(y.y), v[7] = bf16_hi(y.y);
+        } else {
+            GrawaAny16 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+            if (there) x = *(const GrawaAny16 *)(p + lo * 4), y = *(const GrawaAny16 *)(p + hi * 4);
 #pragma unroll
-        for (int i = 0; i < 8 / N; ++i) {
-            if (there) {
-                piece.load(p + i * 16, N);
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[i * N + j] = piece[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[i * N + j] = 0.f;
-            }
+            for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(x[j]), v[4 + j] = __uint_as_float(y[j]);
         }
     }
-    __device__ __forceinline__ void store(char *p) const
+    __device__ __forceinline__ void store(char *p, int lo, int hi) const
     {
-        constexpr int N = GrawaPiece<BF16>::N;
+        if constexpr (BF16) {
+            typedef __bf16 B4 __attribute__((ext_vector_type(4)));
+            const B4 x = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]}, y = {(__bf16)v[4], (__bf16)v[5], (__bf16)v[6], (__bf16)v[7]};
+            *(GrawaAny8 *)(p + lo * 2) = __builtin_bit_cast(GrawaAny8, x);
+            *(GrawaAny8 *)(p + hi * 2) = __builtin_bit_cast(GrawaAny8, y);
+        } else {
+            GrawaAny16 x, y;
 #pragma unroll
-        for (int i = 0; i < 8 / N; ++i) store_piece<BF16>(p + i * 16, N, v + i * N);
+            for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(v[j]), y[j] = __float_as_uint(v[4 + j]);
+            *(GrawaAny16 *)(p + lo * 4) = x;
+            *(GrawaAny16 *)(p + hi * 4) = y;
+        }
     }
 };
 
+template <int CTRL> __device__ __forceinline__ float moved(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// Sum over the 8 or 16 lanes of a row: neighbours, pairs, quads from the other end, eights from the other end.
 template <int LPR> __device__ __forceinline__ float row_total(float v)
 {
-#pragma unroll
-    for (int m = 1; m < LPR; m <<= 1) v += __shfl_xor(v, m, 64);
+    v += moved<0xb1>(v);
+    v += moved<0x4e>(v);
+    v += moved<0x141>(v);
+    if constexpr (LPR == 16) v += moved<0x140>(v);
     return v;
 }
 
-// Elements e0 ... e0 + 7 of a row and what they are turned with.
-struct Turn {
-    float cos[8], sin[8]; // sin with the sign that it has in y_e = x_e cos + x_partner sin
-    int partner;          // first of the partners, where pairs are halves apart
-    bool whole;           // they are read by fours
+// Sine and cosine of part turns, |part| <= 1/2: quarter turns off, then the series of both up to the tenth power of an angle of at most
+// an eighth of a turn, where what is left out is below 2^-28.
+__device__ __forceinline__ void sine_cosine(float part, float &s, float &c)
+{
+    const float quarters = __builtin_rintf(4.f * part), x = (4.f * part - quarters) * 1.57079633f, x2 = x * x;
+    const float sx = x * (1.f + x2 * (-1.f / 6 + x2 * (1.f / 120 + x2 * (-1.f / 5040 + x2 * (1.f / 362880)))));
+    const float cx = 1.f + x2 * (-0.5f + x2 * (1.f / 24 + x2 * (-1.f / 720 + x2 * (1.f / 40320 - x2 * (1.f / 3628800)))));
+    const int q = (int)quarters & 3;
+    s = q & 1 ? cx : sx;
+    c = q & 1 ? sx : cx;
+    s = q & 2 ? -s : s;
+    c = (q + 1) & 2 ? -c : c;
+}
 
-    __device__ __forceinline__ void init(const HeadNorm &a, int64_t position, int e0)
+// What the lane's eight elements are turned with.  Pairs of neighbours are j and j ^ 1; pairs of halves are j and j ^ 4, `lo` and `hi` being
+// half the rotated elements apart.  Where that half is no multiple of four the partners are APART and come from LDS.
+template <Pairs P> struct Turn {
+    float cos[8], sin[8]; // sin with the sign that it has in y_e = x_e cos + x_partner sin
+
+    __device__ __forceinline__ void init(const HeadNorm &a, int64_t position, int lo, int hi)
     {
         const int half = a.rotary / 2;
-        partner = e0;
-        whole = half % 4 == 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int e = e0 + j;
+            const int e = j < 4 ? lo + j : hi + j - 4;
             cos[j] = 1.f;
             sin[j] = 0.f;
             if (e >= a.rotary) continue;
-            if (a.interleaved && j % 2) {
-                cos[j] = cos[j - 1];
-                sin[j] = -sin[j - 1];
+            const int before = P == NEIGHBOURS ? j & 6 : P == HALVES ? j & 3 : j; // the pair's first
+            if (before != j) {
+                cos[j] = cos[before];
+                sin[j] = -sin[before];
                 continue;
             }
-            const bool second = !a.interleaved && e >= half;
-            const double turns = (double)position * a.turns[a.interleaved ? e / 2 : second ? e - half : e];
-            const float part = (float)(2.0 * (turns - __builtin_rint(turns))); // of half a turn
-            float s, c;
-            s = sinpif(part);
-            c = cospif(part);
-            cos[j] = c;
+            const bool second = P == APART && e >= half;
+            const double turns = (double)position * a.turns[P == NEIGHBOURS ? e / 2 : second ? e - half : e];
+            float s;
+            sine_cosine((float)(turns - __builtin_rint(turns)), s, cos[j]);
             sin[j] = second ? s : -s;
         }
     }
-    static __device__ __forceinline__ int partner_of(const HeadNorm &a, int e)
+    // The partners of v; row: the row's own place in LDS.
+    __device__ __forceinline__ void partners(const HeadNorm &a, const float *v, float *row, int lo, int hi, float *p) const
     {
-        const int half = a.rotary / 2;
-        return e < half ? e + half : e < a.rotary ? e - half : e;
-    }
-    // The partners of v; row: the wave's own place in LDS for a row.
-    __device__ __forceinline__ void partners(const HeadNorm &a, const float *v, float *row, int e0, float *p) const
-    {
-        if (a.interleaved || a.rotary == 0) {
+        if constexpr (P == APART) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = v[j ^ 1];
-            return;
-        }
-        *(float4 *)(row + e0) = make_float4(v[0], v[1], v[2], v[3]);
-        *(float4 *)(row + e0 + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("" ::: "memory");
-        if (whole) {
-            const float4 x = *(const float4 *)(row + partner_of(a, e0)), y = *(const float4 *)(row + partner_of(a, e0 + 4));
-            p[0] = x.x, p[1] = x.y, p[2] = x.z, p[3] = x.w, p[4] = y.x, p[5] = y.y, p[6] = y.z, p[7] = y.w;
+            for (int j = 0; j < 8; ++j) row[j < 4 ? lo + j : hi + j - 4] = v[j];
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
+            const int half = a.rotary / 2;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int e = j < 4 ? lo + j : hi + j - 4;
+                p[j] = row[e < half ? e + half : e < a.rotary ? e - half : e];
+            }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = row[partner_of(a, e0 + j)];
+            for (int j = 0; j < 8; ++j) p[j] = P == NEIGHBOURS ? v[j ^ 1] : v[j ^ 4];
         }
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("" ::: "memory");
     }
 };
 
-__device__ __forceinline__ int64_t byte_of(const GrawaHeads &h, int k, int n, int s, int head)
+__device__ __forceinline__ int64_t byte_of(const GrawaHeads &h, int k, int n, int s)
 {
-    return (int64_t)k * h.worker + (int64_t)n * h.seq + (int64_t)s * h.token + (int64_t)head * h.head;
+    return (int64_t)k * h.worker + (int64_t)n * h.seq + (int64_t)s * h.token;
 }
 #endif
 
 // LPR lanes have a row of up to 8 LPR elements.  An item is `heads` rows of a token; blocks of a worker take items in turn.
-template <bool BF16, int LPR, bool BACK> __global__ __launch_bounds__(256) void k_head_norm([[maybe_unused]] HeadNorm a)
+// Bound by memory; what the angles take is shared by an item's rows and there is no exchange between lanes but a row's sums.
+template <bool BF16, int LPR, Pairs P, bool BACK> __global__ __launch_bounds__(256) void k_head_norm([[maybe_unused]] HeadNorm a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int ROWS = 256 / LPR, DP = LPR * 8, ES = BF16 ? 2 : 4, U = BACK ? 2 : 4;
-    __shared__ float lds[BACK ? ROWS * 2 * DP : ROWS * DP];
-    const int row = threadIdx.x / LPR, e0 = threadIdx.x % LPR * 8, k = blockIdx.y;
-    const bool there = e0 < a.D;
-    const int all = a.H + a.G, chunks = (all + a.heads - 1) / a.heads;
-    const int64_t items = (int64_t)a.N * a.S * chunks;
+    __shared__ float lds[BACK ? ROWS * 2 * DP : P == APART ? ROWS * DP : 1];
+    const int row = threadIdx.x / LPR, c = threadIdx.x % LPR, k = blockIdx.y;
+    const bool there = c * 8 < a.D;
+    // the lane's elements: pairs of halves stay together
+    const bool paired = P == HALVES && c * 8 < a.rotary;
+    const int lo = paired ? 4 * c : 8 * c, hi = paired ? a.rotary / 2 + 4 * c : 8 * c + 4;
+    const uint32_t all = a.H + a.G, chunks = (all + a.heads - 1) / a.heads, items = (uint32_t)a.N * a.S * chunks; // below 2^31
     Eight<BF16> wq, wk;
-    wq.load(a.wq.p + ((int64_t)k * a.wq.worker + e0) * ES, there);
-    wk.load(a.wk.p + ((int64_t)k * a.wk.worker + e0) * ES, there);
+    wq.load(a.wq.p + (int64_t)k * a.wq.worker * ES, lo, hi, there);
+    wk.load(a.wk.p + (int64_t)k * a.wk.worker * ES, lo, hi, there);
     float sq[8], sk[8];
     if (BACK)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sq[j] = sk[j] = 0.f;
     // all rows of a wave go round alike: what a wave's last items do not have is left out row by row
-    for (int64_t base = (int64_t)blockIdx.x * ROWS; base < items; base += (int64_t)gridDim.x * ROWS) {
-        const int64_t item = base + row;
+    for (uint32_t base = blockIdx.x * ROWS; base < items; base += gridDim.x * ROWS) {
+        const uint32_t item = base + row;
         const bool live = item < items;
-        const int64_t token = live ? item / chunks : 0;
-        const int h0 = live ? (int)(item - token * chunks) * a.heads : all, h1 = min(h0 + a.heads, all);
-        const int n = (int)(token / a.S), s = (int)(token - (int64_t)n * a.S);
-        Turn turn;
-        turn.init(a, (a.starts ? (int64_t)a.starts[k * a.N + n] : 0) + s, e0);
+        const uint32_t token = live ? item / chunks : 0;
+        const int h0 = live ? (int)(item - token * chunks) * a.heads : (int)all, h1 = min(h0 + a.heads, (int)all);
+        const int n = (int)(token / (uint32_t)a.S), s = (int)(token - (uint32_t)n * a.S);
+        Turn<P> turn;
+        turn.init(a, (a.starts ? (int64_t)a.starts[k * a.N + n] : 0) + s, lo, hi);
+        const char *pq = a.q.p + byte_of(a.q, k, n, s), *pk = a.k.p + byte_of(a.k, k, n, s) - a.H * a.k.head;
+        char *yq = a.yq.p + byte_of(a.yq, k, n, s), *yk = a.yk.p + byte_of(a.yk, k, n, s) - a.H * a.yk.head;
+        const char *gq = BACK ? a.gq.p + byte_of(a.gq, k, n, s) : nullptr, *gk = BACK ? a.gk.p + byte_of(a.gk, k, n, s) - a.H * a.gk.head : nullptr;
         for (int first = 0; first < a.heads; first += U) {
             Eight<BF16> x[U], g[BACK ? U : 1];
 #pragma unroll
             for (int u = 0; u < U; ++u) { // all on their way before the first is waited for
                 const int h = h0 + first + u;
-                const bool has = there && first + u < a.heads && h < h1;
-                const bool key = h >= a.H;
-                x[u].load((key ? a.k.p + byte_of(a.k, k, n, s, h - a.H) : a.q.p + byte_of(a.q, k, n, s, h)) + e0 * ES, has);
-                if constexpr (BACK) g[u].load((key ? a.gk.p + byte_of(a.gk, k, n, s, h - a.H) : a.gq.p + byte_of(a.gq, k, n, s, h)) + e0 * ES, has);
+                const bool has = there && first + u < a.heads && h < h1, key = h >= a.H;
+                x[u].load(key ? pk + h * a.k.head : pq + h * a.q.head, lo, hi, has);
+                if constexpr (BACK) g[u].load(key ? gk + h * a.gk.head : gq + h * a.gq.head, lo, hi, has);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -171,18 +197,22 @@ template <bool BF16, int LPR, bool BACK> __global__ __launch_bounds__(256) void 
                 Eight<BF16> y;
                 if constexpr (!BACK) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) y.v[j] = x[u].v[j] * r * (key ? wk.v[j] : wq.v[j]);
-                    turn.partners(a, y.v, lds + row * DP, e0, p);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y.v[j] = e0 + j >= a.rotary ? y.v[j] * turn.cos[j] : y.v[j] * turn.cos[j] + p[j] * turn.sin[j];
-                } else {
-                    turn.partners(a, g[u].v, lds + row * DP, e0, p);
-                    float dot = 0.f, c[8];
+                    for (int j = 0; j < 8; ++j) x[u].v[j] = x[u].v[j] * r * (key ? wk.v[j] : wq.v[j]);
+                    turn.partners(a, x[u].v, lds + row * DP, lo, hi, p);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float dn = e0 + j >= a.rotary ? g[u].v[j] * turn.cos[j] : g[u].v[j] * turn.cos[j] - p[j] * turn.sin[j];
+                        const bool turned = (j < 4 ? lo + j : hi + j - 4) < a.rotary;
+                        y.v[j] = turned ? x[u].v[j] * turn.cos[j] + p[j] * turn.sin[j] : x[u].v[j];
+                    }
+                } else {
+                    turn.partners(a, g[u].v, lds + row * DP, lo, hi, p);
+                    float dot = 0.f, d[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool turned = (j < 4 ? lo + j : hi + j - 4) < a.rotary;
+                        const float dn = turned ? g[u].v[j] * turn.cos[j] - p[j] * turn.sin[j] : g[u].v[j];
                         x[u].v[j] *= r;
-                        c[j] = dn * x[u].v[j];
+                        d[j] = dn * x[u].v[j];
                         y.v[j] = dn * (key ? wk.v[j] : wq.v[j]);
                         dot += y.v[j] * x[u].v[j];
                     }
@@ -190,11 +220,11 @@ template <bool BF16, int LPR, bool BACK> __global__ __launch_bounds__(256) void 
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         y.v[j] = r * (y.v[j] - x[u].v[j] * dot);
-                        if (has && key) sk[j] += c[j];
-                        if (has && !key) sq[j] += c[j];
+                        if (has && key) sk[j] += d[j];
+                        if (has && !key) sq[j] += d[j];
                     }
                 }
-                if (has) y.store((key ? a.yk.p + byte_of(a.yk, k, n, s, h - a.H) : a.yq.p + byte_of(a.yq, k, n, s, h)) + e0 * ES);
+                if (has) y.store(key ? yk + h * a.yk.head : yq + h * a.yq.head, lo, hi);
             }
         }
     }
@@ -202,8 +232,9 @@ template <bool BF16, int LPR, bool BACK> __global__ __launch_bounds__(256) void 
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            lds[(row * 2) * DP + e0 + j] = sq[j];
-            lds[(row * 2 + 1) * DP + e0 + j] = sk[j];
+            const int e = j < 4 ? lo + j : hi + j - 4; // below 8 LPR, for lanes without elements too
+            lds[(row * 2) * DP + e] = sq[j];
+            lds[(row * 2 + 1) * DP + e] = sk[j];
         }
         __syncthreads();
         const int which = threadIdx.x / DP, e = threadIdx.x % DP;
@@ -243,21 +274,27 @@ int heads_of(const grawa_attention_plan *s, int64_t tokens)
     return rows >= 1 << 18 ? 16 : rows >= 1 << 15 ? 8 : 4;
 }
 
-template <bool BACK> hipError_t launch(const grawa_attention_plan *s, HeadNorm a, int blocks, hipStream_t st)
+template <bool BACK, Pairs P> hipError_t launch_one(const grawa_attention_plan *s, const HeadNorm &a, dim3 grid, hipStream_t st)
 {
-    const dim3 grid((uint32_t)blocks, (uint32_t)s->K);
     if (s->dtype == GRAWA_BF16) {
         if (s->D <= 64)
-            hipLaunchKernelGGL((k_head_norm<true, 8, BACK>), grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL((k_head_norm<true, 8, P, BACK>), grid, dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL((k_head_norm<true, 16, BACK>), grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL((k_head_norm<true, 16, P, BACK>), grid, dim3(256), 0, st, a);
     } else {
         if (s->D <= 64)
-            hipLaunchKernelGGL((k_head_norm<false, 8, BACK>), grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL((k_head_norm<false, 8, P, BACK>), grid, dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL((k_head_norm<false, 16, BACK>), grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL((k_head_norm<false, 16, P, BACK>), grid, dim3(256), 0, st, a);
     }
     return hipGetLastError();
+}
+
+template <bool BACK> hipError_t launch(const grawa_attention_plan *s, const HeadNorm &a, int blocks, hipStream_t st)
+{
+    const dim3 grid((uint32_t)blocks, (uint32_t)s->K);
+    if (s->interleaved) return launch_one<BACK, NEIGHBOURS>(s, a, grid, st);
+    return s->rotary % 8 ? launch_one<BACK, APART>(s, a, grid, st) : launch_one<BACK, HALVES>(s, a, grid, st);
 }
 
 int64_t blocks_of(const grawa_attention_plan *s, int64_t tokens, int heads, int64_t most)
@@ -281,7 +318,7 @@ hipError_t grawa_launch_head_norm(const grawa_attention_plan *s, int64_t N, int6
     if (N * S == 0) return hipSuccess;
     HeadNorm a{};
     a.q = q, a.k = k, a.yq = qo, a.yk = ko, a.wq = qw, a.wk = kw, a.starts = starts, a.turns = s->turns, a.eps = eps;
-    a.N = (int)N, a.S = (int)S, a.H = s->H, a.G = s->G, a.D = s->D, a.rotary = s->rotary, a.interleaved = s->interleaved;
+    a.N = (int)N, a.S = (int)S, a.H = s->H, a.G = s->G, a.D = s->D, a.rotary = s->rotary;
     a.heads = heads_of(s, N * S);
     return launch<false>(s, a, (int)blocks_of(s, N * S, a.heads, 1 << 20), st);
 }
@@ -293,7 +330,7 @@ hipError_t grawa_launch_head_norm_backward(const grawa_attention_plan *s, int64_
     HeadNorm a{};
     a.q = q, a.k = k, a.yq = dq, a.yk = dk, a.gq = dqo, a.gk = dko, a.wq = qw, a.wk = kw, a.dwq = dqw, a.dwk = dkw;
     a.starts = starts, a.turns = s->turns, a.part = s->norm_part, a.eps = eps, a.accumulate = accumulate;
-    a.N = (int)N, a.S = (int)S, a.H = s->H, a.G = s->G, a.D = s->D, a.rotary = s->rotary, a.interleaved = s->interleaved;
+    a.N = (int)N, a.S = (int)S, a.H = s->H, a.G = s->G, a.D = s->D, a.rotary = s->rotary;
     a.heads = heads_of(s, N * S);
     const int blocks = (int)blocks_of(s, N * S, a.heads, s->norm_blocks);
     if (blocks > 0) {
