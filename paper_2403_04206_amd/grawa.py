@@ -95,7 +95,8 @@ def lib():
         fn.restype = res
         fn.argtypes = args
     for name in ("grawa_lgrawa_update", "grawa_local_step_scored", "grawa_local_lgrawa_update", "grawa_local_mgrawa_update", "grawa_layer_norm",
-                 "grawa_layer_norm_backward", "grawa_sublayer_save_bytes", "grawa_ffn", "grawa_ffn_backward", "grawa_dropout"):
+                 "grawa_layer_norm_backward", "grawa_sublayer_save_bytes", "grawa_ffn", "grawa_ffn_backward", "grawa_dropout", "grawa_head_norm",
+                 "grawa_head_norm_backward", "grawa_attention", "grawa_attention_backward"):
         _addresses[name] = C.cast(getattr(L, name), vp).value
     _lib = L
     return L
@@ -135,6 +136,7 @@ def _stream_no_tensors(stream=None):
 try:
     from ._rows import built_for, rows as _native_rows, scored as _native_scored, local as _native_local, lgrawa as _native_lgrawa
     from ._rows import norm as _native_norm, norm_back as _native_norm_back, feed as _native_feed, feed_back as _native_feed_back, drop as _native_drop
+    from ._rows import head_norm as _native_head_norm, head_norm_back as _native_head_norm_back, attend as _native_attend, attend_back as _native_attend_back
     if built_for != buildlib.rows_built_for():
         raise ImportError("_rows.so is for %s" % built_for)
 except Exception:                        # not built, or not for this torch: the Python checks alone
@@ -144,6 +146,7 @@ except Exception:                        # not built, or not for this torch: the
     def _native_scored(*args):
         return None
     _native_local = _native_lgrawa = _native_norm = _native_norm_back = _native_feed = _native_feed_back = _native_drop = _native_scored
+    _native_head_norm = _native_head_norm_back = _native_attend = _native_attend_back = _native_scored
 
 
 _NULL = C.c_void_p(0)
@@ -737,20 +740,6 @@ def log_buckets(buckets, far):
     return out
 
 
-def _heads(t, shape, dtype, what):
-    """[K, N, S, heads, D] with unit stride in the last axis, for the C call."""
-    if t is None or t.dtype is not dtype or t.ndim != 5 or not _on_device(t):
-        raise TypeError("%s must be a %s CUDA tensor [K, N, S, heads, D]" % (what, str(dtype).replace("torch.", "")))
-    if tuple(t.shape) != shape:
-        raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), shape))
-    stride = t.stride()
-    if shape[4] > 1 and stride[4] != 1:
-        raise TypeError("%s: elements of a row must be adjacent" % what)
-    if t.numel():
-        _covers(t, sum((n - 1) * s for n, s in zip(shape[:4], stride)) + shape[4], what)
-    return C.byref(_HeadsArg(t.data_ptr(), *stride[:4]))
-
-
 class AttentionPlan:
     """grawa_attention_plan_t: the attention of K workers (norms of heads with rotation, attention through a window with first tokens
     that stay visible, learned bias by buckets), its shape, tables and device workspace.  `sequences` and `length` are the most that a
@@ -776,6 +765,8 @@ class AttentionPlan:
                           1 if interleaved else 0, freq.ctypes.data, self.buckets, of.size, of.ctypes.data)
         self._h = C.c_void_p()
         _check(lib().grawa_attention_create(C.byref(self._h), C.byref(shape)), "grawa_attention_create")
+        self._device = torch.cuda.current_device()
+        self._dims = (self.K, self.N, self.S, self.H, self.G, self.D, _DTYPES[dtype], self._device)
 
     def destroy(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -796,6 +787,37 @@ class AttentionPlan:
     def __exit__(self, *exc):
         self.destroy()
 
+    def _here(self):
+        """The handle of the current stream of the plan's device."""
+        if _raw_stream is not None:
+            return _raw_stream(self._device)
+        return torch.cuda.current_stream(self._device).cuda_stream
+
+    def _on(self, stream):
+        return C.c_void_p(self._here()) if stream is None else _stream(stream)
+
+    def _same(self, t, what):
+        if t is not None and t.is_cuda and t.get_device() != self._device:
+            raise ValueError("%s is on device %d, the plan on %d" % (what, t.get_device(), self._device))
+        return t
+
+    def _heads(self, t, N, S, heads, what):
+        """[K, N, S, heads, D] with unit stride in the last axis, for the C call."""
+        shape = (self.K, N, S, heads, self.D)
+        if t is None or t.dtype is not self.dtype or t.ndim != 5 or not _on_device(t):
+            raise TypeError("%s must be a %s CUDA tensor [K, N, S, heads, D]" % (what, str(self.dtype).replace("torch.", "")))
+        if tuple(t.shape) != shape:
+            raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), shape))
+        stride = self._same(t, what).stride()
+        if self.D > 1 and stride[4] != 1:
+            raise TypeError("%s: elements of a row must be adjacent" % what)
+        if t.numel():
+            _covers(t, sum((n - 1) * s for n, s in zip(shape[:4], stride)) + self.D, what)
+        return C.byref(_HeadsArg(t.data_ptr(), *stride[:4]))
+
+    def _owned(self, t, shape, what):
+        return _mats(self._same(t, what), (self.K,) + shape, self.dtype, what)
+
     def _tokens_of(self, t, what):
         """Sequences and tokens of a call's tensor."""
         if t is None or t.ndim != 5:
@@ -808,7 +830,7 @@ class AttentionPlan:
     def _places(self, t, N, what):
         if t is None:
             return _NULL
-        if t.dtype is not torch.int32 or not t.is_contiguous() or not _on_device(t):
+        if t.dtype is not torch.int32 or not t.is_contiguous() or not _on_device(self._same(t, what)):
             raise TypeError("%s must be a contiguous int32 CUDA tensor" % what)
         if tuple(t.shape) != (self.K, N):
             raise ValueError("%s has shape %r, expected %r" % (what, tuple(t.shape), (self.K, N)))
@@ -817,57 +839,71 @@ class AttentionPlan:
 
     def _bias(self, t, what):
         if self.buckets:
-            return _mats(t, (self.K, self.H, self.buckets), self.dtype, what)
+            return self._owned(t, (self.H, self.buckets), what)
         if t is not None:
             raise ValueError("%s: the plan has no buckets" % what)
         return None
-
-    def head_norm(self, q, k, qweight, kweight, q_out, k_out, eps=1e-6, starts=None, stream=None):
-        """grawa_head_norm: each head divided by its root mean square, times the weight, turned by its position (start + index)."""
-        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
-        N, S = self._tokens_of(q, "q")
-        sq, sk = (K, N, S, H, D), (K, N, S, G, D)
-        _check(lib().grawa_head_norm(
-            self._h, N, S, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _mats(qweight, (K, D), dt, "qweight"), _mats(kweight, (K, D), dt, "kweight"),
-            float(eps), self._places(starts, N, "starts"), _heads(q_out, sq, dt, "q_out"), _heads(k_out, sk, dt, "k_out"), _stream(stream)),
-            "grawa_head_norm")
-
-    def head_norm_backward(self, dq_out, dk_out, q, k, qweight, kweight, dq, dk, dqweight, dkweight, eps=1e-6, starts=None, accumulate=False, stream=None):
-        """grawa_head_norm_backward: dq, dk and the gradients of the weights, added to what those hold with accumulate."""
-        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
-        N, S = self._tokens_of(q, "q")
-        sq, sk = (K, N, S, H, D), (K, N, S, G, D)
-        _check(lib().grawa_head_norm_backward(
-            self._h, N, S, _heads(dq_out, sq, dt, "dq_out"), _heads(dk_out, sk, dt, "dk_out"), _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"),
-            _mats(qweight, (K, D), dt, "qweight"), _mats(kweight, (K, D), dt, "kweight"), float(eps), self._places(starts, N, "starts"),
-            _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"), _mats(dqweight, (K, D), dt, "dqweight"), _mats(dkweight, (K, D), dt, "dkweight"),
-            1 if accumulate else 0, _stream(stream)), "grawa_head_norm_backward")
 
     def _lse(self, t, N, Sq, what, optional):
         if t is None and optional:
             return _NULL
         if t is None:
             raise TypeError("%s is required" % what)
-        return _table(t, (self.K, N, self.H, Sq), what)
+        return _table(self._same(t, what), (self.K, N, self.H, Sq), what)
+
+    def head_norm(self, q, k, qweight, kweight, q_out, k_out, eps=1e-6, starts=None, stream=None):
+        """grawa_head_norm: each head divided by its root mean square, times the weight, turned by its position (start + index)."""
+        if stream is None:
+            st = _native_head_norm(_addresses.get("grawa_head_norm"), self._h.value, self._dims, q, k, qweight, kweight, q_out, k_out, eps, starts, self._here)
+            if st is not None:
+                return _check(st, "grawa_head_norm")
+        H, G, D = self.H, self.G, self.D
+        N, S = self._tokens_of(q, "q")
+        _check(lib().grawa_head_norm(
+            self._h, N, S, self._heads(q, N, S, H, "q"), self._heads(k, N, S, G, "k"), self._owned(qweight, (D,), "qweight"), self._owned(kweight, (D,), "kweight"),
+            float(eps), self._places(starts, N, "starts"), self._heads(q_out, N, S, H, "q_out"), self._heads(k_out, N, S, G, "k_out"), self._on(stream)),
+            "grawa_head_norm")
+
+    def head_norm_backward(self, dq_out, dk_out, q, k, qweight, kweight, dq, dk, dqweight, dkweight, eps=1e-6, starts=None, accumulate=False, stream=None):
+        """grawa_head_norm_backward: dq, dk and the gradients of the weights, added to what those hold with accumulate."""
+        if stream is None:
+            st = _native_head_norm_back(_addresses.get("grawa_head_norm_backward"), self._h.value, self._dims, dq_out, dk_out, q, k, qweight, kweight, dq, dk,
+                                        dqweight, dkweight, eps, starts, accumulate, self._here)
+            if st is not None:
+                return _check(st, "grawa_head_norm_backward")
+        H, G, D = self.H, self.G, self.D
+        N, S = self._tokens_of(q, "q")
+        _check(lib().grawa_head_norm_backward(
+            self._h, N, S, self._heads(dq_out, N, S, H, "dq_out"), self._heads(dk_out, N, S, G, "dk_out"), self._heads(q, N, S, H, "q"), self._heads(k, N, S, G, "k"),
+            self._owned(qweight, (D,), "qweight"), self._owned(kweight, (D,), "kweight"), float(eps), self._places(starts, N, "starts"),
+            self._heads(dq, N, S, H, "dq"), self._heads(dk, N, S, G, "dk"), self._owned(dqweight, (D,), "dqweight"), self._owned(dkweight, (D,), "dkweight"),
+            1 if accumulate else 0, self._on(stream)), "grawa_head_norm_backward")
 
     def attention(self, q, k, v, out, lse_out=None, bias=None, lengths=None, starts=None, stream=None):
         """grawa_attention: out = softmax(scale q k^T + bias) v over the keys that each query sees; lse_out: float32 [K, N, heads, Sq] for
         the backward pass."""
-        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
+        if stream is None:
+            st = _native_attend(_addresses.get("grawa_attention"), self._h.value, self._dims, self.buckets, q, k, v, out, lse_out, bias, lengths, starts, self._here)
+            if st is not None:
+                return _check(st, "grawa_attention")
+        H, G = self.H, self.G
         (N, Sq), Sk = self._tokens_of(q, "q"), self._tokens_of(k, "k")[1]
-        sq, sk = (K, N, Sq, H, D), (K, N, Sk, G, D)
         _check(lib().grawa_attention(
-            self._h, N, Sq, Sk, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"), self._bias(bias, "bias"),
-            self._places(lengths, N, "lengths"), self._places(starts, N, "starts"), _heads(out, sq, dt, "out"), self._lse(lse_out, N, Sq, "lse_out", True),
-            _stream(stream)), "grawa_attention")
+            self._h, N, Sq, Sk, self._heads(q, N, Sq, H, "q"), self._heads(k, N, Sk, G, "k"), self._heads(v, N, Sk, G, "v"), self._bias(bias, "bias"),
+            self._places(lengths, N, "lengths"), self._places(starts, N, "starts"), self._heads(out, N, Sq, H, "out"), self._lse(lse_out, N, Sq, "lse_out", True),
+            self._on(stream)), "grawa_attention")
 
     def attention_backward(self, dout, q, k, v, out, lse, dq, dk, dv, bias=None, dbias=None, lengths=None, starts=None, accumulate=False, stream=None):
         """grawa_attention_backward: dq, dk, dv and, with buckets, dbias, added to what it holds with accumulate."""
-        K, H, G, D, dt = self.K, self.H, self.G, self.D, self.dtype
+        if stream is None:
+            st = _native_attend_back(_addresses.get("grawa_attention_backward"), self._h.value, self._dims, self.buckets, dout, q, k, v, out, lse, dq, dk, dv, bias, dbias,
+                                     lengths, starts, accumulate, self._here)
+            if st is not None:
+                return _check(st, "grawa_attention_backward")
+        H, G = self.H, self.G
         (N, Sq), Sk = self._tokens_of(q, "q"), self._tokens_of(k, "k")[1]
-        sq, sk = (K, N, Sq, H, D), (K, N, Sk, G, D)
         _check(lib().grawa_attention_backward(
-            self._h, N, Sq, Sk, _heads(dout, sq, dt, "dout"), _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
-            self._bias(bias, "bias"), self._places(lengths, N, "lengths"), self._places(starts, N, "starts"), _heads(out, sq, dt, "out"),
-            self._lse(lse, N, Sq, "lse", False), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"), _heads(dv, sk, dt, "dv"),
-            self._bias(dbias, "dbias"), 1 if accumulate else 0, _stream(stream)), "grawa_attention_backward")
+            self._h, N, Sq, Sk, self._heads(dout, N, Sq, H, "dout"), self._heads(q, N, Sq, H, "q"), self._heads(k, N, Sk, G, "k"), self._heads(v, N, Sk, G, "v"),
+            self._bias(bias, "bias"), self._places(lengths, N, "lengths"), self._places(starts, N, "starts"), self._heads(out, N, Sq, H, "out"),
+            self._lse(lse, N, Sq, "lse", False), self._heads(dq, N, Sq, H, "dq"), self._heads(dk, N, Sk, G, "dk"), self._heads(dv, N, Sk, G, "dv"),
+            self._bias(dbias, "dbias"), 1 if accumulate else 0, self._on(stream)), "grawa_attention_backward")
