@@ -12,43 +12,59 @@ struct Running {
     float m, l;
 };
 
-// Exponentials of a column's scores against its running maximum, in place.  SCALED: the scores are in units of log2 already.
-template <bool SCALED, int NS, int DT>
-__device__ __forceinline__ void soften(grawa_f32x16 (&s)[NS], float c2, Running &run, grawa_f32x16 (&o)[DT])
+// Exponentials of a column's scores against its running maximum, as operands, and their sum, taken before they are rounded (the
+// gradients start from it).  SCALED: the scores are in units of log2 already.
+// The maximum need not be a tile's: the sums hold exponentials above 1 as well.  It is looked for where a column has none yet or where a
+// lane's exponentials add up to more than 2^13 (or to infinity); other tiles need neither the maximum nor what the other half of the
+// wave has.
+template <bool SCALED, int NS, int DT, class V>
+__device__ __forceinline__ void soften(const grawa_f32x16 (&s)[NS], float c2, Running &run, grawa_f32x16 (&o)[DT], V (&p)[2 * NS])
 {
-    float top = s[0][0];
+    float sum;
+    const auto exponentials = [&]() __attribute__((always_inline)) {
+        const float base = run.m == -__builtin_inff() ? 0.f : run.m;
+        float sums[2] = {0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < NS; ++u)
+        for (int u = 0; u < NS; ++u)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
-    top = fmaxf(top, other_half(top));
-    if (!SCALED) top *= c2;
-    // The maximum moves only where it would grow by more than 2^8: until then the sums are of exponentials up to 2^8.
-    if (__any(top > run.m + 8.f)) {
+            for (int h = 0; h < 2; ++h) {
+                grawa_f32x16 e;
+#pragma unroll
+                for (int r = 8 * h; r < 8 * h + 8; ++r) {
+                    e[r] = __builtin_amdgcn_exp2f(SCALED ? s[u][r] - base : __builtin_fmaf(s[u][r], c2, -base));
+                    sums[r % 2] += e[r];
+                }
+                as_operand(e, h, p[2 * u + h]);
+            }
+        sum = sums[0] + sums[1];
+    };
+    exponentials();
+    if (__any(sum > 8192.f || run.m == -__builtin_inff())) {
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
+        top = fmaxf(top, other_half(top));
+        if (!SCALED) top *= c2;
         const float m2 = fmaxf(run.m, top), f = m2 == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(run.m - m2);
         run.m = m2;
         run.l *= f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= f;
+        exponentials();
     }
-    const float base = run.m == -__builtin_inff() ? 0.f : run.m;
-#pragma unroll
-    for (int u = 0; u < NS; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[u][r] = __builtin_amdgcn_exp2f(SCALED ? s[u][r] - base : __builtin_fmaf(s[u][r], c2, -base));
-            run.l += s[u][r]; // before it is rounded: the gradients start from this sum
-        }
+    run.l += sum;
 }
 #endif
 
-// A block has 128 CT queries of one head, a wave 32 CT of them, and all waves share tiles of 64 keys and values, two in LDS.
+// A block has 128 queries of one head, a wave 32 of them, and all waves share tiles of 64 keys and values, two in LDS.
 // splits > 1: that many blocks share the keys, and k_attend_join puts their results together.
-template <bool BF16, int DP, int CT, bool BIAS>
-__global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[maybe_unused]] GrawaAttend a)
+template <bool BF16, int DP, bool BIAS>
+__global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 1) void k_attend([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int BK = 64, COLS = 128 * CT, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32;
+    constexpr int BK = 64, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32;
     typedef HeadTile<BF16, DP, BK, 4> Tile;
     typedef typename Tile::V V;
     __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES]; // two buffers of keys and values
@@ -61,17 +77,14 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
     const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
     const Place at = place_of(a, kn);
 
-    // The lane's columns.
-    const int i0 = qb * COLS + wave * 32 * CT + (lane & 31), pos0 = at.start + i0; // column c: 32 c more
-    const auto there = [&](int c) { return i0 + 32 * c < a.Sq; };
-    const auto counts = [&](int c) { return there(c) && pos0 + 32 * c >= 0 && pos0 + 32 * c < at.length; };
-    V q[CT][KS];
+    // The lane's column.
+    const int i = qb * 128 + wave * 32 + (lane & 31), pos = at.start + i;
+    const bool there = i < a.Sq, counts = there && pos >= 0 && pos < at.length;
+    V q[KS];
     {
-        const char *row = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i0 * a.q.token + (int64_t)head * a.q.head;
+        const char *row = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq + (int64_t)i * a.q.token + (int64_t)head * a.q.head;
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[c][ks] = load_line<BF16>(row + (int64_t)(32 * c) * a.q.token, 16 * ks + 8 * half, a.D, counts(c));
+        for (int ks = 0; ks < KS; ++ks) q[ks] = load_line<BF16>(row, 16 * ks + 8 * half, a.D, counts);
     }
     const float c2 = a.scale * LOG2E;
     float far = 0.f;
@@ -82,7 +95,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
     }
 
     // Tiles: those with first tokens, then those of the window.
-    const int p0 = at.start + qb * COLS, p1 = at.start + min((qb + 1) * COLS, a.Sq) - 1, w0 = p0 + wave * 32 * CT, w1 = w0 + 32 * CT - 1;
+    const int p0 = at.start + qb * 128, p1 = at.start + min((qb + 1) * 128, a.Sq) - 1, w0 = p0 + wave * 32, w1 = w0 + 31;
     const int end = min(p1, at.length - 1) + 1, begin = max(0, max(p0, 0) - a.window + 1);
     const bool any = p1 >= 0 && p0 < at.length;
     const int t0 = begin / BK, first_tiles = any ? min(t0, (min(a.sinks, end) + BK - 1) / BK) : 0, tiles = any ? first_tiles + (end + BK - 1) / BK - t0 : 0;
@@ -100,145 +113,117 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend([[mayb
     };
     const auto none = [&](int j0, int j1) { return j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0, int j1) { return j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks); };
-    // Scores of 32 keys and a set of columns: masked, with a bias in units of log2.
-    const auto scores = [&](int j0, int c, grawa_f32x16 &s) __attribute__((always_inline)) {
+    // Scores of 32 keys: masked, with a bias in units of log2.
+    const auto scores = [&](int j0, grawa_f32x16 &s) __attribute__((always_inline)) {
         if constexpr (BIAS) {
-            const bool is_far = w0 - (j0 + 31) >= a.distances - 1;
+            if (w0 - (j0 + 31) >= a.distances - 1) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int d = pos0 + 32 * c - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half);
-                s[r] = s[r] * c2 + (is_far ? far : table[clamp_int(d, 0, a.distances - 1)]);
+                for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], c2, far);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[r] = __builtin_fmaf(s[r], c2, table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)]);
             }
         }
         if (!all(j0, j0 + 31))
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = sees(a, pos0 + 32 * c, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : -__builtin_inff();
+            for (int r = 0; r < 16; ++r) s[r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : -__builtin_inff();
     };
 
-    grawa_f32x16 o[CT][DT];
-    Running run[CT];
+    grawa_f32x16 o[DT];
+    Running run{-__builtin_inff(), 0.f};
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        run[c] = Running{-__builtin_inff(), 0.f};
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[c][d] = grawa_f32x16{};
-    }
-    const auto step = [&](const char *buf, int j0) __attribute__((always_inline)) {
-        constexpr int A = BF16 ? 4 : 2;
-        V f[A];
-        const uint32_t rows = Tile::rows_of(buf, lane), columns = Tile::columns_of(buf + Tile::BYTES, lane);
-        const auto key = [&](int i) { return Tile::by_rows(rows, i % 2 * 32, i / 2); };
-        const auto value = [&](int i) { return Tile::by_columns(columns, i / DT * 16, i % DT); };
-        grawa_f32x16 s[CT][2];
-#pragma unroll
-        for (int c = 0; c < CT; ++c) s[c][0] = s[c][1] = grawa_f32x16{};
-        ask(f, key);
-        flow<2 * KS>(f, key, [&](int i, const V &x) __attribute__((always_inline)) {
-#pragma unroll
-            for (int c = 0; c < CT; ++c) s[c][i % 2] = mfma(x, q[c][i / 2], s[c][i % 2]);
-        });
-        ask(f, value);
-        V p[CT][4];
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) scores(j0 + 32 * u, c, s[c][u]);
-            soften<BIAS>(s[c], c2, run[c], o[c]);
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) as_operand(s[c][u], h, p[c][2 * u + h]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        flow<4 * DT>(f, value, [&](int i, const V &x) __attribute__((always_inline)) {
-#pragma unroll
-            for (int c = 0; c < CT; ++c) o[c][i % DT] = mfma(x, p[c][i / DT], o[c][i % DT]);
-        });
-    };
+    for (int d = 0; d < DT; ++d) o[d] = grawa_f32x16{};
     if (from < to) load(from, lds);
     for (int it = from; it < to; ++it) {
         const char *buf = lds + ((it - from) & 1) * 2 * Tile::BYTES;
         landed();
         if (it + 1 < to) load(it + 1, lds + ((it + 1 - from) & 1) * 2 * Tile::BYTES);
-        const int j0 = tile_of(it), j1 = j0 + BK - 1;
-        if (!none(j0, j1)) step(buf, j0);
+        const int j0 = tile_of(it);
+        if (none(j0, j0 + BK - 1)) continue;
+        constexpr int A = BF16 ? 4 : 2;
+        V f[A], p[4];
+        const uint32_t rows = Tile::rows_of(buf, lane), columns = Tile::columns_of(buf + Tile::BYTES, lane);
+        const auto key = [&](int i) { return Tile::by_rows(rows, i % 2 * 32, i / 2); };
+        const auto value = [&](int i) { return Tile::by_columns(columns, i / DT * 16, i % DT); };
+        grawa_f32x16 s[2] = {};
+        ask(f, key);
+        flow<2 * KS>(f, key, [&](int i, const V &x) __attribute__((always_inline)) { s[i % 2] = mfma(x, q[i / 2], s[i % 2]); });
+        ask(f, value);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) scores(j0 + 32 * u, s[u]);
+        soften<BIAS>(s, c2, run, o, p);
+        __builtin_amdgcn_sched_barrier(0);
+        flow<4 * DT>(f, value, [&](int i, const V &x) __attribute__((always_inline)) { o[i % DT] = mfma(x, p[i / DT], o[i % DT]); });
     }
 
-    const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row0 = ((int64_t)kn * a.H + head) * a.Sq + i0;
-    float *part = a.part + (int64_t)split * rows * DP + row0 * DP, *part_lse = a.part + (int64_t)a.splits * rows * DP + (int64_t)split * rows + row0;
-    char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i0 * a.o.token + (int64_t)head * a.o.head;
-    float f[CT]; // what the sums are divided by
-    bool odd = false;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const float l = run[c].l + other_half(run[c].l);
-        const bool sum = counts(c) && !(l == 0.f);
-        const float lse2 = sum ? run[c].m + __builtin_amdgcn_logf(l) : -__builtin_inff();
-        f[c] = sum ? 1.f / l : 0.f;
-        if (half == 0 && there(c)) {
-            if (a.splits > 1)
-                part_lse[32 * c] = lse2;
-            else if (a.lse)
-                a.lse[row0 + 32 * c] = lse2 * LN2;
-        }
-        if (sum)
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) odd |= o[c][d][r] != o[c][d][r];
+    const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row = ((int64_t)kn * a.H + head) * a.Sq + i;
+    float *part = a.part + ((int64_t)split * rows + row) * DP;
+    char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i * a.o.token + (int64_t)head * a.o.head;
+    const float l = run.l + other_half(run.l);
+    const bool sum = counts && !(l == 0.f);
+    const float lse2 = sum ? run.m + __builtin_amdgcn_logf(l) : -__builtin_inff(), f = sum ? 1.f / l : 0.f;
+    if (half == 0 && there) {
+        if (a.splits > 1)
+            a.part[(int64_t)a.splits * rows * DP + (int64_t)split * rows + row] = lse2;
+        else if (a.lse)
+            a.lse[row] = lse2 * LN2;
     }
-    const auto put = [&](int c, int d, const grawa_f32x16 &sums) {
-        if (!there(c)) return;
+    const auto put = [&](int d, const grawa_f32x16 &sums) {
+        if (!there) return;
         grawa_f32x16 v;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) v[r] = f[c] == 0.f ? 0.f : sums[r] * f[c];
+        for (int r = 0; r < 16; ++r) v[r] = sum ? sums[r] * f : 0.f;
         if (a.splits > 1)
-            store_column<false>((char *)(part + 32 * c * DP), lane, d, DP, v, 1.f);
+            store_column<false>((char *)part, lane, d, DP, v, 1.f);
         else
-            store_column<BF16>(out + (int64_t)(32 * c) * a.o.token, lane, d, a.D, v, 1.f);
+            store_column<BF16>(out, lane, d, a.D, v, 1.f);
     };
+    bool odd = false;
+    if (sum)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) odd |= o[d][r] != o[d][r];
     // What is no number may come from a token that the column does not see: once more then, with care.
     if (__builtin_expect(!__syncthreads_or(odd), 1)) {
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) put(c, d, o[c][d]);
+        for (int d = 0; d < DT; ++d) put(d, o[d]);
         return;
     }
+    const float base = run.m == -__builtin_inff() ? 0.f : run.m;
 #pragma unroll 1
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const float base = run[c].m == -__builtin_inff() ? 0.f : run[c].m;
-            grawa_f32x16 sums = {};
-            for (int it = from; it < to; ++it) {
-                landed();
-                load(it, lds);
-                landed();
+    for (int d = 0; d < DT; ++d) {
+        grawa_f32x16 sums = {};
 #pragma unroll 1
-                for (int u = 0; u < 2; ++u) {
-                    const int j0 = tile_of(it) + 32 * u, j1 = j0 + 31;
-                    if (none(j0, j1)) continue;
-                    grawa_f32x16 s = {};
+        for (int it = from; it < to; ++it) {
+            landed();
+            load(it, lds);
+            landed();
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u) {
+                const int j0 = tile_of(it) + 32 * u, j1 = j0 + 31;
+                if (none(j0, j1)) continue;
+                grawa_f32x16 s = {};
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(Tile::rows_of(lds + 32 * u * Tile::RB, lane), 0, ks), q[c][ks], s);
-                    scores(j0, c, s);
+                for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(Tile::rows_of(lds + 32 * u * Tile::RB, lane), 0, ks), q[ks], s);
+                scores(j0, s);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(BIAS ? s[r] - base : __builtin_fmaf(s[r], c2, -base));
+                for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(BIAS ? s[r] - base : __builtin_fmaf(s[r], c2, -base));
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        V p;
-                        as_operand(s, h, p);
-                        const V v = Tile::by_columns(Tile::columns_of(lds + Tile::BYTES + (32 * u + 16 * h) * Tile::RB, lane), 0, d);
-                        if (all(j0, j1))
-                            sums = mfma(v, p, sums);
-                        else
-                            product_of_some(sums, v, p, marks<V>(a, pos0 + 32 * c, j0 + 16 * h, half));
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    V p;
+                    as_operand(s, h, p);
+                    const V v = Tile::by_columns(Tile::columns_of(lds + Tile::BYTES + (32 * u + 16 * h) * Tile::RB, lane), 0, d);
+                    if (all(j0, j1))
+                        sums = mfma(v, p, sums);
+                    else
+                        product_of_some(sums, v, p, marks<V>(a, pos, j0 + 16 * h, half));
                 }
             }
-            put(c, d, sums);
         }
+        put(d, sums);
+    }
 #endif
 }
 
@@ -323,18 +308,17 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
             if (!all)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[0][r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[0][r] : -__builtin_inff();
-            soften<BIAS>(s, c2, run, o);
+            V p[2];
+            soften<BIAS>(s, c2, run, o, p);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                V p;
-                as_operand(s[0], h, p);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const V v = Tile::by_columns(Tile::columns_of(buf + Tile::BYTES + wave * 32 * Tile::RB, lane), 16 * h, d);
                     if (careful.value && !all)
-                        product_of_some(o[d], v, p, marks<V>(a, pos, j0 + 16 * h, half));
+                        product_of_some(o[d], v, p[h], marks<V>(a, pos, j0 + 16 * h, half));
                     else
-                        o[d] = mfma(v, p, o[d]);
+                        o[d] = mfma(v, p[h], o[d]);
                 }
             }
         }
@@ -458,14 +442,10 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
         const uint32_t grid = grid_of(kn * a.G, (int64_t)a.blocks * a.splits, a.by_xcd);
         hipLaunchKernelGGL((k_attend_few<BF16, DP, BIAS, KW>), dim3(grid), dim3(KW * 64), 0, st, a);
     } else {
-        const bool wide = BF16 && DP == 64 && kn * a.H * ((a.Sq + 255) / 256) >= 512;
-        a.blocks = wide ? (a.Sq + 255) / 256 : (a.Sq + 127) / 128;
+        a.blocks = (a.Sq + 127) / 128;
         a.splits = splits_of(kn * a.H * a.blocks, rows, DP, (seen + 63) / 64, part_floats);
         const uint32_t grid = grid_of(kn * a.H, (int64_t)a.blocks * a.splits, a.by_xcd);
-        if (wide)
-            hipLaunchKernelGGL((k_attend<BF16, DP, BF16 && DP == 64 ? 2 : 1, BIAS>), dim3(grid), dim3(256), 0, st, a);
-        else
-            hipLaunchKernelGGL((k_attend<BF16, DP, 1, BIAS>), dim3(grid), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_attend<BF16, DP, BIAS>), dim3(grid), dim3(256), 0, st, a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     if (half == 0 && i < a.row_pitch) {
         const int64_t row = ((int64_t)kn * a.H + head) * a.row_pitch + i;
         a.row_lse[row] = lse;
-        a.row_dot[row] = delta;
+        a.row_dot[row] = -delta;
     }
 
     const float c2 = a.scale * LOG2E;
@@ -79,10 +79,13 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     };
     const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0) { return j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
+    grawa_f32x16 minus_dot;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) minus_dot[r] = -delta;
     constexpr int A = BF16 ? 4 : 2;
     // dS of 32 keys; leaves the first fragments of `then` in f.
     const auto slopes = [&](const char *buf, int u, int j0, V (&f)[A], auto &&then) __attribute__((always_inline)) {
-        grawa_f32x16 s = {}, dp = {};
+        grawa_f32x16 s = {}, dp = minus_dot;
         const uint32_t rows[2] = {Tile::rows_of(buf + 32 * u * Tile::RB, lane), Tile::rows_of(buf + Tile::BYTES + 32 * u * Tile::RB, lane)};
         const auto both = [&](int i) { return Tile::by_rows(rows[i % 2], 0, i / 2); };
         ask(f, both);
@@ -98,7 +101,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         for (int r = 0; r < 16; ++r) {
             float b = -lse;
             if constexpr (BIAS) b += is_far ? far : table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, b)) * (dp[r] - delta);
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, b)) * dp[r];
         }
         if (!all(j0))
 #pragma unroll
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     typedef HeadTile<BF16, DP, BKV, NW> Values;
     typedef typename Tile::V V;
     __shared__ __attribute__((aligned(1024))) char lds[BUFS * 2 * Tile::BYTES]; // queries and gradients of outputs
-    __shared__ __attribute__((aligned(1024))) float of_rows[2][2][BQ];          // log2 of the sums of exponentials, do . o
+    __shared__ __attribute__((aligned(1024))) float of_rows[2][2][BQ];          // log2 of the sums of exponentials, -do . o
     __shared__ __attribute__((aligned(1024))) char values[KEEP ? 16 : Values::BYTES];
     __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -345,7 +348,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
         for (int x = 0; x < 4; ++x) {
             const grawa_f32x4v dot = *(const grawa_f32x4v *)(of_rows[b][1] + 32 * u + 8 * x + 4 * half);
 #pragma unroll
-            for (int y = 0; y < 4; ++y) dp[4 * x + y] = -dot[y];
+            for (int y = 0; y < 4; ++y) dp[4 * x + y] = dot[y];
         }
         V v[KEEP ? 1 : 2]; // values, asked for two before they are used
         if constexpr (!KEEP) v[0] = value(0), v[1] = value(1);

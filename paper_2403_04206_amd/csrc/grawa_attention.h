@@ -22,7 +22,7 @@ struct grawa_attention_plan {
     char *ws;
     double *turns;          // [rotary / 2] turns a position
     int *bucket_of;         // [distances]
-    float *rows;            // two of [K N][H][S rounded up to 256]: log2 of the sum of exponentials, do . o
+    float *rows;            // two of [K N][H][S rounded up to 256]: log2 of the sum of exponentials, -do . o
     float *norm_part;       // [K][norm_blocks][2][D] sums of the weights' gradients
     float *bias_part;       // [K N][H][blocks of queries][buckets]
     float *part;            // outputs and sums of blocks that share them
@@ -45,7 +45,7 @@ struct GrawaAttend {
     float *lse;                  // [K][N][H][Sq] or null
     GrawaMat bias, dbias;        // [H][buckets] of every worker
     const int *bucket_of;
-    float *row_lse, *row_dot;    // [K N][H][row_pitch]: log2 of the sum of exponentials (infinity: the row counts for nothing), do . o
+    float *row_lse, *row_dot;    // [K N][H][row_pitch]: log2 of the sum of exponentials (infinity: the row counts for nothing), -do . o
     float *bias_part, *part;
     int64_t row_pitch;           // Sq rounded up to 256
     int K, N, H, G, D, Sq, Sk, share; // share = H / G
