@@ -100,52 +100,52 @@ template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS_AT void *)(lds + (wave + NW * i) * 1024), 16, first[i % TURNS] + (uint32_t)(i / TURNS) * step, 0, 0, 0);
     }
 
-    // Fragments: an address of the lane's that all of a tile's share, of which a fragment's differs by some of its low bits and by a constant.
-    static __device__ __forceinline__ uint32_t rows_of(const char *lds, int lane)
+    // Fragments: an offset of the lane's that all of a tile's share, of which a fragment's differs by some of its low bits and by a constant.
+    // Tiles are arrays by themselves and a fragment is read from its array: the compiler then knows that loads on their way into another
+    // one need not land first.
+    static __device__ __forceinline__ uint32_t rows_of(int lane)
     {
         const int row = lane & 31, half = lane >> 5;
-        return (uint32_t)(uintptr_t)(GRAWA_LDS_AT const char *)lds + row * RB + (((BF16 ? half : 2 * half) ^ key(row)) << 4);
+        return row * RB + (((BF16 ? half : 2 * half) ^ key(row)) << 4);
     }
-    static __device__ __forceinline__ uint32_t columns_of(const char *lds, int lane)
+    static __device__ __forceinline__ uint32_t columns_of(int lane)
     {
         const int half = lane >> 5, s = lane & 15, row = 4 * half + (s >> 2), m = lane & 31;
-        const uint32_t at = (uint32_t)(uintptr_t)(GRAWA_LDS_AT const char *)lds;
-        if constexpr (BF16) return at + row * RB + (((2 * ((lane >> 4) & 1) + ((s & 3) >> 1)) ^ key(row)) << 4) + (s & 1) * 8;
-        return at + 4 * half * RB + (((m >> 2) ^ key(4 * half)) << 4) + (m & 3) * 4;
+        if constexpr (BF16) return row * RB + (((2 * ((lane >> 4) & 1) + ((s & 3) >> 1)) ^ key(row)) << 4) + (s & 1) * 8;
+        return 4 * half * RB + (((m >> 2) ^ key(4 * half)) << 4) + (m & 3) * 4;
     }
-    template <class T> static __device__ __forceinline__ T read(uint32_t at, int constant) { return *(GRAWA_LDS_AT const T *)((GRAWA_LDS_AT const char *)(uintptr_t)at + constant); }
 
     // Lines row0 ... row0 + 31 (a multiple of 32), elements 16 ks ... of the head.
-    static __device__ __forceinline__ V by_rows(uint32_t at, int row0, int ks)
+    static __device__ __forceinline__ V by_rows(const char *tile, uint32_t at, int row0, int ks)
     {
         if constexpr (BF16) {
-            return read<V>(at ^ (ks << 5), row0 * RB);
+            return *(const V *)(tile + row0 * RB + (at ^ (ks << 5)));
         } else {
-            const grawa_f32x4v a = read<grawa_f32x4v>(at ^ (ks << 6), row0 * RB), b = read<grawa_f32x4v>(at ^ (ks << 6) ^ 16, row0 * RB);
+            const grawa_f32x4v a = *(const grawa_f32x4v *)(tile + row0 * RB + (at ^ (ks << 6))), b = *(const grawa_f32x4v *)(tile + row0 * RB + (at ^ (ks << 6) ^ 16));
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
     // Lines: elements 32 dt ... of the head, k: tokens row0 ... row0 + 15 (a multiple of 16) in the order of a product's registers.
-    static __device__ __forceinline__ V by_columns(uint32_t at, int row0, int dt)
+    static __device__ __forceinline__ V by_columns(const char *tile, uint32_t at, int row0, int dt)
     {
         if constexpr (BF16) {
             const uint32_t lower = at ^ (dt << 6), upper = lower ^ 32; // eight rows on, the key's second bit is another
-            const grawa_s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)lower + row0 * RB));
-            const grawa_s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)((GRAWA_LDS_AT char *)(uintptr_t)upper + (row0 + 8) * RB));
+            const grawa_s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)(tile + row0 * RB + lower));
+            const grawa_s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GRAWA_LDS_AT grawa_s16x4v *)(tile + (row0 + 8) * RB + upper));
             return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             V v;
 #pragma unroll
             for (int j = 0; j < 8; ++j) { // rows 4 (lane / 32) + j % 4 + 8 (j / 4): what their keys differ in
                 const int row = (j & 3) + 8 * (j >> 2);
-                v[j] = read<float>(at ^ (dt << 7) ^ (key(row) << 4), (row0 + row) * RB);
+                v[j] = *(const float *)(tile + (row0 + row) * RB + (at ^ (dt << 7) ^ (key(row) << 4)));
             }
             return v;
         }
     }
 };
 
-// Keeps what an address differs in from being formed ahead for all fragments and held in registers.
+// Keeps what an offset differs in from being formed ahead for all fragments and held in registers.
 __device__ __forceinline__ uint32_t here(uint32_t at)
 {
     asm volatile("" : "+v"(at));

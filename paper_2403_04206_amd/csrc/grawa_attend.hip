@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
     constexpr int BK = 64, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32;
     typedef HeadTile<BF16, DP, BK, 4> Tile;
     typedef typename Tile::V V;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES]; // two buffers of keys and values
+    __shared__ __attribute__((aligned(1024))) char buf0[2 * Tile::BYTES], buf1[2 * Tile::BYTES]; // keys and values
     __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];              // the bias by distance
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int heads = a.K * a.N * a.H;
@@ -134,18 +134,16 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
     Running run{-__builtin_inff(), 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = grawa_f32x16{};
-    if (from < to) load(from, lds);
-    for (int it = from; it < to; ++it) {
-        const char *buf = lds + ((it - from) & 1) * 2 * Tile::BYTES;
+    const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
+    const auto step = [&](int it, const char *buf, char *ahead) __attribute__((always_inline)) {
         landed();
-        if (it + 1 < to) load(it + 1, lds + ((it + 1 - from) & 1) * 2 * Tile::BYTES);
+        if (it + 1 < to) load(it + 1, ahead);
         const int j0 = tile_of(it);
-        if (none(j0, j0 + BK - 1)) continue;
+        if (none(j0, j0 + BK - 1)) return;
         constexpr int A = BF16 ? 4 : 2;
         V f[A], p[4];
-        const uint32_t rows = Tile::rows_of(buf, lane), columns = Tile::columns_of(buf + Tile::BYTES, lane);
-        const auto key = [&](int i) { return Tile::by_rows(rows, i % 2 * 32, i / 2); };
-        const auto value = [&](int i) { return Tile::by_columns(columns, i / DT * 16, i % DT); };
+        const auto key = [&](int i) { return Tile::by_rows(buf, rows_at, i % 2 * 32, i / 2); };
+        const auto value = [&](int i) { return Tile::by_columns(buf + Tile::BYTES, columns_at, i / DT * 16, i % DT); };
         grawa_f32x16 s[2] = {};
         ask(f, key);
         flow<2 * KS>(f, key, [&](int i, const V &x) __attribute__((always_inline)) { s[i % 2] = mfma(x, q[i / 2], s[i % 2]); });
@@ -155,6 +153,11 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
         soften<BIAS>(s, c2, run, o, p);
         __builtin_amdgcn_sched_barrier(0);
         flow<4 * DT>(f, value, [&](int i, const V &x) __attribute__((always_inline)) { o[i % DT] = mfma(x, p[i / DT], o[i % DT]); });
+    };
+    if (from < to) load(from, buf0);
+    for (int it = from; it < to; it += 2) {
+        step(it, buf0, buf1);
+        if (it + 1 < to) step(it + 1, buf1, buf0);
     }
 
     const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row = ((int64_t)kn * a.H + head) * a.Sq + i;
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
 #pragma unroll 1
         for (int it = from; it < to; ++it) {
             landed();
-            load(it, lds);
+            load(it, buf0);
             landed();
 #pragma unroll 1
             for (int u = 0; u < 2; ++u) {
@@ -206,7 +209,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
                 if (none(j0, j1)) continue;
                 grawa_f32x16 s = {};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(Tile::rows_of(lds + 32 * u * Tile::RB, lane), 0, ks), q[ks], s);
+                for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf0 + 32 * u * Tile::RB, rows_at, 0, ks), q[ks], s);
                 scores(j0, s);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(BIAS ? s[r] - base : __builtin_fmaf(s[r], c2, -base));
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
                 for (int h = 0; h < 2; ++h) {
                     V p;
                     as_operand(s, h, p);
-                    const V v = Tile::by_columns(Tile::columns_of(lds + Tile::BYTES + (32 * u + 16 * h) * Tile::RB, lane), 0, d);
+                    const V v = Tile::by_columns(buf0 + Tile::BYTES + (32 * u + 16 * h) * Tile::RB, columns_at, 0, d);
                     if (all(j0, j1))
                         sums = mfma(v, p, sums);
                     else
@@ -236,7 +239,11 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
     constexpr int BK = 32 * NW, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32;
     typedef HeadTile<BF16, DP, BK, NW> Tile;
     typedef typename Tile::V V;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES]; // two buffers of keys and values
+    __shared__ __attribute__((aligned(1024))) char buf0[2 * Tile::BYTES], buf1[2 * Tile::BYTES]; // keys and values
+    constexpr int PITCH = DP + 4;
+    __shared__ float ml[NW * 64]; // of each wave, joined at the end
+    static_assert(NW / 2 * 32 * PITCH * 4 <= 2 * Tile::BYTES, "room for half the waves' sums in a buffer");
+    const auto sums_of = [&](int w, int column) { return (float *)(w < NW / 2 ? buf0 : buf1) + (w % (NW / 2) * 32 + column) * PITCH; };
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int groups = a.K * a.N * a.G;
     const Turn turn = turn_of(blockIdx.x, groups, a.by_xcd);
@@ -278,21 +285,20 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 
     grawa_f32x16 o[DT];
     Running run;
+    const uint32_t rows_at = Tile::rows_of(lane) + wave * 32 * Tile::RB, columns_at = Tile::columns_of(lane) + wave * 32 * Tile::RB;
     const auto go = [&](auto careful) __attribute__((always_inline)) {
         run = Running{-__builtin_inff(), 0.f};
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] = grawa_f32x16{};
-        if (from < to) load(from, lds);
-        for (int it = from; it < to; ++it) {
-            const char *buf = lds + ((it - from) & 1) * 2 * Tile::BYTES;
+        const auto step = [&](int it, const char *buf, char *ahead) __attribute__((always_inline)) {
             landed();
-            if (it + 1 < to) load(it + 1, lds + ((it + 1 - from) & 1) * 2 * Tile::BYTES);
+            if (it + 1 < to) load(it + 1, ahead);
             const int j0 = tile_of(it) + wave * 32, j1 = j0 + 31;
-            if (j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks)) continue; // none of the wave's pairs count
+            if (j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks)) return; // none of the wave's pairs count
             const bool all = j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks);
             grawa_f32x16 s[1] = {};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[0] = mfma(Tile::by_rows(Tile::rows_of(buf + wave * 32 * Tile::RB, lane), 0, ks), q[ks], s[0]);
+            for (int ks = 0; ks < KS; ++ks) s[0] = mfma(Tile::by_rows(buf, rows_at, 0, ks), q[ks], s[0]);
             if constexpr (BIAS) {
                 if (w0 - j1 >= a.distances - 1) {
 #pragma unroll
@@ -311,16 +317,20 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
             V p[2];
             soften<BIAS>(s, c2, run, o, p);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    const V v = Tile::by_columns(Tile::columns_of(buf + Tile::BYTES + wave * 32 * Tile::RB, lane), 16 * h, d);
+                    const V v = Tile::by_columns(buf + Tile::BYTES, columns_at, 16 * h, d);
                     if (careful.value && !all)
                         product_of_some(o[d], v, p[h], marks<V>(a, pos, j0 + 16 * h, half));
                     else
                         o[d] = mfma(v, p[h], o[d]);
                 }
-            }
+        };
+        if (from < to) load(from, buf0);
+        for (int it = from; it < to; it += 2) {
+            step(it, buf0, buf1);
+            if (it + 1 < to) step(it + 1, buf1, buf0);
         }
         bool odd = false;
         if (!careful.value && counts)
@@ -334,14 +344,11 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
     if (__builtin_expect(go(Is<false>()), 0)) go(Is<true>());
 
     const float l = run.l + other_half(run.l);
-    constexpr int PITCH = DP + 4;
-    float *sums = (float *)lds, *ml = sums + NW * 32 * PITCH;
-    static_assert((NW * 32 * PITCH + NW * 64) * 4 <= 4 * Tile::BYTES, "room for the waves' sums");
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            *(grawa_f32x4v *)(sums + (wave * 32 + (lane & 31)) * PITCH + 32 * d + 8 * r + 4 * half) = grawa_f32x4v{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+            *(grawa_f32x4v *)(sums_of(wave, lane & 31) + 32 * d + 8 * r + 4 * half) = grawa_f32x4v{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
     if (half == 0) ml[wave * 64 + lane] = run.m, ml[wave * 64 + 32 + lane] = l;
     __syncthreads();
     constexpr int LPC = NW * 2, EPL = DP / LPC; // threads of a column, elements of each
@@ -358,7 +365,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
         const float f = __builtin_amdgcn_exp2f(mw - top);
         total += lw * f;
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) v[e] += sums[(w * 32 + cl) * PITCH + e0 + e] * f;
+        for (int e = 0; e < EPL; ++e) v[e] += sums_of(w, cl)[e0 + e] * f;
     }
     const bool sum = p >= 0 && p < at.length && !(total == 0.f);
     const float f = sum ? 1.f / total : 0.f, lse2 = sum ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();

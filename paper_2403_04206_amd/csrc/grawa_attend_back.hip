@@ -15,7 +15,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     constexpr int BK = 64, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
     typedef HeadTile<BF16, DP, BK, 4> Tile;
     typedef typename Tile::V V;
-    __shared__ __attribute__((aligned(1024))) char lds[BUFS * 2 * Tile::BYTES]; // keys and values
+    __shared__ __attribute__((aligned(1024))) char buf0[2 * Tile::BYTES], buf1[BUFS == 2 ? 2 * Tile::BYTES : 16]; // keys and values
     __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];                     // the bias by distance
     __shared__ float by_distance[BIAS ? 4 : 1][BIAS ? GRAWA_MAX_DISTANCES : 1]; // of each wave: sums of dS
     __shared__ float square[BIAS ? 4 : 1][BIAS ? 32 * 33 : 1];
@@ -79,6 +79,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     };
     const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0) { return j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
+    const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
     grawa_f32x16 minus_dot;
 #pragma unroll
     for (int r = 0; r < 16; ++r) minus_dot[r] = -delta;
@@ -86,8 +87,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     // dS of 32 keys; leaves the first fragments of `then` in f.
     const auto slopes = [&](const char *buf, int u, int j0, V (&f)[A], auto &&then) __attribute__((always_inline)) {
         grawa_f32x16 s = {}, dp = minus_dot;
-        const uint32_t rows[2] = {Tile::rows_of(buf + 32 * u * Tile::RB, lane), Tile::rows_of(buf + Tile::BYTES + 32 * u * Tile::RB, lane)};
-        const auto both = [&](int i) { return Tile::by_rows(rows[i % 2], 0, i / 2); };
+        const auto both = [&](int i) { return Tile::by_rows(buf + i % 2 * Tile::BYTES, rows_at + 32 * u * Tile::RB, 0, i / 2); };
         ask(f, both);
         flow<2 * KS>(f, both, [&](int i, const V &x) __attribute__((always_inline)) {
             if (i % 2)
@@ -115,8 +115,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
     const auto step = [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
         V f[A];
-        const uint32_t at = Tile::columns_of(buf + 32 * u * Tile::RB, lane);
-        const auto columns = [&](int i) { return Tile::by_columns(at, i / DT * 16, i % DT); };
+        const auto columns = [&](int i) { return Tile::by_columns(buf, columns_at + 32 * u * Tile::RB, i / DT * 16, i % DT); };
         const grawa_f32x16 s = slopes(buf, u, j0, f, columns);
         if constexpr (BIAS) {
             if (w0 - (j0 + 31) >= a.distances - 1) {
@@ -145,18 +144,29 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         __builtin_amdgcn_sched_barrier(0);
         flow<2 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) { dq[i % DT] = mfma(x, w[i / DT], dq[i % DT]); });
     };
-    if (BUFS == 2 && tiles) load(0, lds);
-    for (int it = 0; it < tiles; ++it) {
-        char *buf = lds + (BUFS == 2 ? it & 1 : 0) * 2 * Tile::BYTES;
-        if (BUFS == 1) {
-            landed();
-            load(it, buf);
-        }
-        landed();
-        if (BUFS == 2 && it + 1 < tiles) load(it + 1, lds + ((it + 1) & 1) * 2 * Tile::BYTES);
+    const auto both_halves = [&](int it, const char *buf) __attribute__((always_inline)) {
         for (int u = 0; u < 2; ++u) {
             const int j0 = tile_of(it) + 32 * u;
             if (!none(j0)) step(buf, u, j0);
+        }
+    };
+    if constexpr (BUFS == 2) {
+        if (tiles) load(0, buf0);
+        for (int it = 0; it < tiles; it += 2) {
+            landed();
+            if (it + 1 < tiles) load(it + 1, buf1);
+            both_halves(it, buf0);
+            if (it + 1 == tiles) break;
+            landed();
+            if (it + 2 < tiles) load(it + 2, buf0);
+            both_halves(it + 1, buf1);
+        }
+    } else {
+        for (int it = 0; it < tiles; ++it) {
+            landed();
+            load(it, buf0);
+            landed();
+            both_halves(it, buf0);
         }
     }
     bool odd = false;
@@ -183,19 +193,19 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             grawa_f32x16 sums = {};
             for (int it = 0; it < tiles; ++it) {
                 landed();
-                load(it, lds);
+                load(it, buf0);
                 landed();
 #pragma unroll 1
                 for (int u = 0; u < 2; ++u) {
                     const int j0 = tile_of(it) + 32 * u;
                     if (none(j0)) continue;
                     V f[A];
-                    const grawa_f32x16 s = slopes(lds, u, j0, f, [&](int) { return V{}; });
+                    const grawa_f32x16 s = slopes(buf0, u, j0, f, [&](int) { return V{}; });
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         V w;
                         as_operand(s, h, w);
-                        const V c = Tile::by_columns(Tile::columns_of(lds + (32 * u + 16 * h) * Tile::RB, lane), 0, d);
+                        const V c = Tile::by_columns(buf0 + (32 * u + 16 * h) * Tile::RB, columns_at, 0, d);
                         if (all(j0))
                             sums = mfma(c, w, sums);
                         else
@@ -249,8 +259,8 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     typedef HeadTile<BF16, DP, BQ, NW> Tile;
     typedef HeadTile<BF16, DP, BKV, NW> Values;
     typedef typename Tile::V V;
-    __shared__ __attribute__((aligned(1024))) char lds[BUFS * 2 * Tile::BYTES]; // queries and gradients of outputs
-    __shared__ __attribute__((aligned(1024))) float of_rows[2][2][BQ];          // log2 of the sums of exponentials, -do . o
+    __shared__ __attribute__((aligned(1024))) char buf0[2 * Tile::BYTES], buf1[BUFS == 2 ? 2 * Tile::BYTES : 16]; // queries and gradients of outputs
+    __shared__ __attribute__((aligned(1024))) float rows0[2 * BQ], rows1[2 * BQ]; // log2 of the sums of exponentials, -do . o
     __shared__ __attribute__((aligned(1024))) char values[KEEP ? 16 : Values::BYTES];
     __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -282,12 +292,12 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
         lv.load(values, wave, Values::rsrc(a.v.p + (int64_t)k * a.v.worker + (int64_t)n * a.v.seq + (int64_t)b0 * a.v.token + (int64_t)g * a.v.head,
                                            at.length - b0, (uint32_t)a.v.token, a.D));
     }
-    const uint32_t values_at = Values::rows_of(values + (KEEP ? 0 : wave * 32 * Values::RB), lane);
+    const uint32_t values_at = Values::rows_of(lane) + wave * 32 * Values::RB;
     const auto value = [&](int ks) {
         if constexpr (KEEP)
             return vf[ks];
         else
-            return Values::by_rows(here(values_at), 0, ks);
+            return Values::by_rows(values, here(values_at), 0, ks);
     };
     const float c2 = a.scale * LOG2E;
 
@@ -307,15 +317,14 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
         const int h = it / tiles;
         return At{h, (t0 + it - h * tiles) * BQ};
     };
-    const auto load = [&](At t, int b) {
+    const auto load = [&](At t, char *buf, float *rows) {
         const int head = g * a.share + t.h;
-        char *buf = lds + b * 2 * Tile::BYTES;
         lq.load(buf, wave, Tile::rsrc(qp + (int64_t)t.tile * a.q.token + (int64_t)head * a.q.head, last + 1 - t.tile, (uint32_t)a.q.token, a.D));
         lg.load(buf + Tile::BYTES, wave, Tile::rsrc(gp + (int64_t)t.tile * a.go.token + (int64_t)head * a.go.head, last + 1 - t.tile, (uint32_t)a.go.token, a.D));
         if (wave < 2) { // rows up to the pitch, a multiple of a tile, are there
             const float *p = (wave ? a.row_dot : a.row_lse) + ((int64_t)kn * a.H + head) * a.row_pitch + t.tile;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, BQ * 4, 0x00020000),
-                                                     (GRAWA_LDS_AT void *)of_rows[b][wave], 4, (uint32_t)lane * 4, 0, 0, 0);
+                                                     (GRAWA_LDS_AT void *)(rows + wave * BQ), 4, (uint32_t)lane * 4, 0, 0, 0);
         }
     };
     const auto next = [&](At t) {
@@ -337,16 +346,17 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     // p0: position of the first of 32 queries
     const auto none = [&](int p0) { return w0 > p0 + 31 || w0 >= at.length || (w1 <= p0 - a.window && w0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int p0) { return w1 <= p0 && (p0 + 31 - w0 < a.window || w1 < a.sinks); };
+    const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
     constexpr int A = BF16 ? 4 : 2;
     // P and dS of 32 queries; leaves the first fragments of `then` in f.
-    const auto slopes = [&](const char *buf, int b, int u, int p0, grawa_f32x16 &s, grawa_f32x16 &dp, V (&f)[A], auto &&then) __attribute__((always_inline)) {
-        const uint32_t at = Tile::rows_of(buf + 32 * u * Tile::RB, lane);
-        const auto rows = [&](int i) { return Tile::by_rows(KEEP ? at : here(at), i / KS * (Tile::BYTES / Tile::RB), i % KS); };
+    const auto slopes = [&](const char *buf, const float *of_rows, int u, int p0, grawa_f32x16 &s, grawa_f32x16 &dp, V (&f)[A], auto &&then) __attribute__((always_inline)) {
+        const uint32_t at = rows_at + 32 * u * Tile::RB;
+        const auto rows = [&](int i) { return Tile::by_rows(buf + i / KS * Tile::BYTES, KEEP ? at : here(at), 0, i % KS); };
         s = grawa_f32x16{};
         ask(f, rows);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            const grawa_f32x4v dot = *(const grawa_f32x4v *)(of_rows[b][1] + 32 * u + 8 * x + 4 * half);
+            const grawa_f32x4v dot = *(const grawa_f32x4v *)(of_rows + BQ + 32 * u + 8 * x + 4 * half);
 #pragma unroll
             for (int y = 0; y < 4; ++y) dp[4 * x + y] = dot[y];
         }
@@ -366,7 +376,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
         const bool is_far = BIAS && p0 - w1 >= a.distances - 1;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            const grawa_f32x4v lse = *(const grawa_f32x4v *)(of_rows[b][0] + 32 * u + 8 * x + 4 * half);
+            const grawa_f32x4v lse = *(const grawa_f32x4v *)(of_rows + 32 * u + 8 * x + 4 * half);
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 const int r = 4 * x + y;
@@ -388,40 +398,52 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     grawa_f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = grawa_f32x16{};
-    if (from < to) {
-        At t = place(from), ahead = t;
-        if (BUFS == 2) load(t, 0);
-        for (int it = from; it < to; ++it, t = next(t)) {
-            const int b = BUFS == 2 ? (it - from) & 1 : 0;
-            const char *buf = lds + b * 2 * Tile::BYTES;
-            if (BUFS == 1) {
-                landed();
-                load(t, 0);
-            }
-            landed();
-            if (BUFS == 2 && it + 1 < to) load(ahead = next(ahead), b ^ 1);
-            tabulate(t.h);
-            // One way through the step, masked or not: with two the sums change their registers between them.
+    // One way through the step, masked or not: with two the sums change their registers between them.
+    const auto step = [&](At t, const char *buf, const float *of_rows) __attribute__((always_inline)) {
+        tabulate(t.h);
 #pragma unroll 1
-            for (int u = 0; u < 2; ++u) {
-                const int p0 = at.start + t.tile + 32 * u;
-                if (none(p0)) continue;
-                grawa_f32x16 s, dp;
-                V f[A], w[4];
-                const uint32_t at = Tile::columns_of(buf + 32 * u * Tile::RB, lane);
-                const auto columns = [&](int i) { return Tile::by_columns(KEEP ? at : here(at), (1 - i / (2 * DT)) * (Tile::BYTES / Tile::RB) + i / DT % 2 * 16, i % DT); };
-                slopes(buf, b, u, p0, s, dp, f, columns);
-                as_operand(s, 0, w[0]);
-                as_operand(s, 1, w[1]);
-                as_operand(dp, 0, w[2]);
-                as_operand(dp, 1, w[3]);
-                __builtin_amdgcn_sched_barrier(0);
-                flow<4 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) {
-                    if (i < 2 * DT)
-                        dv[i % DT] = mfma(x, w[i / DT], dv[i % DT]);
-                    else
-                        dk[i % DT] = mfma(x, w[i / DT], dk[i % DT]);
-                });
+        for (int u = 0; u < 2; ++u) {
+            const int p0 = at.start + t.tile + 32 * u;
+            if (none(p0)) continue;
+            grawa_f32x16 s, dp;
+            V f[A], w[4];
+            const uint32_t lines = columns_at + 32 * u * Tile::RB;
+            const auto columns = [&](int i) { return Tile::by_columns(buf + (1 - i / (2 * DT)) * Tile::BYTES, KEEP ? lines : here(lines), i / DT % 2 * 16, i % DT); };
+            slopes(buf, of_rows, u, p0, s, dp, f, columns);
+            as_operand(s, 0, w[0]);
+            as_operand(s, 1, w[1]);
+            as_operand(dp, 0, w[2]);
+            as_operand(dp, 1, w[3]);
+            __builtin_amdgcn_sched_barrier(0);
+            flow<4 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) {
+                if (i < 2 * DT)
+                    dv[i % DT] = mfma(x, w[i / DT], dv[i % DT]);
+                else
+                    dk[i % DT] = mfma(x, w[i / DT], dk[i % DT]);
+            });
+        }
+    };
+    if (from < to) {
+        At t = place(from);
+        if constexpr (BUFS == 2) {
+            load(t, buf0, rows0);
+            for (int it = from; it < to; it += 2) {
+                const At t1 = next(t), t2 = next(t1);
+                landed();
+                if (it + 1 < to) load(t1, buf1, rows1);
+                step(t, buf0, rows0);
+                if (it + 1 == to) break;
+                landed();
+                if (it + 2 < to) load(t2, buf0, rows0);
+                step(t1, buf1, rows1);
+                t = t2;
+            }
+        } else {
+            for (int it = from; it < to; ++it, t = next(t)) {
+                landed();
+                load(t, buf0, rows0);
+                landed();
+                step(t, buf0, rows0);
             }
         }
     }
@@ -457,7 +479,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
         for (int it = from; it < to; ++it) {
             const At t = place(it);
             landed();
-            load(t, 0);
+            load(t, buf0, rows0);
             landed();
             tabulate(t.h);
 #pragma unroll 1
@@ -466,7 +488,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
                 if (none(p0)) continue;
                 grawa_f32x16 s, dp;
                 V f[A];
-                slopes(lds, 0, u, p0, s, dp, f, [&](int) { return V{}; });
+                slopes(buf0, rows0, u, p0, s, dp, f, [&](int) { return V{}; });
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = keys ? dp[r] : s[r];
 #pragma unroll
@@ -475,7 +497,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
 #pragma unroll
                     for (int r = 0; r < 8; ++r) seen[r] = sees(a, p0 + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, j) ? 1.f : 0.f;
                     as_operand(s, h, w);
-                    product_of_some(sums, Tile::by_columns(Tile::columns_of(lds + (keys ? 0 : Tile::BYTES) + (32 * u + 16 * h) * Tile::RB, lane), 0, d), w, seen);
+                    product_of_some(sums, Tile::by_columns(buf0 + (keys ? 0 : Tile::BYTES) + (32 * u + 16 * h) * Tile::RB, columns_at, 0, d), w, seen);
                 }
             }
         }
