@@ -284,25 +284,27 @@ template <class V> __device__ __forceinline__ V marks(const GrawaAttend &a, int 
     return v;
 }
 
-// Which head and which of its blocks a workgroup has.  Workgroups go round the eight XCDs; each XCD gets heads of its own, so that
-// blocks that read the same keys share its L2, and takes the first block of all of them, then the second: blocks are numbered from the
-// longest on, and the short ones fill the end.  Few heads that eight does not divide are dealt out one by one.
+// Which head and which of its blocks a workgroup has.  Workgroups go round the eight XCDs.  The `share` heads that read the same keys stay
+// on one, so that their blocks share its L2, and such groups are dealt out one by one, so that long sequences are spread.  An XCD takes the
+// first block of all its heads, then the second: blocks are numbered from the longest on, and the short ones fill the end.  Few groups that
+// eight does not divide are dealt out head by head.  4 workers' 3 sequences of 600, 300 and fewer tokens, float32, in runs of heads: FIGURE_C.
 struct Turn {
     int head, block;
 };
-__device__ __forceinline__ Turn turn_of(uint32_t id, uint32_t heads, int by_xcd)
+__device__ __forceinline__ Turn turn_of(uint32_t id, uint32_t groups, uint32_t share, int by_xcd)
 {
+    const uint32_t heads = groups * share;
     if (!by_xcd) return Turn{(int)(id % heads), (int)(id / heads)};
-    const uint32_t each = (heads + 7) / 8, r = id / 8;
-    return Turn{(int)(id % 8 * each + r % each), (int)(r / each)};
+    const uint32_t each = (groups + 7) / 8 * share, r = id / 8, h = r % each;
+    return Turn{(int)((id % 8 + 8 * (h / share)) * share + h % share), (int)(r / each)};
 }
 #endif // __HIP_DEVICE_COMPILE__
 
 // The grid for turn_of; heads that are not there have workgroups that end at once.
-inline uint32_t grid_of(int64_t heads, int64_t blocks, int &by_xcd)
+inline uint32_t grid_of(int64_t groups, int64_t share, int64_t blocks, int &by_xcd)
 {
-    by_xcd = heads % 8 == 0 || heads >= 64;
-    return (uint32_t)((by_xcd ? (heads + 7) / 8 * 8 : heads) * blocks);
+    by_xcd = groups % 8 == 0 || groups >= 64;
+    return (uint32_t)((by_xcd ? (groups + 7) / 8 * 8 : groups) * share * blocks);
 }
 
 } // namespace

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
     __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];              // the bias by distance
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int heads = a.K * a.N * a.H;
-    const Turn turn = turn_of(blockIdx.x, heads, a.by_xcd);
+    const Turn turn = turn_of(blockIdx.x, a.K * a.N * a.G, a.share, a.by_xcd);
     if (turn.head >= heads) return;
     const int qb = a.blocks - 1 - turn.block / a.splits, split = turn.block % a.splits;
     const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
     const auto sums_of = [&](int w, int column) { return (float *)(w < NW / 2 ? buf0 : buf1) + (w % (NW / 2) * 32 + column) * PITCH; };
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int groups = a.K * a.N * a.G;
-    const Turn turn = turn_of(blockIdx.x, groups, a.by_xcd);
+    const Turn turn = turn_of(blockIdx.x, groups, 1, a.by_xcd);
     if (turn.head >= groups) return;
     const int cb = turn.block / a.splits, split = turn.block % a.splits;
     const int kn = turn.head / a.G, g = turn.head - kn * a.G, k = kn / a.N, n = kn - k * a.N;
@@ -446,12 +446,12 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     if ((int64_t)a.share * a.Sq <= KEYS_COLUMNS) {
         a.blocks = (a.share * a.Sq + 31) / 32;
         a.splits = splits_of(kn * a.G * a.blocks, rows, DP, (seen + 32 * KW - 1) / (32 * KW), part_floats);
-        const uint32_t grid = grid_of(kn * a.G, (int64_t)a.blocks * a.splits, a.by_xcd);
+        const uint32_t grid = grid_of(kn * a.G, 1, (int64_t)a.blocks * a.splits, a.by_xcd);
         hipLaunchKernelGGL((k_attend_few<BF16, DP, BIAS, KW>), dim3(grid), dim3(KW * 64), 0, st, a);
     } else {
         a.blocks = (a.Sq + 127) / 128;
         a.splits = splits_of(kn * a.H * a.blocks, rows, DP, (seen + 63) / 64, part_floats);
-        const uint32_t grid = grid_of(kn * a.H, (int64_t)a.blocks * a.splits, a.by_xcd);
+        const uint32_t grid = grid_of(kn * a.G, a.share, (int64_t)a.blocks * a.splits, a.by_xcd);
         hipLaunchKernelGGL((k_attend<BF16, DP, BIAS>), dim3(grid), dim3(256), 0, st, a);
     }
     const hipError_t e = hipGetLastError();

@@ -16,12 +16,13 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     typedef HeadTile<BF16, DP, BK, 4> Tile;
     typedef typename Tile::V V;
     __shared__ __attribute__((aligned(1024))) char buf0[2 * Tile::BYTES], buf1[BUFS == 2 ? 2 * Tile::BYTES : 16]; // keys and values
-    __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];                     // the bias by distance
-    __shared__ float by_distance[BIAS ? 4 : 1][BIAS ? GRAWA_MAX_DISTANCES : 1]; // of each wave: sums of dS
-    __shared__ float square[BIAS ? 4 : 1][BIAS ? 32 * 33 : 1];
+    __shared__ float diagonals[BIAS ? 4 : 1][BIAS ? 16 * 64 : 1]; // of each wave: dS of 16 keys, a key a row of 64, of which it has 32
+    extern __shared__ float tables[];                             // the bias by distance; of each wave: sums of dS by distance; buckets by distance
+    float *const table = tables, *const by_distance = tables + (1 + (threadIdx.x >> 6)) * a.distances;
+    int *const bucket_of = (int *)(tables + 5 * a.distances);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int heads = a.K * a.N * a.H;
-    const Turn turn = turn_of(blockIdx.x, heads, a.by_xcd);
+    const Turn turn = turn_of(blockIdx.x, a.K * a.N * a.G, a.share, a.by_xcd);
     if (turn.head >= heads) return;
     const int qb = a.blocks - 1 - turn.block;
     const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
@@ -58,8 +59,12 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     if constexpr (BIAS) {
         const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + head * a.buckets) * ES;
         far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
-        for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
-        for (int d = lane; d < a.distances; d += 64) by_distance[wave][d] = 0.f;
+        for (int d = threadIdx.x; d < a.distances; d += 256) {
+            bucket_of[d] = a.bucket_of[d];
+            table[d] = load_one<BF16>(bias + bucket_of[d] * ES) * LOG2E;
+        }
+        for (int d = lane; d < a.distances; d += 64) by_distance[d] = 0.f;
+        for (int d = lane; d < 16 * 64; d += 64) diagonals[wave][d] = 0.f;
     }
 
     const int p0 = at.start + qb * 128, p1 = at.start + min((qb + 1) * 128, a.Sq) - 1, w0 = p0 + wave * 32, w1 = w0 + 31;
@@ -96,12 +101,15 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
                 s = mfma(x, q[i / 2], s);
         });
         ask(f, then);
-        const bool is_far = BIAS && w0 - (j0 + 31) >= a.distances - 1;
+        if (BIAS && w0 - (j0 + 31) < a.distances - 1) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            float b = -lse;
-            if constexpr (BIAS) b += is_far ? far : table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, b)) * dp[r];
+            for (int r = 0; r < 16; ++r) {
+                const float bias = table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, bias - lse)) * dp[r];
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, far - lse)) * dp[r];
         }
         if (!all(j0))
 #pragma unroll
@@ -121,21 +129,29 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             if (w0 - (j0 + 31) >= a.distances - 1) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) far_sum += s[r];
-            } else { // along the diagonals of the square: lane x has those that are x - 31 above the first
-                float *sq = square[wave];
+            } else {
+                // Sixteen keys at a time: key y and query c are c - y + 15 places along row y, so that a column has one distance; what a
+                // row does not have there stays 0.  A lane adds up a column.
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sq[((r & 3) + 8 * (r >> 2) + 4 * half) * 33 + (lane & 31)] = s[r];
-                wave_order();
-                float sum = 0.f;
-                const int x = lane - 31;
-                for (int r = 0; r < 32; ++r)
-                    if (r + x >= 0 && r + x < 32) sum += sq[r * 33 + r + x];
-                const int d = w0 - j0 + x;
-                if (d >= a.distances - 1)
-                    far_sum += sum;
-                else if (d >= 0 && lane < 63)
-                    by_distance[wave][d] += sum;
-                wave_order();
+                for (int h = 0; h < 2; ++h) {
+                    float *const at_row = diagonals[wave] + (lane & 31) + 15;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const int y = (r & 3) + 8 * (r >> 2) + 4 * half;
+                        at_row[y * 63] = s[8 * h + r];
+                    }
+                    wave_order();
+                    float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) sums[y % 4] += diagonals[wave][y * 64 + lane];
+                    const float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                    const int d = w0 - (j0 + 16 * h) + lane - 15;
+                    if (d >= a.distances - 1)
+                        far_sum += sum;
+                    else if (d >= 0)
+                        by_distance[d] += sum;
+                    wave_order();
+                }
             }
         }
         V w[2];
@@ -219,12 +235,19 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     if constexpr (BIAS) {
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) far_sum += __shfl_xor(far_sum, m, 64);
-        if (lane == 0) by_distance[wave][a.distances - 1] = far_sum;
+        if (lane == 0) by_distance[a.distances - 1] = far_sum;
+        __syncthreads();
+        for (int d = threadIdx.x; d < a.distances; d += 256) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 1; w < 5; ++w) sum += tables[w * a.distances + d];
+            table[d] = sum;
+        }
         __syncthreads();
         for (int b = threadIdx.x; b < a.buckets; b += 256) {
             float sum = 0.f;
-            for (int d = 0; d < a.distances; ++d)
-                if (a.bucket_of[d] == b) sum += (by_distance[0][d] + by_distance[1][d]) + (by_distance[2][d] + by_distance[3][d]);
+#pragma unroll 8
+            for (int d = 0; d < a.distances; ++d) sum += bucket_of[d] == b ? table[d] : 0.f;
             a.bias_part[(((int64_t)kn * a.H + head) * a.blocks + qb) * a.buckets + b] = sum;
         }
     }
@@ -264,8 +287,8 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     __shared__ __attribute__((aligned(1024))) char values[KEEP ? 16 : Values::BYTES];
     __shared__ float table[BIAS ? GRAWA_MAX_DISTANCES : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int sink_items = a.sink_blocks * a.sink_splits, per = sink_items + (a.key_blocks - a.sink_blocks) * a.splits, groups = a.K * a.N * a.G;
-    const Turn turn = turn_of(blockIdx.x, groups, a.by_xcd);
+    const int sink_items = a.sink_blocks * a.sink_splits, groups = a.K * a.N * a.G;
+    const Turn turn = turn_of(blockIdx.x, groups, 1, a.by_xcd);
     if (turn.head >= groups) return;
     const int hd = turn.head, item = turn.block;
     const bool sink = item < sink_items;
@@ -347,7 +370,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     const auto none = [&](int p0) { return w0 > p0 + 31 || w0 >= at.length || (w1 <= p0 - a.window && w0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int p0) { return w1 <= p0 && (p0 + 31 - w0 < a.window || w1 < a.sinks); };
     const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
-    constexpr int A = BF16 ? 4 : 2;
+    constexpr int A = BF16 ? (DP == 128 ? 2 : 4) : 2;
     // P and dS of 32 queries; leaves the first fragments of `then` in f.
     const auto slopes = [&](const char *buf, const float *of_rows, int u, int p0, grawa_f32x16 &s, grawa_f32x16 &dp, V (&f)[A], auto &&then) __attribute__((always_inline)) {
         const uint32_t at = rows_at + 32 * u * Tile::RB;
@@ -373,18 +396,26 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
             }
         });
         ask(f, then);
-        const bool is_far = BIAS && p0 - w1 >= a.distances - 1;
+        const float far = BIAS ? table[a.distances - 1] : 0.f;
+        const auto form = [&](auto near) __attribute__((always_inline)) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const grawa_f32x4v lse = *(const grawa_f32x4v *)(of_rows + 32 * u + 8 * x + 4 * half);
+            for (int x = 0; x < 4; ++x) {
+                const grawa_f32x4v lse = *(const grawa_f32x4v *)(of_rows + 32 * u + 8 * x + 4 * half);
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int r = 4 * x + y;
-                float c = -lse[y];
-                if constexpr (BIAS) c += table[is_far ? a.distances - 1 : clamp_int(p0 + 8 * x + 4 * half + y - j, 0, a.distances - 1)];
-                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, c));
-                dp[r] *= s[r];
+                for (int y = 0; y < 4; ++y) {
+                    const float bias = near.value ? table[clamp_int(p0 + 8 * x + 4 * half + y - j, 0, a.distances - 1)] : far;
+                    s[4 * x + y] = __builtin_fmaf(s[4 * x + y], c2, bias - lse[y]);
+                }
             }
+        };
+        if (BIAS && p0 - w1 < a.distances - 1)
+            form(Is<BIAS>());
+        else
+            form(Is<false>());
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(s[r]);
+            dp[r] *= s[r];
         }
         if (!all(p0))
 #pragma unroll
@@ -542,8 +573,8 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     hipError_t e;
     if (a.Sq > 0) {
         a.blocks = (a.Sq + 127) / 128;
-        const uint32_t grid = grid_of(kn * a.H, a.blocks, a.by_xcd);
-        hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3(grid), dim3(256), 0, st, a);
+        const uint32_t grid = grid_of(kn * a.G, a.share, a.blocks, a.by_xcd);
+        hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3(grid), dim3(256), BIAS ? (uint32_t)a.distances * 6 * sizeof(float) : 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (BIAS) {
@@ -572,7 +603,7 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     a.sink_splits = (int)sink_splits;
     a.slots = (int)((sink_splits > 1 ? a.sink_blocks * sink_splits : 0) + (splits > 1 ? regular * splits : 0));
     const int64_t per = (int64_t)a.sink_blocks * a.sink_splits + regular * a.splits;
-    const uint32_t grid = grid_of(groups, per, a.by_xcd);
+    const uint32_t grid = grid_of(groups, 1, per, a.by_xcd);
     hipLaunchKernelGGL((k_attend_dkv<BF16, DP, BIAS, NW>), dim3(grid), dim3(NW * 64), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int first = a.sink_splits > 1 ? 0 : a.sink_blocks, end = a.splits > 1 ? a.key_blocks : a.sink_blocks;
