@@ -460,13 +460,17 @@ grawa_status_t grawa_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype, c
  * tokens; keys from there on are not read, and queries at positions from there on, or
  * below 0, see nothing.  Training and prompts: Sq = Sk, start 0, shorter sequences
  * padded behind.  Single tokens and chunks over a cache: start = length - Sq.
- * A row that sees nothing, or whose visible scores are all -infinity, gives 0 and passes no
- * gradient on.  What a row does not see does not reach it, infinities and NaN included.
+ * A row that sees nothing, or whose visible scores are all -infinity, gives 0 and passes
+ * no gradient on; a bias below -2^100, the type's lowest number among them, hides a key
+ * as -infinity does.  What a row does not see does not reach it, infinities and NaN
+ * included; what it sees that is not finite leaves no finite number where it counts, but
+ * may give NaN where IEEE arithmetic has an infinity.
  *
  * Types.  One type a plan, as in the sublayer.  Scores, softmax statistics, sums and
  * angles are float32 (angles are reduced in 64 bits).  With bfloat16 exp(s_ij - max)
  * and the gradient of s_ij are rounded to bfloat16 once, as the matrix instructions
  * take them, and the gradients use o as rounded; with float32 products are float32.
+ * The gradients form exp(s_ij - lse_i): scores beyond 2^20 in size leave them no digits.
  *
  * Layouts.  grawa_heads_t is K x N x S x heads rows of D elements: worker k's sequence
  * n, token s, head h starts at data + k * worker + n * sequence + s * token + h * head

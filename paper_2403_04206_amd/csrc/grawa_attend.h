@@ -275,6 +275,14 @@ __device__ __forceinline__ bool sees(const GrawaAttend &a, int pos, int j)
     return d >= 0 && (d < a.window || j < a.sinks);
 }
 
+// A bias in units of log2.  The type's lowest number hides a key as minus infinity does: a row that sees nothing else would have a sum of
+// exponentials whose logarithm float32 cannot tell from its neighbours'.
+template <bool BF16> __device__ __forceinline__ float bias_of(const char *p)
+{
+    const float b = load_one<BF16>(p);
+    return b < -0x1p100f ? -__builtin_inff() : b * LOG2E;
+}
+
 // Marks of the tokens j0 + ... that a column sees, in the order of an operand.
 template <class V> __device__ __forceinline__ V marks(const GrawaAttend &a, int pos, int j0, int half)
 {

@@ -7,52 +7,73 @@
 namespace {
 
 #ifdef __HIP_DEVICE_COMPILE__
-// The running maximum (of scores times log2 e) and sum of a column's softmax.
+// The running maximum and sum of a column's softmax: m in units of the scores, of which c is in units of log2.
 struct Running {
     float m, l;
+    __device__ __forceinline__ float top(float c) const { return m == -__builtin_inff() ? 0.f : m * c; }
 };
 
-// Exponentials of a column's scores against its running maximum, as operands, and their sum, taken before they are rounded (the
-// gradients start from it).  SCALED: the scores are in units of log2 already.
+// Where scores times their unit are so large that the rounding of their maximum would show (it is a factor of all exponentials, no more).
+constexpr float LARGE = 0x1p20f;
+
+// exp2 of 16 scores times c against the maximum.
+__device__ __forceinline__ void exponentials(grawa_f32x16 &s, float c, const Running &run)
+{
+    const float top = run.top(c);
+    if (__builtin_expect(__any(fabsf(top) > LARGE), 0)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fabsf(top) > LARGE ? (s[r] - run.m) * c : __builtin_fmaf(s[r], c, -top));
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -top));
+    }
+}
+
+// Exponentials of a column's scores times c against its running maximum, as operands, and their sum, taken before they are rounded (the
+// gradients start from it).
 // The maximum need not be a tile's: the sums hold exponentials above 1 as well.  It is looked for where a column has none yet or where a
 // lane's exponentials add up to more than 2^13 (or to infinity); other tiles need neither the maximum nor what the other half of the
 // wave has.
-template <bool SCALED, int NS, int DT, class V>
-__device__ __forceinline__ void soften(const grawa_f32x16 (&s)[NS], float c2, Running &run, grawa_f32x16 (&o)[DT], V (&p)[2 * NS])
+template <int NS, int DT, class V>
+__device__ __forceinline__ void soften(const grawa_f32x16 (&s)[NS], float c, Running &run, grawa_f32x16 (&o)[DT], V (&p)[2 * NS])
 {
-    float sum;
-    const auto exponentials = [&]() __attribute__((always_inline)) {
-        const float base = run.m == -__builtin_inff() ? 0.f : run.m;
-        float sums[2] = {0.f, 0.f};
+    float sums[2] = {0.f, 0.f};
+    const float top0 = run.top(c);
 #pragma unroll
-        for (int u = 0; u < NS; ++u)
+    for (int u = 0; u < NS; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                grawa_f32x16 e;
+        for (int h = 0; h < 2; ++h) {
+            grawa_f32x16 e;
 #pragma unroll
-                for (int r = 8 * h; r < 8 * h + 8; ++r) {
-                    e[r] = __builtin_amdgcn_exp2f(SCALED ? s[u][r] - base : __builtin_fmaf(s[u][r], c2, -base));
-                    sums[r % 2] += e[r];
-                }
-                as_operand(e, h, p[2 * u + h]);
+            for (int r = 8 * h; r < 8 * h + 8; ++r) {
+                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][r], c, -top0));
+                sums[r % 2] += e[r];
             }
-        sum = sums[0] + sums[1];
-    };
-    exponentials();
-    if (__any(sum > 8192.f || run.m == -__builtin_inff())) {
+            as_operand(e, h, p[2 * u + h]);
+        }
+    float sum = sums[0] + sums[1];
+    if (__any(sum > 8192.f || run.m == -__builtin_inff() || fabsf(top0) > LARGE)) {
         float top = s[0][0];
 #pragma unroll
         for (int u = 0; u < NS; ++u)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
         top = fmaxf(top, other_half(top));
-        if (!SCALED) top *= c2;
-        const float m2 = fmaxf(run.m, top), f = m2 == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(run.m - m2);
+        const float m2 = fmaxf(run.m, top), f = m2 == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((run.m - m2) * c);
         run.m = m2;
         run.l *= f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= f;
-        exponentials();
+        sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < NS; ++u) {
+            grawa_f32x16 e = s[u];
+            exponentials(e, c, run);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += e[r];
+            as_operand(e, 0, p[2 * u]);
+            as_operand(e, 1, p[2 * u + 1]);
+        }
     }
     run.l += sum;
 }
@@ -86,12 +107,12 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) q[ks] = load_line<BF16>(row, 16 * ks + 8 * half, a.D, counts);
     }
-    const float c2 = a.scale * LOG2E;
+    const float c2 = a.scale * LOG2E, unit = BIAS ? 1.f : c2; // of a score as it comes, and with its bias
     float far = 0.f;
     if constexpr (BIAS) {
         const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + head * a.buckets) * ES;
-        far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
-        for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
+        far = bias_of<BF16>(bias + a.bucket_of[a.distances - 1] * ES);
+        for (int d = threadIdx.x; d < a.distances; d += 256) table[d] = bias_of<BF16>(bias + a.bucket_of[d] * ES);
     }
 
     // Tiles: those with first tokens, then those of the window.
@@ -150,7 +171,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
         ask(f, value);
 #pragma unroll
         for (int u = 0; u < 2; ++u) scores(j0 + 32 * u, s[u]);
-        soften<BIAS>(s, c2, run, o, p);
+        soften(s, unit, run, o, p);
         __builtin_amdgcn_sched_barrier(0);
         flow<4 * DT>(f, value, [&](int i, const V &x) __attribute__((always_inline)) { o[i % DT] = mfma(x, p[i / DT], o[i % DT]); });
     };
@@ -165,7 +186,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
     char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i * a.o.token + (int64_t)head * a.o.head;
     const float l = run.l + other_half(run.l);
     const bool sum = counts && !(l == 0.f);
-    const float lse2 = sum ? run.m + __builtin_amdgcn_logf(l) : -__builtin_inff(), f = sum ? 1.f / l : 0.f;
+    const float lse2 = sum ? run.top(unit) + __builtin_amdgcn_logf(l) : -__builtin_inff(), f = sum ? 1.f / l : 0.f;
     if (half == 0 && there) {
         if (a.splits > 1)
             a.part[(int64_t)a.splits * rows * DP + (int64_t)split * rows + row] = lse2;
@@ -194,7 +215,6 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
         for (int d = 0; d < DT; ++d) put(d, o[d]);
         return;
     }
-    const float base = run.m == -__builtin_inff() ? 0.f : run.m;
 #pragma unroll 1
     for (int d = 0; d < DT; ++d) {
         grawa_f32x16 sums = {};
@@ -211,8 +231,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) s = mfma(Tile::by_rows(buf0 + 32 * u * Tile::RB, rows_at, 0, ks), q[ks], s);
                 scores(j0, s);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(BIAS ? s[r] - base : __builtin_fmaf(s[r], c2, -base));
+                exponentials(s, unit, run);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     V p;
@@ -261,10 +280,10 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) q[ks] = load_line<BF16>(row, 16 * ks + 8 * half, a.D, counts);
     }
-    const float c2 = a.scale * LOG2E;
+    const float c2 = a.scale * LOG2E, unit = BIAS ? 1.f : c2; // of a score as it comes, and with its bias
     const char *bias = BIAS ? a.bias.p + ((int64_t)k * a.bias.worker + (there ? head : 0) * a.buckets) * ES : nullptr;
     float far = 0.f;
-    if constexpr (BIAS) far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
+    if constexpr (BIAS) far = bias_of<BF16>(bias + a.bucket_of[a.distances - 1] * ES);
 
     const int w0 = at.start, w1 = at.start + a.Sq - 1; // positions
     const int end = min(w1, at.length - 1) + 1, begin = max(0, max(w0, 0) - a.window + 1);
@@ -307,7 +326,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int d = clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1);
-                        s[0][r] = s[0][r] * c2 + load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
+                        s[0][r] = s[0][r] * c2 + bias_of<BF16>(bias + a.bucket_of[d] * ES);
                     }
                 }
             }
@@ -315,7 +334,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[0][r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[0][r] : -__builtin_inff();
             V p[2];
-            soften<BIAS>(s, c2, run, o, p);
+            soften(s, unit, run, o, p);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -349,7 +368,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             *(grawa_f32x4v *)(sums_of(wave, lane & 31) + 32 * d + 8 * r + 4 * half) = grawa_f32x4v{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
-    if (half == 0) ml[wave * 64 + lane] = run.m, ml[wave * 64 + 32 + lane] = l;
+    if (half == 0) ml[wave * 64 + lane] = run.m == -__builtin_inff() ? run.m : run.top(unit), ml[wave * 64 + 32 + lane] = l;
     __syncthreads();
     constexpr int LPC = NW * 2, EPL = DP / LPC; // threads of a column, elements of each
     const int cl = threadIdx.x / LPC, e0 = threadIdx.x % LPC * EPL, c = cb * 32 + cl;

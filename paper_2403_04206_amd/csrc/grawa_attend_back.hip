@@ -58,10 +58,10 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     float far = 0.f;
     if constexpr (BIAS) {
         const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + head * a.buckets) * ES;
-        far = load_one<BF16>(bias + a.bucket_of[a.distances - 1] * ES) * LOG2E;
+        far = bias_of<BF16>(bias + a.bucket_of[a.distances - 1] * ES);
         for (int d = threadIdx.x; d < a.distances; d += 256) {
             bucket_of[d] = a.bucket_of[d];
-            table[d] = load_one<BF16>(bias + bucket_of[d] * ES) * LOG2E;
+            table[d] = bias_of<BF16>(bias + bucket_of[d] * ES);
         }
         for (int d = lane; d < a.distances; d += 64) by_distance[d] = 0.f;
         for (int d = lane; d < 16 * 64; d += 64) diagonals[wave][d] = 0.f;
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
             if (h == table_of) return;
             // the other waves are behind their last look at the table of the head before
             const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + (int64_t)(g * a.share + h) * a.buckets) * ES;
-            for (int d = threadIdx.x; d < a.distances; d += NW * 64) table[d] = load_one<BF16>(bias + a.bucket_of[d] * ES) * LOG2E;
+            for (int d = threadIdx.x; d < a.distances; d += NW * 64) table[d] = bias_of<BF16>(bias + a.bucket_of[d] * ES);
             table_of = h;
             __syncthreads();
         }
@@ -582,6 +582,7 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
         hipLaunchKernelGGL((k_bias_sums<BF16>), dim3((uint32_t)a.H, (uint32_t)a.K), dim3(256), 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
+    if (a.Sk == 0) return hipSuccess;
     constexpr int NW = BF16 && DP == 128 ? 8 : 4, BKV = 32 * NW;
     a.key_blocks = (a.Sk + BKV - 1) / BKV;
     // Blocks of keys that all later queries see, and not only those that the window lets through.
@@ -617,8 +618,7 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
 
 hipError_t grawa_launch_attend_backward(const grawa_attention_plan *s, GrawaAttend a, hipStream_t st)
 {
-    if (a.N == 0 && !a.buckets) return hipSuccess;
-    if (a.N == 0 || a.Sk == 0) { // nothing but the bias's gradient, of no pairs
+    if (a.N == 0) { // nothing but the bias's gradient, of no pairs
         if (!a.buckets) return hipSuccess;
         a.blocks = 0;
         if (s->dtype == GRAWA_BF16)
