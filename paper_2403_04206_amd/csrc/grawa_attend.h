@@ -292,6 +292,8 @@ template <class V> __device__ __forceinline__ V marks(const GrawaAttend &a, int 
     return v;
 }
 
+#endif // __HIP_DEVICE_COMPILE__
+
 // Which head and which of its blocks a workgroup has.  Workgroups go round the eight XCDs.  The `share` heads that read the same keys stay
 // on one, so that their blocks share its L2, and such groups are dealt out one by one, so that long sequences are spread.  An XCD takes the
 // first block of all its heads, then the second: blocks are numbered from the longest on, and the short ones fill the end.  Few groups that
@@ -299,14 +301,13 @@ template <class V> __device__ __forceinline__ V marks(const GrawaAttend &a, int 
 struct Turn {
     int head, block;
 };
-__device__ __forceinline__ Turn turn_of(uint32_t id, uint32_t groups, uint32_t share, int by_xcd)
+__host__ __device__ inline Turn turn_of(uint32_t id, uint32_t groups, uint32_t share, int by_xcd)
 {
     const uint32_t heads = groups * share;
     if (!by_xcd) return Turn{(int)(id % heads), (int)(id / heads)};
     const uint32_t each = (groups + 7) / 8 * share, r = id / 8, h = r % each;
     return Turn{(int)((id % 8 + 8 * (h / share)) * share + h % share), (int)(r / each)};
 }
-#endif // __HIP_DEVICE_COMPILE__
 
 // The grid for turn_of; heads that are not there have workgroups that end at once.
 inline uint32_t grid_of(int64_t groups, int64_t share, int64_t blocks, int &by_xcd)

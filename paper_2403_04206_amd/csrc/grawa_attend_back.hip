@@ -594,7 +594,7 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     if (splits > most / 2) splits = most / 2;
     if (splits > 1 && splits > room / 2 / regular) splits = room / 2 / regular;
     if (splits < 1) splits = 1;
-    if (a.sink_blocks) { // as long as the others
+    if (a.sink_blocks && most > 0) { // as long as the others
         sink_splits = (tiles * a.share + most - 1) / most * splits;
         const int64_t left = room - (splits > 1 ? regular * splits : 0);
         if (sink_splits > left / a.sink_blocks) sink_splits = left / a.sink_blocks;

@@ -263,3 +263,14 @@ def test_a_cache_of_more_than_four_gibibytes():
     for name, got in (("o", o), ("dq", dq), ("dk", near(grads[0])), ("dv", near(grads[1]))):
         ref.check(got, *want[name], name)
     assert not bool(grads[:, :, :, sinks:low].any())
+
+
+def test_no_queries_with_first_tokens():
+    """Keys without a query, a window and first tokens that stay visible: gradients of 0."""
+    with grawa.AttentionPlan(1, 2, 300, 2, 1, 64, dtype=torch.float32, window=50, sinks=3) as plan:
+        q, k, lse = torch.ones((1, 2, 0, 2, 64), device="cuda"), torch.ones((1, 2, 300, 1, 64), device="cuda"), torch.ones((1, 2, 2, 0), device="cuda")
+        dk, dv = torch.full_like(k, 7.0), torch.full_like(k, 7.0)
+        plan.attention(q, k, k, q)
+        plan.attention_backward(q, q, k, k, q, lse, q, dk, dv)
+        torch.cuda.synchronize()
+        assert not bool(dk.any()) and not bool(dv.any())
