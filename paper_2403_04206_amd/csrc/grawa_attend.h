@@ -145,6 +145,34 @@ template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
     }
 };
 
+// Where the tiles of keys and values of a head are read from, one after the other: first those with first tokens, then those of the window.
+template <class Tile, int BK> struct Tiles {
+    const char *k, *v;           // the next one's
+    int64_t k_step, v_step;
+    uint32_t k_token, v_token, bytes;
+    int left;                    // tokens from the next one on
+    int jump, gap;               // where the window's tiles do not follow the first tokens': behind `jump` tiles, by `gap`
+
+    __device__ __forceinline__ void init(const char *k0, const char *v0, uint32_t kt, uint32_t vt, int length, int D, int from, int first_tiles, int t0)
+    {
+        const int j0 = (from < first_tiles ? from : from - first_tiles + t0) * BK;
+        k_token = kt, v_token = vt, bytes = D * Tile::ES;
+        k_step = (int64_t)kt * BK, v_step = (int64_t)vt * BK;
+        k = k0 + (int64_t)j0 * kt, v = v0 + (int64_t)j0 * vt;
+        left = length - j0;
+        jump = from < first_tiles ? first_tiles - from : -1;
+        gap = t0 - first_tiles;
+    }
+    __device__ __forceinline__ void load(const Tile &lk, const Tile &lv, char *buf, int wave)
+    {
+        const uint32_t n = left < BK ? left : BK; // more than 0: tiles beyond the length are not asked for
+        lk.load(buf, wave, __builtin_amdgcn_make_buffer_rsrc((void *)k, 0, (n - 1) * k_token + bytes, 0x00020000));
+        lv.load(buf + Tile::BYTES, wave, __builtin_amdgcn_make_buffer_rsrc((void *)v, 0, (n - 1) * v_token + bytes, 0x00020000));
+        k += k_step, v += v_step, left -= BK;
+        if (--jump == 0) k += gap * k_step, v += gap * v_step, left -= gap * BK;
+    }
+};
+
 // Keeps what an offset differs in from being formed ahead for all fragments and held in registers.
 __device__ __forceinline__ uint32_t here(uint32_t at)
 {

@@ -127,11 +127,10 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
     lk.init(wave, lane, (uint32_t)a.k.token, a.D);
     lv.init(wave, lane, (uint32_t)a.v.token, a.D);
     const auto tile_of = [&](int it) { return (it < first_tiles ? it : it - first_tiles + t0) * BK; };
-    const auto load = [&](int it, char *buf) {
-        const int j0 = tile_of(it);
-        lk.load(buf, wave, Tile::rsrc(kp + (int64_t)j0 * a.k.token, at.length - j0, (uint32_t)a.k.token, a.D));
-        lv.load(buf + Tile::BYTES, wave, Tile::rsrc(vp + (int64_t)j0 * a.v.token, at.length - j0, (uint32_t)a.v.token, a.D));
-    };
+    Tiles<Tile, BK> tiles_at;
+    const auto restart = [&]() __attribute__((always_inline)) { tiles_at.init(kp, vp, (uint32_t)a.k.token, (uint32_t)a.v.token, at.length, a.D, from, first_tiles, t0); };
+    const auto load = [&](char *buf) __attribute__((always_inline)) { tiles_at.load(lk, lv, buf, wave); };
+    restart();
     const auto none = [&](int j0, int j1) { return j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0, int j1) { return j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks); };
     // Scores of 32 keys: masked, with a bias in units of log2.
@@ -156,29 +155,36 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = grawa_f32x16{};
     const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
-    const auto step = [&](int it, const char *buf, char *ahead) __attribute__((always_inline)) {
-        landed();
-        if (it + 1 < to) load(it + 1, ahead);
-        const int j0 = tile_of(it);
-        if (none(j0, j0 + BK - 1)) return;
-        constexpr int A = BF16 ? 4 : 2;
-        V f[A], p[4];
-        const auto key = [&](int i) { return Tile::by_rows(buf, rows_at, i % 2 * 32, i / 2); };
-        const auto value = [&](int i) { return Tile::by_columns(buf + Tile::BYTES, columns_at, i / DT * 16, i % DT); };
-        grawa_f32x16 s[2] = {};
-        ask(f, key);
-        flow<2 * KS>(f, key, [&](int i, const V &x) __attribute__((always_inline)) { s[i % 2] = mfma(x, q[i / 2], s[i % 2]); });
-        ask(f, value);
+    // 64 keys, or with float32, whose products are long, each half of them by itself where the wave sees any of it.
+    const auto step = [&](int it, const char *buf) __attribute__((always_inline)) {
+        constexpr int NS = BF16 ? 2 : 1, A = BF16 ? 4 : 2;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) scores(j0 + 32 * u, s[u]);
-        soften(s, unit, run, o, p);
-        __builtin_amdgcn_sched_barrier(0);
-        flow<4 * DT>(f, value, [&](int i, const V &x) __attribute__((always_inline)) { o[i % DT] = mfma(x, p[i / DT], o[i % DT]); });
+        for (int part = 0; part < 2 / NS; ++part) {
+            const int j0 = tile_of(it) + 32 * part;
+            if (none(j0, j0 + 32 * NS - 1)) continue;
+            V f[A], p[2 * NS];
+            const auto key = [&](int i) { return Tile::by_rows(buf + 32 * part * Tile::RB, rows_at, i % NS * 32, i / NS); };
+            const auto value = [&](int i) { return Tile::by_columns(buf + Tile::BYTES + 32 * part * Tile::RB, columns_at, i / DT * 16, i % DT); };
+            grawa_f32x16 s[NS] = {};
+            ask(f, key);
+            flow<NS * KS>(f, key, [&](int i, const V &x) __attribute__((always_inline)) { s[i % NS] = mfma(x, q[i / NS], s[i % NS]); });
+            ask(f, value);
+#pragma unroll
+            for (int u = 0; u < NS; ++u) scores(j0 + 32 * u, s[u]);
+            soften(s, unit, run, o, p);
+            __builtin_amdgcn_sched_barrier(0);
+            flow<2 * NS * DT>(f, value, [&](int i, const V &x) __attribute__((always_inline)) { o[i % DT] = mfma(x, p[i / DT], o[i % DT]); });
+        }
     };
-    if (from < to) load(from, buf0);
+    if (from < to) load(buf0);
     for (int it = from; it < to; it += 2) {
-        step(it, buf0, buf1);
-        if (it + 1 < to) step(it + 1, buf1, buf0);
+        landed();
+        if (it + 1 < to) load(buf1);
+        step(it, buf0);
+        if (it + 1 == to) break;
+        landed();
+        if (it + 2 < to) load(buf0);
+        step(it + 1, buf1);
     }
 
     const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row = ((int64_t)kn * a.H + head) * a.Sq + i;
@@ -218,10 +224,11 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
 #pragma unroll 1
     for (int d = 0; d < DT; ++d) {
         grawa_f32x16 sums = {};
+        restart();
 #pragma unroll 1
         for (int it = from; it < to; ++it) {
             landed();
-            load(it, buf0);
+            load(buf0);
             landed();
 #pragma unroll 1
             for (int u = 0; u < 2; ++u) {
@@ -296,11 +303,8 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
     lk.init(wave, lane, (uint32_t)a.k.token, a.D);
     lv.init(wave, lane, (uint32_t)a.v.token, a.D);
     const auto tile_of = [&](int it) { return (it < first_tiles ? it : it - first_tiles + t0) * BK; };
-    const auto load = [&](int it, char *buf) {
-        const int j0 = tile_of(it);
-        lk.load(buf, wave, Tile::rsrc(kp + (int64_t)j0 * a.k.token, at.length - j0, (uint32_t)a.k.token, a.D));
-        lv.load(buf + Tile::BYTES, wave, Tile::rsrc(vp + (int64_t)j0 * a.v.token, at.length - j0, (uint32_t)a.v.token, a.D));
-    };
+    Tiles<Tile, BK> tiles_at;
+    const auto load = [&](char *buf) __attribute__((always_inline)) { tiles_at.load(lk, lv, buf, wave); };
 
     grawa_f32x16 o[DT];
     Running run;
@@ -309,9 +313,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
         run = Running{-__builtin_inff(), 0.f};
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] = grawa_f32x16{};
-        const auto step = [&](int it, const char *buf, char *ahead) __attribute__((always_inline)) {
-            landed();
-            if (it + 1 < to) load(it + 1, ahead);
+        const auto step = [&](int it, const char *buf) __attribute__((always_inline)) {
             const int j0 = tile_of(it) + wave * 32, j1 = j0 + 31;
             if (j0 > w1 || j0 >= at.length || (j1 <= w0 - a.window && j0 >= a.sinks)) return; // none of the wave's pairs count
             const bool all = j1 <= w0 && (w1 - j0 < a.window || j1 < a.sinks);
@@ -346,10 +348,16 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
                         o[d] = mfma(v, p[h], o[d]);
                 }
         };
-        if (from < to) load(from, buf0);
+        tiles_at.init(kp, vp, (uint32_t)a.k.token, (uint32_t)a.v.token, at.length, a.D, from, first_tiles, t0);
+        if (from < to) load(buf0);
         for (int it = from; it < to; it += 2) {
-            step(it, buf0, buf1);
-            if (it + 1 < to) step(it + 1, buf1, buf0);
+            landed();
+            if (it + 1 < to) load(buf1);
+            step(it, buf0);
+            if (it + 1 == to) break;
+            landed();
+            if (it + 2 < to) load(buf0);
+            step(it + 1, buf1);
         }
         bool odd = false;
         if (!careful.value && counts)
@@ -407,27 +415,42 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #endif
 }
 
-// o = sum over the splits of o_s exp(lse_s - lse): a wave has 64 / (DP / 8) rows.
+// o = sum over the splits of o_s exp(lse_s - lse): eight elements a lane, all splits' asked for before the first is used (eight at a time).
 template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_join([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int LPR = DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N;
+    constexpr int LPR = DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N, U = 8;
     const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     const int e0 = threadIdx.x % LPR * 8;
     if (row >= rows) return;
-    const float *lse = a.part + (int64_t)a.splits * rows * DP + row;
-    float top = -__builtin_inff();
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, lse[s * rows]);
-    float total = 0.f, v[8] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float ls = lse[s * rows];
-        if (ls == -__builtin_inff()) continue;
-        const float f = __builtin_amdgcn_exp2f(ls - top);
-        total += f;
-        const grawa_f32x4v *p = (const grawa_f32x4v *)(a.part + ((int64_t)s * rows + row) * DP + e0);
-        const grawa_f32x4v x = p[0], y = p[1];
+    const float *lse = a.part + (int64_t)a.splits * rows * DP + row, *part = a.part + row * DP + e0;
+    float top = -__builtin_inff(), total = 0.f, v[8] = {};
+    for (int s0 = 0; s0 < a.splits; s0 += U) {
+        float l[U];
+        grawa_f32x4v x[U], y[U];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] += x[j] * f, v[4 + j] += y[j] * f;
+        for (int u = 0; u < U; ++u) {
+            const int s = s0 + u < a.splits ? s0 + u : a.splits - 1; // what is read twice is left out below
+            l[u] = lse[s * rows];
+            x[u] = *(const grawa_f32x4v *)(part + (int64_t)s * rows * DP);
+            y[u] = *(const grawa_f32x4v *)(part + (int64_t)s * rows * DP + 4);
+        }
+        float m = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) m = fmaxf(m, l[u]);
+        const float base = m == -__builtin_inff() ? 0.f : m, before = __builtin_amdgcn_exp2f(top - base); // no numbers pass the maximum by
+        top = m;
+        total *= before;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= before;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u >= a.splits || l[u] == -__builtin_inff()) continue;
+            const float f = __builtin_amdgcn_exp2f(l[u] - base);
+            total += f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += x[u][j] * f, v[4 + j] += y[u][j] * f;
+        }
     }
     const bool any = !(total == 0.f);
 #pragma unroll

@@ -77,11 +77,10 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     lk.init(wave, lane, (uint32_t)a.k.token, a.D);
     lv.init(wave, lane, (uint32_t)a.v.token, a.D);
     const auto tile_of = [&](int it) { return (it < first_tiles ? it : it - first_tiles + t0) * BK; };
-    const auto load = [&](int it, char *buf) {
-        const int j0 = tile_of(it);
-        lk.load(buf, wave, Tile::rsrc(kp + (int64_t)j0 * a.k.token, at.length - j0, (uint32_t)a.k.token, a.D));
-        lv.load(buf + Tile::BYTES, wave, Tile::rsrc(vp + (int64_t)j0 * a.v.token, at.length - j0, (uint32_t)a.v.token, a.D));
-    };
+    Tiles<Tile, BK> tiles_at;
+    const auto restart = [&]() __attribute__((always_inline)) { tiles_at.init(kp, vp, (uint32_t)a.k.token, (uint32_t)a.v.token, at.length, a.D, 0, first_tiles, t0); };
+    const auto load = [&](char *buf) __attribute__((always_inline)) { tiles_at.load(lk, lv, buf, wave); };
+    restart();
     const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0) { return j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
     const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
@@ -167,20 +166,20 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         }
     };
     if constexpr (BUFS == 2) {
-        if (tiles) load(0, buf0);
+        if (tiles) load(buf0);
         for (int it = 0; it < tiles; it += 2) {
             landed();
-            if (it + 1 < tiles) load(it + 1, buf1);
+            if (it + 1 < tiles) load(buf1);
             both_halves(it, buf0);
             if (it + 1 == tiles) break;
             landed();
-            if (it + 2 < tiles) load(it + 2, buf0);
+            if (it + 2 < tiles) load(buf0);
             both_halves(it + 1, buf1);
         }
     } else {
         for (int it = 0; it < tiles; ++it) {
             landed();
-            load(it, buf0);
+            load(buf0);
             landed();
             both_halves(it, buf0);
         }
@@ -207,9 +206,10 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
 #pragma unroll 1
         for (int d = 0; d < DT; ++d) {
             grawa_f32x16 sums = {};
+            restart();
             for (int it = 0; it < tiles; ++it) {
                 landed();
-                load(it, buf0);
+                load(buf0);
                 landed();
 #pragma unroll 1
                 for (int u = 0; u < 2; ++u) {
@@ -274,11 +274,11 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums([[maybe_
 // after the other.  Keys and the sums of dk and dv stay in registers, values too where heads have 64 elements; with 128 they do not fit
 // and are read from LDS (in registers all the same, 8 heads of 32 x 16384 tokens spilled and took 22.6 ms).  splits > 1 (sink_splits for the keys that all queries see): that many blocks share the queries of a block of keys.
 template <bool BF16, int DP, bool BIAS, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_dkv([[maybe_unused]] GrawaAttend a)
+__global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : DP == 64 ? 2 : 1) void k_attend_dkv([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int BQ = 64, BKV = 32 * NW, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
-    constexpr bool KEEP = DP == 64; // values in registers
+    constexpr int BQ = 64, BKV = 32 * NW, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 ? 2 : 1;
+    constexpr bool KEEP = BF16 && DP == 64; // values in registers
     typedef HeadTile<BF16, DP, BQ, NW> Tile;
     typedef HeadTile<BF16, DP, BKV, NW> Values;
     typedef typename Tile::V V;
@@ -335,25 +335,30 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : BF16 ? 2 : 1) void k_attend_
     const char *qp = a.q.p + (int64_t)k * a.q.worker + (int64_t)n * a.q.seq, *gp = a.go.p + (int64_t)k * a.go.worker + (int64_t)n * a.go.seq;
     struct At {
         int h, tile; // head of the group, first query of the tile
+        const char *q, *go;
+        const float *rows;
+    };
+    const auto head_of = [&](int h, int tile) __attribute__((always_inline)) {
+        const int head = g * a.share + h;
+        return At{h, tile, qp + (int64_t)tile * a.q.token + (int64_t)head * a.q.head, gp + (int64_t)tile * a.go.token + (int64_t)head * a.go.head,
+                  (wave ? a.row_dot : a.row_lse) + ((int64_t)kn * a.H + head) * a.row_pitch + tile};
     };
     const auto place = [&](int it) {
         const int h = it / tiles;
-        return At{h, (t0 + it - h * tiles) * BQ};
+        return head_of(h, (t0 + it - h * tiles) * BQ);
     };
-    const auto load = [&](At t, char *buf, float *rows) {
-        const int head = g * a.share + t.h;
-        lq.load(buf, wave, Tile::rsrc(qp + (int64_t)t.tile * a.q.token + (int64_t)head * a.q.head, last + 1 - t.tile, (uint32_t)a.q.token, a.D));
-        lg.load(buf + Tile::BYTES, wave, Tile::rsrc(gp + (int64_t)t.tile * a.go.token + (int64_t)head * a.go.head, last + 1 - t.tile, (uint32_t)a.go.token, a.D));
-        if (wave < 2) { // rows up to the pitch, a multiple of a tile, are there
-            const float *p = (wave ? a.row_dot : a.row_lse) + ((int64_t)kn * a.H + head) * a.row_pitch + t.tile;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, BQ * 4, 0x00020000),
+    const uint32_t q_token = (uint32_t)a.q.token, go_token = (uint32_t)a.go.token, bytes = a.D * ES;
+    const auto load = [&](At t, char *buf, float *rows) __attribute__((always_inline)) {
+        const uint32_t n = last + 1 - t.tile < BQ ? last + 1 - t.tile : BQ; // more than 0
+        lq.load(buf, wave, __builtin_amdgcn_make_buffer_rsrc((void *)t.q, 0, (n - 1) * q_token + bytes, 0x00020000));
+        lg.load(buf + Tile::BYTES, wave, __builtin_amdgcn_make_buffer_rsrc((void *)t.go, 0, (n - 1) * go_token + bytes, 0x00020000));
+        if (wave < 2) // rows up to the pitch, a multiple of a tile, are there
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)t.rows, 0, BQ * 4, 0x00020000),
                                                      (GRAWA_LDS_AT void *)(rows + wave * BQ), 4, (uint32_t)lane * 4, 0, 0, 0);
-        }
     };
-    const auto next = [&](At t) {
-        t.tile += BQ;
-        if (t.tile >= (t0 + tiles) * BQ) t.tile = t0 * BQ, ++t.h;
-        return t;
+    const auto next = [&](At t) __attribute__((always_inline)) {
+        if (t.tile + BQ >= (t0 + tiles) * BQ) return head_of(t.h + 1, t0 * BQ);
+        return At{t.h, t.tile + BQ, t.q + (int64_t)BQ * a.q.token, t.go + (int64_t)BQ * a.go.token, t.rows + BQ};
     };
     int table_of = -1;
     const auto tabulate = [&](int h) {
@@ -590,7 +595,7 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     a.sink_blocks = a.window == GRAWA_NO_WINDOW ? 0 : (int)(sink_blocks < a.key_blocks ? sink_blocks : a.key_blocks);
     const int64_t groups = kn * a.G, room = part_floats / ((int64_t)BKV * 2 * DP) / groups; // for so many blocks of a group
     const int64_t regular = a.key_blocks - a.sink_blocks, most = (tiles < window_tiles ? tiles : window_tiles) * a.share;
-    int64_t splits = regular ? 512 / (groups * regular) : 1, sink_splits = 1;
+    int64_t splits = regular ? (BF16 ? 512 : 1024) / (groups * regular) : 1, sink_splits = 1;
     if (splits > most / 2) splits = most / 2;
     if (splits > 1 && splits > room / 2 / regular) splits = room / 2 / regular;
     if (splits < 1) splits = 1;
