@@ -263,6 +263,7 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums([[maybe_
     float sum = 0.f;
     for (int n = 0; n < a.N; ++n) {
         const float *p = a.bias_part + ((int64_t)(k * a.N + n) * a.H + head) * a.blocks * a.buckets + b;
+#pragma unroll 8
         for (int i = 0; i < a.blocks; ++i) sum += p[(int64_t)i * a.buckets];
     }
     char *out = a.dbias.p + ((int64_t)k * a.dbias.worker + (int64_t)head * a.buckets + b) * (BF16 ? 2 : 4);
@@ -595,16 +596,17 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     a.sink_blocks = a.window == GRAWA_NO_WINDOW ? 0 : (int)(sink_blocks < a.key_blocks ? sink_blocks : a.key_blocks);
     const int64_t groups = kn * a.G, room = part_floats / ((int64_t)BKV * 2 * DP) / groups; // for so many blocks of a group
     const int64_t regular = a.key_blocks - a.sink_blocks, most = (tiles < window_tiles ? tiles : window_tiles) * a.share;
-    int64_t splits = regular ? (BF16 ? 512 : 1024) / (groups * regular) : 1, sink_splits = 1;
+    // Items enough for every CU (twice as many, float32, 4 workers of 3 sequences of 600 and less: no faster).  A block of first keys is
+    // shared as often as makes its items as long as the others.
+    const int64_t as_long = a.sink_blocks && most > 0 ? (tiles * a.share + most - 1) / most : 1;
+    int64_t splits = regular ? 512 / (groups * regular) : 1;
     if (splits > most / 2) splits = most / 2;
-    if (splits > 1 && splits > room / 2 / regular) splits = room / 2 / regular;
+    if (splits > room / (regular + a.sink_blocks * as_long)) splits = room / (regular + a.sink_blocks * as_long);
     if (splits < 1) splits = 1;
-    if (a.sink_blocks && most > 0) { // as long as the others
-        sink_splits = (tiles * a.share + most - 1) / most * splits;
-        const int64_t left = room - (splits > 1 ? regular * splits : 0);
-        if (sink_splits > left / a.sink_blocks) sink_splits = left / a.sink_blocks;
-        if (sink_splits < 1) sink_splits = 1;
-    }
+    int64_t sink_splits = as_long * splits;
+    const int64_t left = room - (splits > 1 ? regular * splits : 0);
+    if (a.sink_blocks && sink_splits > left / a.sink_blocks) sink_splits = left / a.sink_blocks;
+    if (!a.sink_blocks || sink_splits < 1) sink_splits = 1;
     a.splits = (int)splits;
     a.sink_splits = (int)sink_splits;
     a.slots = (int)((sink_splits > 1 ? a.sink_blocks * sink_splits : 0) + (splits > 1 ? regular * splits : 0));
