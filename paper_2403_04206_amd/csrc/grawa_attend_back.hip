@@ -1,5 +1,5 @@
 // Gradients of the attention of grawa_attend.hip:
-//   P_ij = exp(s_ij - lse_i), dP = do v^T, delta_i = do_i . o_i, dS = P (dP - delta)
+//   P_ij = exp(s_ij - lse_i), dP = do v^T, delta_i = do_i . o_i = sum_j P_ij dP_ij, dS = P (dP - delta)
 //   dq = scale dS k,  dk = scale dS^T q,  dv = P^T do,  dbias[b] = sum of dS over the pairs whose distance is in bucket b
 // Two kernels form P and dS tile by tile, one for blocks of queries (dq, dbias, delta), one for blocks of keys (dk and dv of all heads
 // that share them): nothing is added up in an order that depends on timing.
@@ -7,7 +7,14 @@
 
 namespace {
 
+// delta is do . o, and o was rounded to bfloat16: off by 2^-9 |do||o| or so, the same for all keys of a row, where each dS is off by its own
+// 2^-9.  Over many keys that is little beside them, over few it is what dq and dk are off by most (windows of 32 and 4 first keys: 2.7e-3
+// against 2.3e-3).  Queries whose block has so few tiles of keys go over them once more before, for delta = sum P dP in float32:
+// 2048 tokens without a window 4 blocks of 16, and 3 % of dq's time; all blocks, that would be 70 %.
+constexpr int OWN_DOT_TILES = 8;
+
 // A block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.
+
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
 {
@@ -48,11 +55,6 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     }
     float lse = counts ? a.lse[((int64_t)kn * a.H + head) * a.Sq + i] * LOG2E : __builtin_inff();
     if (lse == -__builtin_inff()) lse = __builtin_inff(); // the row sees nothing
-    if (half == 0 && i < a.row_pitch) {
-        const int64_t row = ((int64_t)kn * a.H + head) * a.row_pitch + i;
-        a.row_lse[row] = lse;
-        a.row_dot[row] = -delta;
-    }
 
     const float c2 = a.scale * LOG2E;
     float far = 0.f;
@@ -84,9 +86,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0) { return j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
     const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
-    grawa_f32x16 minus_dot;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) minus_dot[r] = -delta;
+    grawa_f32x16 minus_dot = {};
     constexpr int A = BF16 ? 4 : 2;
     // dS of 32 keys; leaves the first fragments of `then` in f.
     const auto slopes = [&](const char *buf, int u, int j0, V (&f)[A], auto &&then) __attribute__((always_inline)) {
@@ -115,6 +115,56 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             for (int r = 0; r < 16; ++r) s[r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : 0.f;
         return s;
     };
+
+    // All of the wave's pairs, 32 keys at a time.
+    const auto walk = [&](auto &&step) __attribute__((always_inline)) {
+        const auto both_halves = [&](int it, const char *buf) __attribute__((always_inline)) {
+            for (int u = 0; u < 2; ++u) {
+                const int j0 = tile_of(it) + 32 * u;
+                if (!none(j0)) step(buf, u, j0);
+            }
+        };
+        if constexpr (BUFS == 2) {
+            if (tiles) load(buf0);
+            for (int it = 0; it < tiles; it += 2) {
+                landed();
+                if (it + 1 < tiles) load(buf1);
+                both_halves(it, buf0);
+                if (it + 1 == tiles) break;
+                landed();
+                if (it + 2 < tiles) load(buf0);
+                both_halves(it + 1, buf1);
+            }
+        } else {
+            for (int it = 0; it < tiles; ++it) {
+                landed();
+                load(buf0);
+                landed();
+                both_halves(it, buf0);
+            }
+        }
+    };
+    if constexpr (BF16) {
+        if (tiles <= OWN_DOT_TILES) {
+            delta = 0.f;
+            walk([&](const char *buf, int u, int j0) __attribute__((always_inline)) {
+                V f[A];
+                const grawa_f32x16 s = slopes(buf, u, j0, f, [&](int) { return V{}; });
+#pragma unroll
+                for (int r = 0; r < 16; ++r) delta += s[r];
+            });
+            delta += other_half(delta);
+            restart();
+            landed();
+        }
+    }
+    if (half == 0 && i < a.row_pitch) {
+        const int64_t row = ((int64_t)kn * a.H + head) * a.row_pitch + i;
+        a.row_lse[row] = lse;
+        a.row_dot[row] = -delta;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) minus_dot[r] = -delta;
 
     grawa_f32x16 dq[DT];
     float far_sum = 0.f; // of dS from the last distance of the table on
@@ -159,31 +209,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         __builtin_amdgcn_sched_barrier(0);
         flow<2 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) { dq[i % DT] = mfma(x, w[i / DT], dq[i % DT]); });
     };
-    const auto both_halves = [&](int it, const char *buf) __attribute__((always_inline)) {
-        for (int u = 0; u < 2; ++u) {
-            const int j0 = tile_of(it) + 32 * u;
-            if (!none(j0)) step(buf, u, j0);
-        }
-    };
-    if constexpr (BUFS == 2) {
-        if (tiles) load(buf0);
-        for (int it = 0; it < tiles; it += 2) {
-            landed();
-            if (it + 1 < tiles) load(buf1);
-            both_halves(it, buf0);
-            if (it + 1 == tiles) break;
-            landed();
-            if (it + 2 < tiles) load(buf0);
-            both_halves(it + 1, buf1);
-        }
-    } else {
-        for (int it = 0; it < tiles; ++it) {
-            landed();
-            load(buf0);
-            landed();
-            both_halves(it, buf0);
-        }
-    }
+    walk(step);
     bool odd = false;
     if (counts)
 #pragma unroll

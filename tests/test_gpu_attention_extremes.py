@@ -110,6 +110,22 @@ def test_scores_of_any_size(size, dtype):
     c.plan.destroy()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 3)])
+def test_values_with_a_mean_beside_few_keys(window, sinks, D):
+    """What all values have in common cancels in dS, which the rounding of o would hide: 8 in all values are 2^-8 8 sqrt(2 / 3) / 2 = 1.3 % of dP.
+    Two roundings to bfloat16, of dS and of the result, are off by 2^-8 / sqrt(3) at most in the mean of squares, and together by
+    sqrt(2) of that, 0.0032; keys and queries are independent of each other, so that their sums keep the ratio."""
+    c = Case(1, 1, 200, 200, 2, 1, D, torch.bfloat16, seed=21, window=window, sinks=sinks)
+    c.v.copy_(ref.make(c.v.shape, torch.bfloat16, generator(22), mean=8.0))
+    want = c.want()
+    got = results(c)
+    for name in ("dq", "dk"):
+        exact = want[name][0]
+        assert float((got[name] - exact).norm() / exact.norm()) < 0.0035, name
+    c.plan.destroy()
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_growing_scores_move_the_maximum(dtype):
     """Each token's score is above all before it by a few: the running maximum moves in most tiles."""
