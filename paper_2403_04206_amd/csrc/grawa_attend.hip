@@ -81,6 +81,11 @@ __device__ __forceinline__ void soften(const grawa_f32x16 (&s)[NS], float c, Run
 
 // A block has 128 queries of one head, a wave 32 of them, and all waves share tiles of 64 keys and values, two in LDS.
 // splits > 1: that many blocks share the keys, and k_attend_join puts their results together.
+// Scores are formed transposed, a lane holding one query's, so that what one product leaves in a lane's registers is what the next takes.
+// Heads of 64 are bound by the vector unit: an exponential, a product-sum, a sum and half a conversion a score, 64 % of the time, matrix
+// cores 38 %; 8 workers, 16 heads of 2048 tokens, bf16: 95 us, 720 TFLOP/s of the pairs that count.  Heads of 128 wait for both in turn
+// (55 and 45 %): 32 heads of 16384 tokens, window 4096, 940 us, 1020 TFLOP/s.  float32 is bound by its matrix instructions, 50 % busy:
+// 76 us for 4 workers' 3 ragged sequences of 600.  64 queries a wave, halving what LDS delivers: 2 waves a SIMD less, and slower.
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 1) void k_attend([[maybe_unused]] GrawaAttend a)
 {
@@ -257,7 +262,8 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
 }
 
 // The same for few queries: a block has up to 32 columns, which are the queries of all heads that share their keys, and its NW waves
-// have 32 keys each of a tile; their sums are joined at the end.
+// have 32 keys each of a tile; their sums are joined at the end.  Bound by reading the cache: a token of 32 sequences over up to 16384 keys,
+// window 8192, 8 groups of 4 heads of 128: 172 us, 880 MB, 5.1 TB/s; 4 x 16 heads of 64 over 2048 9 us, half of it a launch's.
 template <bool BF16, int DP, bool BIAS, int NW>
 __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAttend a)
 {
@@ -415,22 +421,23 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #endif
 }
 
-// o = sum over the splits of o_s exp(lse_s - lse): eight elements a lane, all splits' asked for before the first is used (eight at a time).
-template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_join([[maybe_unused]] GrawaAttend a)
+// o = sum over the splits of o_s exp(lse_s - lse): eight elements a lane, eight splits asked for before the first is used.  NW = 4: each of
+// a block's waves has every fourth split of its rows, and the waves' sums are joined in order.
+template <bool BF16, int DP, int NW> __global__ __launch_bounds__(256) void k_attend_join([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int LPR = DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N, U = 8;
-    const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    const int e0 = threadIdx.x % LPR * 8;
-    if (row >= rows) return;
+    constexpr int LPR = DP / 8, ES = BF16 ? 2 : 4, PN = GrawaPiece<BF16>::N, U = 8, THREADS = 256 / NW;
+    __shared__ float tops[NW][THREADS], totals[NW][THREADS], sums[NW][8][NW == 1 ? 1 : THREADS];
+    const int lane = threadIdx.x % THREADS, wave = threadIdx.x / THREADS, e0 = lane % LPR * 8;
+    const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, own = (int64_t)blockIdx.x * (THREADS / LPR) + lane / LPR, row = own < rows ? own : rows - 1;
     const float *lse = a.part + (int64_t)a.splits * rows * DP + row, *part = a.part + row * DP + e0;
     float top = -__builtin_inff(), total = 0.f, v[8] = {};
-    for (int s0 = 0; s0 < a.splits; s0 += U) {
+    for (int s0 = wave; s0 < a.splits; s0 += NW * U) {
         float l[U];
         grawa_f32x4v x[U], y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int s = s0 + u < a.splits ? s0 + u : a.splits - 1; // what is read twice is left out below
+            const int s = s0 + NW * u < a.splits ? s0 + NW * u : s0; // what is read twice is left out below
             l[u] = lse[s * rows];
             x[u] = *(const grawa_f32x4v *)(part + (int64_t)s * rows * DP);
             y[u] = *(const grawa_f32x4v *)(part + (int64_t)s * rows * DP + 4);
@@ -445,13 +452,35 @@ template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_joi
         for (int j = 0; j < 8; ++j) v[j] *= before;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (s0 + u >= a.splits || l[u] == -__builtin_inff()) continue;
+            if (s0 + NW * u >= a.splits || l[u] == -__builtin_inff()) continue;
             const float f = __builtin_amdgcn_exp2f(l[u] - base);
             total += f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] += x[u][j] * f, v[4 + j] += y[u][j] * f;
         }
     }
+    if constexpr (NW > 1) {
+        tops[wave][lane] = top;
+        totals[wave][lane] = total;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[wave][j][lane] = v[j];
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) top = fmaxf(top, tops[w][lane]);
+        const float base = top == -__builtin_inff() ? 0.f : top;
+        total = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(tops[w][lane] - base);
+            total += totals[w][lane] * f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += sums[w][j][lane] * f;
+        }
+    }
+    if (own >= rows) return;
     const bool any = !(total == 0.f);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = any ? v[j] / total : 0.f;
@@ -466,12 +495,15 @@ template <bool BF16, int DP> __global__ __launch_bounds__(256) void k_attend_joi
 #endif
 }
 
-constexpr int KEYS_COLUMNS = 64; // up to this many columns of a group of heads the waves of a block have keys of their own
+// Up to so many columns of a group of heads the waves of a block have keys of their own.  4 sequences over 4096 keys, by keys and by queries:
+// bf16, 16 heads of 64, 64 columns 22 and 24 us, 96 columns 35 and 25; 8 groups of 4 heads of 128, 64 columns 25 and 45, 128 columns 66 and 45;
+// float32, 32 columns of 64 36 and 78, 96 columns 103 and 77.
+constexpr int KEYS_COLUMNS = 64;
 
-// How many blocks share the keys: enough to give the card 512, no more than there are tiles to share or room for their results.
-int splits_of(int64_t blocks, int64_t rows, int DP, int64_t tiles, int64_t part_floats)
+// How many blocks share the keys: enough to give the card `target`, no more than there are tiles to share or room for their results.
+int splits_of(int64_t target, int64_t blocks, int64_t rows, int DP, int64_t tiles, int64_t part_floats)
 {
-    int64_t s = blocks >= 384 ? 1 : 512 / blocks;
+    int64_t s = blocks >= target * 3 / 4 ? 1 : target / blocks;
     if (s > tiles / 2) s = tiles / 2;
     const int64_t room = part_floats / (rows * (DP + 1));
     if (s > room) s = room;
@@ -487,18 +519,26 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     if (seen > a.Sk) seen = a.Sk;
     if ((int64_t)a.share * a.Sq <= KEYS_COLUMNS) {
         a.blocks = (a.share * a.Sq + 31) / 32;
-        a.splits = splits_of(kn * a.G * a.blocks, rows, DP, (seen + 32 * KW - 1) / (32 * KW), part_floats);
+        // One block a CU, which reads ahead far enough: a token over 16384 keys, 8 groups of 128, 20.3 us and with two blocks 26.8; 16 tokens
+        // of 4 heads each over 4096 24.8 and 36.9; 16 x 16 heads of 64 over 4096 46.5 and 49.5; 4 x 16 over 2048 12.1 and 11.7.
+        a.splits = splits_of(256, kn * a.G * a.blocks, rows, DP, (seen + 32 * KW - 1) / (32 * KW), part_floats);
         const uint32_t grid = grid_of(kn * a.G, 1, (int64_t)a.blocks * a.splits, a.by_xcd);
         hipLaunchKernelGGL((k_attend_few<BF16, DP, BIAS, KW>), dim3(grid), dim3(KW * 64), 0, st, a);
     } else {
         a.blocks = (a.Sq + 127) / 128;
-        a.splits = splits_of(kn * a.H * a.blocks, rows, DP, (seen + 63) / 64, part_floats);
+        // Two blocks a CU: 32 queries of 4 heads each over 4096, 8 groups of 128, 39.3 us and with one 46.2.
+        a.splits = splits_of(512, kn * a.H * a.blocks, rows, DP, (seen + 63) / 64, part_floats);
         const uint32_t grid = grid_of(kn * a.G, a.share, (int64_t)a.blocks * a.splits, a.by_xcd);
         hipLaunchKernelGGL((k_attend<BF16, DP, BIAS>), dim3(grid), dim3(256), 0, st, a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    hipLaunchKernelGGL((k_attend_join<BF16, DP>), dim3((uint32_t)((rows * (DP / 8) + 255) / 256)), dim3(256), 0, st, a);
+    // Few rows that many blocks shared are all latency: 32 rows of 128 elements, 64 splits, attention and join 34.5 us by lanes, 26.8 by
+    // waves; 1024 tokens of 8 heads of 128, two sequences, 4 splits: 28.7 by lanes, 35.2 by waves.
+    if (a.splits > 8)
+        hipLaunchKernelGGL((k_attend_join<BF16, DP, 4>), dim3((uint32_t)((rows * (DP / 8) + 63) / 64)), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_attend_join<BF16, DP, 1>), dim3((uint32_t)((rows * (DP / 8) + 255) / 256)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

@@ -10,10 +10,13 @@ namespace {
 // delta is do . o, and o was rounded to bfloat16: off by 2^-9 |do||o| or so, the same for all keys of a row, where each dS is off by its own
 // 2^-9.  Over many keys that is little beside them, over few it is what dq and dk are off by most (windows of 32 and 4 first keys: 2.7e-3
 // against 2.3e-3).  Queries whose block has so few tiles of keys go over them once more before, for delta = sum P dP in float32:
-// 2048 tokens without a window 4 blocks of 16, and 3 % of dq's time; all blocks, that would be 70 %.
+// 2048 tokens without a window, 8 workers of 16 heads of 64: 4 blocks of 16, 130 us and not 122.
 constexpr int OWN_DOT_TILES = 8;
 
-// A block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.
+// A block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.  dS is formed transposed, so that it is
+// an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 130 us, vector unit 50 %, matrix cores 46 %; with a bias of 32
+// buckets to distance 128: 195, of which the sums by distance are the difference; 32 heads of 16384 tokens of 128, window 4096: 1265, matrix
+// cores 65 %.
 
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
@@ -299,7 +302,10 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums([[maybe_
 
 // A block has 32 keys for each of its NW waves; all waves share tiles of 64 queries and the gradients of their outputs, of one head
 // after the other.  Keys and the sums of dk and dv stay in registers, values too where heads have 64 elements; with 128 they do not fit
-// and are read from LDS (in registers all the same, 8 heads of 32 x 16384 tokens spilled and took 22.6 ms).  splits > 1 (sink_splits for the keys that all queries see): that many blocks share the queries of a block of keys.
+// and are read from LDS (in registers all the same they were spilled: 32 heads of 16384 tokens, window 4096, 22.6 ms and not 2.0).
+// splits > 1 (sink_splits for the keys that all queries see): that many blocks share the queries of a block of keys.
+// The four products of a pair and its exponential: 8 workers, 16 heads of 2048 tokens of 64, bf16, 167 us, vector unit 46 %, matrix cores
+// 42 %; heads of 128 as above 1940 to 2020, 49 and 48 %, with eight waves on a CU that wait for each other at every tile.
 template <bool BF16, int DP, bool BIAS, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : DP == 64 ? 2 : 1) void k_attend_dkv([[maybe_unused]] GrawaAttend a)
 {
