@@ -469,7 +469,9 @@ grawa_status_t grawa_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype, c
  * Types.  One type a plan, as in the sublayer.  Scores, softmax statistics, sums and
  * angles are float32 (angles are reduced in 64 bits).  With bfloat16 exp(s_ij - max)
  * and the gradient of s_ij are rounded to bfloat16 once, as the matrix instructions
- * take them, and the gradients use o as rounded; with float32 products are float32.
+ * take them, and the gradients of queries beside many keys use o as rounded (beside few,
+ * about 500, where that would show, they form what they need of it again); with float32
+ * products are float32.
  * The gradients form exp(s_ij - lse_i): scores beyond 2^20 in size leave them no digits.
  *
  * Layouts.  grawa_heads_t is K x N x S x heads rows of D elements: worker k's sequence
@@ -557,8 +559,8 @@ grawa_status_t grawa_attention(grawa_attention_plan_t *plan, int64_t N, int64_t 
 
 /*
  * Its gradients: dq, dk, dv, and dbias where the plan has buckets.  Inputs, o and lse
- * are those of the forward call.  Padding gets 0.  accumulate != 0 adds to dbias instead
- * of replacing it.  Sums are formed in a fixed order.
+ * are those of the forward call; no output may overlap one of them.  Padding gets 0.
+ * accumulate != 0 adds to dbias instead of replacing it.  Sums are formed in a fixed order.
  */
 grawa_status_t grawa_attention_backward(grawa_attention_plan_t *plan, int64_t N, int64_t Sq, int64_t Sk,
                                         const grawa_heads_t *d_o, const grawa_heads_t *q,

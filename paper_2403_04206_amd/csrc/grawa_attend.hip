@@ -83,9 +83,9 @@ __device__ __forceinline__ void soften(const grawa_f32x16 (&s)[NS], float c, Run
 // splits > 1: that many blocks share the keys, and k_attend_join puts their results together.
 // Scores are formed transposed, a lane holding one query's, so that what one product leaves in a lane's registers is what the next takes.
 // Heads of 64 are bound by the vector unit: an exponential, a product-sum, a sum and half a conversion a score, 64 % of the time, matrix
-// cores 38 %; 8 workers, 16 heads of 2048 tokens, bf16: 95 us, 720 TFLOP/s of the pairs that count.  Heads of 128 wait for both in turn
-// (55 and 45 %): 32 heads of 16384 tokens, window 4096, 940 us, 1020 TFLOP/s.  float32 is bound by its matrix instructions, 50 % busy:
-// 76 us for 4 workers' 3 ragged sequences of 600.  64 queries a wave, halving what LDS delivers: 2 waves a SIMD less, and slower.
+// cores 38 %; 8 workers, 16 heads of 2048 tokens, bf16: 92 us, 750 TFLOP/s of the pairs that count.  Heads of 128 wait for both in turn
+// (55 and 45 %): 32 heads of 16384 tokens, window 4096, 917 us, 1050 TFLOP/s.  float32 is bound by its matrix instructions, 50 % busy:
+// 72 us for 4 workers' 3 ragged sequences of 600.  64 queries a wave, halving what LDS delivers: 2 waves a SIMD less, and slower.
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 1) void k_attend([[maybe_unused]] GrawaAttend a)
 {
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
 
 // The same for few queries: a block has up to 32 columns, which are the queries of all heads that share their keys, and its NW waves
 // have 32 keys each of a tile; their sums are joined at the end.  Bound by reading the cache: a token of 32 sequences over up to 16384 keys,
-// window 8192, 8 groups of 4 heads of 128: 172 us, 880 MB, 5.1 TB/s; 4 x 16 heads of 64 over 2048 9 us, half of it a launch's.
+// window 8192, 8 groups of 4 heads of 128: 169 us, 880 MB, 5.2 TB/s; 4 x 16 heads of 64 over 2048 9 us, half of it a launch's.
 template <bool BF16, int DP, bool BIAS, int NW>
 __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAttend a)
 {

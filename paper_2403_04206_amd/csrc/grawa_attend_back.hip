@@ -14,9 +14,9 @@ namespace {
 constexpr int OWN_DOT_TILES = 8;
 
 // A block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.  dS is formed transposed, so that it is
-// an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 130 us, vector unit 50 %, matrix cores 46 %; with a bias of 32
-// buckets to distance 128: 195, of which the sums by distance are the difference; 32 heads of 16384 tokens of 128, window 4096: 1265, matrix
-// cores 65 %.
+// an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 125 to 130 us, vector unit 50 %, matrix cores 46 %; with a bias of 32
+// buckets to distance 128: 195, of which the sums by distance are the difference; 32 heads of 16384 tokens of 128, window 4096: 1230, matrix
+// cores 66 %.
 
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
@@ -157,6 +157,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
                 for (int r = 0; r < 16; ++r) delta += s[r];
             });
             delta += other_half(delta);
+            delta = counts ? delta : 0.f;
             restart();
             landed();
         }
@@ -304,8 +305,8 @@ template <bool BF16> __global__ __launch_bounds__(256) void k_bias_sums([[maybe_
 // after the other.  Keys and the sums of dk and dv stay in registers, values too where heads have 64 elements; with 128 they do not fit
 // and are read from LDS (in registers all the same they were spilled: 32 heads of 16384 tokens, window 4096, 22.6 ms and not 2.0).
 // splits > 1 (sink_splits for the keys that all queries see): that many blocks share the queries of a block of keys.
-// The four products of a pair and its exponential: 8 workers, 16 heads of 2048 tokens of 64, bf16, 167 us, vector unit 46 %, matrix cores
-// 42 %; heads of 128 as above 1940 to 2020, 49 and 48 %, with eight waves on a CU that wait for each other at every tile.
+// The four products of a pair and its exponential: 8 workers, 16 heads of 2048 tokens of 64, bf16, 164 us, vector unit 46 %, matrix cores
+// 42 %; heads of 128 as above 1890 to 2010, 49 and 48 %, with eight waves on a CU that wait for each other at every tile.
 template <bool BF16, int DP, bool BIAS, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : DP == 64 ? 2 : 1) void k_attend_dkv([[maybe_unused]] GrawaAttend a)
 {
