@@ -137,6 +137,29 @@ def test_growing_scores_move_the_maximum(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Sq,length,window,sinks", [(1, 5000, 0, 0), (3, 5000, 0, 0), (1, 90, 0, 0), (1, 4999, 700, 3), (70, 5000, 0, 0), (70, 70, 0, 0), (129, 4321, 0, 0), (5, 3, 0, 0)])
+def test_many_blocks_share_the_keys(Sq, length, window, sinks, D, dtype):
+    """Few rows over many keys: most blocks' shares, some of them, or all but one are empty; what is behind the length is no number."""
+    Sk = 5000
+    c = Case(1, 1, Sq, Sk, 3, 1, D, dtype, seed=23, lengths=[length], starts=[length - Sq], window=window, sinks=sinks)
+    want = c.want(False)
+    for t in (c.k, c.v):
+        t[0, 0, length:] = NAN
+    c.forward()
+    torch.cuda.synchronize()
+    ref.check(c.o, *want["o"], "o")
+    ref.check(c.lse, *want["lse"], "lse")
+    c.v[0, 0, 0] = NAN                                                             # a share that is no number beside others that are
+    c.forward()
+    torch.cuda.synchronize()
+    seen = ref.visible(length - Sq, length, Sq, Sk, window, sinks, "cuda")[0][:, 0]
+    assert bool(c.o[0, 0, seen].isnan().all())
+    ref.check(c.o[:, :, ~seen], want["o"][0][:, :, ~seen], want["o"][1][:, :, ~seen], "o of those that do not see it")
+    c.plan.destroy()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("hidden", [-INF, "lowest"])
 def test_a_bias_that_hides(hidden, dtype):
     """Every distance hidden by minus infinity gives rows of 0; by the type's lowest number, an average of what is equally low."""
