@@ -13,7 +13,10 @@ namespace {
 // 2048 tokens without a window, 8 workers of 16 heads of 64: 4 blocks of 16, 130 us and not 122.
 constexpr int OWN_DOT_TILES = 8;
 
-// A block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.  dS is formed transposed, so that it is
+// bf16: a block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.  float32, whose products are
+// eight times as long: 64 queries, and of the two waves that have the same 32 each has half of a tile's keys; the second's sums go to
+// the first through LDS.  2 workers of 3 sequences of 333 tokens, 6 heads of 40, with a bias, 33 us, and 50 with blocks as in bf16; all
+// gradients of 4096 tokens, 8 heads of 128, 1107 and 1420, of 4 workers' 16 heads of 2048 tokens of 64 996 and 1015.  dS is formed transposed, so that it is
 // an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 125 to 130 us, vector unit 50 %, matrix cores 46 %; with a bias of 32
 // buckets to distance 128: 195, of which the sums by distance are the difference; 32 heads of 16384 tokens of 128, window 4096: 1230, matrix
 // cores 66 %.
@@ -22,7 +25,7 @@ template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int BK = 64, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1;
+    constexpr int BK = 64, ES = BF16 ? 2 : 4, KS = DP / 16, DT = DP / 32, BUFS = BF16 || DP == 64 ? 2 : 1, QW = grawa_dq_queries(BF16) / 32;
     typedef HeadTile<BF16, DP, BK, 4> Tile;
     typedef typename Tile::V V;
     __shared__ __attribute__((aligned(1024))) char buf0[2 * Tile::BYTES], buf1[BUFS == 2 ? 2 * Tile::BYTES : 16]; // keys and values
@@ -31,13 +34,14 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     float *const table = tables, *const by_distance = tables + (1 + (threadIdx.x >> 6)) * a.distances;
     int *const bucket_of = (int *)(tables + 5 * a.distances);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int qw = wave % QW, kw = wave / QW; // the wave's queries, and its keys where they are not all
     const int heads = a.K * a.N * a.H;
     const Turn turn = turn_of(blockIdx.x, a.K * a.N * a.G, a.share, a.by_xcd);
     if (turn.head >= heads) return;
     const int qb = a.blocks - 1 - turn.block;
     const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
     const Place at = place_of(a, kn);
-    const int i = qb * 128 + wave * 32 + (lane & 31), pos = at.start + i;
+    const int i = qb * (32 * QW) + qw * 32 + (lane & 31), pos = at.start + i;
     const bool there = i < a.Sq, counts = there && pos >= 0 && pos < at.length;
 
     V q[KS], go[KS];
@@ -72,7 +76,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         for (int d = lane; d < 16 * 64; d += 64) diagonals[wave][d] = 0.f;
     }
 
-    const int p0 = at.start + qb * 128, p1 = at.start + min((qb + 1) * 128, a.Sq) - 1, w0 = p0 + wave * 32, w1 = w0 + 31;
+    const int p0 = at.start + qb * (32 * QW), p1 = at.start + min((qb + 1) * (32 * QW), a.Sq) - 1, w0 = p0 + qw * 32, w1 = w0 + 31;
     const int end = min(p1, at.length - 1) + 1, begin = max(0, max(p0, 0) - a.window + 1);
     const bool any = p1 >= 0 && p0 < at.length;
     const int t0 = begin / BK, first_tiles = any ? min(t0, (min(a.sinks, end) + BK - 1) / BK) : 0, tiles = any ? first_tiles + (end + BK - 1) / BK - t0 : 0;
@@ -122,7 +126,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     // All of the wave's pairs, 32 keys at a time.
     const auto walk = [&](auto &&step) __attribute__((always_inline)) {
         const auto both_halves = [&](int it, const char *buf) __attribute__((always_inline)) {
-            for (int u = 0; u < 2; ++u) {
+            for (int u = BF16 ? 0 : kw; u < (BF16 ? 2 : kw + 1); ++u) {
                 const int j0 = tile_of(it) + 32 * u;
                 if (!none(j0)) step(buf, u, j0);
             }
@@ -162,7 +166,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             landed();
         }
     }
-    if (half == 0 && i < a.row_pitch) {
+    if (half == 0 && kw == 0 && i < a.row_pitch) {
         const int64_t row = ((int64_t)kn * a.H + head) * a.row_pitch + i;
         a.row_lse[row] = lse;
         a.row_dot[row] = -delta;
@@ -214,6 +218,22 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         flow<2 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) { dq[i % DT] = mfma(x, w[i / DT], dq[i % DT]); });
     };
     walk(step);
+    if constexpr (!BF16) {
+        landed();
+        float *const other = (float *)buf0 + qw * (DT * 16 * 64) + lane;
+        static_assert(2 * DT * 16 * 64 * 4 <= 2 * Tile::BYTES, "room for two waves' sums");
+        if (kw)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) other[(d * 16 + r) * 64] = dq[d][r];
+        __syncthreads();
+        if (!kw)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dq[d][r] += other[(d * 16 + r) * 64];
+    }
     bool odd = false;
     if (counts)
 #pragma unroll
@@ -222,7 +242,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             for (int r = 0; r < 16; ++r) odd |= dq[d][r] != dq[d][r];
     char *out = a.dq.p + (int64_t)k * a.dq.worker + (int64_t)n * a.dq.seq + (int64_t)i * a.dq.token + (int64_t)head * a.dq.head;
     const auto put = [&](int d, const grawa_f32x16 &sums) {
-        if (!there) return;
+        if (!there || kw) return;
         grawa_f32x16 v;
 #pragma unroll
         for (int r = 0; r < 16; ++r) v[r] = counts ? sums[r] : 0.f;
@@ -611,7 +631,7 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     const int64_t kn = (int64_t)a.K * a.N;
     hipError_t e;
     if (a.Sq > 0) {
-        a.blocks = (a.Sq + 127) / 128;
+        a.blocks = (a.Sq + grawa_dq_queries(BF16) - 1) / grawa_dq_queries(BF16);
         const uint32_t grid = grid_of(kn * a.G, a.share, a.blocks, a.by_xcd);
         hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3(grid), dim3(256), BIAS ? (uint32_t)a.distances * 6 * sizeof(float) : 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -173,7 +173,8 @@ grawa_status_t grawa_attention_create(grawa_attention_plan_t **out, const grawa_
     const size_t b_turns = round256((size_t)s->rotary / 2 * sizeof(double)), b_bucket = round256((size_t)s->distances * sizeof(int));
     const size_t b_rows = round256((size_t)knh * (size_t)grawa_round256(s->S) * 2 * sizeof(float));
     const size_t b_norm = round256((size_t)s->K * (size_t)s->norm_blocks * 2 * (size_t)s->D * sizeof(float));
-    const size_t b_bias = round256((size_t)knh * (size_t)((s->S + 127) / 128) * (size_t)s->buckets * sizeof(float));
+    const int block = grawa_dq_queries(s->dtype == GRAWA_BF16);
+    const size_t b_bias = round256((size_t)knh * (size_t)((s->S + block - 1) / block) * (size_t)s->buckets * sizeof(float));
     const size_t b_part = round256((size_t)s->part_floats * sizeof(float));
     if (hipMalloc(&s->ws, b_turns + b_bucket + b_rows + b_norm + b_bias + b_part) != hipSuccess) {
         (void)hipGetLastError();

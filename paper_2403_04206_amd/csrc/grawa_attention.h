@@ -32,6 +32,9 @@ struct grawa_attention_plan {
 
 constexpr int GRAWA_NO_WINDOW = 1 << 30;
 
+// Queries of a block that forms dq and sums for dbias.
+constexpr int grawa_dq_queries(bool bf16) { return bf16 ? 128 : 64; }
+
 // Rows of D elements behind a pointer, strides in bytes.
 struct GrawaHeads {
     char *p;
