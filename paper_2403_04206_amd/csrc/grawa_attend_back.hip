@@ -16,11 +16,10 @@ constexpr int OWN_DOT_TILES = 8;
 // bf16: a block has 128 queries of a head, a wave 32 of them; all waves share tiles of 64 keys and values.  float32, whose products are
 // eight times as long: 64 queries, and of the two waves that have the same 32 each has half of a tile's keys; the second's sums go to
 // the first through LDS.  2 workers of 3 sequences of 333 tokens, 6 heads of 40, with a bias, 33 us, and 50 with blocks as in bf16; all
-// gradients of 4096 tokens, 8 heads of 128, 1107 and 1420, of 4 workers' 16 heads of 2048 tokens of 64 996 and 1015.  dS is formed transposed, so that it is
-// an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 125 to 130 us, vector unit 50 %, matrix cores 46 %; with a bias of 32
-// buckets to distance 128: 195, of which the sums by distance are the difference; 32 heads of 16384 tokens of 128, window 4096: 1230, matrix
-// cores 66 %.
-
+// gradients of 4096 tokens, 8 heads of 128, 1107 and 1420, of 4 workers' 16 heads of 2048 tokens of 64 996 and 1015.
+// dS is formed transposed, so that it is an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 125 to 130 us,
+// vector unit 50 %, matrix cores 46 %; with a bias of 32 buckets to distance 128: 195, of which the sums by distance are the difference;
+// 32 heads of 16384 tokens of 128, window 4096: 1230, matrix cores 66 %.
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
 {
