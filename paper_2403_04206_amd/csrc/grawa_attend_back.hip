@@ -40,8 +40,8 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     const int qb = a.blocks - 1 - turn.block;
     const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
     const Place at = place_of(a, kn);
-    const int i = qb * (32 * QW) + qw * 32 + (lane & 31), pos = at.start + i;
-    const bool there = i < a.Sq, counts = there && pos >= 0 && pos < at.length;
+    const int i = qb * (32 * QW) + qw * 32 + (lane & 31);
+    const bool there = i < a.Sq, placed = there && at.start + i >= 0 && at.start + i < at.length;
 
     V q[KS], go[KS];
     float delta = 0.f;
@@ -51,16 +51,21 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         const char *po = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i * a.o.token + (int64_t)head * a.o.head;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            q[ks] = load_line<BF16>(pq, 16 * ks + 8 * half, a.D, counts);
-            go[ks] = load_line<BF16>(pg, 16 * ks + 8 * half, a.D, counts);
-            const V o = load_line<BF16>(po, 16 * ks + 8 * half, a.D, counts);
+            q[ks] = load_line<BF16>(pq, 16 * ks + 8 * half, a.D, placed);
+            go[ks] = load_line<BF16>(pg, 16 * ks + 8 * half, a.D, placed);
+            const V o = load_line<BF16>(po, 16 * ks + 8 * half, a.D, placed);
 #pragma unroll
             for (int j = 0; j < 8; ++j) delta += (float)o[j] * (float)go[ks][j];
         }
         delta += other_half(delta);
     }
-    float lse = counts ? a.lse[((int64_t)kn * a.H + head) * a.Sq + i] * LOG2E : __builtin_inff();
+    float lse = placed ? a.lse[((int64_t)kn * a.H + head) * a.Sq + i] * LOG2E : __builtin_inff();
     if (lse == -__builtin_inff()) lse = __builtin_inff(); // the row sees nothing
+    // Columns that count for nothing stand where they see no key: 0 would not be enough for what they have with one that is no number.
+    const bool counts = lse != __builtin_inff();
+    const int pos = counts ? at.start + i : -1;
+    const bool whole = __all(counts);
+    delta = counts ? delta : 0.f;
 
     const float c2 = a.scale * LOG2E;
     float far = 0.f;
@@ -90,7 +95,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     const auto load = [&](char *buf) __attribute__((always_inline)) { tiles_at.load(lk, lv, buf, wave); };
     restart();
     const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
-    const auto all = [&](int j0) { return j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
+    const auto all = [&](int j0) { return whole && j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
     const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
     grawa_f32x16 minus_dot = {};
     constexpr int A = BF16 ? 4 : 2;
