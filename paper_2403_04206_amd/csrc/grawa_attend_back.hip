@@ -558,7 +558,8 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : DP == 64 ? 2 : 1) void k_att
         else
             store_column<BF16>(to.p + (int64_t)k * to.worker + (int64_t)n * to.seq + (int64_t)j * to.token + (int64_t)g * to.head, lane, d, a.D, x, keys ? a.scale : 1.f);
     };
-    // What is no number may come from a query that does not see the key: once more then, with care.
+    // What is no number may come from a query that does not see the key, or from one that counts for nothing: its 0 x exp2(-infinity) is no
+    // number beside a key that is none.  Once more then, with care.
     if (__builtin_expect(!__syncthreads_or(odd), 1)) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) put(false, d, dv[d]), put(true, d, dk[d]);
@@ -583,13 +584,15 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : DP == 64 ? 2 : 1) void k_att
                 grawa_f32x16 s, dp;
                 V f[A];
                 slopes(buf0, rows0, u, p0, s, dp, f, [&](int) { return V{}; });
+                // Rows that count for nothing, queries that are not there among them: what they have may be no number, theirs or with this key.
+                const auto counting = [&](int r) { return rows0[32 * u + (r & 3) + 8 * (r >> 2) + 4 * half] != __builtin_inff(); };
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = keys ? dp[r] : s[r];
+                for (int r = 0; r < 16; ++r) s[r] = !counting(r) ? 0.f : keys ? dp[r] : s[r];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     V w, seen;
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) seen[r] = sees(a, p0 + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, j) ? 1.f : 0.f;
+                    for (int r = 0; r < 8; ++r) seen[r] = counting(8 * h + r) && sees(a, p0 + 16 * h + (r & 3) + 8 * (r >> 2) + 4 * half, j) ? 1.f : 0.f;
                     as_operand(s, h, w);
                     product_of_some(sums, Tile::by_columns(buf0 + (keys ? 0 : Tile::BYTES) + (32 * u + 16 * h) * Tile::RB, columns_at, 0, d), w, seen);
                 }
