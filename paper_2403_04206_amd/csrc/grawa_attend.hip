@@ -7,14 +7,21 @@
 namespace {
 
 #ifdef __HIP_DEVICE_COMPILE__
+// Where scores times their unit are so large that the rounding of their maximum would show (it is a factor of all exponentials, no more).
+constexpr float LARGE = 0x1p20f;
+
 // The running maximum and sum of a column's softmax: m in units of the scores, of which c is in units of log2.
 struct Running {
     float m, l;
     __device__ __forceinline__ float top(float c) const { return m == -__builtin_inff() ? 0.f : m * c; }
+    // A sum of the column's exponentials as one of exp2(score c - m c), of which top(c) is a rounding: what the sums of several waves or blocks
+    // are joined by.  Logarithms of the sums would not do: beside a large maximum float32 has no digits for them.
+    __device__ __forceinline__ float joined(float sum, float c) const
+    {
+        const float t = top(c);
+        return m == -__builtin_inff() || fabsf(t) > LARGE ? sum : sum * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, c, -t));
+    }
 };
-
-// Where scores times their unit are so large that the rounding of their maximum would show (it is a factor of all exponentials, no more).
-constexpr float LARGE = 0x1p20f;
 
 // exp2 of 16 scores times c against the maximum.
 __device__ __forceinline__ void exponentials(grawa_f32x16 &s, float c, const Running &run)
@@ -197,12 +204,15 @@ __global__ __launch_bounds__(256, BF16 && DP == 64 ? 3 : BF16 || DP == 64 ? 2 : 
     char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)i * a.o.token + (int64_t)head * a.o.head;
     const float l = run.l + other_half(run.l);
     const bool sum = counts && !(l == 0.f);
-    const float lse2 = sum ? run.top(unit) + __builtin_amdgcn_logf(l) : -__builtin_inff(), f = sum ? 1.f / l : 0.f;
+    const float f = sum ? 1.f / l : 0.f;
     if (half == 0 && there) {
-        if (a.splits > 1)
-            a.part[(int64_t)a.splits * rows * DP + (int64_t)split * rows + row] = lse2;
-        else if (a.lse)
-            a.lse[row] = lse2 * LN2;
+        if (a.splits > 1) {
+            float *const at_row = a.part + (int64_t)a.splits * rows * DP + (int64_t)split * rows + row;
+            at_row[0] = run.m;
+            at_row[(int64_t)a.splits * rows] = sum ? run.joined(l, unit) : 0.f;
+        } else if (a.lse) {
+            a.lse[row] = sum ? (run.top(unit) + __builtin_amdgcn_logf(l)) * LN2 : -__builtin_inff();
+        }
     }
     const auto put = [&](int d, const grawa_f32x16 &sums) {
         if (!there) return;
@@ -382,7 +392,7 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             *(grawa_f32x4v *)(sums_of(wave, lane & 31) + 32 * d + 8 * r + 4 * half) = grawa_f32x4v{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
-    if (half == 0) ml[wave * 64 + lane] = run.m == -__builtin_inff() ? run.m : run.top(unit), ml[wave * 64 + 32 + lane] = l;
+    if (half == 0) ml[wave * 64 + lane] = run.m, ml[wave * 64 + 32 + lane] = l;
     __syncthreads();
     constexpr int LPC = NW * 2, EPL = DP / LPC; // threads of a column, elements of each
     const int cl = threadIdx.x / LPC, e0 = threadIdx.x % LPC * EPL, c = cb * 32 + cl;
@@ -395,13 +405,13 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
     for (int w = 0; w < NW; ++w) {
         const float mw = ml[w * 64 + cl], lw = ml[w * 64 + 32 + cl];
         if (lw == 0.f) continue;
-        const float f = __builtin_amdgcn_exp2f(mw - top);
+        const float f = Running{mw, 0.f}.joined(__builtin_amdgcn_exp2f((mw - top) * unit), unit);
         total += lw * f;
 #pragma unroll
         for (int e = 0; e < EPL; ++e) v[e] += sums_of(w, cl)[e0 + e] * f;
     }
     const bool sum = p >= 0 && p < at.length && !(total == 0.f);
-    const float f = sum ? 1.f / total : 0.f, lse2 = sum ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
+    const float f = sum ? 1.f / total : 0.f;
     const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, row = ((int64_t)kn * a.H + h) * a.Sq + ii;
 #pragma unroll
     for (int e = 0; e < EPL; ++e) v[e] = sum ? v[e] * f : 0.f;
@@ -409,7 +419,11 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
         float *part = a.part + ((int64_t)split * rows + row) * DP + e0;
 #pragma unroll
         for (int e = 0; e < EPL; e += 4) *(grawa_f32x4v *)(part + e) = grawa_f32x4v{v[e], v[e + 1], v[e + 2], v[e + 3]};
-        if (e0 == 0) a.part[(int64_t)a.splits * rows * DP + (int64_t)split * rows + row] = lse2;
+        if (e0 == 0) {
+            float *const at_row = a.part + (int64_t)a.splits * rows * DP + (int64_t)split * rows + row;
+            at_row[0] = top;
+            at_row[(int64_t)a.splits * rows] = sum ? total : 0.f;
+        }
         return;
     }
     char *out = a.o.p + (int64_t)k * a.o.worker + (int64_t)n * a.o.seq + (int64_t)ii * a.o.token + (int64_t)h * a.o.head;
@@ -417,12 +431,12 @@ __global__ __launch_bounds__(NW * 64) void k_attend_few([[maybe_unused]] GrawaAt
 #pragma unroll
     for (int e = 0; e < EPL; e += PN)
         if (e0 + e < a.D) store_piece<BF16>(out + (e0 + e) * ES, PN, v + e);
-    if (a.lse && e0 == 0) a.lse[row] = lse2 * LN2;
+    if (a.lse && e0 == 0) a.lse[row] = sum ? (top * unit + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 #endif
 }
 
-// o = sum over the splits of o_s exp(lse_s - lse): eight elements a lane, eight splits asked for before the first is used.  NW = 4: each of
-// a block's waves has every fourth split of its rows, and the waves' sums are joined in order.
+// o = sum over the splits of o_s l_s exp2((m_s - m) unit) / l, of the splits' maxima and sums: eight elements a lane, eight splits asked for
+// before the first is used.  NW = 4: each of a block's waves has every fourth split of its rows, and the waves' sums are joined in order.
 template <bool BF16, int DP, int NW> __global__ __launch_bounds__(256) void k_attend_join([[maybe_unused]] GrawaAttend a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -430,30 +444,32 @@ template <bool BF16, int DP, int NW> __global__ __launch_bounds__(256) void k_at
     __shared__ float tops[NW][THREADS], totals[NW][THREADS], sums[NW][8][NW == 1 ? 1 : THREADS];
     const int lane = threadIdx.x % THREADS, wave = threadIdx.x / THREADS, e0 = lane % LPR * 8;
     const int64_t rows = (int64_t)a.K * a.N * a.H * a.Sq, own = (int64_t)blockIdx.x * (THREADS / LPR) + lane / LPR, row = own < rows ? own : rows - 1;
-    const float *lse = a.part + (int64_t)a.splits * rows * DP + row, *part = a.part + row * DP + e0;
+    const float *tops_at = a.part + (int64_t)a.splits * rows * DP + row, *sums_at = tops_at + (int64_t)a.splits * rows, *part = a.part + row * DP + e0;
+    const float unit = a.buckets ? 1.f : a.scale * LOG2E;
     float top = -__builtin_inff(), total = 0.f, v[8] = {};
     for (int s0 = wave; s0 < a.splits; s0 += NW * U) {
-        float l[U];
+        float m[U], l[U];
         grawa_f32x4v x[U], y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = s0 + NW * u < a.splits ? s0 + NW * u : s0; // what is read twice is left out below
-            l[u] = lse[s * rows];
+            m[u] = tops_at[s * rows];
+            l[u] = sums_at[s * rows];
             x[u] = *(const grawa_f32x4v *)(part + (int64_t)s * rows * DP);
             y[u] = *(const grawa_f32x4v *)(part + (int64_t)s * rows * DP + 4);
         }
-        float m = top;
+        float m2 = top;
 #pragma unroll
-        for (int u = 0; u < U; ++u) m = fmaxf(m, l[u]);
-        const float base = m == -__builtin_inff() ? 0.f : m, before = __builtin_amdgcn_exp2f(top - base); // no numbers pass the maximum by
-        top = m;
+        for (int u = 0; u < U; ++u) m2 = fmaxf(m2, m[u]);
+        const float base = m2 == -__builtin_inff() ? 0.f : m2, before = __builtin_amdgcn_exp2f((top - base) * unit);
+        top = m2;
         total *= before;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= before;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (s0 + NW * u >= a.splits || l[u] == -__builtin_inff()) continue;
-            const float f = __builtin_amdgcn_exp2f(l[u] - base);
+            if (s0 + NW * u >= a.splits || l[u] == 0.f) continue; // sums that are no numbers pass
+            const float f = l[u] * __builtin_amdgcn_exp2f((m[u] - base) * unit);
             total += f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] += x[u][j] * f, v[4 + j] += y[u][j] * f;
@@ -474,7 +490,7 @@ template <bool BF16, int DP, int NW> __global__ __launch_bounds__(256) void k_at
         for (int j = 0; j < 8; ++j) v[j] = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float f = __builtin_amdgcn_exp2f(tops[w][lane] - base);
+            const float f = __builtin_amdgcn_exp2f((tops[w][lane] - base) * unit);
             total += totals[w][lane] * f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += sums[w][j][lane] * f;
@@ -491,7 +507,7 @@ template <bool BF16, int DP, int NW> __global__ __launch_bounds__(256) void k_at
 #pragma unroll
     for (int j = 0; j < 8; j += PN)
         if (e0 + j < a.D) store_piece<BF16>(out + (e0 + j) * ES, PN, v + j);
-    if (a.lse && e0 == 0) a.lse[row] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+    if (a.lse && e0 == 0) a.lse[row] = any ? (top * unit + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 #endif
 }
 
@@ -505,7 +521,7 @@ int splits_of(int64_t target, int64_t blocks, int64_t rows, int DP, int64_t tile
 {
     int64_t s = blocks >= target * 3 / 4 ? 1 : target / blocks;
     if (s > tiles / 2) s = tiles / 2;
-    const int64_t room = part_floats / (rows * (DP + 1));
+    const int64_t room = part_floats / (rows * (DP + 2)); // a row's result, maximum and sum
     if (s > room) s = room;
     return s < 1 ? 1 : (int)s;
 }
