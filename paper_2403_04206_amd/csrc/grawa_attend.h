@@ -26,6 +26,9 @@ typedef short grawa_s16x8v __attribute__((ext_vector_type(8)));
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// Where scores in units of log2 are so large that the roundings of what their exponentials are taken against would show: of the maximum,
+// which is a factor of all exponentials, or of the logarithm of their sum.
+constexpr float LARGE = 0x1p20f;
 
 template <bool BF16> struct Frag;
 template <> struct Frag<true> {

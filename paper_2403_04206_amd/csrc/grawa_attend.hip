@@ -7,9 +7,6 @@
 namespace {
 
 #ifdef __HIP_DEVICE_COMPILE__
-// Where scores times their unit are so large that the rounding of their maximum would show (it is a factor of all exponentials, no more).
-constexpr float LARGE = 0x1p20f;
-
 // The running maximum and sum of a column's softmax: m in units of the scores, of which c is in units of log2.
 struct Running {
     float m, l;

@@ -61,6 +61,9 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     }
     float lse = placed ? a.lse[((int64_t)kn * a.H + head) * a.Sq + i] * LOG2E : __builtin_inff();
     if (lse == -__builtin_inff()) lse = __builtin_inff(); // the row sees nothing
+    // P = exp2(score - lse) is at most 1, but beside a large lse the four roundings on its way here (the maximum's, the sum's, to natural
+    // logarithms and back; the constants' product is 0.2 more) could make it any number: one that is 6 of them larger is above all scores.
+    if (fabsf(lse) > LARGE) lse = __builtin_fmaf(fabsf(lse), 0x1.8p-22f, lse);
     // Columns that count for nothing stand where they see no key: 0 would not be enough for what they have with one that is no number.
     const bool counts = lse != __builtin_inff();
     const int pos = counts ? at.start + i : -1;
@@ -69,9 +72,11 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
 
     const float c2 = a.scale * LOG2E;
     float far = 0.f;
+    bool fold = true; // the last distance's bias and lse into one number: not where the bias leaves no digits for the other
     if constexpr (BIAS) {
         const char *bias = a.bias.p + ((int64_t)k * a.bias.worker + head * a.buckets) * ES;
         far = bias_of<BF16>(bias + a.bucket_of[a.distances - 1] * ES);
+        fold = __builtin_amdgcn_readfirstlane(!(fabsf(far) > LARGE && fabsf(far) < __builtin_inff()));
         for (int d = threadIdx.x; d < a.distances; d += 256) {
             bucket_of[d] = a.bucket_of[d];
             table[d] = bias_of<BF16>(bias + bucket_of[d] * ES);
@@ -111,11 +116,11 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
                 s = mfma(x, q[i / 2], s);
         });
         ask(f, then);
-        if (BIAS && w0 - (j0 + 31) < a.distances - 1) {
+        if (BIAS && (w0 - (j0 + 31) < a.distances - 1 || !fold)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float bias = table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
-                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, bias - lse)) * dp[r];
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, bias) - lse) * dp[r]; // the score as the forward pass has it
             }
         } else {
 #pragma unroll
@@ -466,8 +471,12 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 1 : DP == 64 ? 2 : 1) void k_att
                 const grawa_f32x4v lse = *(const grawa_f32x4v *)(of_rows + 32 * u + 8 * x + 4 * half);
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    const float bias = near.value ? table[clamp_int(p0 + 8 * x + 4 * half + y - j, 0, a.distances - 1)] : far;
-                    s[4 * x + y] = __builtin_fmaf(s[4 * x + y], c2, bias - lse[y]);
+                    if constexpr (BIAS) { // the score as the forward pass has it
+                        const float bias = near.value ? table[clamp_int(p0 + 8 * x + 4 * half + y - j, 0, a.distances - 1)] : far;
+                        s[4 * x + y] = __builtin_fmaf(s[4 * x + y], c2, bias) - lse[y];
+                    } else {
+                        s[4 * x + y] = __builtin_fmaf(s[4 * x + y], c2, -lse[y]);
+                    }
                 }
             }
         };

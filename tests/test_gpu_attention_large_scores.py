@@ -12,7 +12,7 @@ import torch
 
 import attention_reference as ref
 from paper_2403_04206_amd import grawa
-from test_gpu_attention import generator
+from test_gpu_attention import Case, generator
 
 pytestmark = pytest.mark.gpu
 DTYPES = [torch.bfloat16, torch.float32]
@@ -94,3 +94,65 @@ def test_scores_a_little_apart(base, where, Sq, Sk, length, H, G, D, dtype):
         j = torch.arange(Sk, device="cuda")
         units = torch.where(j < 40 if where == "first" else j >= length - 40, 2.0, units.clamp(max=1.0))
     Keys(Sq, Sk, length, H, G, D, dtype, base, units, 2.0 ** -7, 44).check(False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("S,D,window", [(200, 64, 1), (200, 128, 0), (700, 64, 0), (700, 128, 300), (33, 64, 0)])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("size", [2.0 ** 24, 2.0 ** 30])
+def test_gradients_beside_large_scores(size, biased, S, D, window, dtype):
+    """Scores of `size` leave the gradients no digits, but exponentials stay about 1 at most and what is formed of them is no more than that
+    gives: |dv| <= sum |do|, |dS| <= |dP| + |delta|, and |delta| <= sum |dP| or |do||o|.  Exponents are taken above lse where that is beyond
+    2^20 in units of log2; for the rows of smaller scores lse is off by the roundings of the maximum, of the logarithm added, to
+    natural logarithms and back, and by the constants' product, 0.2 of one: 4.2 E 2^20 = 0.27, a factor of 2^0.27.  Other roundings: a few
+    of the type's half steps, and of the sums (S + 2 D) E."""
+    c = Case(1, 1, S, S, 2, 1, D, dtype, seed=45, window=window, **(dict(buckets=2, far=3) if biased else {}))
+    c.q.mul_(size)
+    if biased:
+        c.q.mul_(2.0 ** -30)
+        c.bias.mul_(size)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    q, k, v, do, o = (t[0, 0].double() for t in (c.q, c.k, c.v, c.do, c.o))
+    seen = ref.visible(0, S, S, S, window, 0, "cuda")[0]
+    more = 2.0 ** 0.27 * (1 + 4 * ref.half_step(dtype) + (S + 2 * D) * ref.E)
+    dv, dk = torch.zeros_like(v[:, 0]), torch.zeros_like(v[:, 0])
+    for h in range(2):
+        dP = torch.where(seen, do[:, h].abs() @ v[:, 0].abs().T, 0.0)
+        delta = torch.maximum(dP.sum(1, keepdim=True), (do[:, h] * o[:, h]).abs().sum(1, keepdim=True))
+        dS = torch.where(seen, dP + delta, 0.0)
+        dv += seen.double().T @ do[:, h].abs()
+        dk += dS.T @ q[:, h].abs() * D ** -0.5
+        assert bool((c.dq[0, 0, :, h].double().abs() <= more * (dS @ k[:, 0].abs()) * D ** -0.5).all()), "dq"
+        if biased:
+            assert bool((c.dbias[0, h].double().abs() <= more * dS.sum()).all()), "dbias"
+    assert bool((c.dv[0, 0, :, 0].double().abs() <= more * dv).all()), "dv"
+    assert bool((c.dk[0, 0, :, 0].double().abs() <= more * dk).all()), "dk"
+    c.plan.destroy()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("base", [2.0 ** 21, -2.0 ** 23])
+def test_gradients_where_scores_and_bias_cancel(base, D, dtype):
+    """Queries and keys of a large score and a bias that takes all but 0, 1 or 2 units of it away again: sums and exponentials are ordinary,
+    and dv = P^T do has its digits.  lse is below 16 then, and the 4.2 roundings of it in units of log2 (23) and of the exponent are 128 E."""
+    gen = generator(46)
+    S = 190
+    c = Keys(S, S, S, 2, 1, D, dtype, abs(base), torch.randint(0, 3, (S,), device="cuda", generator=gen).float(), 2.0 ** -7, 47, bias=-base)
+    if base < 0:
+        c.k[..., 0].neg_()
+    do, dq, dk, dv = ref.make(c.q.shape, dtype, gen), torch.empty_like(c.q), torch.empty_like(c.k), torch.empty_like(c.v)
+    dbias = torch.empty_like(c.bias)
+    c.plan.attention(c.q, c.k, c.v, c.o, lse_out=c.lse, bias=c.bias)
+    c.plan.attention_backward(do, c.q, c.k, c.v, c.o, c.lse, dq, dk, dv, bias=c.bias, dbias=dbias)
+    torch.cuda.synchronize()
+    assert bool((c.lse.abs() < 16).all())
+    seen = ref.visible(0, S, S, S, 0, 0, "cuda")[0]
+    P = torch.where(seen, torch.exp(c.units), 0.0)
+    P = P / P.sum(1, keepdim=True)
+    U, near = ref.half_step(dtype), (S / 8 + 64 + 128) * ref.E + (ref.half_step(dtype) if dtype is torch.bfloat16 else 0.0)
+    want = sum(P.T @ do[0, 0, :, h].double() for h in range(2))
+    ref.check(dv[0, 0, :, 0], want, near * sum(P.T @ do[0, 0, :, h].double().abs() for h in range(2)) + U * want.abs() + 1e-38, "dv")
+    c.plan.destroy()
