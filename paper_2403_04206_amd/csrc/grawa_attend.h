@@ -38,6 +38,29 @@ template <> struct Frag<false> {
     typedef grawa_f32x8 V;
 };
 
+// Which pieces of a tile the lanes load and where: NW waves, 64 lanes of 16 bytes each a load.
+template <bool BF16, int DP, int ROWS, int NW> struct TilePieces {
+    static constexpr int ES = BF16 ? 2 : 4, RB = DP * ES, PPR = RB / 16, BYTES = ROWS * RB, LOADS = BYTES / 1024 / NW;
+    static constexpr int RPL = NW * 64 / PPR, TURNS = RPL < 16 ? 16 / RPL : 1; // rows that the waves load at a time; loads until the keys repeat
+    static_assert(LOADS * NW * 1024 == BYTES && LOADS % TURNS == 0, "whole loads of whole groups of rows");
+
+    static __host__ __device__ __forceinline__ int key(int row)
+    {
+        if constexpr (!BF16) return (((row >> 2) & 1) << 3) | ((row & 3) << 1) | ((row >> 3) & 1);
+        if constexpr (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+        return (((row >> 1) & 1) << 2) | ((row >> 2) & 1) | (((row >> 3) & 1) << 1); // rows of 128 bytes: their lowest bit is a bank's
+    }
+    // Offsets of rows of below 2^24 bytes each.  Pieces that the head does not have are beyond every descriptor of the tile in all its loads: up to
+    // 128 rows end below 2^31, where such pieces begin, and with them end below 2^32; more rows leave no room to go on in, and such pieces stay.
+    static constexpr uint32_t NONE = ROWS <= 128 ? 0x80000000u : 0xffffff00u;
+    static __host__ __device__ __forceinline__ uint32_t first_of(int id, int turn, uint32_t token, int D)
+    {
+        const int row = id / PPR + turn * RPL, c = (id % PPR) ^ key(row);
+        return c * 16 < D * ES ? (uint32_t)row * token + (uint32_t)c * 16 : NONE;
+    }
+    static __host__ __device__ __forceinline__ uint32_t later(uint32_t first, uint32_t by) { return ROWS > 128 && first == NONE ? NONE : first + by; }
+};
+
 #ifdef __HIP_DEVICE_COMPILE__
 __device__ __forceinline__ grawa_f32x16 mfma(const grawa_bf16x8 &a, const grawa_bf16x8 &b, const grawa_f32x16 &c)
 {
@@ -65,29 +88,17 @@ __device__ __forceinline__ void as_operand(const grawa_f32x16 &s, int t, grawa_f
 // What the other half of the wave has.
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
-template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
+template <bool BF16, int DP, int ROWS, int NW> struct HeadTile : TilePieces<BF16, DP, ROWS, NW> {
     typedef typename Frag<BF16>::V V;
-    static constexpr int ES = BF16 ? 2 : 4, RB = DP * ES, PPR = RB / 16, BYTES = ROWS * RB, LOADS = BYTES / 1024 / NW;
-    static constexpr int RPL = NW * 64 / PPR, TURNS = RPL < 16 ? 16 / RPL : 1; // rows that the waves load at a time; loads until the keys repeat
-    static_assert(LOADS * NW * 1024 == BYTES && LOADS % TURNS == 0, "whole loads of whole groups of rows");
-
-    static __device__ __forceinline__ int key(int row)
-    {
-        if constexpr (!BF16) return (((row >> 2) & 1) << 3) | ((row & 3) << 1) | ((row >> 3) & 1);
-        if constexpr (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
-        return (((row >> 1) & 1) << 2) | ((row >> 2) & 1) | (((row >> 3) & 1) << 1); // rows of 128 bytes: their lowest bit is a bank's
-    }
+    typedef TilePieces<BF16, DP, ROWS, NW> Pieces;
+    using Pieces::ES, Pieces::RB, Pieces::BYTES, Pieces::LOADS, Pieces::RPL, Pieces::TURNS, Pieces::key;
 
     // Loads: the lane's offset in the wave's first ones, until the keys repeat.
     uint32_t first[TURNS], step;
     __device__ __forceinline__ void init(int wave, int lane, uint32_t token, int D)
     {
-        const int id = wave * 64 + lane;
 #pragma unroll
-        for (int i = 0; i < TURNS; ++i) {
-            const int row = id / PPR + i * RPL, c = (id % PPR) ^ key(row);
-            first[i] = c * 16 < D * ES ? (uint32_t)row * token + (uint32_t)c * 16 : 0x80000000u;
-        }
+        for (int i = 0; i < TURNS; ++i) first[i] = Pieces::first_of(wave * 64 + lane, i, token, D);
         step = RPL * TURNS * token;
     }
     // rows: what the sequence has from the tile's first token on; none: nothing is read and all comes as zeros.
@@ -100,7 +111,7 @@ template <bool BF16, int DP, int ROWS, int NW> struct HeadTile {
     {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS_AT void *)(lds + (wave + NW * i) * 1024), 16, first[i % TURNS] + (uint32_t)(i / TURNS) * step, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GRAWA_LDS_AT void *)(lds + (wave + NW * i) * 1024), 16, Pieces::later(first[i % TURNS], (uint32_t)(i / TURNS) * step), 0, 0, 0);
     }
 
     // Fragments: an offset of the lane's that all of a tile's share, of which a fragment's differs by some of its low bits and by a constant.
