@@ -485,7 +485,8 @@ grawa_status_t grawa_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype, c
  *
  * Limits: 1 <= K <= GRAWA_MAX_WORKERS, K N H <= 2^20, K N H S <= 2^30, S <= 2^28, D a multiple of 8
  * up to 128, H a multiple of G, at most GRAWA_MAX_DISTANCES distances and
- * GRAWA_MAX_BUCKETS buckets; UNSUPPORTED beyond.  N = 0 and tokens = 0 are no errors.
+ * GRAWA_MAX_BUCKETS buckets, strides below 2^40 elements and all rows within 2^56 of the
+ * first; UNSUPPORTED beyond.  N = 0 and tokens = 0 are no errors.
  */
 #define GRAWA_MAX_DISTANCES 1024
 #define GRAWA_MAX_BUCKETS 256

@@ -49,17 +49,21 @@ grawa_status_t check_shape(const grawa_attention_shape_t *s)
     return GRAWA_OK;
 }
 
-// Strides whose products with the counts stay far from 63 bits; outputs with rows that do not overlap, whatever the order of the
-// axes.  By tiles: what the attention's loads ask for.
+// Rows that lie within 2^56 elements of the first one, so that no address passes 63 bits (heads of keys are counted from the H of queries on,
+// which 2^20 times a stride of 2^40 elements still allows); outputs with rows that do not overlap, whatever the order of the axes.  By
+// tiles: what the attention's loads ask for.
 grawa_status_t check_heads(const grawa_attention_plan *s, const grawa_heads_t *r, int64_t N, int64_t S, int heads, bool tiles, bool out, GrawaHeads &v)
 {
     if (!r) return GRAWA_ERR_INVALID_ARG;
     const int64_t counts[4] = {s->K, N, S, heads}, es = element(s->dtype), limit = (int64_t)1 << 40;
-    int64_t strides[4] = {r->worker, r->sequence, r->token, r->head};
+    int64_t strides[4] = {r->worker, r->sequence, r->token, r->head}, room = (int64_t)1 << 56;
     for (int i = 0; i < 4; ++i) {
         if (strides[i] < 0) return GRAWA_ERR_INVALID_ARG;
         if (counts[i] <= 1) strides[i] = 0;
-        if (strides[i] >= limit) return GRAWA_ERR_UNSUPPORTED;
+    }
+    for (int i = 0; i < 4; ++i) {
+        if (strides[i] >= limit || (counts[i] > 1 && strides[i] > room / (counts[i] - 1))) return GRAWA_ERR_UNSUPPORTED;
+        if (counts[i] > 1) room -= strides[i] * (counts[i] - 1);
     }
     v = GrawaHeads{static_cast<char *>(r->data), strides[0] * es, strides[1] * es, strides[2] * es, strides[3] * es};
     if (N == 0 || S == 0) return GRAWA_OK; // no row is looked at
