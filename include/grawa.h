@@ -527,7 +527,8 @@ grawa_status_t grawa_attention_destroy(grawa_attention_plan_t *plan);
 /*
  * Norm and rotation of N sequences of S tokens.  qweight, kweight: vectors of D for
  * each worker, shared by its heads.  starts: device int32 [K][N], position of each
- * sequence's first token, or NULL for 0; any value.  q_out may be q and k_out k.
+ * sequence's first token, or NULL for 0; any value.  q_out may be q and k_out k.  Rows may
+ * be of any size that the type has; with eps = 0, of normal numbers.
  */
 grawa_status_t grawa_head_norm(grawa_attention_plan_t *plan, int64_t N, int64_t S, const grawa_heads_t *q,
                                const grawa_heads_t *k, const grawa_mats_t *qweight,

@@ -18,7 +18,7 @@ struct HeadNorm {
     const int *starts;
     const double *turns;
     float *part;
-    float eps;
+    float eps, least; // rows whose squares are less in all are taken larger first
     int N, S, H, G, D, rotary;
     int heads; // of an item: so many rows share a token's angles
     int accumulate;
@@ -139,6 +139,10 @@ template <Pairs P> struct Turn {
     }
 };
 
+template <bool B> struct Is {
+    static constexpr bool value = B;
+};
+
 __device__ __forceinline__ int64_t byte_of(const GrawaHeads &h, int k, int n, int s)
 {
     return (int64_t)k * h.worker + (int64_t)n * h.seq + (int64_t)s * h.token;
@@ -178,55 +182,77 @@ template <bool BF16, int LPR, Pairs P, bool BACK> __global__ __launch_bounds__(2
         const char *pq = a.q.p + byte_of(a.q, k, n, s), *pk = a.k.p + byte_of(a.k, k, n, s) - a.H * a.k.head;
         char *yq = a.yq.p + byte_of(a.yq, k, n, s), *yk = a.yk.p + byte_of(a.yk, k, n, s) - a.H * a.yk.head;
         const char *gq = BACK ? a.gq.p + byte_of(a.gq, k, n, s) : nullptr, *gk = BACK ? a.gk.p + byte_of(a.gk, k, n, s) - a.H * a.gk.head : nullptr;
+        const auto has = [&](int i) { return there && i < a.heads && h0 + i < h1; };
+        const auto load = [&](int i, Eight<BF16> &x, Eight<BF16> &g) __attribute__((always_inline)) {
+            const int h = h0 + i;
+            const bool key = h >= a.H;
+            x.load(key ? pk + h * a.k.head : pq + h * a.q.head, lo, hi, has(i));
+            if constexpr (BACK) g.load(key ? gk + h * a.gk.head : gq + h * a.gq.head, lo, hi, has(i));
+        };
+        // Whether the row's squares are such that float32 does not hold them, or not with all their digits where eps is as small.  Such rows
+        // are left as they are the first time, and formed with care, from squares of the row times a power of two, the second.
+        const auto form = [&](int i, Eight<BF16> x, const Eight<BF16> &g, auto careful) __attribute__((always_inline)) {
+            const int h = h0 + i;
+            const bool key = h >= a.H;
+            float squares = 0.f, p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) squares += x.v[j] * x.v[j];
+            squares = row_total<LPR>(squares);
+            const bool odd = !(squares < 0x1p120f) || squares < a.least, mine = has(i) && odd == careful.value;
+            float r = 1.f / sqrtf(squares / (float)a.D + a.eps);
+            if constexpr (careful.value) {
+                const float f = squares < a.least ? 0x1p90f : 0x1p-70f;
+                squares = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) squares += x.v[j] * f * (x.v[j] * f);
+                r = fminf(f / sqrtf(row_total<LPR>(squares) / (float)a.D + a.eps * f * f), 0x1.fffffep127f);
+            }
+            Eight<BF16> y;
+            if constexpr (!BACK) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x.v[j] = x.v[j] * r * (key ? wk.v[j] : wq.v[j]);
+                turn.partners(a, x.v, lds + row * DP, lo, hi, p);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool turned = (j < 4 ? lo + j : hi + j - 4) < a.rotary;
+                    y.v[j] = turned ? x.v[j] * turn.cos[j] + p[j] * turn.sin[j] : x.v[j];
+                }
+            } else {
+                turn.partners(a, g.v, lds + row * DP, lo, hi, p);
+                float dot = 0.f, d[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool turned = (j < 4 ? lo + j : hi + j - 4) < a.rotary;
+                    const float dn = turned ? g.v[j] * turn.cos[j] - p[j] * turn.sin[j] : g.v[j];
+                    x.v[j] *= r;
+                    d[j] = dn * x.v[j];
+                    y.v[j] = dn * (key ? wk.v[j] : wq.v[j]);
+                    dot += y.v[j] * x.v[j];
+                }
+                dot = row_total<LPR>(dot) / (float)a.D;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    y.v[j] = r * (y.v[j] - x.v[j] * dot);
+                    if (mine && key) sk[j] += d[j];
+                    if (mine && !key) sq[j] += d[j];
+                }
+            }
+            if (mine) y.store(key ? yk + h * a.yk.head : yq + h * a.yq.head, lo, hi);
+            return odd;
+        };
         for (int first = 0; first < a.heads; first += U) {
             Eight<BF16> x[U], g[BACK ? U : 1];
+            bool odd = false;
 #pragma unroll
-            for (int u = 0; u < U; ++u) { // all on their way before the first is waited for
-                const int h = h0 + first + u;
-                const bool has = there && first + u < a.heads && h < h1, key = h >= a.H;
-                x[u].load(key ? pk + h * a.k.head : pq + h * a.q.head, lo, hi, has);
-                if constexpr (BACK) g[u].load(key ? gk + h * a.gk.head : gq + h * a.gq.head, lo, hi, has);
-            }
+            for (int u = 0; u < U; ++u) load(first + u, x[u], g[BACK ? u : 0]); // all on their way before the first is waited for
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = h0 + first + u;
-                const bool has = there && first + u < a.heads && h < h1, key = h >= a.H;
-                float squares = 0.f, p[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) squares += x[u].v[j] * x[u].v[j];
-                const float r = 1.f / sqrtf(row_total<LPR>(squares) / (float)a.D + a.eps);
-                Eight<BF16> y;
-                if constexpr (!BACK) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[u].v[j] = x[u].v[j] * r * (key ? wk.v[j] : wq.v[j]);
-                    turn.partners(a, x[u].v, lds + row * DP, lo, hi, p);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool turned = (j < 4 ? lo + j : hi + j - 4) < a.rotary;
-                        y.v[j] = turned ? x[u].v[j] * turn.cos[j] + p[j] * turn.sin[j] : x[u].v[j];
-                    }
-                } else {
-                    turn.partners(a, g[u].v, lds + row * DP, lo, hi, p);
-                    float dot = 0.f, d[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool turned = (j < 4 ? lo + j : hi + j - 4) < a.rotary;
-                        const float dn = turned ? g[u].v[j] * turn.cos[j] - p[j] * turn.sin[j] : g[u].v[j];
-                        x[u].v[j] *= r;
-                        d[j] = dn * x[u].v[j];
-                        y.v[j] = dn * (key ? wk.v[j] : wq.v[j]);
-                        dot += y.v[j] * x[u].v[j];
-                    }
-                    dot = row_total<LPR>(dot) / (float)a.D;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        y.v[j] = r * (y.v[j] - x[u].v[j] * dot);
-                        if (has && key) sk[j] += d[j];
-                        if (has && !key) sq[j] += d[j];
-                    }
+            for (int u = 0; u < U; ++u) odd |= form(first + u, x[u], g[BACK ? u : 0], Is<false>());
+            if (__builtin_expect(__any(odd), 0))
+#pragma unroll 1
+                for (int u = 0; u < U; ++u) {
+                    load(first + u, x[0], g[0]);
+                    form(first + u, x[0], g[0], Is<true>());
                 }
-                if (has) y.store(key ? yk + h * a.yk.head : yq + h * a.yq.head, lo, hi);
-            }
         }
     }
     if constexpr (BACK) {
@@ -299,6 +325,9 @@ template <bool BACK> hipError_t launch(const grawa_attention_plan *s, const Head
     return s->rotary % 8 ? launch_one<BACK, APART>(s, a, grid, st) : launch_one<BACK, HALVES>(s, a, grid, st);
 }
 
+// Squares below 2^-126 lose digits, which shows in sums below 2^-100 to which no larger eps is added.
+float least_of(float eps) { return eps < 0x1p-110f ? 0x1p-100f : 0.f; }
+
 int64_t blocks_of(const grawa_attention_plan *s, int64_t tokens, int heads, int64_t most)
 {
     const int rows = s->D <= 64 ? 32 : 16;
@@ -319,7 +348,7 @@ hipError_t grawa_launch_head_norm(const grawa_attention_plan *s, int64_t N, int6
 {
     if (N * S == 0) return hipSuccess;
     HeadNorm a{};
-    a.q = q, a.k = k, a.yq = qo, a.yk = ko, a.wq = qw, a.wk = kw, a.starts = starts, a.turns = s->turns, a.eps = eps;
+    a.q = q, a.k = k, a.yq = qo, a.yk = ko, a.wq = qw, a.wk = kw, a.starts = starts, a.turns = s->turns, a.eps = eps, a.least = least_of(eps);
     a.N = (int)N, a.S = (int)S, a.H = s->H, a.G = s->G, a.D = s->D, a.rotary = s->rotary;
     a.heads = heads_of(s, N * S);
     return launch<false>(s, a, (int)blocks_of(s, N * S, a.heads, 1 << 20), st);
@@ -331,7 +360,7 @@ hipError_t grawa_launch_head_norm_backward(const grawa_attention_plan *s, int64_
 {
     HeadNorm a{};
     a.q = q, a.k = k, a.yq = dq, a.yk = dk, a.gq = dqo, a.gk = dko, a.wq = qw, a.wk = kw, a.dwq = dqw, a.dwk = dkw;
-    a.starts = starts, a.turns = s->turns, a.part = s->norm_part, a.eps = eps, a.accumulate = accumulate;
+    a.starts = starts, a.turns = s->turns, a.part = s->norm_part, a.eps = eps, a.least = least_of(eps), a.accumulate = accumulate;
     a.N = (int)N, a.S = (int)S, a.H = s->H, a.G = s->G, a.D = s->D, a.rotary = s->rotary;
     a.heads = heads_of(s, N * S);
     const int blocks = (int)blocks_of(s, N * S, a.heads, s->norm_blocks);
