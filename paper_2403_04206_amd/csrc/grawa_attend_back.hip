@@ -35,8 +35,8 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int qw = wave % QW, kw = wave / QW; // the wave's queries, and its keys where they are not all
     const int heads = a.K * a.N * a.H;
-    const Turn turn = turn_of(blockIdx.x, a.K * a.N * a.G, a.share, a.by_xcd);
-    if (turn.head >= heads) return;
+    const Turn turn = turn_of(blockIdx.y * gridDim.x + blockIdx.x, a.K * a.N * a.G, a.share, a.by_xcd);
+    if (turn.head >= heads || turn.block >= a.blocks) return;
     const int qb = a.blocks - 1 - turn.block;
     const int kn = turn.head / a.H, head = turn.head - kn * a.H, k = kn / a.N, n = kn - k * a.N, g = head / a.share;
     const Place at = place_of(a, kn);
@@ -649,7 +649,9 @@ template <bool BF16, int DP, bool BIAS> hipError_t launch(GrawaAttend a, int64_t
     if (a.Sq > 0) {
         a.blocks = (a.Sq + grawa_dq_queries(BF16) - 1) / grawa_dq_queries(BF16);
         const uint32_t grid = grid_of(kn * a.G, a.share, a.blocks, a.by_xcd);
-        hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3(grid), dim3(256), BIAS ? (uint32_t)a.distances * 6 * sizeof(float) : 0, st, a);
+        // 2^24 blocks, which float32 comes to, are more threads than an axis of a grid takes: two rows of them then, each of whole turns of the XCDs.
+        const uint32_t rows = grid < 1u << 24 ? 1 : 2;
+        hipLaunchKernelGGL((k_attend_dq<BF16, DP, BIAS>), dim3(rows == 1 ? grid : (grid + 15) / 16 * 8, rows), dim3(256), BIAS ? (uint32_t)a.distances * 6 * sizeof(float) : 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (BIAS) {
