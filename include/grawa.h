@@ -472,8 +472,9 @@ grawa_status_t grawa_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype, c
  * take them, and the gradients of queries beside many keys use o as rounded (beside few,
  * about 500, where that would show, they form what they need of it again); with float32
  * products are float32.
+ * Sums over keys are formed before they are divided: values may be up to 2^90 in size.
  * The gradients form exp(s_ij - lse_i): an lse beyond 2^20 in size leaves them no digits, but
- * exponentials stay below 1.
+ * exponentials stay about 1 at most.
  *
  * Layouts.  grawa_heads_t is K x N x S x heads rows of D elements: worker k's sequence
  * n, token s, head h starts at data + k * worker + n * sequence + s * token + h * head

@@ -156,3 +156,21 @@ def test_gradients_where_scores_and_bias_cancel(base, D, dtype):
     want = sum(P.T @ do[0, 0, :, h].double() for h in range(2))
     ref.check(dv[0, 0, :, 0], want, near * sum(P.T @ do[0, 0, :, h].double().abs() for h in range(2)) + U * want.abs() + 1e-38, "dv")
     c.plan.destroy()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("Sq", [1, 5, 700])
+@pytest.mark.parametrize("size", [2.0 ** -80, 2.0 ** 87])
+def test_values_of_any_size(size, Sq, dtype):
+    """Values of up to 2^90 beside scores that grow by a few from token to token: sums before the division hold them."""
+    c = Case(1, 1, Sq, 700, 2, 1, 64, dtype, seed=48)
+    c.k[..., 0] = (torch.arange(700, device="cuda", dtype=torch.float32) / 16)[:, None].to(dtype)
+    c.q[..., 0] = 24.0
+    c.v.mul_(size)
+    want = c.want(False)
+    c.forward()
+    torch.cuda.synchronize()
+    assert bool(c.o.isfinite().all())
+    for name, (value, off) in want.items():
+        ref.check(getattr(c, name), value, off, name)
+    c.plan.destroy()
