@@ -64,7 +64,6 @@ struct GrawaAttend {
 static inline int64_t grawa_round256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 static inline int grawa_padded_width(int D) { return D <= 64 ? 64 : 128; }
 
-int64_t grawa_attend_part_floats(const grawa_attention_plan *s);
 int grawa_head_norm_blocks(const grawa_attention_plan *s);
 
 hipError_t grawa_launch_head_norm(const grawa_attention_plan *s, int64_t N, int64_t S, GrawaHeads q, GrawaHeads k, GrawaMat qw, GrawaMat kw, float eps,
