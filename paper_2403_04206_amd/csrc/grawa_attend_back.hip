@@ -96,9 +96,8 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     lv.init(wave, lane, (uint32_t)a.v.token, a.D);
     const auto tile_of = [&](int it) { return (it < first_tiles ? it : it - first_tiles + t0) * BK; };
     Tiles<Tile, BK> tiles_at;
-    const auto restart = [&]() __attribute__((always_inline)) { tiles_at.init(kp, vp, (uint32_t)a.k.token, (uint32_t)a.v.token, at.length, a.D, 0, first_tiles, t0); };
+    const auto restart = [&](int from) __attribute__((always_inline)) { tiles_at.init(kp, vp, (uint32_t)a.k.token, (uint32_t)a.v.token, at.length, a.D, from, first_tiles, t0); };
     const auto load = [&](char *buf) __attribute__((always_inline)) { tiles_at.load(lk, lv, buf, wave); };
-    restart();
     const auto none = [&](int j0) { return j0 > w1 || j0 >= at.length || (j0 + 31 <= w0 - a.window && j0 >= a.sinks); }; // of the wave's pairs count
     const auto all = [&](int j0) { return whole && j0 + 31 <= w0 && (w1 - j0 < a.window || j0 + 31 < a.sinks); };
     const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
@@ -132,8 +131,9 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         return s;
     };
 
-    // All of the wave's pairs, 32 keys at a time.
-    const auto walk = [&](auto &&step) __attribute__((always_inline)) {
+    // All of the wave's pairs from a tile on, 32 keys at a time.
+    const auto walk = [&](int from, auto &&step) __attribute__((always_inline)) {
+        restart(from);
         const auto both_halves = [&](int it, const char *buf) __attribute__((always_inline)) {
             for (int u = BF16 ? 0 : kw; u < (BF16 ? 2 : kw + 1); ++u) {
                 const int j0 = tile_of(it) + 32 * u;
@@ -141,8 +141,8 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             }
         };
         if constexpr (BUFS == 2) {
-            if (tiles) load(buf0);
-            for (int it = 0; it < tiles; it += 2) {
+            if (from < tiles) load(buf0);
+            for (int it = from; it < tiles; it += 2) {
                 landed();
                 if (it + 1 < tiles) load(buf1);
                 both_halves(it, buf0);
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
                 both_halves(it + 1, buf1);
             }
         } else {
-            for (int it = 0; it < tiles; ++it) {
+            for (int it = from; it < tiles; ++it) {
                 landed();
                 load(buf0);
                 landed();
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     if constexpr (BF16) {
         if (tiles <= OWN_DOT_TILES) {
             delta = 0.f;
-            walk([&](const char *buf, int u, int j0) __attribute__((always_inline)) {
+            walk(0, [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
                 V f[A];
                 const grawa_f32x16 s = slopes(buf, u, j0, f, [&](int) { return V{}; });
 #pragma unroll
@@ -171,7 +171,6 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             });
             delta += other_half(delta);
             delta = counts ? delta : 0.f;
-            restart();
             landed();
         }
     }
@@ -184,7 +183,34 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     for (int r = 0; r < 16; ++r) minus_dot[r] = -delta;
 
     grawa_f32x16 dq[DT];
-    float far_sum = 0.f; // of dS from the last distance of the table on
+    // Sums of dS: of the lane's column where all distances are the table's last or beyond, of the lane's column where they are not, and of such
+    // distances found there.
+    float far_sum = 0.f, near_sum = 0.f, far_diagonals = 0.f;
+    // Sums by distance, 16 keys at a time: key y and query c are c - y + 15 places along row y, so that a column has one distance; what a row does not
+    // have there stays 0.  A lane adds up a column.
+    const auto add_by_distance = [&](const grawa_f32x16 &s, int j0) __attribute__((always_inline)) {
+        if constexpr (BIAS)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float *const at_row = diagonals[wave] + (lane & 31) + 15;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const int y = (r & 3) + 8 * (r >> 2) + 4 * half;
+                    at_row[y * 63] = s[8 * h + r];
+                }
+                wave_order();
+                float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int y = 0; y < 16; ++y) sums[y % 4] += diagonals[wave][y * 64 + lane];
+                const float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                const int d = w0 - (j0 + 16 * h) + lane - 15;
+                if (d >= a.distances - 1)
+                    far_diagonals += sum;
+                else if (d >= 0)
+                    by_distance[d] += sum;
+                wave_order();
+            }
+    };
 #pragma unroll
     for (int d = 0; d < DT; ++d) dq[d] = grawa_f32x16{};
     const auto step = [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
@@ -196,28 +222,10 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
 #pragma unroll
                 for (int r = 0; r < 16; ++r) far_sum += s[r];
             } else {
-                // Sixteen keys at a time: key y and query c are c - y + 15 places along row y, so that a column has one distance; what a
-                // row does not have there stays 0.  A lane adds up a column.
+                if constexpr (BF16)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float *const at_row = diagonals[wave] + (lane & 31) + 15;
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const int y = (r & 3) + 8 * (r >> 2) + 4 * half;
-                        at_row[y * 63] = s[8 * h + r];
-                    }
-                    wave_order();
-                    float sums[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int y = 0; y < 16; ++y) sums[y % 4] += diagonals[wave][y * 64 + lane];
-                    const float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-                    const int d = w0 - (j0 + 16 * h) + lane - 15;
-                    if (d >= a.distances - 1)
-                        far_sum += sum;
-                    else if (d >= 0)
-                        by_distance[d] += sum;
-                    wave_order();
-                }
+                    for (int r = 0; r < 16; ++r) near_sum += s[r];
+                add_by_distance(s, j0);
             }
         }
         V w[2];
@@ -226,7 +234,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
         __builtin_amdgcn_sched_barrier(0);
         flow<2 * DT>(f, columns, [&](int i, const V &x) __attribute__((always_inline)) { dq[i % DT] = mfma(x, w[i / DT], dq[i % DT]); });
     };
-    walk(step);
+    walk(0, step);
     if constexpr (!BF16) {
         landed();
         float *const other = (float *)buf0 + qw * (DT * 16 * 64) + lane;
@@ -265,7 +273,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
 #pragma unroll 1
         for (int d = 0; d < DT; ++d) {
             grawa_f32x16 sums = {};
-            restart();
+            restart(0);
             for (int it = 0; it < tiles; ++it) {
                 landed();
                 load(buf0);
@@ -290,6 +298,42 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             }
             put(d, sums);
         }
+    }
+    if constexpr (BF16 && BIAS) {
+        if (tiles > OWN_DOT_TILES) {
+            // dS of a row add up to 0.  What they add up to instead is what delta is off by, and each of them is off by P times that: it comes off the
+            // sums by distance, in one more walk over the tiles that have any distance before the table's last.  P add up to 1, so that what these
+            // have of it leaves what the last distance has.
+            float off = near_sum + far_sum, taken = 0.f;
+            off += other_half(off);
+            off = counts ? off : 0.f;
+            int from = tiles;
+            while (from > 0 && p0 - (tile_of(from - 1) + BK - 1) < a.distances - 1) --from;
+            landed();
+            walk(from, [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
+                if (w0 - (j0 + 31) >= a.distances - 1) return;
+                V f[A];
+                const auto keys = [&](int i) { return Tile::by_rows(buf, rows_at + 32 * u * Tile::RB, 0, i); };
+                grawa_f32x16 s = {};
+                ask(f, keys);
+                flow<KS>(f, keys, [&](int i, const V &x) __attribute__((always_inline)) { s = mfma(x, q[i], s); });
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float bias = table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
+                    s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, bias) - lse) * -off;
+                }
+                if (!all(j0))
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) taken += s[r];
+                add_by_distance(s, j0);
+            });
+            far_sum -= taken + (half == 0 ? off : 0.f);
+        }
+        far_sum += far_diagonals;
+    } else if constexpr (BIAS) {
+        far_sum += far_diagonals;
     }
     if constexpr (BIAS) {
 #pragma unroll
