@@ -469,9 +469,10 @@ grawa_status_t grawa_dropout(int K, int64_t T, int64_t d, grawa_dtype_t dtype, c
  * Types.  One type a plan, as in the sublayer.  Scores, softmax statistics, sums and
  * angles are float32 (angles are reduced in 64 bits).  With bfloat16 exp(s_ij - max)
  * and the gradient of s_ij are rounded to bfloat16 once, as the matrix instructions
- * take them, and the gradients of queries beside many keys use o as rounded (beside few,
- * about 500, where that would show, they form what they need of it again); with float32
- * products are float32.
+ * take them, and dq and dk of queries beside many keys use o as rounded (beside few, about
+ * 500, where that would show most, they form what they need of it again): values whose mean
+ * is their spread bring dq's error from 0.24 to 0.4 %, a mean of eight times that to 2.4 %.
+ * With float32 products are float32.
  * Sums over keys are formed before they are divided: values may be up to 2^90 in size.
  * The gradients form exp(s_ij - lse_i): an lse beyond 2^20 in size leaves them no digits, but
  * exponentials stay about 1 at most.

@@ -8,8 +8,9 @@
 namespace {
 
 // delta is do . o, and o was rounded to bfloat16: off by 2^-9 |do||o| or so, the same for all keys of a row, where each dS is off by its own
-// 2^-9.  Over many keys that is little beside them, over few it is what dq and dk are off by most (windows of 32 and 4 first keys: 2.7e-3
-// against 2.3e-3).  Queries whose block has so few tiles of keys go over them once more before, for delta = sum P dP in float32:
+// 2^-9.  Over many keys that is little beside them as long as o is small there, values without a mean: dq is off by 0.24 % then, by 0.4 % where
+// their mean is their spread, by 2.4 % where it is eight times that, dk by half as much; sums of dS for dbias are put right below.  Over few it is
+// what dq and dk are off by most (windows of 32 and 4 first keys: 2.7e-3 against 2.3e-3).  Queries whose block has so few tiles of keys go over them once more before, for delta = sum P dP in float32:
 // 2048 tokens without a window, 8 workers of 16 heads of 64: 4 blocks of 16, 130 us and not 122.
 constexpr int OWN_DOT_TILES = 8;
 
@@ -18,8 +19,8 @@ constexpr int OWN_DOT_TILES = 8;
 // the first through LDS.  2 workers of 3 sequences of 333 tokens, 6 heads of 40, with a bias, 33 us, and 50 with blocks as in bf16; all
 // gradients of 4096 tokens, 8 heads of 128, 1107 and 1420, of 4 workers' 16 heads of 2048 tokens of 64 996 and 1015.
 // dS is formed transposed, so that it is an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 125 to 130 us,
-// vector unit 50 %, matrix cores 46 %; with a bias of 32 buckets to distance 128: 195, of which the sums by distance are the difference;
-// 32 heads of 16384 tokens of 128, window 4096: 1230, matrix cores 66 %.
+// vector unit 50 %, matrix cores 46 %; with a bias of 32 buckets to distance 128: 235, of which the sums by distance are the difference, 40 for
+// what delta is off by (with delta formed first in every block 75); 32 heads of 16384 tokens of 128, window 4096: 1230 to 1250, matrix cores 66 %.
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
 {

@@ -150,8 +150,10 @@ __device__ __forceinline__ int64_t byte_of(const GrawaHeads &h, int k, int n, in
 #endif
 
 // LPR lanes have a row of up to 8 LPR elements.  An item is `heads` rows of a token; blocks of a worker take items in turn.
-// Bound by memory; what the angles take is shared by an item's rows and there is no exchange between lanes but a row's sums.
-// 8 workers, 2048 tokens of 2 x 16 heads of 64, bf16: forward 25 us (134 MB, 5.4 TB/s), backward 42 (201 MB, 4.8 TB/s); one token 4.5.
+// Bound by memory forward, and backward by it and the vector unit, which is busy 76 % of both: angles are formed in each, in 64 bits; what they
+// take is shared by an item's rows, of which few heads leave many empty, and there is no exchange between lanes but a row's sums.
+// 8 workers, 2048 tokens of 2 x 16 heads of 64, bf16: forward 26 us (134 MB, 5.2 TB/s), backward 44 (201 MB, 4.6 TB/s); one token 4.6.
+// Rows of odd size in a pass of their own: with a way aside for each row 12 us more over 3 heads of 2^17 tokens, so 4.
 template <bool BF16, int LPR, Pairs P, bool BACK> __global__ __launch_bounds__(256) void k_head_norm([[maybe_unused]] HeadNorm a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
