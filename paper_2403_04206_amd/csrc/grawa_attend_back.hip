@@ -104,8 +104,9 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     const uint32_t rows_at = Tile::rows_of(lane), columns_at = Tile::columns_of(lane);
     grawa_f32x16 minus_dot = {};
     constexpr int A = BF16 ? 4 : 2;
+    float far_weight = 0.f; // sum of the column's P from the last distance of the table on, as far as it is asked for
     // dS of 32 keys; leaves the first fragments of `then` in f.
-    const auto slopes = [&](const char *buf, int u, int j0, V (&f)[A], auto &&then) __attribute__((always_inline)) {
+    const auto slopes = [&](const char *buf, int u, int j0, V (&f)[A], auto &&then, auto weigh) __attribute__((always_inline)) {
         grawa_f32x16 s = {}, dp = minus_dot;
         const auto both = [&](int i) { return Tile::by_rows(buf + i % 2 * Tile::BYTES, rows_at + 32 * u * Tile::RB, 0, i / 2); };
         ask(f, both);
@@ -121,6 +122,17 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             for (int r = 0; r < 16; ++r) {
                 const float bias = table[clamp_int(pos - (j0 + (r & 3) + 8 * (r >> 2) + 4 * half), 0, a.distances - 1)];
                 s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, bias) - lse) * dp[r]; // the score as the forward pass has it
+            }
+        } else if constexpr (weigh.value) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, far - lse));
+            if (!all(j0))
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                far_weight += s[r];
+                s[r] *= dp[r];
             }
         } else {
 #pragma unroll
@@ -166,7 +178,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
             delta = 0.f;
             walk(0, [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
                 V f[A];
-                const grawa_f32x16 s = slopes(buf, u, j0, f, [&](int) { return V{}; });
+                const grawa_f32x16 s = slopes(buf, u, j0, f, [&](int) { return V{}; }, Is<false>());
 #pragma unroll
                 for (int r = 0; r < 16; ++r) delta += s[r];
             });
@@ -217,7 +229,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     const auto step = [&](const char *buf, int u, int j0) __attribute__((always_inline)) {
         V f[A];
         const auto columns = [&](int i) { return Tile::by_columns(buf, columns_at + 32 * u * Tile::RB, i / DT * 16, i % DT); };
-        const grawa_f32x16 s = slopes(buf, u, j0, f, columns);
+        const grawa_f32x16 s = slopes(buf, u, j0, f, columns, Is<BF16 && BIAS>());
         if constexpr (BIAS) {
             if (w0 - (j0 + 31) >= a.distances - 1) {
 #pragma unroll
@@ -284,7 +296,7 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
                     const int j0 = tile_of(it) + 32 * u;
                     if (none(j0)) continue;
                     V f[A];
-                    const grawa_f32x16 s = slopes(buf0, u, j0, f, [&](int) { return V{}; });
+                    const grawa_f32x16 s = slopes(buf0, u, j0, f, [&](int) { return V{}; }, Is<false>());
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         V w;
@@ -303,9 +315,8 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
     if constexpr (BF16 && BIAS) {
         if (tiles > OWN_DOT_TILES) {
             // dS of a row add up to 0.  What they add up to instead is what delta is off by, and each of them is off by P times that: it comes off the
-            // sums by distance, in one more walk over the tiles that have any distance before the table's last.  P add up to 1, so that what these
-            // have of it leaves what the last distance has.
-            float off = near_sum + far_sum, taken = 0.f;
+            // sums by distance, the last distance's by the P added up on the way, the others' in one more walk over the tiles that have any of them.
+            float off = near_sum + far_sum;
             off += other_half(off);
             off = counts ? off : 0.f;
             int from = tiles;
@@ -326,11 +337,9 @@ __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[m
                 if (!all(j0))
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = sees(a, pos, j0 + (r & 3) + 8 * (r >> 2) + 4 * half) ? s[r] : 0.f;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) taken += s[r];
                 add_by_distance(s, j0);
             });
-            far_sum -= taken + (half == 0 ? off : 0.f);
+            far_sum -= off * far_weight;
         }
         far_sum += far_diagonals;
     } else if constexpr (BIAS) {

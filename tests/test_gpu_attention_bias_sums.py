@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import attention_reference as ref
+from paper_2403_04206_amd import grawa
 from test_gpu_attention import Case, generator
 
 pytestmark = pytest.mark.gpu
@@ -26,3 +27,17 @@ def test_only_the_result_is_rounded(S, buckets, far, window, sinks, mean, D):
     print("[case]", off, flush=True)
     assert off <= 2.0 ** -8 + 2.0 ** -12
     c.plan.destroy()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("last,low", [(700, 0.0), (690, -20.0), (300, -20.0), (5, -30.0), (600, 0.0)])
+def test_distances_of_no_pair_or_of_small_weight(last, low, D):
+    """The last bucket begins at a distance that no pair has, a few pairs have, or whose bias leaves them little: 0, or what little they have."""
+    c = Case(1, 2, 700, 700, 2, 1, D, torch.bfloat16, seed=83, buckets=2, far=3)
+    c.plan.destroy()
+    c.bucket_of = [0] * last + [1]
+    c.plan = grawa.AttentionPlan(1, 2, 700, 2, 1, D, dtype=torch.bfloat16, buckets=2, bucket_of=c.bucket_of)
+    c.bias[:, :, 1] += low
+    want = c.want()
+    assert last < 700 or not bool(want["dbias"][0][:, :, 1].any())
+    c.check()
