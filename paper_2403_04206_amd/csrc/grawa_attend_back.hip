@@ -19,7 +19,7 @@ constexpr int OWN_DOT_TILES = 8;
 // the first through LDS.  2 workers of 3 sequences of 333 tokens, 6 heads of 40, with a bias, 33 us, and 50 with blocks as in bf16; all
 // gradients of 4096 tokens, 8 heads of 128, 1107 and 1420, of 4 workers' 16 heads of 2048 tokens of 64 996 and 1015.
 // dS is formed transposed, so that it is an operand where it stands.  bf16, 8 workers, 16 heads of 2048 tokens of 64: 125 to 130 us,
-// vector unit 50 %, matrix cores 46 %; with a bias of 32 buckets to distance 128: 235, of which the sums by distance are the difference, 40 for
+// vector unit 50 %, matrix cores 46 %; with a bias of 32 buckets to distance 128: 230, of which the sums by distance are the difference, 35 for
 // what delta is off by (with delta formed first in every block 75); 32 heads of 16384 tokens of 128, window 4096: 1230 to 1250, matrix cores 66 %.
 template <bool BF16, int DP, bool BIAS>
 __global__ __launch_bounds__(256, BF16 || DP == 64 ? 2 : 1) void k_attend_dq([[maybe_unused]] GrawaAttend a)
