@@ -207,7 +207,8 @@ template <bool BF16, int LPR, Pairs P, bool BACK> __global__ __launch_bounds__(2
                 squares = 0.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) squares += x.v[j] * f * (x.v[j] * f);
-                r = fminf(f / sqrtf(row_total<LPR>(squares) / (float)a.D + a.eps * f * f), 0x1.fffffep127f);
+                squares = row_total<LPR>(squares) / (float)a.D + a.eps * f * f;
+                r = squares > 0.f ? fminf(f / sqrtf(squares), 0x1.fffffep127f) : r; // rows of zeros beside an eps of 0 stay what they are: no numbers
             }
             Eight<BF16> y;
             if constexpr (!BACK) {

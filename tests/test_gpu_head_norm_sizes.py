@@ -42,3 +42,23 @@ def test_rows_of_any_size(size, eps, D, R, interleaved, dtype):
         held = want.abs() + off < limit                                          # dy / x may be more than the type holds
         ref.check(dx[i][held], want[held], off[held], "dx")
         ref.check(dw[i], dweight, dweight_off, "dw")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("value", [0.0, float("inf"), float("nan")])
+def test_rows_without_a_norm(value, dtype):
+    """Zeros beside an eps of 0, infinities and no numbers: what 0 / 0 and infinity / infinity are; rows beside them are as without."""
+    gen = torch.Generator(device="cuda").manual_seed(72)
+    x = [ref.make((1, 1, 20, h, 64), dtype, gen) for h in (2, 1)]
+    w = [ref.make((1, 64), dtype, gen, 0.2, 1.0) for _ in range(2)]
+    y = [torch.full_like(t, 7.0) for t in x]
+    want = [ref.head_norm(t, v, 0.0, ref.angles(torch.zeros((1, 1), device="cuda"), 20, []), False, dtype) for t, v in zip(x, w)]
+    for t in x:
+        t[:, :, 5] = value
+    with grawa.AttentionPlan(1, 1, 20, 2, 1, 64, dtype=dtype) as plan:
+        plan.head_norm(*x, *w, *y, eps=0.0)
+        torch.cuda.synchronize()
+    other = torch.arange(20, device="cuda") != 5
+    for t, (n, off) in zip(y, want):
+        assert bool(t[:, :, 5].isnan().all())
+        ref.check(t[:, :, other], n[:, :, other], off[:, :, other], "y")
